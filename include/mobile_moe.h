@@ -110,7 +110,8 @@ int moe_device_info(int32_t* n_cu, int32_t* is_gfx950);
  * moe_profile_enable(1) also clears earlier records.  moe_profile_read waits for the events of
  * one kind and returns how many launch sites were recorded and their summed duration.
  * Kinds: 0 router GEMM, 1 softmax/top-k/importance, 2 dispatch, 3 FFN gate+up (SwiGLU),
- * 4 FFN down, 5 combine, 6 token confidence, 7 whole decode step (moe_layer_decode). */
+ * 4 FFN down, 5 combine, 6 token confidence, 7 whole decode step (moe_layer_decode), 8 row quantisation,
+ * 9 8-bit product, 10 log probabilities. */
 int moe_profile_enable(int on);
 int moe_profile_read(int kind, int64_t* launches, double* total_ms);
 
@@ -473,6 +474,83 @@ int moe_prefetcher_predicted(moe_prefetcher_t* p, int32_t layer, int32_t* ids);
  * Returns the number of requests made (>= 0) or a negative error. */
 int moe_prefetcher_advance(moe_prefetcher_t* p, int32_t layer, int32_t distance, int32_t* issued_layers,
                            int32_t* limits_used, moe_fetch_stats* issued_stats, void* compute_stream);
+
+/* ------------------------------------------------------------------------------------------
+ * The output head (not in the paper, whose method starts behind it: Alg. 1 compares the largest probability of
+ * the head's softmax with gamma).  hidden states -> logits over a whole vocabulary, as a product of 8-bit
+ * integers, and what is read off the logits: moe_token_logprobs.  The product serves any other projection too.
+ *
+ * Codes and scales of a row x[0..K):      a = max_k |x[k]|,   scale = a / 127 (rounded to fp32),
+ *     q[k] = the integer nearest to 127 x[k] / a, ties to even; the quotient is that of the real numbers, so
+ *            the codes do not depend on how it is computed.
+ *     A row of zeros has scale 0 and codes 0.  A row that holds a NaN or an infinity has scale NaN and codes 0:
+ *     every product with it is NaN.
+ * Product:   out[t][n] = (x_scale[t] * sum_k x[t][k] w[n][k]) * w_scale[n] + bias[n]
+ *     The sum of the codes' products is exact (32-bit integers, K <= 131071); it is rounded to fp32, the two scales
+ *     multiply it in this order, the bias is added by a fused multiply-add, and the result is rounded to the output
+ *     type.  An output therefore has the same bits whatever the other tokens and outputs of the call are.
+ *
+ * moe_quantize_rows   codes and scales of `rows` rows of K values; for weights once, for tokens that several
+ *                     products read.
+ *   x      device [rows, ldx] dtype (MOE_BF16 or MOE_FP32), ldx >= K elements from row to row; any alignment of elements
+ *   q      device [rows, ldq] int8, ldq >= K and a multiple of 16, 16-byte aligned; the columns K .. ldq get zeros
+ *   scale  device [rows] fp32
+ * moe_matmul_int8     x device [T, ldx] int8, x_scale device [T] fp32, w device [N, ldw] int8, w_scale device [N] fp32,
+ *                     bias device [N] fp32 or NULL, out device [T, ldo] out_dtype.  ldx, ldw >= K and multiples of 16,
+ *                     x and w 16-byte aligned; every row, the last one too, holds ldx or ldw bytes, and what
+ *                     stands in them behind K does not matter.  Codes may be any of -128 .. 127.
+ * moe_linear_int8     the same with float tokens, x device [T, ldx] x_dtype, quantised by the call as
+ *                     moe_quantize_rows does (same bits as the two calls); ws: device scratch of
+ *                     moe_linear_int8_workspace_bytes(cfg) bytes, 256-byte aligned.
+ * A leading dimension of 0 means dense rows: K of x and w (then K % 16 == 0 for codes), N of out.
+ * T == 0 and rows == 0 are legal: nothing is enqueued. */
+typedef struct moe_int8_config {
+  int32_t T;         /* tokens                                                               */
+  int32_t N;         /* outputs (weight rows)                                                */
+  int32_t K;         /* inner dimension, 1 .. MOE_INT8_MAX_K                                 */
+  int32_t x_dtype;   /* MOE_BF16 | MOE_FP32: tokens of moe_linear_int8 (moe_matmul_int8 ignores it) */
+  int32_t out_dtype; /* MOE_BF16 | MOE_FP32                                                  */
+  int32_t reserved;  /* 0                                                                    */
+  int64_t ldx, ldw, ldo; /* elements from row to row of x, w, out; below 2^22 each (0 = dense) */
+} moe_int8_config;
+#define MOE_INT8_MAX_K 131071
+int moe_quantize_rows(const void* x, int32_t dtype, int32_t rows, int32_t K, int64_t ldx, int8_t* q, int64_t ldq,
+                      float* scale, void* stream);
+int moe_matmul_int8(const moe_int8_config* cfg, const int8_t* x, const float* x_scale, const int8_t* w,
+                    const float* w_scale, const float* bias, void* out, void* stream);
+size_t moe_linear_int8_workspace_bytes(const moe_int8_config* cfg); /* 0 on a bad config */
+int moe_linear_int8(const moe_int8_config* cfg, const void* x, const int8_t* w, const float* w_scale,
+                    const float* bias, void* out, void* ws, size_t ws_bytes, void* stream);
+
+/* Log probabilities of given tokens, entropy, confidence and the most probable tokens of T output distributions
+ * p = softmax(logits[t]), natural logarithms:
+ *   token_logp[t][g] = log p at tokens[t][g]; an id outside [0, V) (padding) gives 0
+ *   entropy[t]       = -sum_v p_v log p_v  (a masked entry, -inf, adds nothing)
+ *   conf[t]          = max_v p_v, the confidence of Alg. 1 (as moe_token_confidence, which has no workspace and
+ *                      takes fp32 only; the two may differ in the last bits)
+ *   top_idx[t][j], j < n_top: tokens in the order (logit descending, id ascending), a NaN logit counting as -inf
+ *   top_logp[t][j]   = log p at top_idx[t][j]
+ * A row without a distribution (all entries -inf, a NaN or a +inf among them) gives NaN for every number but those
+ * of padding ids; top_idx follows the order above all the same.
+ * The sum beside the largest entry is kept apart from it, so that log p of a nearly certain token keeps its digits.
+ * logits     device [T, ld] dtype (MOE_FP32 or MOE_BF16), ld >= V elements from row to row (0 = V), any alignment of elements
+ * tokens     device [T, n_given] int32 (NULL if n_given == 0)        token_logp device [T, n_given] fp32
+ * entropy, conf device [T] fp32, either may be NULL                  top_idx [T, n_top] int32, top_logp [T, n_top] fp32
+ * ws         device scratch of moe_token_logprobs_workspace_bytes(cfg) bytes, 256-byte aligned (a size of 0: NULL will do)
+ * n_top <= min(V, MOE_MAX_ALTERNATIVES), n_given <= MOE_MAX_GIVEN. */
+#define MOE_MAX_ALTERNATIVES 32
+#define MOE_MAX_GIVEN 64
+typedef struct moe_logprobs_config {
+  int32_t T, V;
+  int32_t dtype;     /* MOE_BF16 | MOE_FP32 */
+  int32_t n_given, n_top;
+  int32_t reserved;  /* 0 */
+  int64_t ld;
+} moe_logprobs_config;
+size_t moe_token_logprobs_workspace_bytes(const moe_logprobs_config* cfg); /* 0 on a bad config too */
+int moe_token_logprobs(const moe_logprobs_config* cfg, const void* logits, const int32_t* tokens, float* token_logp,
+                       float* entropy, float* conf, int32_t* top_idx, float* top_logp, void* ws, size_t ws_bytes,
+                       void* stream);
 
 #ifdef __cplusplus
 }

@@ -21,6 +21,7 @@ LIB_PATH = os.path.join(_PKG, "libmobile_moe.so")
 MOE_BF16, MOE_FP32, MOE_BF16_W8, MOE_BF16_MXFP4 = 0, 1, 2, 3
 MOE_FETCH_DEMAND, MOE_FETCH_PREFETCH = 0, 1
 MOE_MAX_SHARED = 4
+MOE_INT8_MAX_K, MOE_MAX_ALTERNATIVES, MOE_MAX_GIVEN = 131071, 32, 64
 MOE_OK = 0
 ERRORS = {-1: "MOE_E_BADARG", -2: "MOE_E_SHAPE", -3: "MOE_E_UNSUPPORTED", -4: "MOE_E_HIP",
           -5: "MOE_E_CACHE_FULL", -6: "MOE_E_WORKSPACE"}
@@ -34,7 +35,8 @@ EXPORTS = ("moe_last_error", "moe_device_info", "moe_profile_enable", "moe_profi
            "moe_cache_expert_table", "expert_cache_fetch", "moe_expert_ffn_cached", "moe_cache_snapshot", "moe_cache_sync",
            "moe_cache_set_prefetch_limit", "moe_cache_emulate_link", "moe_prefetcher_create", "moe_prefetcher_destroy",
            "moe_prefetcher_set_in_flight_limit", "moe_prefetcher_set_yield_to_demand", "moe_prefetcher_predict", "moe_prefetcher_predicted",
-           "moe_prefetcher_advance")
+           "moe_prefetcher_advance", "moe_quantize_rows", "moe_matmul_int8", "moe_linear_int8_workspace_bytes", "moe_linear_int8",
+           "moe_token_logprobs_workspace_bytes", "moe_token_logprobs")
 
 
 class MoeError(RuntimeError):
@@ -55,6 +57,15 @@ class moe_step_buffers(ctypes.Structure):
                                                "sorted_rank", "inv_pos", "y", "shared_out", "out")] + [
         ("dispatch_ws", ctypes.c_void_p), ("dispatch_ws_bytes", ctypes.c_size_t),
         ("ffn_ws", ctypes.c_void_p), ("ffn_ws_bytes", ctypes.c_size_t)]
+
+
+class moe_int8_config(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("T", "N", "K", "x_dtype", "out_dtype", "reserved")] + [
+        (n, ctypes.c_int64) for n in ("ldx", "ldw", "ldo")]
+
+
+class moe_logprobs_config(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("T", "V", "dtype", "n_given", "n_top", "reserved")] + [("ld", ctypes.c_int64)]
 
 
 class moe_fetch_stats(ctypes.Structure):
@@ -154,6 +165,17 @@ def load_library() -> ctypes.CDLL:
                  "moe_expert_ffn", "moe_combine", "expert_cache_fetch", "moe_expert_ffn_cached", "moe_cache_snapshot",
                  "moe_cache_sync", "moe_cache_set_prefetch_limit", "moe_cache_emulate_link"):
         getattr(lib, name).restype = ctypes.c_int
+    i64 = ctypes.c_int64
+    lib.moe_quantize_rows.argtypes = [vp, i32, i32, i32, i64, vp, i64, vp, vp]
+    lib.moe_matmul_int8.argtypes = [ctypes.POINTER(moe_int8_config), vp, vp, vp, vp, vp, vp, vp]
+    lib.moe_linear_int8_workspace_bytes.argtypes = [ctypes.POINTER(moe_int8_config)]
+    lib.moe_linear_int8_workspace_bytes.restype = sz
+    lib.moe_linear_int8.argtypes = [ctypes.POINTER(moe_int8_config), vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.moe_token_logprobs_workspace_bytes.argtypes = [ctypes.POINTER(moe_logprobs_config)]
+    lib.moe_token_logprobs_workspace_bytes.restype = sz
+    lib.moe_token_logprobs.argtypes = [ctypes.POINTER(moe_logprobs_config)] + [vp] * 8 + [sz, vp]
+    for name in ("moe_quantize_rows", "moe_matmul_int8", "moe_linear_int8", "moe_token_logprobs"):
+        getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
 
@@ -210,7 +232,7 @@ def moe_device_info():
 
 
 PROFILE_KINDS = ("router_gemm", "route_topk", "dispatch", "ffn_gate_up", "ffn_down", "combine",
-                 "token_confidence", "decode_step")
+                 "token_confidence", "decode_step", "quantize_rows", "int8_product", "token_logprobs")
 
 
 def moe_profile_enable(on: bool) -> None:
@@ -472,7 +494,152 @@ def moe_prefetcher_advance(p: int, layer: int, distance: int, n_layers: int, str
     return [(int(ls[i]), int(lim[i]), st[i]) for i in range(rc)]
 
 
+def moe_quantize_rows(x, q, scale, stream=None) -> None:
+    """x: [rows, K] float rows; q: int8 [rows, ldq] whole rows, ldq >= K a multiple of 16; scale: [rows] fp32."""
+    assert q.shape[0] == x.shape[0] and q.is_contiguous()
+    _check(load_library().moe_quantize_rows(_rows(x), _float_type(x), x.shape[0], x.shape[1], _ld(x), _ptr(q), q.shape[1], _ptr(scale),
+                                            _stream(stream)))
+
+
+def moe_matmul_int8(cfg: moe_int8_config, x, x_scale, w, w_scale, bias, out, stream=None) -> None:
+    _check(load_library().moe_matmul_int8(ctypes.byref(cfg), _rows(x), _ptr(x_scale), _rows(w), _ptr(w_scale), _ptr(bias), _rows(out),
+                                          _stream(stream)))
+
+
+def moe_linear_int8_workspace_bytes(cfg: moe_int8_config) -> int:
+    return int(load_library().moe_linear_int8_workspace_bytes(ctypes.byref(cfg)))
+
+
+def moe_linear_int8(cfg: moe_int8_config, x, w, w_scale, bias, out, ws, ws_bytes: int, stream=None) -> None:
+    _check(load_library().moe_linear_int8(ctypes.byref(cfg), _rows(x), _rows(w), _ptr(w_scale), _ptr(bias), _rows(out), _ptr(ws),
+                                          ws_bytes, _stream(stream)))
+
+
+def moe_token_logprobs_workspace_bytes(cfg: moe_logprobs_config) -> int:
+    return int(load_library().moe_token_logprobs_workspace_bytes(ctypes.byref(cfg)))
+
+
+def moe_token_logprobs(cfg: moe_logprobs_config, logits, tokens, token_logp, entropy, conf, top_idx, top_logp, ws, ws_bytes: int,
+                       stream=None) -> None:
+    _check(load_library().moe_token_logprobs(ctypes.byref(cfg), _rows(logits), _ptr(tokens), _ptr(token_logp), _ptr(entropy), _ptr(conf),
+                                             _ptr(top_idx), _ptr(top_logp), _ptr(ws), ws_bytes, _stream(stream)))
+
+
 # ------------------------------------------------------------------------------ plumbing helpers
+def _rows(t: Optional[torch.Tensor]):
+    """Address of a matrix whose rows are dense and may lie apart."""
+    if t is None:
+        return None
+    assert t.dim() == 2 and (t.shape[1] <= 1 or t.stride(1) == 1), "rows passed to the C ABI must be dense"
+    return ctypes.c_void_p(t.data_ptr())
+
+
+def _ld(t: torch.Tensor) -> int:
+    # a single row has no next one: torch gives such a dimension any stride
+    return int(t.stride(0)) if t.shape[0] > 1 else max(int(t.stride(0)), int(t.shape[1]))
+
+
+def _float_type(t: torch.Tensor) -> int:
+    return {torch.bfloat16: MOE_BF16, torch.float32: MOE_FP32}[t.dtype]
+
+
+def int8_config(x: torch.Tensor, w: torch.Tensor, out: torch.Tensor) -> moe_int8_config:
+    """The description of out[T, N] = x[T, K] w[N, K]^T by the tensors' shapes, types and strides."""
+    c = moe_int8_config()
+    (c.T, c.K), c.N = x.shape, w.shape[0]
+    assert w.shape[1] == c.K and tuple(out.shape) == (c.T, c.N), "shapes of x, w and out do not fit"
+    c.x_dtype = MOE_BF16 if x.dtype == torch.int8 else _float_type(x)
+    c.out_dtype = _float_type(out)
+    c.ldx, c.ldw, c.ldo = _ld(x), _ld(w), _ld(out)
+    return c
+
+
+def quantize_rows(x: torch.Tensor, stream=None):
+    """-> (codes int8 [rows, K], a view of rows padded to 16 bytes; scales fp32 [rows]) of float rows [rows, K]."""
+    rows, K = x.shape
+    q = torch.empty((rows, (K + 15) // 16 * 16), dtype=torch.int8, device=x.device)
+    scale = torch.empty((rows,), dtype=torch.float32, device=x.device)
+    moe_quantize_rows(x, q, scale, stream)
+    return q[:, :K], scale
+
+
+def _torch_stream(stream) -> torch.cuda.Stream:
+    if stream is None:
+        return torch.cuda.current_stream()
+    return stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream))
+
+
+class Int8Linear:
+    """A projection with 8-bit weights: codes w [N, K] (rows padded to 16 bytes, as quantize_rows makes them), w_scale [N] and
+    an optional bias [N] in fp32.  Calling it enqueues one product on `stream`; the workspace for float tokens is kept and
+    grows with the largest call, so calls that may overlap (streams without order between them) need an object each."""
+
+    def __init__(self, w: torch.Tensor, w_scale: torch.Tensor, bias: Optional[torch.Tensor] = None):
+        self.w, self.w_scale, self.bias = w, w_scale, bias
+        self.ws = self.ws_stream = None
+
+    @classmethod
+    def quantize(cls, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, stream=None) -> "Int8Linear":
+        """From a float weight [N, K]."""
+        return cls(*quantize_rows(weight, stream), bias)
+
+    def _workspace(self, need: int, device, stream) -> torch.Tensor:
+        # memory belongs to the stream it was taken on: its reuse after a larger call has replaced it waits for every stream that read it
+        if self.ws is None or self.ws.numel() < need:
+            self.ws_stream = _torch_stream(stream)
+            with torch.cuda.stream(self.ws_stream):
+                self.ws = torch.empty((need,), dtype=torch.uint8, device=device)
+        elif stream is not None or torch.cuda.current_stream() != self.ws_stream:
+            s = _torch_stream(stream)
+            if s != self.ws_stream:
+                self.ws.record_stream(s)
+        return self.ws
+
+    def __call__(self, x: torch.Tensor, x_scale: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                 stream=None) -> torch.Tensor:
+        """x: float tokens [T, K], or their codes with x_scale [T].  out: [T, N] bf16 or fp32 (default: a new fp32 tensor)."""
+        if out is None:
+            with torch.cuda.stream(_torch_stream(stream)):
+                out = torch.empty((x.shape[0], self.w.shape[0]), dtype=torch.float32, device=x.device)
+        c = int8_config(x, self.w, out)
+        if x.dtype == torch.int8:
+            assert x_scale is not None, "codes come with their scales"
+            moe_matmul_int8(c, x, x_scale, self.w, self.w_scale, self.bias, out, stream)
+            return out
+        ws = self._workspace(moe_linear_int8_workspace_bytes(c), x.device, stream)
+        moe_linear_int8(c, x, self.w, self.w_scale, self.bias, out, ws, ws.numel(), stream)
+        return out
+
+
+class LogprobBuffers:
+    """Device buffers of moe_token_logprobs for T rows of V logits."""
+
+    def __init__(self, T: int, n_given: int, n_top: int, V: int, device="cuda"):
+        f32 = dict(dtype=torch.float32, device=device)
+        self.T, self.V, self.n_given, self.n_top = T, V, n_given, n_top
+        self.token_logp = torch.empty((T, n_given), **f32)
+        self.entropy, self.conf = torch.empty((T,), **f32), torch.empty((T,), **f32)
+        self.top_idx = torch.empty((T, n_top), dtype=torch.int32, device=device)
+        self.top_logp = torch.empty((T, n_top), **f32)
+        self.c = {}
+        need = 0
+        for dtype in (MOE_BF16, MOE_FP32):
+            c = self.c[dtype] = moe_logprobs_config()
+            c.T, c.V, c.dtype, c.n_given, c.n_top, c.ld = T, V, dtype, n_given, n_top, V
+            need = max(need, moe_token_logprobs_workspace_bytes(c))
+        self.ws = torch.empty((need,), dtype=torch.uint8, device=device)
+
+    def run(self, logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, stream=None) -> "LogprobBuffers":
+        """logits [T, V] bf16 or fp32, tokens int32 [T, n_given]."""
+        assert tuple(logits.shape) == (self.T, self.V), "logits do not fit the buffers"
+        assert self.n_given == 0 or (tokens.dtype == torch.int32 and tuple(tokens.shape) == (self.T, self.n_given))
+        c = self.c[_float_type(logits)]
+        c.ld = _ld(logits)
+        moe_token_logprobs(c, logits, tokens, self.token_logp, self.entropy, self.conf, self.top_idx, self.top_logp, self.ws,
+                           self.ws.numel(), stream)
+        return self
+
+
 def torch_dtype(cfg: LayerConfig):
     return torch.float32 if cfg.dtype == "fp32" else torch.bfloat16
 

@@ -22,7 +22,8 @@ int validate_config(const moe_config* cfg);
 
 // ---- optional per-kernel timing (moe_profile_*): an event pair around each launch site -------
 enum ProfKind { kProfRouterGemm = 0, kProfRouteTopk, kProfDispatch, kProfFfnGateUp, kProfFfnDown,
-                kProfCombine, kProfConfidence, kProfDecodeStep, kProfKinds };
+                kProfCombine, kProfConfidence, kProfDecodeStep, kProfQuantize, kProfInt8Product, kProfLogprobs,
+                kProfKinds };
 void prof_mark(int kind, bool begin, hipStream_t s);
 struct ProfScope {
   int kind; hipStream_t s;
@@ -154,5 +155,19 @@ int launch_combine(const moe_config& c, const float* y, const float* w, const in
 // out[t] += sum over the ranks j_lo <= j < k_t[t]; tokens without such ranks are not written
 int launch_combine_add(const moe_config& c, const float* y, const float* w, const int32_t* inv_pos,
                        const int32_t* k_t, int j_lo, void* out, hipStream_t s);
+
+// ---- the output head: 8-bit product and log probabilities (head_api.hip resolves the dense leading dimensions) -----
+int launch_quantize_rows(const void* x, int dtype, int rows, int K, int64_t ldx, int8_t* q, int64_t ldq, float* scale, hipStream_t s);
+struct Int8Args {
+  int T, N, K, out_dtype;
+  int64_t ldx, ldw, ldo;
+  const int8_t* x; const float* x_scale;
+  const int8_t* w; const float* w_scale; const float* bias;
+  void* out;
+};
+int launch_int8_product(const Int8Args& a, hipStream_t s);
+int launch_logprobs(const moe_logprobs_config& c, const void* logits, const int32_t* tokens, float* token_logp, float* entropy, float* conf,
+                    int32_t* top_idx, float* top_logp, void* ws, hipStream_t s);
+size_t logprobs_workspace_bytes(const moe_logprobs_config& c);
 
 }  // namespace mm
