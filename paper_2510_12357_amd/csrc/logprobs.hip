@@ -1,15 +1,19 @@
 // Log probabilities of given tokens, entropy, confidence and most probable tokens of output distributions.
 //
-// One pass over a row.  A wave keeps the best n entries it has seen as a sorted list, entry j in lane j; m is the first of them.  For
-// every other entry z, with d = z - m:
-//     R += e^d        A += e^d d        so that   log sum = log(1 + R),   entropy = log(1 + R) - A / (1 + R)   where the wave saw the whole row.
-// The largest entry itself is in no sum: log p of a nearly certain token is -log(1 + R) with all digits of R.
-// A batch of a wave (kPerLane entries per lane) is compared with the list's last entry by one maximum per lane and one ballot.  Only where
-// some entry is above it are entries exchanged with the list's, what leaves the list is summed with the batch, and m moves (R and A
-// are rescaled); there are about n log(V / n) such entries in a row.  So the ordinary batch costs a difference, an
-// exponential and three further operations per entry, and no reference to other lanes.
+// One pass over a row.  A wave keeps the best n entries it has seen as a sorted list, entry j in lane j.  For every other entry z, with
+// d = z log2 e - c, c an fp32 number not far below the wave's largest entry times log2 e:
+//     R += 2^d,    A += 2^d d        (one fused multiply-add rounds d once; c is what it is, so nothing is lost in it).
+// With m the row's largest entry, R and A of all entries but that one, and relative to m:
+//     log sum = log(1 + R),    entropy = log(1 + R) - ln 2 A / (1 + R),    log p of z = (z - m) - log(1 + R).
+// The largest entry itself is in no sum, so log p of a nearly certain token, -log(1 + R), has all digits of R.
+//
+// A batch of a wave (kPerLane entries per lane) is compared with the list's last entry by one maximum per lane and one ballot, on the exponents d,
+// which follow the order of the entries.  Only where one is not below it, entries go to the list, and what the list drops is summed.  A lower bound of the n-th entry is known from the
+// start: the n-th of the lanes' maxima over the first batches, which wait in registers; about n (1 + log(V / seen)) entries of a row are
+// above what is known when they come.  So the ordinary batch costs a multiply-add, an exponential and three and a half
+// further operations per entry, and nothing crosses the lanes.
 // Waves of a row (and workgroups, where rows are few) take batches in turn and are joined at the end: sums by the rule of a
-// streaming softmax, lists by counting for each candidate how many come before it.
+// streaming softmax, lists by counting for each candidate how many come before it.  Nothing depends on which wave is first.
 #include "internal.h"
 #include "int8_device.h"
 #include "route_device.h"
@@ -18,278 +22,312 @@ namespace mm {
 namespace {
 
 typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
+typedef unsigned long long u64;
 
 constexpr int kList = MOE_MAX_ALTERNATIVES;
-constexpr int kPerLaneE = 32;                              // entries of a lane in a batch
-constexpr int kBatch = 64 * kPerLaneE;
-constexpr int kNone = 0x7fffffff;                          // id of an entry that is not there
-constexpr int kMaxParts = 16;                              // workgroups of a row
+constexpr int kPerLaneB = 16;                              // entries of a lane in a batch
+constexpr int kBatch = 64 * kPerLaneB;
+constexpr int ring(size_t bytes) { return bytes == 2 ? 4 : 2; }   // batches of a wave in registers or on their way
+constexpr int kMaxParts = 16;                              // workgroups of a row, a power of two as the waves are
+constexpr float kLead = 20.f;                              // entries may lie this far above the reference: e^20 is far from overflow
+constexpr float kLeadD = 28.f;                             // ... its exponent, less a little
+constexpr float kFloor = -200.f;                           // d is held here beside 2^d = 0
 
 struct LogprobArgs {
   const void* logits; int64_t ld;
   int V, n_given, n_top, parts;
   const int32_t* tokens;
   float* token_logp; float* entropy; float* conf; int32_t* top_idx; float* top_logp;
-  float* ws;                                               // [T][parts] of partial_floats(n) (parts > 1)
+  u64* ws;                                                 // [T][parts][partial_words(n)] (parts > 1)
 };
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 __device__ __forceinline__ float lane_f(float v, int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane)); }
 
-// (value, id) in the order value descending, id ascending
-__device__ __forceinline__ bool before(float av, int aid, float bv, int bid) { return av > bv || (av == bv && aid < bid); }
-
-// unsigned integers in the order of the floats (no NaN; the zeros are one number)
+// Entries are compared as one integer in the order (value ascending, id descending): the value's bits in the order of the floats (the
+// zeros are one number), then the id's complement.  0: no entry.  A NaN never becomes one.
 __device__ __forceinline__ unsigned order_key(float v) {
   const unsigned b = __float_as_uint(v + 0.f);
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float key_value(unsigned k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
-// the largest float below the one of the key
-__device__ __forceinline__ float below(unsigned key) { return key == 0x80000000u ? -0x1p-149f : key_value(key - 1); }
+__device__ __forceinline__ u64 entry_key(float v, int id) { return (u64)order_key(v) << 32 | (unsigned)~id; }
+__device__ __forceinline__ float entry_value(u64 k) { return k ? key_value((unsigned)(k >> 32)) : -INFINITY; }
+__device__ __forceinline__ int entry_id(u64 k) { return (int)~(unsigned)k; }
 constexpr unsigned kKeyNegInf = 0x007fffffu;               // order_key(-inf)
+// the largest float below the one of the key; -inf for what lies under all numbers
+__device__ __forceinline__ float below(unsigned key) {
+  return key <= kKeyNegInf ? -INFINITY : (key == 0x80000000u ? -0x1p-149f : key_value(key - 1));
+}
+__device__ __forceinline__ u64 lane_key(u64 v, int lane) {
+  return (u64)(unsigned)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)v, lane);
+}
 
-// What a wave (or a workgroup) knows of a row.  list_v / list_id: entry `lane` of the list, -inf / kNone where there is none.
-struct Partial { float m, R, A; };
+// A lower bound of the n-th largest key of a wave's lanes: its upper 16 bits, by halving.
+__device__ __forceinline__ unsigned nth_bound(unsigned key, int n) {
+  unsigned t = 0;
+#pragma unroll 1
+  for (unsigned bit = 0x80000000u; bit >= 0x10000u; bit >>= 1)
+    if (__popcll(__ballot(key >= (t | bit))) >= n) t |= bit;
+  return t;
+}
+
+// The exponent of an entry: z scale - c.  Where z log2 e could overflow, numbers are so far apart that an entry equals the largest or
+// is nothing beside it: any small power of two does as the scale.
+struct Exponent {
+  float scale, c;
+  __device__ __forceinline__ static bool huge(float v) { return !(fabsf(v) < 1e38f); }
+  __device__ __forceinline__ static Exponent of(float ref) {
+    const float s = huge(ref) ? 0x1p-30f : 1.44269504088896341f;
+    return {s, ref * s};
+  }
+  // of ref, seen from the reference `to` >= ref
+  __device__ __forceinline__ static float between(float ref, float to) {
+    if (ref == to) return 0.f;
+    return huge(ref) || huge(to) ? kFloor : fmaxf(of(ref).c - of(to).c, kFloor);
+  }
+};
+
+// Sums of everything but the entries of a list, relative to Exponent::of(ref); ref = -inf: of nothing.
+struct Sums {
+  float ref, R, A;
+  __device__ __forceinline__ void add(float z, Exponent x) {   // -inf adds nothing, a NaN makes R one
+    const float d = fmaf(z, x.scale, -x.c), e = __builtin_amdgcn_exp2f(d);
+    R += e;
+    A = fmaf(e, fmaxf(d, kFloor), A);
+  }
+  __device__ __forceinline__ Sums seen_from(float m) const {
+    const float d = Exponent::between(ref, m), f = __builtin_amdgcn_exp2f(d);
+    return {m, f * R, f * fmaf(d, R, A)};
+  }
+};
 
 // The state of a wave on its share of a row.
 struct Stream {
-  float lv = -INFINITY; int lid = kNone;                   // the list, entry j in lane j
-  float m = -INFINITY, ref = 0.f;                          // ref: m, or 0 while there is nothing
+  u64 list = 0;                                            // entry j in lane j
   float last = -INFINITY;                                  // the list's n-th entry
+  float ref = -INFINITY, limit = -INFINITY;                // limit: ref + kLead
+  Exponent x = {1.f, 0.f};
   float R[4] = {0.f, 0.f, 0.f, 0.f}, A[4] = {0.f, 0.f, 0.f, 0.f};   // four chains each: sums of at most V / 256 links
 
-  // entry (v, id), the same in all lanes, takes its place in the list; returns what leaves it
-  __device__ __forceinline__ float insert(float v, int id, int n, int lane) {
-    const float out = lane_f(lv, n - 1);
-    const float uv = __uint_as_float(__builtin_amdgcn_update_dpp(0x7f800000, __float_as_uint(lv), 0x138, 0xf, 0xf, false));   // of the lane before; +inf in lane 0
-    const int uid = __builtin_amdgcn_update_dpp(-1, lid, 0x138, 0xf, 0xf, false);
-    const bool b = lane < n && before(v, id, lv, lid), bu = lane > 0 && before(v, id, uv, uid);
-    lv = b ? (bu ? uv : v) : lv;
-    lid = b ? (bu ? uid : id) : lid;
-    return out;
+  __device__ __forceinline__ float exponent(float z) const { return fmaf(z, x.scale, -x.c); }
+  __device__ __forceinline__ void add(int chain, float d) {
+    const float e = __builtin_amdgcn_exp2f(d);
+    float held;                                            // fmaxf would bring a signalling NaN into order first; any NaN is in R already
+    asm("v_max_f32 %0, %1, %2" : "=v"(held) : "s"(kFloor), "v"(d));
+    R[chain] += e;
+    A[chain] = fmaf(e, held, A[chain]);
+  }
+  __device__ __forceinline__ void refer_to(float top) {
+    const float d = Exponent::between(ref, top), f = __builtin_amdgcn_exp2f(d);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) { A[c] = f * fmaf(d, R[c], A[c]); R[c] *= f; }
+    ref = top;
+    limit = top + kLead;
+    x = Exponent::of(top);
   }
 
-  // entries of x above `thr` change places with the list's.  x_max: the largest of each vector of kVec.
-  template <int N, int VEC, typename Id>
-  __device__ __forceinline__ void exchange(float (&x)[N], const float (&x_max)[N / VEC], float lane_max, float thr, int n, int lane, Id id_of) {
-    const unsigned long long hit = __ballot(lane_max > thr);
-    if (__popcll(hit) > n) {
-      // Many lanes (the first batch, rising rows): the list's last entry will be at least the n-th largest of the lanes' maxima.  Found in its
-      // upper 16 bits by halving; entries below it need not be looked at.
-      const unsigned key = order_key(lane_max);
-      unsigned t = 0;
+  // Entries of v above thr go to the list, in each turn the first lane's best one that comes before the list's last, and what the list drops to
+  // the sums.  id(j): of entry j, rising with j.
+  template <int N, typename Id>
+  __device__ __forceinline__ void exchange(float (&v)[N], float thr, int n, int lane, Id id) {
+    float top = v[0];
 #pragma unroll
-      for (int bit = 31; bit >= 16; --bit) {
-        const unsigned c = t | (1u << bit);
-        if (__popcll(__ballot(key >= c)) >= n) t = c;
-      }
-      if (t > kKeyNegInf) thr = fmaxf(thr, below(t));
+    for (int j = 1; j < N; ++j) top = fmaxf(top, v[j]);
+    if (__ballot(top > limit)) refer_to(wave_max(top));
+    // many lanes (rising rows): what is below the n-th largest of the lanes' maxima need not be looked at
+    if (__popcll(__ballot(top > thr)) > n) thr = fmaxf(thr, below(nth_bound(order_key(top), n)));
+    u64 least = lane_key(list, n - 1);
+#pragma unroll 1
+    while (__ballot(top > thr)) {
+      int at = 0;
+#pragma unroll
+      for (int j = N - 1; j > 0; --j) at = v[j] == top ? j : at;
+      at = v[0] == top ? 0 : at;
+      const u64 key = top > thr ? entry_key(top, id(at)) : 0, hit = __ballot(key > least);
+      if (!hit) break;
+      const int src = __builtin_ctzll(hit);
+      const u64 k = lane_key(key, src), out = least;
+      // the entry of the lane before; one above all in lane 0
+      const u64 up = (u64)(unsigned)__builtin_amdgcn_update_dpp(-1, (int)(list >> 32), 0x138, 0xf, 0xf, false) << 32 |
+                     (unsigned)__builtin_amdgcn_update_dpp(-1, (int)list, 0x138, 0xf, 0xf, false);
+      if (k > list && lane < n) list = k > up ? up : k;
+      least = lane_key(list, n - 1);
+      if (least) thr = fmaxf(thr, below((unsigned)(least >> 32)));
+      at = lane == src ? at : -1;
+      top = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < N; ++j) { v[j] = at == j ? -INFINITY : v[j]; top = fmaxf(top, v[j]); }
+      if (out) add(0, exponent(lane == src ? entry_value(out) : -INFINITY));
     }
-#pragma unroll
-    for (int u = 0; u < N / VEC; ++u) {
-      if (!__ballot(x_max[u] > thr)) continue;
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        unsigned long long todo = __ballot(x[u * VEC + e] > thr && x[u * VEC + e] >= last);
-        while (todo) {
-          const int src = __builtin_ctzll(todo);
-          todo &= todo - 1;
-          const float v = lane_f(x[u * VEC + e], src);
-          const int id = uniform(id_of(u, e, src));
-          if (!before(v, id, last, __builtin_amdgcn_readlane(lid, n - 1))) continue;
-          const float out = insert(v, id, n, lane);
-          if (lane == src) x[u * VEC + e] = out;
-          last = lane_f(lv, n - 1);
-        }
-      }
-    }
-    const float top = lane_f(lv, 0);
-    if (top != m) {
-      const float d = m > -INFINITY ? fmaxf(m - top, -200.f) : 0.f, f = __expf(d);
-#pragma unroll
-      for (int c = 0; c < 4; ++c) { A[c] = f * fmaf(d, R[c], A[c]); R[c] *= f; }
-      m = ref = top;
-    }
+    last = entry_value(least);
   }
 
-  // d of the lowest values and of -inf is held at -200 beside e^d = 0; a NaN stays one in e^d
-  template <int N>
-  __device__ __forceinline__ void sum(const float (&x)[N]) {
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const float d = x[j] - ref, e = __builtin_amdgcn_exp2f(d * 1.44269504088896341f);
-      R[j & 3] += e;
-      A[j & 3] = fmaf(e, fmaxf(d, -200.f), A[j & 3]);
-    }
-  }
-
-  // the list but for its first entry joins the sums; -> the wave's part, the same in all lanes
-  __device__ __forceinline__ Partial close(int n, int lane) {
-    float r = (R[0] + R[1]) + (R[2] + R[3]), a = (A[0] + A[1]) + (A[2] + A[3]);
-    if (lane > 0 && lane < n && lid != kNone) {
-      const float d = lv - ref, e = __builtin_amdgcn_exp2f(d * 1.44269504088896341f);
-      r += e;
-      a = fmaf(e, fmaxf(d, -200.f), a);
-    }
-    return {m, wave_sum(r), wave_sum(a)};
+  __device__ __forceinline__ Sums sums() const {           // the same in all lanes
+    return {ref, wave_sum((R[0] + R[1]) + (R[2] + R[3])), wave_sum((A[0] + A[1]) + (A[2] + A[3]))};
   }
 };
 
-// ---- what is written for a row: lane j < n_top holds the j-th entry (kNone: there is none) ----
-struct RowEnd {
-  float m, log_sum, sum, A;
-  __device__ __forceinline__ RowEnd(Partial p) : m(p.m), log_sum(log1pf(p.R)), sum(1.f + p.R), A(p.A) {
-    if (!(fabsf(m) < INFINITY)) log_sum = sum = NAN;
-  }
-};
+// What is written for a row by one wave: entry j of the list in lane j, s the sums of everything else.
 template <typename S>
-__device__ __forceinline__ void write_row(const LogprobArgs& a, int64_t t, Partial p, float lv, int lid, int lane) {
+__device__ __forceinline__ void write_row(const LogprobArgs& a, int64_t t, u64 list, Sums s, int lane) {
   const S* row = static_cast<const S*>(a.logits) + t * a.ld;
-  const RowEnd r(p);
-  if (lane == 0 && a.entropy) a.entropy[t] = r.log_sum - r.A / r.sum;
-  if (lane == 0 && a.conf) a.conf[t] = 1.f / r.sum;
+  float given = 0.f;
+  int id_given = -1;
   if (lane < a.n_given) {
-    const int id = a.tokens[t * a.n_given + lane];
-    a.token_logp[t * a.n_given + lane] = id < 0 || id >= a.V ? 0.f : (to_f32(row[id]) - r.m) - r.log_sum;
+    id_given = a.tokens[t * a.n_given + lane];
+    if (id_given >= 0 && id_given < a.V) given = to_f32(row[id_given]);
   }
+  const float m = entry_value(lane_key(list, 0));
+  const bool proper = fabsf(m) < INFINITY;
+  const Exponent x = Exponent::of(proper ? m : 0.f);
+  Sums rest = {m, 0.f, 0.f};
+  if (lane > 0) rest.add(entry_value(list), x);
+  s = s.seen_from(m);
+  s.R += wave_sum(rest.R);
+  s.A += wave_sum(rest.A);
+  const float off = fmaf(proper ? m : 0.f, x.scale, -x.c), f = __builtin_amdgcn_exp2f(-off);   // from c to the largest entry itself
+  const float R = f * s.R, A = f * fmaf(-off, s.R, s.A) * 0.693147180559945309f;
+  const float log_sum = proper ? log1pf(R) : NAN, sum = 1.f + R;
+  if (lane == 0 && a.entropy) a.entropy[t] = log_sum - A / sum;
+  if (lane == 0 && a.conf) a.conf[t] = proper ? 1.f / sum : NAN;
+  if (lane < a.n_given) a.token_logp[t * a.n_given + lane] = id_given >= 0 && id_given < a.V ? (float)(((double)given - m) - log_sum) : 0.f;
   if (!a.n_top) return;
-  const int found = __popcll(__ballot(lane < a.n_top && lid != kNone));
+  const int found = __popcll(__ballot(lane < a.n_top && list));
+  int id = entry_id(list);
   if (found < a.n_top) {
     // every entry above -inf is in the list, so the places behind them go to the lowest ids that are not in it (of the first 64: at most
     // 31 are); these are n_top - found <= V - found many
     bool free_id = lane < a.V;
-    for (int j = 0; j < found; ++j) free_id &= __builtin_amdgcn_readlane(lid, j) != lane;
-    unsigned long long ids = __ballot(free_id);
+    for (int j = 0; j < found; ++j) free_id &= __builtin_amdgcn_readlane(id, j) != lane;
+    u64 ids = __ballot(free_id);
     for (int j = found; j < a.n_top; ++j) {
-      const int id = __builtin_ctzll(ids);
+      const int next = __builtin_ctzll(ids);
       ids &= ids - 1;
-      if (lane == j) lid = id;
+      if (lane == j) id = next;
     }
   }
   if (lane < a.n_top) {
-    a.top_idx[t * a.n_top + lane] = lid;
-    a.top_logp[t * a.n_top + lane] = (lv - r.m) - r.log_sum;
+    a.top_idx[t * a.n_top + lane] = id;
+    a.top_logp[t * a.n_top + lane] = (float)(((double)entry_value(list) - m) - log_sum);
   }
 }
 
-// ---- joining of parts in LDS ----
+// ---- joining of lists and sums in LDS ----
 constexpr int kMaxLists = 16;
+constexpr int kMaxRanked = 256;
 struct Joint {
-  float m[kMaxLists], R[kMaxLists], A[kMaxLists];
-  float v[kMaxLists * kList]; int id[kMaxLists * kList];   // list w from w * n on
-  float cv[kMaxLists * kList]; int cid[kMaxLists * kList]; // candidates
-  float ov[kList]; int oid[kList];
-  int count;
-  unsigned bound;                                          // key of the largest n-th entry of any list so far
+  u64 cand[kMaxLists * kList + 8];
+  u64 out[kList];
+  float ref[kMaxLists], R[kMaxLists], A[kMaxLists];
+  int found[kMaxLists], count;
+  unsigned low, bound;                                     // keys: lower bounds of the row's n-th entry
+  unsigned key[kMaxRanked];
 };
-// One workgroup joins `lists` lists of n entries; the result is for its first wave: lane j has the j-th entry.
-__device__ __forceinline__ Partial join(Joint& s, int lists, int n, int tid, int threads, float& lv, int& lid) {
-  const int lane = tid & 63;
-  if (tid < kList) s.oid[tid] = kNone;
-  if (tid < kList) s.ov[tid] = -INFINITY;
-  if (tid == 0) s.count = 0;
-  float tau = -INFINITY;
-  for (int w = 0; w < lists; ++w) tau = fmaxf(tau, s.v[w * n + n - 1]);
-  __syncthreads();
-  for (int i = tid; i < lists * n; i += threads) {
-    if (s.id[i] != kNone && s.v[i] >= tau) {
-      const int at = atomicAdd(&s.count, 1);
-      s.cv[at] = s.v[i];
-      s.cid[at] = s.id[i];
-    }
+__device__ __forceinline__ void open_joint(Joint& s, int tid) {
+  if (tid < kList) s.out[tid] = 0;
+  if (tid == 0) { s.count = 0; s.bound = 0; s.low = ~0u; }
+}
+
+// A lower bound of the n-th of a workgroup's lane maxima (`waves` waves have one).  The k-th of a wave, k = n / waves, the smallest of the
+// waves': k lanes of each are no less, in all about 4 n lanes; their maxima are ranked.
+__device__ __forceinline__ unsigned joint_bound(Joint& s, float top, bool any, int waves, int n, int tid) {
+  const int lane = tid & 63, k = (n + waves - 1) / waves;
+  const unsigned key = order_key(top);
+  if (any) {
+    const unsigned t = k == 1 ? order_key(wave_max(top)) : nth_bound(key, k);
+    if (lane == 0) atomicMin(&s.low, t);
   }
+  __syncthreads();
+  const unsigned low = s.low;
+  const bool in = any && key >= low;
+  const u64 mask = __ballot(in);
+  int at = 0;
+  if (mask && lane == 0) at = atomicAdd(&s.count, __popcll(mask));
+  at = uniform(at) + __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0));
+  if (in && at < kMaxRanked) s.key[at] = key;
   __syncthreads();
   const int count = s.count;
-  for (int i = tid; i < count; i += threads) {
-    const float v = s.cv[i];
-    const int id = s.cid[i];
+  if (count <= kMaxRanked && tid < count) {
+    const unsigned mine = s.key[tid];
     int rank = 0;
-    for (int k = 0; k < count; ++k) rank += before(s.cv[k], s.cid[k], v, id);
-    if (rank < n) { s.ov[rank] = v; s.oid[rank] = id; }
+    for (int i = 0; i < count; ++i) rank += s.key[i] > mine || (s.key[i] == mine && i < tid);
+    if (rank == n - 1) s.bound = mine;
   }
   __syncthreads();
-  Partial p = {0.f, 0.f, 0.f};
-  if (tid < 64) {
-    lv = lane < n ? s.ov[lane] : -INFINITY;
-    lid = lane < n ? s.oid[lane] : kNone;
-    const bool in = lane < lists;
-    const float mw = in ? s.m[lane] : -INFINITY;
-    p.m = wave_max(mw);
-    const int first = __builtin_ctzll(__ballot(mw == p.m) | (1ull << 63));
-    float r = 0.f, q = 0.f;
-    if (in) {
-      r = s.R[lane];
-      q = s.A[lane];
-      if (lane != first) {                                 // its largest entry is one of the others now
-        const float d = fmaxf(mw - p.m, -200.f), f = __expf(d);
-        q = f * (fmaf(d, r, q) + d);
-        r = f * (r + 1.f);
-        if (mw == -INFINITY) q = r = s.R[lane] * 0.f;      // nothing in it (or a NaN)
-      }
-    }
-    p.R = wave_sum(r);
-    p.A = wave_sum(q);
-  }
-  return p;
+  return max(low, s.bound);
 }
 
-__host__ __device__ constexpr int partial_floats(int n) { return 4 + 2 * n; }
+// A wave's list (no gaps) goes behind those of the waves before it: the order of the sums must not depend on who comes first.
+__device__ __forceinline__ void put_list(Joint& s, int lists, int w, int n, int lane, u64 list) {
+  const int found = __popcll(__ballot(lane < n && list));
+  if (lane == 0) s.found[w] = found;
+  __syncthreads();
+  const int f = lane < lists ? s.found[lane] : 0;
+  const int at = wave_reduce(lane < w ? f : 0, 0, [](int x, int y) { return x + y; });
+  if (lane < found) s.cand[at + lane] = list;
+  if (w == lists - 1 && lane == 0) s.count = at + found;
+}
+// Candidates and sums are in place (no barrier since).  -> for the first wave: the n best, and the sums of everything else.
+__device__ __forceinline__ Sums join(Joint& s, int lists, int n, int tid, u64& list) {
+  __syncthreads();
+  const int count = s.count, lane = tid & 63;
+  if (tid < count) {
+    const u64 mine = s.cand[tid];
+    int rank = 0;
+    for (int k = 0; k < count; k += 8) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) rank += k + i < count && s.cand[k + i] > mine;
+    }
+    if (rank < n) s.out[rank] = mine;
+  }
+  __syncthreads();
+  Sums sum = {-INFINITY, 0.f, 0.f};
+  if (tid < 64) {
+    list = lane < n ? s.out[lane] : 0;
+    const u64 least = lane_key(list, n - 1);
+    sum.ref = entry_value(lane_key(list, 0));
+    const Exponent x = Exponent::of(sum.ref);
+    for (int i = lane; i < count; i += 64) if (s.cand[i] < least) sum.add(entry_value(s.cand[i]), x);
+    if (lane < lists) {
+      const Sums w = Sums{s.ref[lane], s.R[lane], s.A[lane]}.seen_from(sum.ref);
+      sum.R += w.R;
+      sum.A += w.A;
+    }
+    sum.R = wave_sum(sum.R);
+    sum.A = wave_sum(sum.A);
+  }
+  return sum;
+}
+
+__host__ __device__ constexpr int partial_words(int n) { return 2 + n; }
 
 // W waves per row part; W == 1: a workgroup is one wave with a row of its own.
 template <typename S, int W>
 __global__ __launch_bounds__(W * 64) void logprobs_kernel(const LogprobArgs a) {
-  constexpr int kVec = 16 / sizeof(S), U = kPerLaneE / kVec;
-  __shared__ Joint s;
+  constexpr int kVec = 16 / sizeof(S), U = kPerLaneB / kVec, kRing = ring(sizeof(S));
+  __shared__ Joint s_joint;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int n = a.n_top > 1 ? a.n_top : 1;
   const int part = a.parts > 1 ? (int)(blockIdx.x % (unsigned)a.parts) : 0;
   const int64_t t = a.parts > 1 ? blockIdx.x / (unsigned)a.parts : blockIdx.x;
   const S* row = static_cast<const S*>(a.logits) + t * a.ld;
-  // vectors of 16 bytes on their own alignment; the row starts `shift` entries behind the first one's
-  const int shift = (int)(((uintptr_t)row & 15) / sizeof(S));
-  const S* base = row - shift;
-  const int end = shift + a.V;
-  const int batches = (end + kBatch - 1) / kBatch, stride = W * a.parts;
-  if (W > 1) {
-    if (tid == 0) s.bound = 0;
-    __syncthreads();
-  }
+  // `head` entries up to the first multiple of 16 bytes, `vectors` vectors of 16 bytes in batches, the last of them not full, and `tail`
+  // entries; head and tail are one further batch at the end, one entry a lane
+  const int head = min(a.V, (int)((-(uintptr_t)row & 15) / sizeof(S)));
+  const int vectors = (a.V - head) / kVec, tail = (a.V - head) % kVec;
+  const int full = vectors / (64 * U), stride = W * a.parts, first = part * W + wave;
+  const char* body = reinterpret_cast<const char*>(row + head);
+  constexpr unsigned kNegInf2 = sizeof(S) == 2 ? 0xff80ff80u : 0xff800000u;
   auto load = [&](int b, u32x4 (&raw)[U]) {
-    const int e0 = b * kBatch;
-    if (e0 >= shift && e0 + kBatch <= end) {
-      const u32x4* p = reinterpret_cast<const u32x4*>(base + e0) + lane;
+    const char* p = body + (int64_t)b * (64 * U * 16);
 #pragma unroll
-      for (int u = 0; u < U; ++u) raw[u] = p[u * 64];
-    } else {
-      // an edge of the row: only entries of it are read, the others are -inf
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int e = e0 + (u * 64 + lane) * kVec;
-        if (e >= shift && e + kVec <= end) {
-          raw[u] = *reinterpret_cast<const u32x4*>(base + e);
-        } else {
-          constexpr S kNegInf = (S)(sizeof(S) == 2 ? 0xff80 : 0);
-          S part[kVec];
-#pragma unroll
-          for (int i = 0; i < kVec; ++i) {
-            if constexpr (sizeof(S) == 2) part[i] = kNegInf; else part[i] = -INFINITY;
-            if (e + i >= shift && e + i < end) part[i] = base[e + i];
-          }
-          raw[u] = __builtin_bit_cast(u32x4, part);
-        }
-      }
-    }
+    for (int u = 0; u < U; ++u) raw[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + (unsigned)lane * 16u + u * 1024));
   };
-  Stream st;
-  u32x4 raw[U], next[U];
-  int b = part * W + wave;
-  if (b < batches) load(b, raw);
-  for (; b < batches; b += stride) {
-    if (b + stride < batches) load(b + stride, next);
-    float x[kPerLaneE], x_max[U];
+  float x[kPerLaneB];
+  auto widen = [&](const u32x4 (&raw)[U]) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
+    for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if constexpr (sizeof(S) == 2) {
@@ -299,77 +337,131 @@ __global__ __launch_bounds__(W * 64) void logprobs_kernel(const LogprobArgs a) {
           x[u * 4 + i] = __uint_as_float(raw[u][i]);
         }
       }
-      x_max[u] = x[u * kVec];
+  };
+  Stream st;
+  float bound = -INFINITY;
+  // the batch in x.  rising: its ids lie behind all that the list has
+  auto process = [&](bool rising, auto id) {
+    const float thr = fmaxf(rising ? st.last : below(order_key(st.last)), bound);
+    const float thr_d = fminf(thr > -INFINITY && st.ref > -INFINITY ? st.exponent(thr) : -INFINITY, kLeadD);
+    float d[kPerLaneB], top = -INFINITY;
 #pragma unroll
-      for (int e = 1; e < kVec; ++e) x_max[u] = fmaxf(x_max[u], x[u * kVec + e]);
-    }
-    float top = x_max[0];
+    for (int j = 0; j < kPerLaneB; ++j) { d[j] = st.exponent(x[j]); top = fmaxf(top, d[j]); }
+    if (__ballot(top >= thr_d)) {
+      st.exchange(x, thr, n, lane, id);
 #pragma unroll
-    for (int u = 1; u < U; ++u) top = fmaxf(top, x_max[u]);
-    // A wave's own ids rise, so an entry equal to its list's last comes behind it; one equal to another wave's may come before.
-    // What is above m always enters, so that m bounds what is summed.
-    float thr = st.last;
-    if (W > 1) {
-      const unsigned k = *(volatile unsigned*)&s.bound;
-      if (k > kKeyNegInf) thr = fmaxf(thr, fminf(below(k), st.m));
+      for (int j = 0; j < kPerLaneB; ++j) d[j] = st.exponent(x[j]);
     }
-    if (__ballot(top > thr)) {
-      const float was = st.last;
-      st.template exchange<kPerLaneE, kVec>(x, x_max, top, thr, n, lane, [&](int u, int e, int l) { return b * kBatch + (u * 64 + l) * kVec + e - shift; });
-      if (W > 1 && st.last > was && lane == 0) atomicMax(&s.bound, order_key(st.last));
-    }
-    st.sum(x);
 #pragma unroll
-    for (int u = 0; u < U; ++u) raw[u] = next[u];
+    for (int j = 0; j < kPerLaneB; ++j) st.add(j & 3, d[j]);
+  };
+  u32x4 raw[kRing][U];
+  const int last = first < full ? first + (full - 1 - first) / stride * stride : -1;   // this wave's last full batch
+  if (last >= 0) {
+#pragma unroll
+    for (int i = 0; i < kRing; ++i) load(min(first + i * stride, last), raw[i]);
   }
-  Partial p = st.close(n, lane);
+  if (W > 1 ? part * W < full : last >= 0) {
+    float top = -INFINITY;
+    if (last >= 0) {
+#pragma unroll
+      for (int i = 0; i < kRing; ++i) {
+        widen(raw[i]);
+#pragma unroll
+        for (int j = 0; j < kPerLaneB; ++j) top = fmaxf(top, x[j]);   // a NaN is dropped; a batch that is there twice counts as one
+      }
+    }
+    if constexpr (W > 1) {
+      open_joint(s_joint, tid);
+      __syncthreads();
+      bound = below(joint_bound(s_joint, top, last >= 0, min(W, full - part * W), n, tid));
+    } else {
+      bound = below(nth_bound(order_key(top), n));
+    }
+  } else if (W > 1) {
+    open_joint(s_joint, tid);
+  }
+  for (int b = first; b <= last; b += kRing * stride) {
+#pragma unroll
+    for (int i = 0; i < kRing; ++i) {
+      const int at = b + i * stride;
+      if (at > last) break;
+      widen(raw[i]);
+      load(min(at + kRing * stride, last), raw[i]);
+      // a wave's ids rise from batch to batch, so an entry equal to its list's last comes behind it; one equal to another wave's may come before
+      process(true, [&](int j) { return head + ((at * U + j / kVec) * 64 + lane) * kVec + j % kVec; });
+    }
+  }
+  // the batch that is not full, then head and tail
+#pragma unroll 1
+  for (int b = full + ((first - full) & (stride - 1)); b < full + 2; b += stride) {
+    const bool ends = b > full;
+    if (ends ? head + tail == 0 : vectors % (64 * U) == 0) continue;
+    u32x4 rest[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      rest[u] = u32x4{kNegInf2, kNegInf2, kNegInf2, kNegInf2};
+      const int v = (full * U + u) * 64 + lane;
+      if (!ends && v < vectors) rest[u] = reinterpret_cast<const u32x4*>(body)[v];
+    }
+    const int at = lane < head ? lane : (lane >= 32 && lane - 32 < tail ? a.V - tail + lane - 32 : -1);
+    if (ends && at >= 0) {
+      if constexpr (sizeof(S) == 2) rest[0][0] = 0xff800000u | row[at]; else rest[0][0] = __float_as_uint(row[at]);
+    }
+    widen(rest);
+    process(false, [&](int j) { return ends ? at : head + ((full * U + j / kVec) * 64 + lane) * kVec + j % kVec; });
+  }
+  Sums sum = st.sums();
   if constexpr (W > 1) {
-    if (lane == 0) { s.m[wave] = p.m; s.R[wave] = p.R; s.A[wave] = p.A; }
-    if (lane < n) { s.v[wave * n + lane] = st.lv; s.id[wave * n + lane] = st.lid; }
-    __syncthreads();
-    p = join(s, W, n, tid, W * 64, st.lv, st.lid);
+    Joint& s = s_joint;
+    if (lane == 0) { s.ref[wave] = sum.ref; s.R[wave] = sum.R; s.A[wave] = sum.A; }
+    put_list(s, W, wave, n, lane, st.list);
+    sum = join(s, W, n, tid, st.list);
     if (wave) return;
   }
   if (a.parts > 1) {
-    float* o = a.ws + (t * a.parts + part) * partial_floats(n);
-    if (lane == 0) { o[0] = p.m; o[1] = p.R; o[2] = p.A; }
-    if (lane < n) { o[4 + lane] = st.lv; o[4 + n + lane] = __int_as_float(st.lid); }
+    u64* o = a.ws + (t * a.parts + part) * partial_words(n);
+    if (lane == 0) { o[0] = (u64)__float_as_uint(sum.R) << 32 | __float_as_uint(sum.ref); o[1] = __float_as_uint(sum.A); }
+    if (lane < n) o[2 + lane] = st.list;
     return;
   }
-  write_row<S>(a, t, p, st.lv, st.lid, lane);
+  write_row<S>(a, t, st.list, sum, lane);
 }
 
-// Joins the parts of a row.
+// Joins the parts of a row: one wave for each.
 template <typename S>
-__global__ __launch_bounds__(256) void logprobs_join_kernel(const LogprobArgs a) {
+__global__ __launch_bounds__(kMaxParts * 64) void logprobs_join_kernel(const LogprobArgs a) {
   __shared__ Joint s;
-  const int tid = threadIdx.x, lane = tid & 63;
+  const int tid = threadIdx.x, lane = tid & 63, part = uniform(tid >> 6);
   const int n = a.n_top > 1 ? a.n_top : 1;
   const int64_t t = blockIdx.x;
-  const float* in = a.ws + t * a.parts * partial_floats(n);
-  for (int i = tid; i < a.parts * n; i += 256) {
-    const int w = i / n, j = i - w * n;
-    s.v[i] = in[w * partial_floats(n) + 4 + j];
-    s.id[i] = __float_as_int(in[w * partial_floats(n) + 4 + n + j]);
+  const u64* in = a.ws + (t * a.parts + part) * partial_words(n);
+  u64 list = lane < n ? in[2 + lane] : 0;
+  const u64 w0 = in[0], w1 = in[1];
+  open_joint(s, tid);
+  if (lane == 0) {
+    s.ref[part] = __uint_as_float((unsigned)w0);
+    s.R[part] = __uint_as_float((unsigned)(w0 >> 32));
+    s.A[part] = __uint_as_float((unsigned)w1);
   }
-  if (tid < a.parts) { s.m[tid] = in[tid * partial_floats(n)]; s.R[tid] = in[tid * partial_floats(n) + 1]; s.A[tid] = in[tid * partial_floats(n) + 2]; }
-  __syncthreads();
-  float lv; int lid;
-  const Partial p = join(s, a.parts, n, tid, 256, lv, lid);
-  if (tid < 64) write_row<S>(a, t, p, lv, lid, lane);
+  put_list(s, a.parts, part, n, lane, list);
+  const Sums sum = join(s, a.parts, n, tid, list);
+  if (tid < 64) write_row<S>(a, t, list, sum, lane);
 }
+static_assert(kMaxParts <= kMaxLists && kList <= 64, "one thread per candidate");
 
-// Waves per row part and parts per row.
+// Waves per row part and parts per row.  us, waves x parts: 4096 rows of 131072 bf16 1x1 208, 4x1 223; 1999 of 50257 bf16 1x1 55.3, 4x1 54.0, 8x1 64;
+// 600 of 100000 fp32 1x1 64.3, 4x1 54.5, 8x1 60.7; 300 of 50257 bf16 1x1 38.4, 4x1 21.7, 8x1 18.5, 8x2 24.0; 128 of 151001 fp32 8x1 31.5, 8x2 30.5,
+// 8x4 38.0; 64 of 131072 fp32 8x1 32.6, 8x4 24.9, 8x8 34.5; 1 of 131072 bf16 8x1 18.3, 8x4 13.0, 8x8 12.6.  Sixteen waves were slower
+// than eight everywhere.
 struct Split { int waves, parts; };
 Split split_of(int T, int V) {
   const int batches = V / kBatch + 1;
-  if (T >= 1024) return {1, 1};
-  int waves = T >= 256 ? 4 : 16;
-  while (waves > 4 && waves > batches) waves /= 2;
-  if (batches < 4) waves = 1;
+  if (T >= 2048 || batches < 4) return {1, 1};
+  if (T >= 400 || batches < 8) return {4, 1};
   int parts = 1;
-  if (waves == 16) while (parts < kMaxParts && T * parts * 2 <= 256 && batches >= 16 * parts * 2) parts *= 2;
-  return {waves, parts};
+  while (parts < kMaxParts && T * parts * 2 <= 256 && batches >= 64 * parts) parts *= 2;
+  return {8, parts};
 }
 
 template <typename S>
@@ -378,12 +470,11 @@ int launch(const LogprobArgs& a, int T, int waves, hipStream_t s) {
   switch (waves) {
     case 1: hipLaunchKernelGGL((logprobs_kernel<S, 1>), grid, dim3(64), 0, s, a); break;
     case 4: hipLaunchKernelGGL((logprobs_kernel<S, 4>), grid, dim3(256), 0, s, a); break;
-    case 8: hipLaunchKernelGGL((logprobs_kernel<S, 8>), grid, dim3(512), 0, s, a); break;
-    default: hipLaunchKernelGGL((logprobs_kernel<S, 16>), grid, dim3(1024), 0, s, a); break;
+    default: hipLaunchKernelGGL((logprobs_kernel<S, 8>), grid, dim3(512), 0, s, a); break;
   }
   int rc = hip_fail(hipGetLastError(), "logprobs_kernel launch");
   if (rc || a.parts == 1) return rc;
-  hipLaunchKernelGGL(logprobs_join_kernel<S>, dim3((unsigned)T), dim3(256), 0, s, a);
+  hipLaunchKernelGGL(logprobs_join_kernel<S>, dim3((unsigned)T), dim3((unsigned)(a.parts * 64)), 0, s, a);
   return hip_fail(hipGetLastError(), "logprobs_join_kernel launch");
 }
 
@@ -391,14 +482,14 @@ int launch(const LogprobArgs& a, int T, int waves, hipStream_t s) {
 
 size_t logprobs_workspace_bytes(const moe_logprobs_config& c) {
   const Split sp = split_of(c.T, c.V);
-  return sp.parts == 1 ? 0 : align256((size_t)c.T * sp.parts * partial_floats(c.n_top > 1 ? c.n_top : 1) * sizeof(float));
+  return sp.parts == 1 ? 0 : align256((size_t)c.T * sp.parts * partial_words(c.n_top > 1 ? c.n_top : 1) * sizeof(u64));
 }
 
 int launch_logprobs(const moe_logprobs_config& c, const void* logits, const int32_t* tokens, float* token_logp, float* entropy, float* conf,
                     int32_t* top_idx, float* top_logp, void* ws, hipStream_t s) {
   ProfScope ps(kProfLogprobs, s);
   const Split sp = split_of(c.T, c.V);
-  const LogprobArgs a = {logits, c.ld, c.V, c.n_given, c.n_top, sp.parts, tokens, token_logp, entropy, conf, top_idx, top_logp, static_cast<float*>(ws)};
+  const LogprobArgs a = {logits, c.ld, c.V, c.n_given, c.n_top, sp.parts, tokens, token_logp, entropy, conf, top_idx, top_logp, static_cast<u64*>(ws)};
   return c.dtype == MOE_FP32 ? launch<float>(a, c.T, sp.waves, s) : launch<uint16_t>(a, c.T, sp.waves, s);
 }
 
