@@ -100,7 +100,7 @@ extern "C" int moe_matmul_int8(const moe_int8_config* cfg, const int8_t* x, cons
   if (!rc) rc = check_aligned(call, "x_scale", x_scale, 4);
   if (!rc) rc = check_product(call, c, w, w_scale, bias, out);
   if (rc) return rc;
-  const Int8Args a = {c.T, c.N, c.K, c.out_dtype, c.ldx, c.ldw, c.ldo, x, x_scale, w, w_scale, bias, out};
+  const Int8Args a = {c.T, c.N, c.K, c.out_dtype, c.K & ~15, c.K & 15, c.ldx, c.ldw, c.ldo, x, x_scale, w, w_scale, bias, out};
   return launch_int8_product(a, static_cast<hipStream_t>(stream));
 }
 
@@ -125,10 +125,10 @@ extern "C" int moe_linear_int8(const moe_int8_config* cfg, const void* x, const 
   int8_t* q = static_cast<int8_t*>(ws);
   float* scale = reinterpret_cast<float*>(q + codes_bytes(c));
   hipStream_t s = static_cast<hipStream_t>(stream);
+  const Int8Args a = {c.T, c.N, c.K, c.out_dtype, (int)code_ld(c.K), 0, code_ld(c.K), c.ldw, c.ldo, q, scale, w, w_scale, bias, out};
+  if (int8_quantises_itself(c.T, c.K)) return launch_int8_stream_float(a, x, c.x_dtype, c.ldx, s);
   rc = launch_quantize_rows(x, c.x_dtype, c.T, c.K, c.ldx, q, code_ld(c.K), scale, s);
-  if (rc) return rc;
-  const Int8Args a = {c.T, c.N, c.K, c.out_dtype, code_ld(c.K), c.ldw, c.ldo, q, scale, w, w_scale, bias, out};
-  return launch_int8_product(a, s);
+  return rc ? rc : launch_int8_product(a, s);
 }
 
 extern "C" size_t moe_token_logprobs_workspace_bytes(const moe_logprobs_config* cfg) {

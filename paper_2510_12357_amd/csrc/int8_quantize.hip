@@ -1,4 +1,7 @@
 // Rows of floats -> 8-bit codes and one scale per row (moe_quantize_rows).
+//
+// A workgroup per row, which it holds in registers between the largest magnitude and the codes (what does not fit is read twice), so that
+// the bound is memory: each value is read once.  One wave where it holds a row by itself, four where not.
 #include "internal.h"
 #include "route_device.h"
 #include "int8_device.h"
@@ -6,37 +9,63 @@
 namespace mm {
 namespace {
 
-// One workgroup per row, two sweeps: the largest magnitude, then the codes.
-template <typename S>
-__global__ __launch_bounds__(256) void quantize_kernel(const S* __restrict__ x, int K, int64_t ldx, int8_t* __restrict__ q, int64_t ldq,
-                                                       float* __restrict__ scale) {
-  __shared__ unsigned s_max[4];
+constexpr int kHeld = 4;                                   // vectors of 16 bytes that a thread holds
+
+template <typename X, int THREADS>
+__global__ __launch_bounds__(THREADS) void quantize_kernel(const X* __restrict__ x, int K, int64_t ldx, int8_t* __restrict__ q, int64_t ldq,
+                                                           float* __restrict__ scale) {
+  constexpr int kVec = 16 / sizeof(X);
+  __shared__ unsigned s_max[THREADS / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const S* row = x + (int64_t)blockIdx.x * ldx;
-  // magnitudes compare as their bits do, and a NaN or an infinity is above every number
+  const X* row = x + (int64_t)blockIdx.x * ldx;
+  float v[kHeld][kVec];
   unsigned top = 0;
-  for (int k = tid; k < K; k += 256) top = max(top, __float_as_uint(to_f32(row[k])) & 0x7fffffffu);
+#pragma unroll
+  for (int u = 0; u < kHeld; ++u) load_floats(row, (u * THREADS + tid) * kVec, K, v[u]);
+#pragma unroll
+  for (int u = 0; u < kHeld; ++u) top = max(top, magnitude(v[u]));
+  for (int k = (kHeld * THREADS + tid) * kVec; k < K; k += THREADS * kVec) {
+    float w[kVec];
+    load_floats(row, k, K, w);
+    top = max(top, magnitude(w));
+  }
   top = wave_reduce(top, 0u, [](unsigned a, unsigned b) { return max(a, b); });
-  if (lane == 0) s_max[wave] = top;
-  __syncthreads();
-  top = max(max(s_max[0], s_max[1]), max(s_max[2], s_max[3]));
-  const bool bad = top >= 0x7f800000u;
-  const float a = __uint_as_float(top);
-  const CodeScale c(a);
+  if constexpr (THREADS > 64) {
+    if (lane == 0) s_max[wave] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) top = max(top, s_max[w]);
+  }
+  const RowScale r(top);
   int8_t* out = q + (int64_t)blockIdx.x * ldq;
-  for (int k = tid; k < ldq; k += 256) out[k] = k < K && !bad ? (int8_t)c.code(to_f32(row[k])) : (int8_t)0;
-  if (tid == 0) scale[blockIdx.x] = bad ? NAN : a / 127.f;
+#pragma unroll
+  for (int u = 0; u < kHeld; ++u) {
+    const int k = (u * THREADS + tid) * kVec;
+    if (k < ldq) store_codes(out + k, r, v[u]);
+  }
+  for (int k = (kHeld * THREADS + tid) * kVec; k < ldq; k += THREADS * kVec) {
+    float w[kVec];
+    load_floats(row, k, K, w);
+    store_codes(out + k, r, w);
+  }
+  if (tid == 0) scale[blockIdx.x] = r.scale();
+}
+
+template <typename X>
+int launch(const void* x, int rows, int K, int64_t ldx, int8_t* q, int64_t ldq, float* scale, hipStream_t s) {
+  constexpr int kHeldByWave = 64 * kHeld * (16 / sizeof(X));
+  if (K <= kHeldByWave)
+    hipLaunchKernelGGL((quantize_kernel<X, 64>), dim3((unsigned)rows), dim3(64), 0, s, static_cast<const X*>(x), K, ldx, q, ldq, scale);
+  else
+    hipLaunchKernelGGL((quantize_kernel<X, 256>), dim3((unsigned)rows), dim3(256), 0, s, static_cast<const X*>(x), K, ldx, q, ldq, scale);
+  return hip_fail(hipGetLastError(), "quantize_kernel launch");
 }
 
 }  // namespace
 
 int launch_quantize_rows(const void* x, int dtype, int rows, int K, int64_t ldx, int8_t* q, int64_t ldq, float* scale, hipStream_t s) {
   ProfScope ps(kProfQuantize, s);
-  if (dtype == MOE_FP32)
-    hipLaunchKernelGGL(quantize_kernel<float>, dim3((unsigned)rows), dim3(256), 0, s, static_cast<const float*>(x), K, ldx, q, ldq, scale);
-  else
-    hipLaunchKernelGGL(quantize_kernel<uint16_t>, dim3((unsigned)rows), dim3(256), 0, s, static_cast<const uint16_t*>(x), K, ldx, q, ldq, scale);
-  return hip_fail(hipGetLastError(), "quantize_kernel launch");
+  return dtype == MOE_FP32 ? launch<float>(x, rows, K, ldx, q, ldq, scale, s) : launch<uint16_t>(x, rows, K, ldx, q, ldq, scale, s);
 }
 
 }  // namespace mm

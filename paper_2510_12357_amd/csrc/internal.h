@@ -160,12 +160,19 @@ int launch_combine_add(const moe_config& c, const float* y, const float* w, cons
 int launch_quantize_rows(const void* x, int dtype, int rows, int K, int64_t ldx, int8_t* q, int64_t ldq, float* scale, hipStream_t s);
 struct Int8Args {
   int T, N, K, out_dtype;
+  int K16, k_tail;         // codes in whole vectors of 16; codes of the last vector that count where it is not all of them (0: the tokens' are zero behind K)
   int64_t ldx, ldw, ldo;
   const int8_t* x; const float* x_scale;
   const int8_t* w; const float* w_scale; const float* bias;
   void* out;
 };
 int launch_int8_product(const Int8Args& a, hipStream_t s);
+int launch_int8_wide(const Int8Args& a, int token_tiles, int height, hipStream_t s);      // height: rows of a token tile, at most 256
+int launch_int8_tile(const Int8Args& a, int rows, hipStream_t s);                         // rows of a token tile: 64 or 128
+int launch_int8_stream(const Int8Args& a, hipStream_t s);                                 // T <= 64
+// the same on float tokens, quantised by every workgroup; where int8_quantises_itself says so
+bool int8_quantises_itself(int T, int K);
+int launch_int8_stream_float(const Int8Args& a, const void* x, int x_dtype, int64_t ldx, hipStream_t s);
 int launch_logprobs(const moe_logprobs_config& c, const void* logits, const int32_t* tokens, float* token_logp, float* entropy, float* conf,
                     int32_t* top_idx, float* top_logp, void* ws, hipStream_t s);
 size_t logprobs_workspace_bytes(const moe_logprobs_config& c);
