@@ -25,7 +25,13 @@ struct CodeScale {
     a = amax * up;
     inv = a > 0.f ? 127.f / a : 0.f;
   }
-  __device__ __forceinline__ int code(float x) const {
+  // as a float without its sign; near: the quotient decides nothing, exact() has to
+  __device__ __forceinline__ float quick(float x, bool& near) const {
+    const float t = fabsf(x) * up * inv, n = rintf(t);
+    near |= fabsf(t - n) > 0.49996f;
+    return n;
+  }
+  __device__ __forceinline__ float exact(float x) const {
     const float v = fabsf(x) * up, t = v * inv;
     float n = rintf(t);
     if (fabsf(t - n) > 0.49996f) {
@@ -33,21 +39,50 @@ struct CodeScale {
       const double d = 254.0 * (double)v - (double)(2.f * n + 1.f) * (double)a;
       if (d > 0.0 || (d == 0.0 && ((int)n & 1))) n += 1.f;
     }
-    return (int)copysignf(n, x);
+    return n;
   }
 };
 
-// The values k .. k + N of a row of K floats, zeros behind its end.
+typedef __attribute__((ext_vector_type(4))) int i32x4;
+// 16 bytes of a row's floats as numbers
+template <int N> __device__ __forceinline__ void widen(const i32x4 raw, const float*, float (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = __int_as_float(raw[i]);
+}
+template <int N> __device__ __forceinline__ void widen(const i32x4 raw, const uint16_t*, float (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { v[2 * i] = __int_as_float(raw[i] << 16); v[2 * i + 1] = __int_as_float(raw[i] & (int)0xffff0000); }
+}
+// Vector `at`, `at` + per, .. of a row of K floats that starts at any element: the first HELD of them, zeros behind the row's end.  The row's last
+// elements, less than a vector, are one thread's; they are read one by one, apart from the others, which are all on their way by then.
+template <typename X, int HELD>
+struct HeldRow {
+  static constexpr int kVec = 16 / sizeof(X);
+  i32x4 raw[HELD];
+  __device__ __forceinline__ void load(const X* row, int K, int at, int per) {
+    const int whole = K / kVec;
+#pragma unroll
+    for (int u = 0; u < HELD; ++u) {
+      raw[u] = i32x4{0, 0, 0, 0};
+      if (u * per + at < whole) raw[u] = load_unaligned<i32x4>(row + (u * per + at) * kVec);
+    }
+    const int rest = K - whole * kVec, u_rest = whole / per;
+    if (rest && whole - u_rest * per == at) {
+      X e[kVec];
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) e[i] = i < rest ? row[whole * kVec + i] : X(0);
+#pragma unroll
+      for (int u = 0; u < HELD; ++u) if (u == u_rest) raw[u] = __builtin_bit_cast(i32x4, e);
+    }
+  }
+  __device__ __forceinline__ void values(int u, float (&v)[kVec]) const { widen(raw[u], static_cast<const X*>(nullptr), v); }
+};
+// Such a vector by itself, from element k on.
 template <typename X, int N>
 __device__ __forceinline__ void load_floats(const X* row, int k, int K, float (&v)[N]) {
-  if (k + N <= K) {
-    const Unaligned<X, N> raw = *reinterpret_cast<const Unaligned<X, N>*>(row + k);
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = to_f32(raw.v[i]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = k + i < K ? to_f32(row[k + i]) : 0.f;
-  }
+  HeldRow<X, 1> h;
+  h.load(row + k, min(max(K - k, 0), N), 0, 1);
+  h.values(0, v);
 }
 // The largest magnitude as bits: they compare as the magnitudes do, and a NaN or an infinity is above every number.
 template <int N>
@@ -65,19 +100,24 @@ struct RowScale {
 };
 template <int N>
 __device__ __forceinline__ void store_codes(void* p, const RowScale& r, const float (&v)[N]) {
-  unsigned w[N / 4];
+  float n[N];
+  bool near = false;
 #pragma unroll
-  for (int i = 0; i < N / 4; ++i) {
-    w[i] = 0;
+  for (int i = 0; i < N; ++i) n[i] = r.code.quick(v[i], near);
+  if (near) {                                              // about one vector in a thousand
 #pragma unroll
-    for (int j = 0; j < 4; ++j) w[i] |= (unsigned)(r.code.code(v[4 * i + j]) & 0xff) << (8 * j);
-    w[i] = r.bad ? 0u : w[i];
+    for (int i = 0; i < N; ++i) n[i] = r.code.exact(v[i]);
   }
 #pragma unroll
-  for (int i = 0; i < N / 4; ++i) static_cast<unsigned*>(p)[i] = w[i];
+  for (int i = 0; i < N / 4; ++i) {
+    int q[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) q[j] = (int)copysignf(n[4 * i + j], v[4 * i + j]);
+    const unsigned w = __builtin_amdgcn_perm((unsigned)q[1], (unsigned)q[0], 0x0c0c0400u) | __builtin_amdgcn_perm((unsigned)q[3], (unsigned)q[2], 0x04000c0cu);
+    static_cast<unsigned*>(p)[i] = r.bad ? 0u : w;
+  }
 }
 
-typedef __attribute__((ext_vector_type(4))) int i32x4;
 // The first `left` (1 .. 16) of the 16 codes at p, zeros behind them.
 __device__ __forceinline__ i32x4 masked_codes(const int8_t* p, int left) {
   i32x4 v = *reinterpret_cast<const i32x4*>(p);

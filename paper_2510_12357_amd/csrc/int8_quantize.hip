@@ -13,21 +13,20 @@ constexpr int kHeld = 4;                                   // vectors of 16 byte
 
 template <typename X, int THREADS>
 __global__ __launch_bounds__(THREADS) void quantize_kernel(const X* __restrict__ x, int K, int64_t ldx, int8_t* __restrict__ q, int64_t ldq,
-                                                           float* __restrict__ scale) {
+                                                           float* __restrict__ scale, int order) {
   constexpr int kVec = 16 / sizeof(X);
   __shared__ unsigned s_max[THREADS / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const X* row = x + (int64_t)blockIdx.x * ldx;
-  float v[kHeld][kVec];
+  HeldRow<X, kHeld> held;
+  held.load(row, K, tid, THREADS);
   unsigned top = 0;
+  float v[kVec];
 #pragma unroll
-  for (int u = 0; u < kHeld; ++u) load_floats(row, (u * THREADS + tid) * kVec, K, v[u]);
-#pragma unroll
-  for (int u = 0; u < kHeld; ++u) top = max(top, magnitude(v[u]));
+  for (int u = 0; u < kHeld; ++u) { held.values(u, v); top = max(top, magnitude(v)); }
   for (int k = (kHeld * THREADS + tid) * kVec; k < K; k += THREADS * kVec) {
-    float w[kVec];
-    load_floats(row, k, K, w);
-    top = max(top, magnitude(w));
+    load_floats(row, k, K, v);
+    top = max(top, magnitude(v));
   }
   top = wave_reduce(top, 0u, [](unsigned a, unsigned b) { return max(a, b); });
   if constexpr (THREADS > 64) {
@@ -37,35 +36,37 @@ __global__ __launch_bounds__(THREADS) void quantize_kernel(const X* __restrict__
     for (int w = 0; w < THREADS / 64; ++w) top = max(top, s_max[w]);
   }
   const RowScale r(top);
-  int8_t* out = q + (int64_t)blockIdx.x * ldq;
+  int8_t* out = order ? q + (int64_t)blockIdx.x * 16 : q + (int64_t)blockIdx.x * ldq;
+  // of code k: blocks of 64 lanes x 16 codes, 1024 / order k each (order: lanes side by side, rows of the block)
+  auto place = [&](int k) { return order ? (k >> 4) * order * 16 + (k & 15) : k; };
 #pragma unroll
   for (int u = 0; u < kHeld; ++u) {
     const int k = (u * THREADS + tid) * kVec;
-    if (k < ldq) store_codes(out + k, r, v[u]);
+    held.values(u, v);
+    if (k < ldq) store_codes(out + place(k), r, v);
   }
   for (int k = (kHeld * THREADS + tid) * kVec; k < ldq; k += THREADS * kVec) {
-    float w[kVec];
-    load_floats(row, k, K, w);
-    store_codes(out + k, r, w);
+    load_floats(row, k, K, v);
+    store_codes(out + place(k), r, v);
   }
   if (tid == 0) scale[blockIdx.x] = r.scale();
 }
 
 template <typename X>
-int launch(const void* x, int rows, int K, int64_t ldx, int8_t* q, int64_t ldq, float* scale, hipStream_t s) {
+int launch(const void* x, int rows, int K, int64_t ldx, int8_t* q, int64_t ldq, float* scale, CodeOrder order, hipStream_t s) {
   constexpr int kHeldByWave = 64 * kHeld * (16 / sizeof(X));
   if (K <= kHeldByWave)
-    hipLaunchKernelGGL((quantize_kernel<X, 64>), dim3((unsigned)rows), dim3(64), 0, s, static_cast<const X*>(x), K, ldx, q, ldq, scale);
+    hipLaunchKernelGGL((quantize_kernel<X, 64>), dim3((unsigned)rows), dim3(64), 0, s, static_cast<const X*>(x), K, ldx, q, ldq, scale, (int)order);
   else
-    hipLaunchKernelGGL((quantize_kernel<X, 256>), dim3((unsigned)rows), dim3(256), 0, s, static_cast<const X*>(x), K, ldx, q, ldq, scale);
+    hipLaunchKernelGGL((quantize_kernel<X, 256>), dim3((unsigned)rows), dim3(256), 0, s, static_cast<const X*>(x), K, ldx, q, ldq, scale, (int)order);
   return hip_fail(hipGetLastError(), "quantize_kernel launch");
 }
 
 }  // namespace
 
-int launch_quantize_rows(const void* x, int dtype, int rows, int K, int64_t ldx, int8_t* q, int64_t ldq, float* scale, hipStream_t s) {
+int launch_quantize_rows(const void* x, int dtype, int rows, int K, int64_t ldx, int8_t* q, int64_t ldq, float* scale, CodeOrder order, hipStream_t s) {
   ProfScope ps(kProfQuantize, s);
-  return dtype == MOE_FP32 ? launch<float>(x, rows, K, ldx, q, ldq, scale, s) : launch<uint16_t>(x, rows, K, ldx, q, ldq, scale, s);
+  return dtype == MOE_FP32 ? launch<float>(x, rows, K, ldx, q, ldq, scale, order, s) : launch<uint16_t>(x, rows, K, ldx, q, ldq, scale, order, s);
 }
 
 }  // namespace mm

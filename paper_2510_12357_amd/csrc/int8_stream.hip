@@ -1,229 +1,285 @@
-// The 8-bit product for up to 64 tokens: every weight is read once, so memory sets the pace, and for small weights the latency of a launch.
+// The 8-bit product for up to 32 tokens: every weight is read once, so memory sets the pace, and for small weights the latency of a launch.
 //
-// A wave has R blocks of 16 weight rows and all tokens (TB blocks of 16) and goes through K in steps of 64, operands straight from memory
-// into registers, D steps ahead: a load of a weight block is 16 rows x 64 bytes, the next step's the other half of those lines.  The four waves of a
+// A wave has 32 weight rows and all tokens, and a ring of kRing chunks of 128 k of its own in LDS, which loads fill past the registers: eight lanes
+// read a line of a row.  (Operands straight into registers, in the matrix instruction's order, touch a row per lane: 64 lines an instruction,
+// and the address units set the pace; 64 x 131072 x 4096 took 227 us so.)  Nothing is shared between waves, so there is no barrier in the
+// loop.  The tokens' codes come into registers, as far ahead as the weights, because loads end in order.  The four waves of a
 // workgroup have weight rows of their own, or, where rows are few, share them and split K; their sums of integers are joined in LDS, exactly.
-// Float tokens (moe_linear_int8) are quantised by every workgroup for itself while its first weights are on their way, up to a size
-// where that costs less than a launch in front of this one.
-#include <algorithm>
+// Where the codes come from: the caller's rows; the workspace of moe_linear_int8, in the order of the matrix instruction's lanes, so that a load is
+// 1 KB in one piece; or float tokens that every workgroup quantises for itself while its first weights are on their way, up to a
+// size where that costs less than a launch in front of this one.
+#include <atomic>
+#include <type_traits>
 
 #include "internal.h"
+#include "groups.h"
 #include "int8_device.h"
-#include "route_device.h"
 #include "unaligned.h"
 
 namespace mm {
 namespace {
 
-__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((ext_vector_type(16))) int i32x16;
+
+constexpr int kRing = 4, kRowBytes = 128, kStage = 32 * kRowBytes;
+constexpr int kRingBytes = 4 * kRing * kStage;             // of a workgroup
+constexpr int kMaxFused = 16384;                           // elements of float tokens that every workgroup quantises
+constexpr int code_pitch(int K) { return (K + 127) / 128 * 128 + 16; }   // bytes of a token's codes in LDS: 16 tokens start at 16 different banks
+
+// At most N loads of this wave in flight.  An asm block, so that no load moves across it.
+template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory"); }
+
+enum Tokens { kRows, kLanes, kFloats };                    // where codes come from, as above
 
 struct FloatTokens { const void* x; int64_t ldx; };
 
-constexpr int kMaxFused = 16384;        // elements of float tokens that every workgroup quantises
-constexpr int code_pitch(int K) { return (K + 63) / 64 * 64 + 16; }   // bytes of a token's codes in LDS: 16 tokens start at 16 different banks
+// the weights of a lane for one chunk: four k-steps of the 32 x 32 instruction, or two of two blocks of the 16 x 16 one
+__device__ __forceinline__ void read_chunk(i32x4 (&w)[4], const unsigned (&at)[4], unsigned stage) {
+  asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\tds_read_b128 %2, %6\n\tds_read_b128 %3, %7\n\ts_waitcnt lgkmcnt(0)"
+               : "=&v"(w[0]), "=&v"(w[1]), "=&v"(w[2]), "=&v"(w[3]) : "v"(at[0] + stage), "v"(at[1] + stage), "v"(at[2] + stage), "v"(at[3] + stage) : "memory");
+}
 
-// X: the tokens' float type, or int8_t for codes
-template <typename S, typename X, int TB, int R>
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// codes in LDS: two k-steps of the 16 x 16 instruction
+template <int N>
+__device__ __forceinline__ void read_codes(i32x4 (&x)[N], unsigned at) {
+  static_assert(N == 2, "16 x 16 instructions");
+  asm volatile("ds_read_b128 %0, %2\n\tds_read_b128 %1, %2 offset:64\n\ts_waitcnt lgkmcnt(0)" : "=&v"(x[0]), "=&v"(x[1]) : "v"(at) : "memory");
+}
+
+// NARROW: at most 16 tokens, 16 x 16 x 64 instructions; else at most 32, 32 x 32 x 32.  X: type of float tokens.
+template <typename S, Tokens FROM, typename X, bool NARROW>
 __global__ __launch_bounds__(256) void int8_stream_kernel(const Int8Args a, const FloatTokens f, const int split) {
-  constexpr bool kFused = !std::is_same_v<X, int8_t>;
-  constexpr int D = R + TB <= 3 ? 8 : 4;
-  extern __shared__ __attribute__((aligned(16))) char s_mem[];   // codes of float tokens, then the partial sums
+  constexpr int kSteps = NARROW ? 2 : 4, kStepK = 128 / kSteps;
+  extern __shared__ __attribute__((aligned(1024))) char s_mem[];   // the rings, later partial sums; codes of float tokens
   __shared__ unsigned s_max[16];
-  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), g = lane >> 4, c = lane & 15;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const int c = NARROW ? lane & 15 : lane & 31, g = NARROW ? lane >> 4 : lane >> 5;   // token (or weight row) and group of 16 k of a lane's operand
   const int part = wave & (split - 1), group = wave / split;
-  const int n0 = uniform((blockIdx.x * (4 / split) + group) * (16 * R));
+  const int n0 = uniform((blockIdx.x * (4 / split) + group) * 32);
   const bool idle = n0 >= a.N;                             // past the last row: keeps the barriers only
-  const int whole = a.K16 >> 6;                            // steps of four whole vectors
-  const int begin = idle ? 0 : (int)((int64_t)whole * part / split), end = idle ? 0 : (int)((int64_t)whole * (part + 1) / split);
+  const int chunks = (a.K16 + kRowBytes - 1) / kRowBytes;
+  const int begin = idle ? 0 : chunks * part / split, end = idle ? 0 : chunks * (part + 1) / split;
 
-  const char* wbase = reinterpret_cast<const char*>(a.w) + (int64_t)min(n0, a.N - 1) * a.ldw;
-  unsigned woff[R], xoff[TB];
+  // ---- weights: buffer loads into LDS, rows and columns that do not exist are out of range ----
+  const int rows = idle ? 1 : min(a.N - n0, 32);
+  const __amdgpu_buffer_rsrc_t rw = make_rsrc(a.w + (int64_t)(idle ? 0 : n0) * a.ldw, (unsigned)((rows - 1) * (int)a.ldw + a.K16));
+  char* const ring = s_mem + wave * (kRing * kStage);
+  unsigned woff[4];
 #pragma unroll
-  for (int r = 0; r < R; ++r) woff[r] = (unsigned)max(min(16 * r + c, a.N - 1 - n0), 0) * (unsigned)a.ldw + 16u * g;
-  const int pitch = kFused ? code_pitch(a.K) : 0;
+  for (int p = 0; p < 4; ++p) {
+    const int r = 8 * p + (lane >> 3);
+    woff[p] = r < rows ? (unsigned)r * (unsigned)a.ldw : kOob;
+  }
+  auto load_w = [&](int stage, int k) {
 #pragma unroll
-  for (int b = 0; b < TB; ++b) xoff[b] = (unsigned)min(16 * b + c, a.T - 1) * (kFused ? (unsigned)pitch : (unsigned)a.ldx) + 16u * g;
-
-  i32x4 acc[R][TB];
-#pragma unroll
-  for (int r = 0; r < R; ++r)
-#pragma unroll
-    for (int b = 0; b < TB; ++b) acc[r][b] = i32x4{0, 0, 0, 0};
-  i32x4 wf[D][R], xf[D][TB];
-  auto load_w = [&](int d, int k) {
-#pragma unroll
-    for (int r = 0; r < R; ++r) wf[d][r] = __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(wbase + (int64_t)k * 64 + woff[r]));
+    for (int p = 0; p < 4; ++p) {
+      const unsigned at = (unsigned)(k * kRowBytes) + (unsigned)((lane & 7) ^ ((8 * p + (lane >> 3)) >> 1 & 7)) * 16u;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, (lds_void*)(ring + stage * kStage + p * 1024), 16, (int)(at < (unsigned)a.K16 ? woff[p] + at : kOob), 0, 0,
+                                               kStreamOnce);
+    }
   };
+  unsigned w_at[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = NARROW ? (i & 1) * 16 + c : c, col = NARROW ? (i >> 1) * 4 + g : 2 * i + g;
+    w_at[i] = (unsigned)(size_t)ring + (unsigned)(r * kRowBytes + (col ^ (r >> 1 & 7)) * 16);
+  }
+
+  // ---- tokens.  What stands behind K16 meets weights of zero; it only has to be there.  So do tokens behind T, which are not stored ----
+  const int pitch = code_pitch(a.K);
+  i32x4 xf[kRing][kSteps];
+  const unsigned x_at = (unsigned)(size_t)s_mem + (unsigned)(kRingBytes + min(c, a.T - 1) * pitch + 16 * g);   // (kFloats)
+  const char* const xrow = reinterpret_cast<const char*>(a.x) + (FROM == kRows ? (int64_t)min(c, a.T - 1) * a.ldx : lane * 16);
   auto load_x = [&](int d, int k) {
+    if constexpr (FROM == kFloats) { read_codes(xf[d], x_at + (unsigned)(k * 128)); return; }
 #pragma unroll
-    for (int b = 0; b < TB; ++b) xf[d][b] = *reinterpret_cast<const i32x4*>((kFused ? s_mem : reinterpret_cast<const char*>(a.x)) + (int64_t)k * 64 + xoff[b]);
+    for (int i = 0; i < kSteps; ++i) {
+      const int at = k * 128 + i * kStepK + 16 * g;
+      if constexpr (FROM == kLanes) xf[d][i] = *reinterpret_cast<const i32x4*>(xrow + (int64_t)(k * kSteps + i) * 1024);
+      else xf[d][i] = *reinterpret_cast<const i32x4*>(xrow + ((unsigned)at < (unsigned)a.K16 ? at : 0));   // a row holds 16 codes at least
+    }
   };
-  auto multiply = [&](int d) {
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-      for (int b = 0; b < TB; ++b) acc[r][b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[d][r], xf[d][b], acc[r][b], 0, 0, 0);
-  };
-#pragma unroll
-  for (int d = 0; d < D; ++d) if (begin + d < end) { load_w(d, begin + d); if (!kFused) load_x(d, begin + d); }
 
-  if constexpr (kFused) {
-    // `per` threads for a token, in turn for each of its vectors
-    constexpr int kVec = 16 / sizeof(X);
+  typedef std::conditional_t<NARROW, i32x4, i32x16> Acc;
+  constexpr int kAccs = NARROW ? 2 : 1;
+  Acc acc[kAccs] = {};
+  auto multiply = [&](int d, const i32x4 (&w)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (NARROW) acc[i & 1] = __builtin_amdgcn_mfma_i32_16x16x64_i8(xf[d][i >> 1], w[i], acc[i & 1], 0, 0, 0);
+      else acc[0] = __builtin_amdgcn_mfma_i32_32x32x32_i8(xf[d][i], w[i], acc[0], 0, 0, 0);
+    }
+  };
+  constexpr bool kAhead = FROM != kFloats;                 // codes in LDS are read when they are used
+  auto first_loads = [&]() {                               // chunks that are not there fill their stage with zeros
+#pragma unroll
+    for (int d = 0; d < kRing - 1; ++d) { load_w(d, begin + d < end ? begin + d : 1 << 20); if (kAhead) load_x(d, max(min(begin + d, chunks - 1), 0)); }
+  };
+  if constexpr (FROM == kFloats) {
+    // `per` threads for a token, in turn for each of its vectors, of which they hold the first kHeld.  Loads end in order: the tokens' first.
+    constexpr int kVec = 16 / sizeof(X), kHeld = 8;
     int per = 256;
     while (per > 16 && per * a.T > 256) per >>= 1;
     const int t = tid / per, at = tid % per;
     const X* row = static_cast<const X*>(f.x) + (int64_t)min(t, a.T - 1) * f.ldx;
+    HeldRow<X, kHeld> held;
+    held.load(row, a.K, at, per);
     if (tid < 16) s_max[tid] = 0;
-    __syncthreads();
+    asm volatile("" ::: "memory");
+    first_loads();
+    lds_barrier();
     unsigned top = 0;
-    for (int k = at * kVec; k < a.K; k += per * kVec) {
-      float v[kVec];
+    float v[kVec];
+#pragma unroll
+    for (int u = 0; u < kHeld; ++u) if (u * per * kVec < a.K) { held.values(u, v); top = max(top, magnitude(v)); }
+    for (int k = (kHeld * per + at) * kVec; k < a.K; k += per * kVec) {
       load_floats(row, k, a.K, v);
       top = max(top, magnitude(v));
     }
     for (int o = min(per, 64) / 2; o; o >>= 1) top = max(top, (unsigned)__shfl_xor((int)top, o));
     if ((at & 63) == 0 && t < a.T) atomicMax(&s_max[t], top);
-    __syncthreads();
-    if (t < a.T) {
+    lds_barrier();
+    if (t < a.T) {                                         // up to K16: there weights may be anything
       const RowScale code(s_max[t]);
-      for (int k = at * kVec; k < pitch - 16; k += per * kVec) {
-        float v[kVec];
+      char* const codes = s_mem + kRingBytes + t * pitch;
+#pragma unroll
+      for (int u = 0; u < kHeld; ++u) {
+        const int k = (u * per + at) * kVec;
+        if (k < a.K16) { held.values(u, v); store_codes(codes + k, code, v); }
+      }
+      for (int k = (kHeld * per + at) * kVec; k < a.K16; k += per * kVec) {
         load_floats(row, k, a.K, v);
-        store_codes(s_mem + t * pitch + k, code, v);
+        store_codes(codes + k, code, v);
       }
     }
-    __syncthreads();
-#pragma unroll
-    for (int d = 0; d < D; ++d) if (begin + d < end) load_x(d, begin + d);
+    lds_barrier();
+  } else {
+    first_loads();
   }
 
+  // The chunk in stage d.  In flight behind it: the chunks up to kRing - 2 further on, and their tokens' codes.
+  constexpr int kPer = 4 + (kAhead ? kSteps : 0);
+  i32x4 w[4];
   int k = begin;
-  for (; k + 2 * D <= end; k += D) {
+  for (; k + 2 * kRing - 2 < end; k += kRing) {
 #pragma unroll
-    for (int d = 0; d < D; ++d) {
-      multiply(d);
-      load_w(d, k + d + D);
-      load_x(d, k + d + D);
+    for (int d = 0; d < kRing; ++d) {
+      constexpr int kLast = kRing - 1;
+      wait_loads<(kRing - 2) * kPer>();
+      read_chunk(w, w_at, d * kStage);
+      load_w((d + kLast) % kRing, k + d + kLast);
+      if (kAhead) load_x((d + kLast) % kRing, k + d + kLast); else load_x(d, k + d);
+      multiply(d, w);
     }
   }
+  // the last chunks, fewer than 2 kRing - 1
 #pragma unroll
-  for (int d = 0; d < D; ++d) {
+  for (int d = 0; d < 2 * kRing - 2; ++d) {
     if (k + d < end) {
-      multiply(d);
-      if (k + d + D < end) { load_w(d, k + d + D); load_x(d, k + d + D); }
+      if (k + d + kRing - 2 < end) wait_loads<(kRing - 2) * kPer>();
+      else wait_loads<0>();
+      read_chunk(w, w_at, d % kRing * kStage);
+      if (k + d + kRing - 1 < end) { load_w((d + kRing - 1) % kRing, k + d + kRing - 1); if (kAhead) load_x((d + kRing - 1) % kRing, k + d + kRing - 1); }
+      if (!kAhead) load_x(d % kRing, k + d);
+      multiply(d % kRing, w);
     }
   }
-#pragma unroll
-  for (int d = 0; d < D; ++d) if (k + d + D < end) multiply(d);
-  if (part == split - 1 && !idle && ((a.K16 & 63) || a.k_tail)) {
-    // the last step: vectors beyond K are zero, one may count in part
-    const int left = (a.K16 & 63) + a.k_tail - 16 * g;
+  if (FROM == kRows && a.k_tail && part == split - 1 && !idle) {
+    // the last K % 16 codes, in the lanes of the first group
     const i32x4 zero = {0, 0, 0, 0};
 #pragma unroll
-    for (int r = 0; r < R; ++r) wf[0][r] = left > 0 ? *reinterpret_cast<const i32x4*>(wbase + (int64_t)whole * 64 + woff[r]) : zero;
+    for (int i = 0; i < 4; ++i) w[i] = zero;
+    if (g == 0) {
+      xf[0][0] = masked_codes(reinterpret_cast<const int8_t*>(xrow) + a.K16, a.k_tail);
 #pragma unroll
-    for (int b = 0; b < TB; ++b)
-      xf[0][b] = left > 0 ? masked_codes(reinterpret_cast<const int8_t*>((kFused ? s_mem : reinterpret_cast<const char*>(a.x)) + (int64_t)whole * 64 + xoff[b]), min(left, 16)) : zero;
-    multiply(0);
+      for (int i = 0; i < kAccs; ++i) w[i] = *reinterpret_cast<const i32x4*>(a.w + (int64_t)min(n0 + i * 16 + c, a.N - 1) * a.ldw + a.K16);
+    }
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) if (i || g) xf[0][i] = zero;
+    multiply(0, w);
   }
 
   if (split > 1) {
-    i32x4* sums = reinterpret_cast<i32x4*>(s_mem + (kFused ? a.T * pitch : 0));
+    __syncthreads();                                       // the rings have been read
+    Acc* sums = reinterpret_cast<Acc*>(s_mem);
 #pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-      for (int b = 0; b < TB; ++b) sums[((wave * R + r) * TB + b) * 64 + lane] = acc[r][b];
+    for (int i = 0; i < kAccs; ++i) sums[(wave * kAccs + i) * 64 + lane] = acc[i];
     __syncthreads();
+    if (part) return;
+    for (int s = 1; s < split; ++s)
 #pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-      for (int b = 0; b < TB; ++b) {
-        if (((r * TB + b) & (split - 1)) != part) continue;
-        i32x4 sum = {0, 0, 0, 0};
-        for (int w = 0; w < split; ++w) sum += sums[(((group * split + w) * R + r) * TB + b) * 64 + lane];
-        acc[r][b] = sum;
-      }
+      for (int i = 0; i < kAccs; ++i) acc[i] += sums[((wave + s) * kAccs + i) * 64 + lane];
   }
   if (idle) return;
-  // accumulator v of lane l is weight row 4*(l/16) + v, token l%16
+  // a lane's column is a weight row, accumulator v a token: 4*(l/16) + v, or 8*(v/4) + 4*(l/32) + v%4
+  float xs = 0.f;
+  if (lane < a.T) {
+    if constexpr (FROM == kFloats) xs = RowScale(s_max[lane & 15]).scale();
+    else xs = a.x_scale[lane];
+  }
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    const int n = n0 + 16 * r + 4 * g;
-    float ws[4], bias[4];
+  for (int i = 0; i < kAccs; ++i) {
+    const int n = n0 + i * 16 + c;
+    const float ws = a.w_scale[min(n, a.N - 1)], bias = a.bias ? a.bias[min(n, a.N - 1)] : 0.f;
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
-      const int i = min(n + v, a.N - 1);
-      ws[v] = a.w_scale[i];
-      bias[v] = a.bias ? a.bias[i] : 0.f;
-    }
-#pragma unroll
-    for (int b = 0; b < TB; ++b) {
-      const int t = 16 * b + c;
-      if (((r * TB + b) & (split - 1)) != part || t >= a.T) continue;
-      float xs;
-      if constexpr (kFused) xs = RowScale(s_max[t]).scale();
-      else xs = a.x_scale[t];
-      S* p = static_cast<S*>(a.out) + (int64_t)t * a.ldo + n;
-      Unaligned<S, 4> o;
-#pragma unroll
-      for (int v = 0; v < 4; ++v) o.v[v] = to_out<S>(a.bias ? scaled(acc[r][b][v], xs, ws[v], bias[v]) : scaled(acc[r][b][v], xs, ws[v]));
-      if (n + 3 < a.N) {
-        *reinterpret_cast<Unaligned<S, 4>*>(p) = o;
-      } else {
-#pragma unroll
-        for (int v = 0; v < 4; ++v) if (n + v < a.N) p[v] = o.v[v];
-      }
+    for (int v = 0; v < (NARROW ? 4 : 16); ++v) {
+      const int t = NARROW ? 4 * g + v : 8 * (v >> 2) + 4 * g + (v & 3);
+      const float s = __shfl(xs, t);
+      if (t < a.T && n < a.N)
+        static_cast<S*>(a.out)[(int64_t)t * a.ldo + n] = to_out<S>(a.bias ? scaled(acc[i][v], s, ws, bias) : scaled(acc[i][v], s, ws));
     }
   }
 }
 
-// R blocks of weight rows per wave, K split over `split` waves.
-struct Shape { int r, split; };
-Shape shape_of(int T, int N, int K) {
-  const int rows16 = (N + 15) / 16;
-  const int r = rows16 >= 4096 ? 4 : 1;
-  int split = 4;
-  while (split > 1 && (rows16 / r) * split > 8192) split >>= 1;
-  return {r, split};
+// K over as many waves of a workgroup as it takes to have two workgroups for every CU, a wave keeping two chunks at least
+int split_of(int N, int K) {
+  const int blocks = (N + 31) / 32, chunks = (K + 127) / 128;
+  int split = 1;
+  while (split < 4 && blocks * split < 2048 && chunks >= 4 * split) split *= 2;
+  return split;
 }
 
-template <typename S, typename X, int TB, int R>
-int launch_t(const Int8Args& a, const FloatTokens& f, int split, hipStream_t s) {
-  constexpr bool kFused = !std::is_same_v<X, int8_t>;
-  const int rows = 16 * R * (4 / split);
-  const size_t lds = (kFused ? (size_t)a.T * code_pitch(a.K) : 0) + (split > 1 ? 4 * R * TB * 1024 : 0);
-  hipLaunchKernelGGL((int8_stream_kernel<S, X, TB, R>), dim3((unsigned)((a.N + rows - 1) / rows)), dim3(256), lds, s, a, f, split);
+template <typename S, Tokens FROM, typename X, bool NARROW>
+int launch_t(const Int8Args& a, const FloatTokens& f, hipStream_t s) {
+  const int split = split_of(a.N, a.K), rows = 32 * (4 / split);
+  const int lds = kRingBytes + (FROM == kFloats ? a.T * code_pitch(a.K) : 0);
+  static std::atomic<int> ready{0};
+  if (!ready.load(std::memory_order_relaxed)) {
+    if (hipFuncSetAttribute(reinterpret_cast<const void*>(&int8_stream_kernel<S, FROM, X, NARROW>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                            kRingBytes + (FROM == kFloats ? kMaxFused + 16 * 144 : 0)) != hipSuccess)
+      return hip_fail(hipGetLastError(), "int8_stream_kernel: LDS size attribute");
+    ready.store(1, std::memory_order_relaxed);
+  }
+  hipLaunchKernelGGL((int8_stream_kernel<S, FROM, X, NARROW>), dim3((unsigned)((a.N + rows - 1) / rows)), dim3(256), (size_t)lds, s, a, f, split);
   return hip_fail(hipGetLastError(), "int8_stream_kernel launch");
 }
-template <typename S, typename X, int TB>
-int launch_r(const Int8Args& a, const FloatTokens& f, hipStream_t s) {
-  const Shape sh = shape_of(a.T, a.N, a.K);
-  return sh.r == 4 ? launch_t<S, X, TB, 4>(a, f, sh.split, s) : launch_t<S, X, TB, 1>(a, f, sh.split, s);
+template <typename S>
+int launch_s(const Int8Args& a, bool in_lanes, hipStream_t s) {
+  const FloatTokens none = {nullptr, 0};
+  if (in_lanes) return a.T <= 16 ? launch_t<S, kLanes, float, true>(a, none, s) : launch_t<S, kLanes, float, false>(a, none, s);
+  return a.T <= 16 ? launch_t<S, kRows, float, true>(a, none, s) : launch_t<S, kRows, float, false>(a, none, s);
 }
-template <typename X, int TB>
-int launch_s(const Int8Args& a, const FloatTokens& f, hipStream_t s) {
-  return a.out_dtype == MOE_FP32 ? launch_r<float, X, TB>(a, f, s) : launch_r<uint16_t, X, TB>(a, f, s);
+template <typename X>
+int launch_x(const Int8Args& a, const FloatTokens& f, hipStream_t s) {
+  return a.out_dtype == MOE_FP32 ? launch_t<float, kFloats, X, true>(a, f, s) : launch_t<uint16_t, kFloats, X, true>(a, f, s);
 }
 
 }  // namespace
 
-int launch_int8_stream(const Int8Args& a, hipStream_t s) {
-  const FloatTokens none = {nullptr, 0};
-  switch ((a.T + 15) / 16) {
-    case 1: return launch_s<int8_t, 1>(a, none, s);
-    case 2: return launch_s<int8_t, 2>(a, none, s);
-    case 3: return launch_s<int8_t, 3>(a, none, s);
-    default: return launch_s<int8_t, 4>(a, none, s);
-  }
+int launch_int8_stream(const Int8Args& a, bool in_lanes, hipStream_t s) {
+  return a.out_dtype == MOE_FP32 ? launch_s<float>(a, in_lanes, s) : launch_s<uint16_t>(a, in_lanes, s);
 }
 
 bool int8_quantises_itself(int T, int K) { return T <= 16 && (int64_t)T * K <= kMaxFused; }
+size_t int8_lane_codes_bytes(int T, int K) { return (size_t)(T <= 16 ? 16 : 32) * ((K + 127) / 128 * 128); }
 
 int launch_int8_stream_float(const Int8Args& a, const void* x, int x_dtype, int64_t ldx, hipStream_t s) {
   ProfScope ps(kProfInt8Product, s);
   const FloatTokens f = {x, ldx};
-  return x_dtype == MOE_FP32 ? launch_s<float, 1>(a, f, s) : launch_s<uint16_t, 1>(a, f, s);
+  return x_dtype == MOE_FP32 ? launch_x<float>(a, f, s) : launch_x<uint16_t>(a, f, s);
 }
 
 }  // namespace mm

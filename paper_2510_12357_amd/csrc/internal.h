@@ -157,7 +157,10 @@ int launch_combine_add(const moe_config& c, const float* y, const float* w, cons
                        const int32_t* k_t, int j_lo, void* out, hipStream_t s);
 
 // ---- the output head: 8-bit product and log probabilities (head_api.hip resolves the dense leading dimensions) -----
-int launch_quantize_rows(const void* x, int dtype, int rows, int K, int64_t ldx, int8_t* q, int64_t ldq, float* scale, hipStream_t s);
+// Where the codes of a row go: one after the other; or 16 at a time to the lane that needs them, in matrix instructions of 16 x 16 x 64 or
+// 32 x 32 x 32 (lane l: row l % 16, its k from 16 (l / 16) on; row l % 32, k from 16 (l / 32) on).
+enum CodeOrder { kCodeRows = 0, kCodeLanes16 = 16, kCodeLanes32 = 32 };
+int launch_quantize_rows(const void* x, int dtype, int rows, int K, int64_t ldx, int8_t* q, int64_t ldq, float* scale, CodeOrder order, hipStream_t s);
 struct Int8Args {
   int T, N, K, out_dtype;
   int K16, k_tail;         // codes in whole vectors of 16; codes of the last vector that count where it is not all of them (0: the tokens' are zero behind K)
@@ -166,10 +169,13 @@ struct Int8Args {
   const int8_t* w; const float* w_scale; const float* bias;
   void* out;
 };
-int launch_int8_product(const Int8Args& a, hipStream_t s);
+int launch_int8_product(const Int8Args& a, bool in_lanes, hipStream_t s);
+constexpr int kInt8StreamTokens = 32;      // most that the streaming kernel takes
 int launch_int8_wide(const Int8Args& a, int token_tiles, int height, hipStream_t s);      // height: rows of a token tile, at most 256
 int launch_int8_tile(const Int8Args& a, int rows, hipStream_t s);                         // rows of a token tile: 64 or 128
-int launch_int8_stream(const Int8Args& a, hipStream_t s);                                 // T <= 64
+// T <= 32.  in_lanes: x holds the codes in the order that CodeOrder names, not in rows
+int launch_int8_stream(const Int8Args& a, bool in_lanes, hipStream_t s);
+size_t int8_lane_codes_bytes(int T, int K);
 // the same on float tokens, quantised by every workgroup; where int8_quantises_itself says so
 bool int8_quantises_itself(int T, int K);
 int launch_int8_stream_float(const Int8Args& a, const void* x, int x_dtype, int64_t ldx, hipStream_t s);
