@@ -129,7 +129,7 @@ extern "C" int moe_linear_int8(const moe_int8_config* cfg, const void* x, const 
   const Int8Args a = {c.T, c.N, c.K, c.out_dtype, (int)code_ld(c.K), 0, code_ld(c.K), c.ldw, c.ldo, q, scale, w, w_scale, bias, out};
   if (int8_quantises_itself(c.T, c.K)) return launch_int8_stream_float(a, x, c.x_dtype, c.ldx, s);
   const bool lanes = in_lanes(c);
-  rc = launch_quantize_rows(x, c.x_dtype, c.T, c.K, c.ldx, q, code_ld(c.K), scale, !lanes ? kCodeRows : (c.T <= 16 ? kCodeLanes16 : kCodeLanes32), s);
+  rc = launch_quantize_rows(x, c.x_dtype, c.T, c.K, c.ldx, q, code_ld(c.K), scale, !lanes ? kCodeRows : (c.T <= 16 ? kCodeLanes : kCodeLanes2), s);
   return rc ? rc : launch_int8_product(a, lanes, s);
 }
 

@@ -36,9 +36,8 @@ __global__ __launch_bounds__(THREADS) void quantize_kernel(const X* __restrict__
     for (int w = 0; w < THREADS / 64; ++w) top = max(top, s_max[w]);
   }
   const RowScale r(top);
-  int8_t* out = order ? q + (int64_t)blockIdx.x * 16 : q + (int64_t)blockIdx.x * ldq;
-  // of code k: blocks of 64 lanes x 16 codes, 1024 / order k each (order: lanes side by side, rows of the block)
-  auto place = [&](int k) { return order ? (k >> 4) * order * 16 + (k & 15) : k; };
+  int8_t* out = q + (order ? (int64_t)(blockIdx.x / 16 * 1024 + blockIdx.x % 16 * 16) : (int64_t)blockIdx.x * ldq);
+  auto place = [&](int k) { return order ? (k >> 6) * order * 1024 + ((k >> 4) & 3) * 256 + (k & 15) : k; };
 #pragma unroll
   for (int u = 0; u < kHeld; ++u) {
     const int k = (u * THREADS + tid) * kVec;

@@ -1,7 +1,7 @@
 // The 8-bit product for up to 32 tokens: every weight is read once, so memory sets the pace, and for small weights the latency of a launch.
 //
-// A wave has 32 weight rows and all tokens, and a ring of kRing chunks of 128 k of its own in LDS, which loads fill past the registers: eight lanes
-// read a line of a row.  (Operands straight into registers, in the matrix instruction's order, touch a row per lane: 64 lines an instruction,
+// A wave has 16 weight rows and all tokens, and a ring of kRing chunks of 256 k of its own in LDS, which loads fill past the registers: sixteen lanes
+// read 256 bytes of a row.  (Operands straight into registers, in the matrix instruction's order, touch a row per lane: 64 lines an instruction,
 // and the address units set the pace; 64 x 131072 x 4096 took 227 us so.)  Nothing is shared between waves, so there is no barrier in the
 // loop.  The tokens' codes come into registers, as far ahead as the weights, because loads end in order.  The four waves of a
 // workgroup have weight rows of their own, or, where rows are few, share them and split K; their sums of integers are joined in LDS, exactly.
@@ -20,12 +20,12 @@ namespace mm {
 namespace {
 
 typedef __attribute__((address_space(3))) void lds_void;
-typedef __attribute__((ext_vector_type(16))) int i32x16;
 
-constexpr int kRing = 4, kRowBytes = 128, kStage = 32 * kRowBytes;
+constexpr int kRing = 4, kRowBytes = 256, kStage = 16 * kRowBytes;
+constexpr int kSteps = kRowBytes / 64;                     // matrix instructions (16 x 16 x 64) of a chunk
 constexpr int kRingBytes = 4 * kRing * kStage;             // of a workgroup
 constexpr int kMaxFused = 16384;                           // elements of float tokens that every workgroup quantises
-constexpr int code_pitch(int K) { return (K + 127) / 128 * 128 + 16; }   // bytes of a token's codes in LDS: 16 tokens start at 16 different banks
+constexpr int code_pitch(int K) { return (K + 255) / 256 * 256 + 16; }   // bytes of a token's codes in LDS: 16 tokens start at 16 different banks
 
 // At most N loads of this wave in flight.  An asm block, so that no load moves across it.
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory"); }
@@ -34,84 +34,81 @@ enum Tokens { kRows, kLanes, kFloats };                    // where codes come f
 
 struct FloatTokens { const void* x; int64_t ldx; };
 
-// the weights of a lane for one chunk: four k-steps of the 32 x 32 instruction, or two of two blocks of the 16 x 16 one
-__device__ __forceinline__ void read_chunk(i32x4 (&w)[4], const unsigned (&at)[4], unsigned stage) {
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// a lane's weights of one chunk
+__device__ __forceinline__ void read_weights(i32x4 (&w)[4], const unsigned (&at)[4], unsigned stage) {
   asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\tds_read_b128 %2, %6\n\tds_read_b128 %3, %7\n\ts_waitcnt lgkmcnt(0)"
                : "=&v"(w[0]), "=&v"(w[1]), "=&v"(w[2]), "=&v"(w[3]) : "v"(at[0] + stage), "v"(at[1] + stage), "v"(at[2] + stage), "v"(at[3] + stage) : "memory");
 }
-
-__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
-
-// codes in LDS: two k-steps of the 16 x 16 instruction
-template <int N>
-__device__ __forceinline__ void read_codes(i32x4 (&x)[N], unsigned at) {
-  static_assert(N == 2, "16 x 16 instructions");
-  asm volatile("ds_read_b128 %0, %2\n\tds_read_b128 %1, %2 offset:64\n\ts_waitcnt lgkmcnt(0)" : "=&v"(x[0]), "=&v"(x[1]) : "v"(at) : "memory");
+// and, from LDS, its codes
+__device__ __forceinline__ void read_codes(i32x4 (&x)[4], unsigned at) {
+  asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %4 offset:64\n\tds_read_b128 %2, %4 offset:128\n\tds_read_b128 %3, %4 offset:192\n\ts_waitcnt lgkmcnt(0)"
+               : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]) : "v"(at) : "memory");
 }
 
-// NARROW: at most 16 tokens, 16 x 16 x 64 instructions; else at most 32, 32 x 32 x 32.  X: type of float tokens.
-template <typename S, Tokens FROM, typename X, bool NARROW>
+// TB: blocks of 16 tokens, 1 or 2.  X: type of float tokens.
+template <typename S, Tokens FROM, typename X, int TB>
 __global__ __launch_bounds__(256) void int8_stream_kernel(const Int8Args a, const FloatTokens f, const int split) {
-  constexpr int kSteps = NARROW ? 2 : 4, kStepK = 128 / kSteps;
   extern __shared__ __attribute__((aligned(1024))) char s_mem[];   // the rings, later partial sums; codes of float tokens
   __shared__ unsigned s_max[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
-  const int c = NARROW ? lane & 15 : lane & 31, g = NARROW ? lane >> 4 : lane >> 5;   // token (or weight row) and group of 16 k of a lane's operand
+  const int c = lane & 15, g = lane >> 4;                  // token (or weight row) and group of 16 k of a lane's operand
   const int part = wave & (split - 1), group = wave / split;
-  const int n0 = uniform((blockIdx.x * (4 / split) + group) * 32);
+  const int n0 = uniform((blockIdx.x * (4 / split) + group) * 16);
   const bool idle = n0 >= a.N;                             // past the last row: keeps the barriers only
   const int chunks = (a.K16 + kRowBytes - 1) / kRowBytes;
   const int begin = idle ? 0 : chunks * part / split, end = idle ? 0 : chunks * (part + 1) / split;
 
   // ---- weights: buffer loads into LDS, rows and columns that do not exist are out of range ----
-  const int rows = idle ? 1 : min(a.N - n0, 32);
+  const int rows = idle ? 1 : min(a.N - n0, 16);
   const __amdgpu_buffer_rsrc_t rw = make_rsrc(a.w + (int64_t)(idle ? 0 : n0) * a.ldw, (unsigned)((rows - 1) * (int)a.ldw + a.K16));
   char* const ring = s_mem + wave * (kRing * kStage);
   unsigned woff[4];
 #pragma unroll
   for (int p = 0; p < 4; ++p) {
-    const int r = 8 * p + (lane >> 3);
+    const int r = 4 * p + (lane >> 4);
     woff[p] = r < rows ? (unsigned)r * (unsigned)a.ldw : kOob;
   }
   auto load_w = [&](int stage, int k) {
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
-      const unsigned at = (unsigned)(k * kRowBytes) + (unsigned)((lane & 7) ^ ((8 * p + (lane >> 3)) >> 1 & 7)) * 16u;
+      const unsigned at = (unsigned)(k * kRowBytes) + (unsigned)((lane & 15) ^ (4 * p + (lane >> 4))) * 16u;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, (lds_void*)(ring + stage * kStage + p * 1024), 16, (int)(at < (unsigned)a.K16 ? woff[p] + at : kOob), 0, 0,
                                                kStreamOnce);
     }
   };
   unsigned w_at[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = NARROW ? (i & 1) * 16 + c : c, col = NARROW ? (i >> 1) * 4 + g : 2 * i + g;
-    w_at[i] = (unsigned)(size_t)ring + (unsigned)(r * kRowBytes + (col ^ (r >> 1 & 7)) * 16);
-  }
+  for (int i = 0; i < 4; ++i) w_at[i] = (unsigned)(size_t)ring + (unsigned)(c * kRowBytes + ((4 * i + g) ^ c) * 16);
 
   // ---- tokens.  What stands behind K16 meets weights of zero; it only has to be there.  So do tokens behind T, which are not stored ----
   const int pitch = code_pitch(a.K);
-  i32x4 xf[kRing][kSteps];
+  i32x4 xf[kRing][TB][kSteps];
   const unsigned x_at = (unsigned)(size_t)s_mem + (unsigned)(kRingBytes + min(c, a.T - 1) * pitch + 16 * g);   // (kFloats)
-  const char* const xrow = reinterpret_cast<const char*>(a.x) + (FROM == kRows ? (int64_t)min(c, a.T - 1) * a.ldx : lane * 16);
-  auto load_x = [&](int d, int k) {
-    if constexpr (FROM == kFloats) { read_codes(xf[d], x_at + (unsigned)(k * 128)); return; }
+  const char* xrow[TB];
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
-      const int at = k * 128 + i * kStepK + 16 * g;
-      if constexpr (FROM == kLanes) xf[d][i] = *reinterpret_cast<const i32x4*>(xrow + (int64_t)(k * kSteps + i) * 1024);
-      else xf[d][i] = *reinterpret_cast<const i32x4*>(xrow + ((unsigned)at < (unsigned)a.K16 ? at : 0));   // a row holds 16 codes at least
+  for (int b = 0; b < TB; ++b)
+    xrow[b] = reinterpret_cast<const char*>(a.x) + (FROM == kRows ? (int64_t)min(16 * b + c, a.T - 1) * a.ldx : b * 1024 + lane * 16);
+  auto load_x = [&](int d, int k) {
+#pragma unroll
+    for (int b = 0; b < TB; ++b) {
+      if constexpr (FROM == kFloats) { read_codes(xf[d][b], x_at + (unsigned)(k * kRowBytes)); continue; }
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) {
+        const int at = k * kRowBytes + 64 * i + 16 * g;
+        if constexpr (FROM == kLanes) xf[d][b][i] = *reinterpret_cast<const i32x4*>(xrow[b] + (int64_t)(k * kSteps + i) * (TB * 1024));
+        else xf[d][b][i] = *reinterpret_cast<const i32x4*>(xrow[b] + ((unsigned)at < (unsigned)a.K16 ? at : 0));   // a row holds 16 codes at least
+      }
     }
   };
 
-  typedef std::conditional_t<NARROW, i32x4, i32x16> Acc;
-  constexpr int kAccs = NARROW ? 2 : 1;
-  Acc acc[kAccs] = {};
+  i32x4 acc[TB] = {};
   auto multiply = [&](int d, const i32x4 (&w)[4]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if constexpr (NARROW) acc[i & 1] = __builtin_amdgcn_mfma_i32_16x16x64_i8(xf[d][i >> 1], w[i], acc[i & 1], 0, 0, 0);
-      else acc[0] = __builtin_amdgcn_mfma_i32_32x32x32_i8(xf[d][i], w[i], acc[0], 0, 0, 0);
-    }
+    for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+      for (int b = 0; b < TB; ++b) acc[b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(xf[d][b][i], w[i], acc[b], 0, 0, 0);
   };
   constexpr bool kAhead = FROM != kFloats;                 // codes in LDS are read when they are used
   auto first_loads = [&]() {                               // chunks that are not there fill their stage with zeros
@@ -161,7 +158,8 @@ __global__ __launch_bounds__(256) void int8_stream_kernel(const Int8Args a, cons
   }
 
   // The chunk in stage d.  In flight behind it: the chunks up to kRing - 2 further on, and their tokens' codes.
-  constexpr int kPer = 4 + (kAhead ? kSteps : 0);
+  constexpr int kPer = 4 + (kAhead ? TB * kSteps : 0);
+  static_assert((kRing - 2) * kPer < 64, "what the wait can count");
   i32x4 w[4];
   int k = begin;
   for (; k + 2 * kRing - 2 < end; k += kRing) {
@@ -169,7 +167,7 @@ __global__ __launch_bounds__(256) void int8_stream_kernel(const Int8Args a, cons
     for (int d = 0; d < kRing; ++d) {
       constexpr int kLast = kRing - 1;
       wait_loads<(kRing - 2) * kPer>();
-      read_chunk(w, w_at, d * kStage);
+      read_weights(w, w_at, d * kStage);
       load_w((d + kLast) % kRing, k + d + kLast);
       if (kAhead) load_x((d + kLast) % kRing, k + d + kLast); else load_x(d, k + d);
       multiply(d, w);
@@ -181,7 +179,7 @@ __global__ __launch_bounds__(256) void int8_stream_kernel(const Int8Args a, cons
     if (k + d < end) {
       if (k + d + kRing - 2 < end) wait_loads<(kRing - 2) * kPer>();
       else wait_loads<0>();
-      read_chunk(w, w_at, d % kRing * kStage);
+      read_weights(w, w_at, d % kRing * kStage);
       if (k + d + kRing - 1 < end) { load_w((d + kRing - 1) % kRing, k + d + kRing - 1); if (kAhead) load_x((d + kRing - 1) % kRing, k + d + kRing - 1); }
       if (!kAhead) load_x(d % kRing, k + d);
       multiply(d % kRing, w);
@@ -192,79 +190,78 @@ __global__ __launch_bounds__(256) void int8_stream_kernel(const Int8Args a, cons
     const i32x4 zero = {0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = zero;
-    if (g == 0) {
-      xf[0][0] = masked_codes(reinterpret_cast<const int8_t*>(xrow) + a.K16, a.k_tail);
 #pragma unroll
-      for (int i = 0; i < kAccs; ++i) w[i] = *reinterpret_cast<const i32x4*>(a.w + (int64_t)min(n0 + i * 16 + c, a.N - 1) * a.ldw + a.K16);
+    for (int b = 0; b < TB; ++b) {
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i) xf[0][b][i] = zero;
+      if (g == 0) xf[0][b][0] = masked_codes(reinterpret_cast<const int8_t*>(xrow[b]) + a.K16, a.k_tail);
     }
-#pragma unroll
-    for (int i = 0; i < kSteps; ++i) if (i || g) xf[0][i] = zero;
+    if (g == 0) w[0] = *reinterpret_cast<const i32x4*>(a.w + (int64_t)min(n0 + c, a.N - 1) * a.ldw + a.K16);
     multiply(0, w);
   }
 
   if (split > 1) {
     __syncthreads();                                       // the rings have been read
-    Acc* sums = reinterpret_cast<Acc*>(s_mem);
+    i32x4* sums = reinterpret_cast<i32x4*>(s_mem);
 #pragma unroll
-    for (int i = 0; i < kAccs; ++i) sums[(wave * kAccs + i) * 64 + lane] = acc[i];
+    for (int b = 0; b < TB; ++b) sums[(wave * TB + b) * 64 + lane] = acc[b];
     __syncthreads();
     if (part) return;
     for (int s = 1; s < split; ++s)
 #pragma unroll
-      for (int i = 0; i < kAccs; ++i) acc[i] += sums[((wave + s) * kAccs + i) * 64 + lane];
+      for (int b = 0; b < TB; ++b) acc[b] += sums[((wave + s) * TB + b) * 64 + lane];
   }
   if (idle) return;
-  // a lane's column is a weight row, accumulator v a token: 4*(l/16) + v, or 8*(v/4) + 4*(l/32) + v%4
+  // a lane's column is a weight row, accumulator v of block b token 16 b + 4 (l / 16) + v
   float xs = 0.f;
   if (lane < a.T) {
     if constexpr (FROM == kFloats) xs = RowScale(s_max[lane & 15]).scale();
     else xs = a.x_scale[lane];
   }
+  const int n = n0 + c;
+  const float ws = a.w_scale[min(n, a.N - 1)], bias = a.bias ? a.bias[min(n, a.N - 1)] : 0.f;
 #pragma unroll
-  for (int i = 0; i < kAccs; ++i) {
-    const int n = n0 + i * 16 + c;
-    const float ws = a.w_scale[min(n, a.N - 1)], bias = a.bias ? a.bias[min(n, a.N - 1)] : 0.f;
+  for (int b = 0; b < TB; ++b)
 #pragma unroll
-    for (int v = 0; v < (NARROW ? 4 : 16); ++v) {
-      const int t = NARROW ? 4 * g + v : 8 * (v >> 2) + 4 * g + (v & 3);
+    for (int v = 0; v < 4; ++v) {
+      const int t = 16 * b + 4 * g + v;
       const float s = __shfl(xs, t);
       if (t < a.T && n < a.N)
-        static_cast<S*>(a.out)[(int64_t)t * a.ldo + n] = to_out<S>(a.bias ? scaled(acc[i][v], s, ws, bias) : scaled(acc[i][v], s, ws));
+        static_cast<S*>(a.out)[(int64_t)t * a.ldo + n] = to_out<S>(a.bias ? scaled(acc[b][v], s, ws, bias) : scaled(acc[b][v], s, ws));
     }
-  }
 }
 
 // K over as many waves of a workgroup as it takes to have two workgroups for every CU, a wave keeping two chunks at least
 int split_of(int N, int K) {
-  const int blocks = (N + 31) / 32, chunks = (K + 127) / 128;
+  const int blocks = (N + 15) / 16, chunks = (K + kRowBytes - 1) / kRowBytes;
   int split = 1;
-  while (split < 4 && blocks * split < 2048 && chunks >= 4 * split) split *= 2;
+  while (split < 4 && blocks * split < 2048 && chunks >= 2 * split) split *= 2;
   return split;
 }
 
-template <typename S, Tokens FROM, typename X, bool NARROW>
+template <typename S, Tokens FROM, typename X, int TB>
 int launch_t(const Int8Args& a, const FloatTokens& f, hipStream_t s) {
-  const int split = split_of(a.N, a.K), rows = 32 * (4 / split);
+  const int split = split_of(a.N, a.K), rows = 16 * (4 / split);
   const int lds = kRingBytes + (FROM == kFloats ? a.T * code_pitch(a.K) : 0);
   static std::atomic<int> ready{0};
   if (!ready.load(std::memory_order_relaxed)) {
-    if (hipFuncSetAttribute(reinterpret_cast<const void*>(&int8_stream_kernel<S, FROM, X, NARROW>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                            kRingBytes + (FROM == kFloats ? kMaxFused + 16 * 144 : 0)) != hipSuccess)
+    if (hipFuncSetAttribute(reinterpret_cast<const void*>(&int8_stream_kernel<S, FROM, X, TB>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                            kRingBytes + (FROM == kFloats ? kMaxFused + 16 * (kRowBytes + 16) : 0)) != hipSuccess)
       return hip_fail(hipGetLastError(), "int8_stream_kernel: LDS size attribute");
     ready.store(1, std::memory_order_relaxed);
   }
-  hipLaunchKernelGGL((int8_stream_kernel<S, FROM, X, NARROW>), dim3((unsigned)((a.N + rows - 1) / rows)), dim3(256), (size_t)lds, s, a, f, split);
+  hipLaunchKernelGGL((int8_stream_kernel<S, FROM, X, TB>), dim3((unsigned)((a.N + rows - 1) / rows)), dim3(256), (size_t)lds, s, a, f, split);
   return hip_fail(hipGetLastError(), "int8_stream_kernel launch");
 }
 template <typename S>
 int launch_s(const Int8Args& a, bool in_lanes, hipStream_t s) {
   const FloatTokens none = {nullptr, 0};
-  if (in_lanes) return a.T <= 16 ? launch_t<S, kLanes, float, true>(a, none, s) : launch_t<S, kLanes, float, false>(a, none, s);
-  return a.T <= 16 ? launch_t<S, kRows, float, true>(a, none, s) : launch_t<S, kRows, float, false>(a, none, s);
+  if (in_lanes) return a.T <= 16 ? launch_t<S, kLanes, float, 1>(a, none, s) : launch_t<S, kLanes, float, 2>(a, none, s);
+  return a.T <= 16 ? launch_t<S, kRows, float, 1>(a, none, s) : launch_t<S, kRows, float, 2>(a, none, s);
 }
 template <typename X>
 int launch_x(const Int8Args& a, const FloatTokens& f, hipStream_t s) {
-  return a.out_dtype == MOE_FP32 ? launch_t<float, kFloats, X, true>(a, f, s) : launch_t<uint16_t, kFloats, X, true>(a, f, s);
+  return a.out_dtype == MOE_FP32 ? launch_t<float, kFloats, X, 1>(a, f, s) : launch_t<uint16_t, kFloats, X, 1>(a, f, s);
 }
 
 }  // namespace
@@ -274,7 +271,7 @@ int launch_int8_stream(const Int8Args& a, bool in_lanes, hipStream_t s) {
 }
 
 bool int8_quantises_itself(int T, int K) { return T <= 16 && (int64_t)T * K <= kMaxFused; }
-size_t int8_lane_codes_bytes(int T, int K) { return (size_t)(T <= 16 ? 16 : 32) * ((K + 127) / 128 * 128); }
+size_t int8_lane_codes_bytes(int T, int K) { return (size_t)(T <= 16 ? 16 : 32) * ((K + kRowBytes - 1) / kRowBytes * kRowBytes); }
 
 int launch_int8_stream_float(const Int8Args& a, const void* x, int x_dtype, int64_t ldx, hipStream_t s) {
   ProfScope ps(kProfInt8Product, s);

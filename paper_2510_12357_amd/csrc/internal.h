@@ -157,9 +157,9 @@ int launch_combine_add(const moe_config& c, const float* y, const float* w, cons
                        const int32_t* k_t, int j_lo, void* out, hipStream_t s);
 
 // ---- the output head: 8-bit product and log probabilities (head_api.hip resolves the dense leading dimensions) -----
-// Where the codes of a row go: one after the other; or 16 at a time to the lane that needs them, in matrix instructions of 16 x 16 x 64 or
-// 32 x 32 x 32 (lane l: row l % 16, its k from 16 (l / 16) on; row l % 32, k from 16 (l / 32) on).
-enum CodeOrder { kCodeRows = 0, kCodeLanes16 = 16, kCodeLanes32 = 32 };
+// Where the codes of a row go: one after the other (0); or to the lane that needs them in a matrix instruction of 16 x 16 x 64, lane l the 16 codes
+// from 16 (l / 16) on of row l % 16, for 64 k one or two (the number) blocks of 16 rows.
+enum CodeOrder { kCodeRows = 0, kCodeLanes = 1, kCodeLanes2 = 2 };
 int launch_quantize_rows(const void* x, int dtype, int rows, int K, int64_t ldx, int8_t* q, int64_t ldq, float* scale, CodeOrder order, hipStream_t s);
 struct Int8Args {
   int T, N, K, out_dtype;
