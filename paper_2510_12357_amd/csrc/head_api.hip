@@ -50,8 +50,8 @@ int check_product(const char* call, const moe_int8_config& c, const int8_t* w, c
 }
 
 // workspace of moe_linear_int8: the codes, in rows or in the order of the streaming kernel's lanes, then the scales
-bool in_lanes(const moe_int8_config& c) { return c.T <= kInt8StreamTokens && !int8_quantises_itself(c.T, c.K); }
-size_t codes_bytes(const moe_int8_config& c) { return align256(in_lanes(c) ? int8_lane_codes_bytes(c.T, c.K) : (size_t)c.T * code_ld(c.K)); }
+int lane_blocks(const moe_int8_config& c) { return int8_streams(c.T, c.K) && !int8_quantises_itself(c.T, c.K) ? (c.T + 15) / 16 : 0; }
+size_t codes_bytes(const moe_int8_config& c) { return align256(lane_blocks(c) ? int8_lane_codes_bytes(c.T, c.K) : (size_t)c.T * code_ld(c.K)); }
 
 int resolve(const moe_logprobs_config* cfg, moe_logprobs_config* c) {
   if (!cfg) return fail(MOE_E_BADARG, "config is NULL");
@@ -88,7 +88,7 @@ extern "C" int moe_quantize_rows(const void* x, int32_t dtype, int32_t rows, int
   if (!rc) rc = check_aligned(call, "q", q, 16);
   if (!rc) rc = check_aligned(call, "scale", scale, 4);
   if (rc) return rc;
-  return launch_quantize_rows(x, dtype, rows, K, ldx, q, ldq, scale, kCodeRows, static_cast<hipStream_t>(stream));
+  return launch_quantize_rows(x, dtype, rows, K, ldx, q, ldq, scale, 0, static_cast<hipStream_t>(stream));
 }
 
 extern "C" int moe_matmul_int8(const moe_int8_config* cfg, const int8_t* x, const float* x_scale, const int8_t* w, const float* w_scale,
@@ -101,8 +101,8 @@ extern "C" int moe_matmul_int8(const moe_int8_config* cfg, const int8_t* x, cons
   if (!rc) rc = check_aligned(call, "x_scale", x_scale, 4);
   if (!rc) rc = check_product(call, c, w, w_scale, bias, out);
   if (rc) return rc;
-  const Int8Args a = {c.T, c.N, c.K, c.out_dtype, c.K & ~15, c.K & 15, c.ldx, c.ldw, c.ldo, x, x_scale, w, w_scale, bias, out};
-  return launch_int8_product(a, false, static_cast<hipStream_t>(stream));
+  const Int8Args a = {c.T, c.N, c.K, c.out_dtype, c.K & ~15, c.K & 15, 0, c.ldx, c.ldw, c.ldo, x, x_scale, w, w_scale, bias, out};
+  return launch_int8_product(a, static_cast<hipStream_t>(stream));
 }
 
 extern "C" size_t moe_linear_int8_workspace_bytes(const moe_int8_config* cfg) {
@@ -126,11 +126,10 @@ extern "C" int moe_linear_int8(const moe_int8_config* cfg, const void* x, const 
   int8_t* q = static_cast<int8_t*>(ws);
   float* scale = reinterpret_cast<float*>(q + codes_bytes(c));
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const Int8Args a = {c.T, c.N, c.K, c.out_dtype, (int)code_ld(c.K), 0, code_ld(c.K), c.ldw, c.ldo, q, scale, w, w_scale, bias, out};
+  const Int8Args a = {c.T, c.N, c.K, c.out_dtype, (int)code_ld(c.K), 0, lane_blocks(c), code_ld(c.K), c.ldw, c.ldo, q, scale, w, w_scale, bias, out};
   if (int8_quantises_itself(c.T, c.K)) return launch_int8_stream_float(a, x, c.x_dtype, c.ldx, s);
-  const bool lanes = in_lanes(c);
-  rc = launch_quantize_rows(x, c.x_dtype, c.T, c.K, c.ldx, q, code_ld(c.K), scale, !lanes ? kCodeRows : (c.T <= 16 ? kCodeLanes : kCodeLanes2), s);
-  return rc ? rc : launch_int8_product(a, lanes, s);
+  rc = launch_quantize_rows(x, c.x_dtype, c.T, c.K, c.ldx, q, code_ld(c.K), scale, a.lane_blocks, s);
+  return rc ? rc : launch_int8_product(a, s);
 }
 
 extern "C" size_t moe_token_logprobs_workspace_bytes(const moe_logprobs_config* cfg) {

@@ -118,9 +118,8 @@ __device__ __forceinline__ void store_codes(void* p, const RowScale& r, const fl
   }
 }
 
-// The first `left` (1 .. 16) of the 16 codes at p, zeros behind them.
-__device__ __forceinline__ i32x4 masked_codes(const int8_t* p, int left) {
-  i32x4 v = *reinterpret_cast<const i32x4*>(p);
+// The first `left` of 16 codes (all for 16 and more), zeros behind them.
+__device__ __forceinline__ i32x4 keep_codes(i32x4 v, int left) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int n = left - 4 * i;
@@ -128,6 +127,7 @@ __device__ __forceinline__ i32x4 masked_codes(const int8_t* p, int left) {
   }
   return v;
 }
+__device__ __forceinline__ i32x4 masked_codes(const int8_t* p, int left) { return keep_codes(*reinterpret_cast<const i32x4*>(p), left); }
 
 // One output from its exact sum; every kernel of the product ends with this, so that its bits do not depend on the kernel.
 __device__ __forceinline__ float scaled(int sum, float x_scale, float w_scale) { return ((float)sum * x_scale) * w_scale; }

@@ -1,13 +1,15 @@
-// The 8-bit product for up to 32 tokens: every weight is read once, so memory sets the pace, and for small weights the latency of a launch.
+// The 8-bit product for up to 64 tokens: every weight is read once, so memory sets the pace, and for small weights the latency of a launch.
 //
-// A wave has 16 weight rows and all tokens, and a ring of kRing chunks of 256 k of its own in LDS, which loads fill past the registers: sixteen lanes
-// read 256 bytes of a row.  (Operands straight into registers, in the matrix instruction's order, touch a row per lane: 64 lines an instruction,
-// and the address units set the pace; 64 x 131072 x 4096 took 227 us so.)  Nothing is shared between waves, so there is no barrier in the
-// loop.  The tokens' codes come into registers, as far ahead as the weights, because loads end in order.  The four waves of a
-// workgroup have weight rows of their own, or, where rows are few, share them and split K; their sums of integers are joined in LDS, exactly.
+// A workgroup of eight waves, one per CU, keeps the codes of all tokens in its registers: `split` waves share K, each holding its part of it, and
+// weights are all that streams.  A wave goes through blocks of 16 weight rows in chunks of 256 k, by a ring of four chunks of its own in LDS, which
+// loads fill past the registers, sixteen lanes reading 256 bytes of a row; the ring runs on from block to block.  (Operands straight from memory
+// into registers, in the matrix instruction's order, touch a row per lane, 64 lines an instruction, and the address units set the pace: 64 x 131072 x
+// 4096 took 227 us so.  With the codes loaded beside every chunk 180, in tiles of 128 rows that share them in LDS 135 - 144; chunks of 128 bytes of 32
+// rows instead of 256 of 16 cost 9 % with 16 tokens.)  Waves that share K add their sums of integers up in LDS, exactly, one barrier a
+// block; without a split there is no barrier.
 // Where the codes come from: the caller's rows; the workspace of moe_linear_int8, in the order of the matrix instruction's lanes, so that a load is
-// 1 KB in one piece; or float tokens that every workgroup quantises for itself while its first weights are on their way, up to a
-// size where that costs less than a launch in front of this one.
+// 1 KB in one piece; or float tokens that every workgroup quantises for itself, up to a size where that costs less than a launch in
+// front of this one.
 #include <atomic>
 #include <type_traits>
 
@@ -21,244 +23,263 @@ namespace {
 
 typedef __attribute__((address_space(3))) void lds_void;
 
-constexpr int kRing = 4, kRowBytes = 256, kStage = 16 * kRowBytes;
+constexpr int kWavesS = 8, kThreadsS = kWavesS * 64;
+constexpr int kRing = 4, kRowBytes = 256, kStage = 16 * kRowBytes, kRingBytes = kWavesS * kRing * kStage;
 constexpr int kSteps = kRowBytes / 64;                     // matrix instructions (16 x 16 x 64) of a chunk
-constexpr int kRingBytes = 4 * kRing * kStage;             // of a workgroup
+constexpr int kMaxRows = 512;                              // weight rows of a workgroup: their scales and biases are kept in LDS
+constexpr int kScaleBytes = 2 * kMaxRows * 4;
+constexpr int max_chunks(int TB) { return 8 / TB; }        // chunks of a wave's part of K: 128 registers of codes
 constexpr int kMaxFused = 16384;                           // elements of float tokens that every workgroup quantises
-constexpr int code_pitch(int K) { return (K + 255) / 256 * 256 + 16; }   // bytes of a token's codes in LDS: 16 tokens start at 16 different banks
-
-// At most N loads of this wave in flight.  An asm block, so that no load moves across it.
-template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory"); }
+constexpr int code_pitch(int K) { return ((K + 15) / 16 | 1) * 16; }   // bytes of a token's codes in LDS: 16 tokens start at 16 different banks
+constexpr int code_bytes(int T, int K) { return T * code_pitch(K) + kRowBytes; }   // a chunk may reach behind the last token's
+constexpr int sum_bytes(int TB, int split) { return split > 1 ? 2 * (kWavesS / split) * TB * 1024 : 0; }
 
 enum Tokens { kRows, kLanes, kFloats };                    // where codes come from, as above
-
 struct FloatTokens { const void* x; int64_t ldx; };
 
+// At most N loads of this wave in flight.  An asm block, so that no load moves across it; the LDS accesses below are asm blocks too, because the
+// compiler would wait for every load into LDS in front of its own.
+template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory"); }
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
-
-// a lane's weights of one chunk
-__device__ __forceinline__ void read_weights(i32x4 (&w)[4], const unsigned (&at)[4], unsigned stage) {
+__device__ __forceinline__ void read4(i32x4 (&v)[4], unsigned a0, unsigned a1, unsigned a2, unsigned a3) {
   asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\tds_read_b128 %2, %6\n\tds_read_b128 %3, %7\n\ts_waitcnt lgkmcnt(0)"
-               : "=&v"(w[0]), "=&v"(w[1]), "=&v"(w[2]), "=&v"(w[3]) : "v"(at[0] + stage), "v"(at[1] + stage), "v"(at[2] + stage), "v"(at[3] + stage) : "memory");
+               : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]) : "v"(a0), "v"(a1), "v"(a2), "v"(a3) : "memory");
 }
-// and, from LDS, its codes
-__device__ __forceinline__ void read_codes(i32x4 (&x)[4], unsigned at) {
-  asm volatile("ds_read_b128 %0, %4\n\tds_read_b128 %1, %4 offset:64\n\tds_read_b128 %2, %4 offset:128\n\tds_read_b128 %3, %4 offset:192\n\ts_waitcnt lgkmcnt(0)"
-               : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]) : "v"(at) : "memory");
+__device__ __forceinline__ float read_float(unsigned at) {
+  float v;
+  asm volatile("ds_read_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(v) : "v"(at) : "memory");
+  return v;
+}
+// reads a sum and leaves zeros behind
+__device__ __forceinline__ i32x4 take_sum(unsigned at) {
+  i32x4 v, zero = {0, 0, 0, 0};
+  asm volatile("ds_read_b128 %0, %1\n\ts_waitcnt lgkmcnt(0)\n\tds_write_b128 %1, %2" : "=&v"(v) : "v"(at), "v"(zero) : "memory");
+  return v;
+}
+// adds the result of a matrix instruction that may have just been issued
+__device__ __forceinline__ void add_sum(unsigned at, i32x4 v) {
+  asm volatile("s_nop 15\n\tds_add_u32 %0, %1\n\tds_add_u32 %0, %2 offset:4\n\tds_add_u32 %0, %3 offset:8\n\tds_add_u32 %0, %4 offset:12"
+               :: "v"(at), "v"(v[0]), "v"(v[1]), "v"(v[2]), "v"(v[3]) : "memory");
 }
 
-// TB: blocks of 16 tokens, 1 or 2.  X: type of float tokens.
+// TB: blocks of 16 tokens, 1, 2 or 4.  X: type of float tokens.
 template <typename S, Tokens FROM, typename X, int TB>
-__global__ __launch_bounds__(256) void int8_stream_kernel(const Int8Args a, const FloatTokens f, const int split) {
-  extern __shared__ __attribute__((aligned(1024))) char s_mem[];   // the rings, later partial sums; codes of float tokens
+__global__ __launch_bounds__(kThreadsS) __attribute__((amdgpu_waves_per_eu(2, 2))) void int8_stream_kernel(const Int8Args a, const FloatTokens f, const int split,
+                                                                                                          const int turns) {
+  constexpr int kChunks = max_chunks(TB);
+  extern __shared__ __attribute__((aligned(1024))) char s_mem[];   // the rings, scales and biases, sums, codes of float tokens
   __shared__ unsigned s_max[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int c = lane & 15, g = lane >> 4;                  // token (or weight row) and group of 16 k of a lane's operand
-  const int part = wave & (split - 1), group = wave / split;
-  const int n0 = uniform((blockIdx.x * (4 / split) + group) * 16);
-  const bool idle = n0 >= a.N;                             // past the last row: keeps the barriers only
-  const int chunks = (a.K16 + kRowBytes - 1) / kRowBytes;
-  const int begin = idle ? 0 : chunks * part / split, end = idle ? 0 : chunks * (part + 1) / split;
+  const int part = wave & (split - 1), group = wave / split, groups = kWavesS / split;
+  const int row0 = blockIdx.x * turns * groups * 16;       // turn j of this wave's group: rows row0 + 16 (j groups + group) ..
+  const int rows = min(a.N - row0, turns * groups * 16);
+  const int Kw = (a.K + 15) & ~15;                         // behind K, the tokens' codes are zero
+  const int chunks = (Kw + kRowBytes - 1) / kRowBytes, first = chunks * part / split, n = chunks * (part + 1) / split - first;
+  const unsigned lds0 = (unsigned)(size_t)s_mem, scales_at = lds0 + kRingBytes, sums_at = scales_at + kScaleBytes;
+
+  // ---- float tokens: `per` threads for one, in turn for each of its vectors, of which they hold the first ones.  Loads end in order: these first ----
+  constexpr int kVec = 16 / sizeof(X), kHeld = 4;
+  int per = kThreadsS;
+  while (per > 32 && per * a.T > kThreadsS) per >>= 1;
+  const int ft = tid / per, fat = tid % per;
+  const X* const frow = static_cast<const X*>(f.x) + (int64_t)min(ft, a.T - 1) * f.ldx;
+  HeldRow<X, kHeld> held;
+  if constexpr (FROM == kFloats) held.load(frow, a.K, fat, per);
+
+  // ---- codes of the wave's part of K ----
+  i32x4 xf[kChunks][TB][kSteps];
+  if constexpr (FROM != kFloats) {
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
+      if (i >= n) break;
+#pragma unroll
+      for (int b = 0; b < TB; ++b)
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+          const int step = (first + i) * kSteps + s;
+          if constexpr (FROM == kLanes) {
+            xf[i][b][s] = *reinterpret_cast<const i32x4*>(a.x + ((int64_t)step * a.lane_blocks + min(b, a.lane_blocks - 1)) * 1024 + lane * 16);
+          } else {
+            const int8_t* row = a.x + (int64_t)min(16 * b + c, a.T - 1) * a.ldx;
+            const int k = 64 * step + 16 * g;
+            xf[i][b][s] = masked_codes(row + (k < a.K ? k : 0), a.K - k);
+          }
+        }
+    }
+  }
 
   // ---- weights: buffer loads into LDS, rows and columns that do not exist are out of range ----
-  const int rows = idle ? 1 : min(a.N - n0, 16);
-  const __amdgpu_buffer_rsrc_t rw = make_rsrc(a.w + (int64_t)(idle ? 0 : n0) * a.ldw, (unsigned)((rows - 1) * (int)a.ldw + a.K16));
+  const __amdgpu_buffer_rsrc_t rw = make_rsrc(a.w + (int64_t)row0 * a.ldw, (unsigned)((rows - 1) * (int)a.ldw + Kw));
   char* const ring = s_mem + wave * (kRing * kStage);
-  unsigned woff[4];
-#pragma unroll
-  for (int p = 0; p < 4; ++p) {
-    const int r = 4 * p + (lane >> 4);
-    woff[p] = r < rows ? (unsigned)r * (unsigned)a.ldw : kOob;
-  }
-  auto load_w = [&](int stage, int k) {
+  int load_turn = 0, load_chunk = 0, load_stage = 0;       // what is loaded next
+  auto load = [&]() {
+    const int row = 16 * (load_turn * groups + group) + g, k0 = (first + load_chunk) * kRowBytes;
+    const bool there = n > 0 && load_turn < turns;         // behind the last block: zeros, without memory traffic
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
-      const unsigned at = (unsigned)(k * kRowBytes) + (unsigned)((lane & 15) ^ (4 * p + (lane >> 4))) * 16u;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, (lds_void*)(ring + stage * kStage + p * 1024), 16, (int)(at < (unsigned)a.K16 ? woff[p] + at : kOob), 0, 0,
-                                               kStreamOnce);
+      const int r = row + 4 * p, k = k0 + (c ^ (4 * p + g)) * 16;
+      const unsigned off = there && r < rows && k < Kw ? (unsigned)r * (unsigned)a.ldw + (unsigned)k : kOob;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, (lds_void*)(ring + load_stage * kStage + p * 1024), 16, (int)off, 0, 0, kStreamOnce);
     }
+    load_stage = (load_stage + 1) & (kRing - 1);
+    load_chunk = load_chunk + 1 >= n ? 0 : load_chunk + 1;
+    load_turn += load_chunk == 0;
   };
-  unsigned w_at[4];
+  // scales and biases of the rows, the latter zeros where there are none; sums start from zero
+  float ws0[2] = {0.f, 0.f};
+  if (tid < rows) { ws0[0] = a.w_scale[row0 + tid]; if (a.bias) ws0[1] = a.bias[row0 + tid]; }
+  static_assert(kMaxRows <= kThreadsS, "one row a thread");
+  asm volatile("" ::: "memory");
 #pragma unroll
-  for (int i = 0; i < 4; ++i) w_at[i] = (unsigned)(size_t)ring + (unsigned)(c * kRowBytes + ((4 * i + g) ^ c) * 16);
-
-  // ---- tokens.  What stands behind K16 meets weights of zero; it only has to be there.  So do tokens behind T, which are not stored ----
-  const int pitch = code_pitch(a.K);
-  i32x4 xf[kRing][TB][kSteps];
-  const unsigned x_at = (unsigned)(size_t)s_mem + (unsigned)(kRingBytes + min(c, a.T - 1) * pitch + 16 * g);   // (kFloats)
-  const char* xrow[TB];
-#pragma unroll
-  for (int b = 0; b < TB; ++b)
-    xrow[b] = reinterpret_cast<const char*>(a.x) + (FROM == kRows ? (int64_t)min(16 * b + c, a.T - 1) * a.ldx : b * 1024 + lane * 16);
-  auto load_x = [&](int d, int k) {
-#pragma unroll
-    for (int b = 0; b < TB; ++b) {
-      if constexpr (FROM == kFloats) { read_codes(xf[d][b], x_at + (unsigned)(k * kRowBytes)); continue; }
-#pragma unroll
-      for (int i = 0; i < kSteps; ++i) {
-        const int at = k * kRowBytes + 64 * i + 16 * g;
-        if constexpr (FROM == kLanes) xf[d][b][i] = *reinterpret_cast<const i32x4*>(xrow[b] + (int64_t)(k * kSteps + i) * (TB * 1024));
-        else xf[d][b][i] = *reinterpret_cast<const i32x4*>(xrow[b] + ((unsigned)at < (unsigned)a.K16 ? at : 0));   // a row holds 16 codes at least
-      }
-    }
-  };
-
-  i32x4 acc[TB] = {};
-  auto multiply = [&](int d, const i32x4 (&w)[4]) {
-#pragma unroll
-    for (int i = 0; i < kSteps; ++i)
-#pragma unroll
-      for (int b = 0; b < TB; ++b) acc[b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(xf[d][b][i], w[i], acc[b], 0, 0, 0);
-  };
-  constexpr bool kAhead = FROM != kFloats;                 // codes in LDS are read when they are used
-  auto first_loads = [&]() {                               // chunks that are not there fill their stage with zeros
-#pragma unroll
-    for (int d = 0; d < kRing - 1; ++d) { load_w(d, begin + d < end ? begin + d : 1 << 20); if (kAhead) load_x(d, max(min(begin + d, chunks - 1), 0)); }
-  };
+  for (int i = 0; i < kRing - 1; ++i) load();
+  asm volatile("ds_write_b32 %0, %1\n\tds_write_b32 %0, %2 offset:%3" :: "v"(scales_at + 4u * tid), "v"(ws0[0]), "v"(ws0[1]), "n"(4 * kMaxRows) : "memory");
+  for (int i = tid * 16; i < sum_bytes(TB, split); i += kThreadsS * 16) {
+    const i32x4 zero = {0, 0, 0, 0};
+    asm volatile("ds_write_b128 %0, %1" :: "v"(sums_at + (unsigned)i), "v"(zero) : "memory");
+  }
   if constexpr (FROM == kFloats) {
-    // `per` threads for a token, in turn for each of its vectors, of which they hold the first kHeld.  Loads end in order: the tokens' first.
-    constexpr int kVec = 16 / sizeof(X), kHeld = 8;
-    int per = 256;
-    while (per > 16 && per * a.T > 256) per >>= 1;
-    const int t = tid / per, at = tid % per;
-    const X* row = static_cast<const X*>(f.x) + (int64_t)min(t, a.T - 1) * f.ldx;
-    HeldRow<X, kHeld> held;
-    held.load(row, a.K, at, per);
+    const int pitch = code_pitch(a.K);
+    char* const codes = s_mem + kRingBytes + kScaleBytes + sum_bytes(TB, split);
     if (tid < 16) s_max[tid] = 0;
-    asm volatile("" ::: "memory");
-    first_loads();
     lds_barrier();
     unsigned top = 0;
     float v[kVec];
 #pragma unroll
-    for (int u = 0; u < kHeld; ++u) if (u * per * kVec < a.K) { held.values(u, v); top = max(top, magnitude(v)); }
-    for (int k = (kHeld * per + at) * kVec; k < a.K; k += per * kVec) {
-      load_floats(row, k, a.K, v);
+    for (int u = 0; u < kHeld; ++u) { held.values(u, v); top = max(top, magnitude(v)); }
+    for (int k = (kHeld * per + fat) * kVec; k < a.K; k += per * kVec) {
+      load_floats(frow, k, a.K, v);
       top = max(top, magnitude(v));
     }
     for (int o = min(per, 64) / 2; o; o >>= 1) top = max(top, (unsigned)__shfl_xor((int)top, o));
-    if ((at & 63) == 0 && t < a.T) atomicMax(&s_max[t], top);
+    if ((fat & 63) == 0 && ft < a.T) atomicMax(&s_max[ft], top);
     lds_barrier();
-    if (t < a.T) {                                         // up to K16: there weights may be anything
-      const RowScale code(s_max[t]);
-      char* const codes = s_mem + kRingBytes + t * pitch;
+    if (ft < a.T) {
+      const RowScale code(s_max[ft]);
 #pragma unroll
       for (int u = 0; u < kHeld; ++u) {
-        const int k = (u * per + at) * kVec;
-        if (k < a.K16) { held.values(u, v); store_codes(codes + k, code, v); }
+        const int k = (u * per + fat) * kVec;
+        if (k < Kw) { held.values(u, v); store_codes(codes + ft * pitch + k, code, v); }
       }
-      for (int k = (kHeld * per + at) * kVec; k < a.K16; k += per * kVec) {
-        load_floats(row, k, a.K, v);
-        store_codes(codes + k, code, v);
+      for (int k = (kHeld * per + fat) * kVec; k < Kw; k += per * kVec) {
+        load_floats(frow, k, a.K, v);
+        store_codes(codes + ft * pitch + k, code, v);
       }
     }
     lds_barrier();
+    // behind Kw stands anything: weights are zero there
+    const unsigned at = (unsigned)(size_t)codes + (unsigned)(min(c, a.T - 1) * pitch + first * kRowBytes + 16 * g);
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
+      if (i >= n) break;
+      const unsigned k = at + (unsigned)(i * kRowBytes);
+      read4(xf[i][0], k, k + 64u, k + 128u, k + 192u);
+    }
   } else {
-    first_loads();
+    lds_barrier();
   }
-
-  // The chunk in stage d.  In flight behind it: the chunks up to kRing - 2 further on, and their tokens' codes.
-  constexpr int kPer = 4 + (kAhead ? TB * kSteps : 0);
-  static_assert((kRing - 2) * kPer < 64, "what the wait can count");
-  i32x4 w[4];
-  int k = begin;
-  for (; k + 2 * kRing - 2 < end; k += kRing) {
-#pragma unroll
-    for (int d = 0; d < kRing; ++d) {
-      constexpr int kLast = kRing - 1;
-      wait_loads<(kRing - 2) * kPer>();
-      read_weights(w, w_at, d * kStage);
-      load_w((d + kLast) % kRing, k + d + kLast);
-      if (kAhead) load_x((d + kLast) % kRing, k + d + kLast); else load_x(d, k + d);
-      multiply(d, w);
-    }
-  }
-  // the last chunks, fewer than 2 kRing - 1
-#pragma unroll
-  for (int d = 0; d < 2 * kRing - 2; ++d) {
-    if (k + d < end) {
-      if (k + d + kRing - 2 < end) wait_loads<(kRing - 2) * kPer>();
-      else wait_loads<0>();
-      read_weights(w, w_at, d % kRing * kStage);
-      if (k + d + kRing - 1 < end) { load_w((d + kRing - 1) % kRing, k + d + kRing - 1); if (kAhead) load_x((d + kRing - 1) % kRing, k + d + kRing - 1); }
-      if (!kAhead) load_x(d % kRing, k + d);
-      multiply(d % kRing, w);
-    }
-  }
-  if (FROM == kRows && a.k_tail && part == split - 1 && !idle) {
-    // the last K % 16 codes, in the lanes of the first group
-    const i32x4 zero = {0, 0, 0, 0};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = zero;
-#pragma unroll
-    for (int b = 0; b < TB; ++b) {
-#pragma unroll
-      for (int i = 0; i < kSteps; ++i) xf[0][b][i] = zero;
-      if (g == 0) xf[0][b][0] = masked_codes(reinterpret_cast<const int8_t*>(xrow[b]) + a.K16, a.k_tail);
-    }
-    if (g == 0) w[0] = *reinterpret_cast<const i32x4*>(a.w + (int64_t)min(n0 + c, a.N - 1) * a.ldw + a.K16);
-    multiply(0, w);
-  }
-
-  if (split > 1) {
-    __syncthreads();                                       // the rings have been read
-    i32x4* sums = reinterpret_cast<i32x4*>(s_mem);
-#pragma unroll
-    for (int b = 0; b < TB; ++b) sums[(wave * TB + b) * 64 + lane] = acc[b];
-    __syncthreads();
-    if (part) return;
-    for (int s = 1; s < split; ++s)
-#pragma unroll
-      for (int b = 0; b < TB; ++b) acc[b] += sums[((wave + s) * TB + b) * 64 + lane];
-  }
-  if (idle) return;
-  // a lane's column is a weight row, accumulator v of block b token 16 b + 4 (l / 16) + v
-  float xs = 0.f;
-  if (lane < a.T) {
-    if constexpr (FROM == kFloats) xs = RowScale(s_max[lane & 15]).scale();
-    else xs = a.x_scale[lane];
-  }
-  const int n = n0 + c;
-  const float ws = a.w_scale[min(n, a.N - 1)], bias = a.bias ? a.bias[min(n, a.N - 1)] : 0.f;
+  // token scales of the sums that this wave finishes: tokens 16 b + 4 g + v
+  float xs[TB][4];
 #pragma unroll
   for (int b = 0; b < TB; ++b)
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
       const int t = 16 * b + 4 * g + v;
-      const float s = __shfl(xs, t);
-      if (t < a.T && n < a.N)
-        static_cast<S*>(a.out)[(int64_t)t * a.ldo + n] = to_out<S>(a.bias ? scaled(acc[b][v], s, ws, bias) : scaled(acc[b][v], s, ws));
+      if constexpr (FROM == kFloats) xs[b][v] = t < a.T ? RowScale(s_max[t]).scale() : 0.f;
+      else xs[b][v] = a.x_scale[min(t, a.T - 1)];
     }
+
+  const unsigned wlane = lds0 + (unsigned)(wave * (kRing * kStage) + c * kRowBytes);
+  unsigned w_at[kSteps];
+#pragma unroll
+  for (int s = 0; s < kSteps; ++s) w_at[s] = wlane + (unsigned)(((4 * s + g) ^ c) * 16);
+  const bool with_bias = a.bias != nullptr;
+  auto finish = [&](int turn, int b, const i32x4& sum) {
+    const int r = 16 * (turn * groups + group) + c;
+    const float ws = read_float(scales_at + 4u * (unsigned)r), bias = read_float(scales_at + 4u * (unsigned)(kMaxRows + r));
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      const int t = 16 * b + 4 * g + v;
+      if (t < a.T && r < rows)
+        static_cast<S*>(a.out)[(int64_t)t * a.ldo + row0 + r] = to_out<S>(with_bias ? scaled(sum[v], xs[b][v], ws, bias) : scaled(sum[v], xs[b][v], ws));
+    }
+  };
+  int stage = 0;
+  for (int turn = 0; turn < turns; ++turn) {
+    i32x4 acc[TB] = {};
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
+      if (i >= n) break;
+      wait_loads<(kRing - 2) * 4>();                       // the loads behind this chunk's are those of the two after it
+      i32x4 w[kSteps];
+      const unsigned s = (unsigned)(stage * kStage);
+      read4(w, w_at[0] + s, w_at[1] + s, w_at[2] + s, w_at[3] + s);
+      stage = (stage + 1) & (kRing - 1);
+      load();
+#pragma unroll
+      for (int q = 0; q < kSteps; ++q)
+#pragma unroll
+        for (int b = 0; b < TB; ++b) acc[b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(xf[i][b][q], w[q], acc[b], 0, 0, 0);
+    }
+    if (split == 1) {
+#pragma unroll
+      for (int b = 0; b < TB; ++b) finish(turn, b, acc[b]);
+    } else {
+      // Two sets of sums in turn: one is finished, and left at zero, while the other is added to; the barrier of a turn is behind the
+      // finishing of the one before.
+      const unsigned at = sums_at + (unsigned)(((turn & 1) * groups + group) * TB * 1024 + lane * 16);
+      if (n > 0) {
+#pragma unroll
+        for (int b = 0; b < TB; ++b) add_sum(at + b * 1024u, acc[b]);
+      }
+      lds_barrier();
+#pragma unroll
+      for (int b = 0; b < TB; ++b)
+        if ((b & (split - 1)) == part) finish(turn, b, take_sum(at + b * 1024u));
+    }
+  }
+  wait_loads<0>();                                         // the loads behind the last chunk end before the workgroup does
 }
 
-// K over as many waves of a workgroup as it takes to have two workgroups for every CU, a wave keeping two chunks at least
-int split_of(int N, int K) {
-  const int blocks = (N + 15) / 16, chunks = (K + kRowBytes - 1) / kRowBytes;
+// Waves that share K: as few as their registers allow, more while the rows do not give every wave of the chip a block.
+struct Shape { int split, turns; };
+Shape shape_of(int T, int N, int K) {
+  const int tb = T <= 16 ? 1 : (T <= 32 ? 2 : 4);
+  const int blocks = (N + 15) / 16, chunks = (K + kRowBytes - 1) / kRowBytes, cus = device_cu_count();
   int split = 1;
-  while (split < 4 && blocks * split < 2048 && chunks >= 2 * split) split *= 2;
-  return split;
+  while (split * max_chunks(tb) < chunks) split *= 2;
+  while (split < kWavesS && split < chunks && (int64_t)blocks * split < (int64_t)cus * kWavesS) split *= 2;
+  if (tb == 4 && split == 2) split = 4;                    // the sums of four groups of 64 tokens have no room in LDS
+  const int groups = kWavesS / split;
+  int turns = (blocks + cus * groups - 1) / (cus * groups);
+  if (turns > kMaxRows / (16 * groups)) turns = kMaxRows / (16 * groups);
+  return {split, turns};
 }
 
 template <typename S, Tokens FROM, typename X, int TB>
 int launch_t(const Int8Args& a, const FloatTokens& f, hipStream_t s) {
-  const int split = split_of(a.N, a.K), rows = 16 * (4 / split);
-  const int lds = kRingBytes + (FROM == kFloats ? a.T * code_pitch(a.K) : 0);
+  const Shape sh = shape_of(a.T, a.N, a.K);
+  const int rows = 16 * (kWavesS / sh.split) * sh.turns;
+  constexpr int kFixed = kRingBytes + kScaleBytes, kMost = FROM == kFloats ? sum_bytes(1, 2) + kMaxFused + 16 * 31 + kRowBytes : sum_bytes(TB, TB == 4 ? 4 : 2);
+  static_assert(kFixed + kMost + 64 <= 163840, "LDS of a CU");
+  const int lds = kFixed + sum_bytes(TB, sh.split) + (FROM == kFloats ? code_bytes(a.T, a.K) : 0);
   static std::atomic<int> ready{0};
   if (!ready.load(std::memory_order_relaxed)) {
-    if (hipFuncSetAttribute(reinterpret_cast<const void*>(&int8_stream_kernel<S, FROM, X, TB>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                            kRingBytes + (FROM == kFloats ? kMaxFused + 16 * (kRowBytes + 16) : 0)) != hipSuccess)
+    if (hipFuncSetAttribute(reinterpret_cast<const void*>(&int8_stream_kernel<S, FROM, X, TB>), hipFuncAttributeMaxDynamicSharedMemorySize, kFixed + kMost) != hipSuccess)
       return hip_fail(hipGetLastError(), "int8_stream_kernel: LDS size attribute");
     ready.store(1, std::memory_order_relaxed);
   }
-  hipLaunchKernelGGL((int8_stream_kernel<S, FROM, X, TB>), dim3((unsigned)((a.N + rows - 1) / rows)), dim3(256), (size_t)lds, s, a, f, split);
+  hipLaunchKernelGGL((int8_stream_kernel<S, FROM, X, TB>), dim3((unsigned)((a.N + rows - 1) / rows)), dim3(kThreadsS), (size_t)lds, s, a, f, sh.split, sh.turns);
   return hip_fail(hipGetLastError(), "int8_stream_kernel launch");
 }
-template <typename S>
-int launch_s(const Int8Args& a, bool in_lanes, hipStream_t s) {
+template <typename S, Tokens FROM>
+int launch_b(const Int8Args& a, hipStream_t s) {
   const FloatTokens none = {nullptr, 0};
-  if (in_lanes) return a.T <= 16 ? launch_t<S, kLanes, float, 1>(a, none, s) : launch_t<S, kLanes, float, 2>(a, none, s);
-  return a.T <= 16 ? launch_t<S, kRows, float, 1>(a, none, s) : launch_t<S, kRows, float, 2>(a, none, s);
+  if (a.T <= 16) return launch_t<S, FROM, float, 1>(a, none, s);
+  return a.T <= 32 ? launch_t<S, FROM, float, 2>(a, none, s) : launch_t<S, FROM, float, 4>(a, none, s);
 }
+template <typename S>
+int launch_s(const Int8Args& a, hipStream_t s) { return a.lane_blocks ? launch_b<S, kLanes>(a, s) : launch_b<S, kRows>(a, s); }
 template <typename X>
 int launch_x(const Int8Args& a, const FloatTokens& f, hipStream_t s) {
   return a.out_dtype == MOE_FP32 ? launch_t<float, kFloats, X, 1>(a, f, s) : launch_t<uint16_t, kFloats, X, 1>(a, f, s);
@@ -266,12 +287,11 @@ int launch_x(const Int8Args& a, const FloatTokens& f, hipStream_t s) {
 
 }  // namespace
 
-int launch_int8_stream(const Int8Args& a, bool in_lanes, hipStream_t s) {
-  return a.out_dtype == MOE_FP32 ? launch_s<float>(a, in_lanes, s) : launch_s<uint16_t>(a, in_lanes, s);
-}
+bool int8_streams(int T, int K) { return T <= 64 && (K + kRowBytes - 1) / kRowBytes <= kWavesS * max_chunks(T <= 16 ? 1 : (T <= 32 ? 2 : 4)); }
+int launch_int8_stream(const Int8Args& a, hipStream_t s) { return a.out_dtype == MOE_FP32 ? launch_s<float>(a, s) : launch_s<uint16_t>(a, s); }
 
 bool int8_quantises_itself(int T, int K) { return T <= 16 && (int64_t)T * K <= kMaxFused; }
-size_t int8_lane_codes_bytes(int T, int K) { return (size_t)(T <= 16 ? 16 : 32) * ((K + kRowBytes - 1) / kRowBytes * kRowBytes); }
+size_t int8_lane_codes_bytes(int T, int K) { return (size_t)((T + 15) / 16 * 16) * ((K + kRowBytes - 1) / kRowBytes * kRowBytes); }
 
 int launch_int8_stream_float(const Int8Args& a, const void* x, int x_dtype, int64_t ldx, hipStream_t s) {
   ProfScope ps(kProfInt8Product, s);

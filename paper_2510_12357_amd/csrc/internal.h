@@ -157,24 +157,23 @@ int launch_combine_add(const moe_config& c, const float* y, const float* w, cons
                        const int32_t* k_t, int j_lo, void* out, hipStream_t s);
 
 // ---- the output head: 8-bit product and log probabilities (head_api.hip resolves the dense leading dimensions) -----
-// Where the codes of a row go: one after the other (0); or to the lane that needs them in a matrix instruction of 16 x 16 x 64, lane l the 16 codes
-// from 16 (l / 16) on of row l % 16, for 64 k one or two (the number) blocks of 16 rows.
-enum CodeOrder { kCodeRows = 0, kCodeLanes = 1, kCodeLanes2 = 2 };
-int launch_quantize_rows(const void* x, int dtype, int rows, int K, int64_t ldx, int8_t* q, int64_t ldq, float* scale, CodeOrder order, hipStream_t s);
+// Where the codes of a row go: one after the other (lane_blocks 0); or to the lane that needs them in a matrix instruction of 16 x 16 x 64, lane l the
+// 16 codes from 16 (l / 16) on of row l % 16, for each 64 k the blocks of 16 rows one after the other (lane_blocks: as many).
+int launch_quantize_rows(const void* x, int dtype, int rows, int K, int64_t ldx, int8_t* q, int64_t ldq, float* scale, int lane_blocks, hipStream_t s);
 struct Int8Args {
   int T, N, K, out_dtype;
   int K16, k_tail;         // codes in whole vectors of 16; codes of the last vector that count where it is not all of them (0: the tokens' are zero behind K)
+  int lane_blocks;         // x: 0 rows of ldx codes, else the order of the lanes (launch_quantize_rows)
   int64_t ldx, ldw, ldo;
   const int8_t* x; const float* x_scale;
   const int8_t* w; const float* w_scale; const float* bias;
   void* out;
 };
-int launch_int8_product(const Int8Args& a, bool in_lanes, hipStream_t s);
-constexpr int kInt8StreamTokens = 32;      // most that the streaming kernel takes
+int launch_int8_product(const Int8Args& a, hipStream_t s);
 int launch_int8_wide(const Int8Args& a, int token_tiles, int height, hipStream_t s);      // height: rows of a token tile, at most 256
 int launch_int8_tile(const Int8Args& a, int rows, hipStream_t s);                         // rows of a token tile: 64 or 128
-// T <= 32.  in_lanes: x holds the codes in the order that CodeOrder names, not in rows
-int launch_int8_stream(const Int8Args& a, bool in_lanes, hipStream_t s);
+bool int8_streams(int T, int K);           // whether launch_int8_stream takes these sizes
+int launch_int8_stream(const Int8Args& a, hipStream_t s);
 size_t int8_lane_codes_bytes(int T, int K);
 // the same on float tokens, quantised by every workgroup; where int8_quantises_itself says so
 bool int8_quantises_itself(int T, int K);
