@@ -129,8 +129,9 @@ __device__ __forceinline__ i32x4 keep_codes(i32x4 v, int left) {
 }
 __device__ __forceinline__ i32x4 masked_codes(const int8_t* p, int left) { return keep_codes(*reinterpret_cast<const i32x4*>(p), left); }
 
-// One output from its exact sum; every kernel of the product ends with this, so that its bits do not depend on the kernel.
-__device__ __forceinline__ float scaled(int sum, float x_scale, float w_scale) { return ((float)sum * x_scale) * w_scale; }
+// One output from its exact sum; every kernel of the product ends with this, so that its bits do not depend on the kernel.  No bias is one of -0,
+// which leaves every product as it is, zeros of either sign too.
+constexpr float kNoBias = -0.f;
 __device__ __forceinline__ float scaled(int sum, float x_scale, float w_scale, float bias) { return fmaf((float)sum * x_scale, w_scale, bias); }
 
 }  // namespace

@@ -126,8 +126,8 @@ __global__ __launch_bounds__(kThreadsS) __attribute__((amdgpu_waves_per_eu(2, 2)
     load_chunk = load_chunk + 1 >= n ? 0 : load_chunk + 1;
     load_turn += load_chunk == 0;
   };
-  // scales and biases of the rows, the latter zeros where there are none; sums start from zero
-  float ws0[2] = {0.f, 0.f};
+  // scales and biases of the rows, the latter kNoBias where there are none; sums start from zero
+  float ws0[2] = {0.f, kNoBias};
   if (tid < rows) { ws0[0] = a.w_scale[row0 + tid]; if (a.bias) ws0[1] = a.bias[row0 + tid]; }
   static_assert(kMaxRows <= kThreadsS, "one row a thread");
   asm volatile("" ::: "memory");
@@ -193,7 +193,6 @@ __global__ __launch_bounds__(kThreadsS) __attribute__((amdgpu_waves_per_eu(2, 2)
   unsigned w_at[kSteps];
 #pragma unroll
   for (int s = 0; s < kSteps; ++s) w_at[s] = wlane + (unsigned)(((4 * s + g) ^ c) * 16);
-  const bool with_bias = a.bias != nullptr;
   auto finish = [&](int turn, int b, const i32x4& sum) {
     const int r = 16 * (turn * groups + group) + c;
     const float ws = read_float(scales_at + 4u * (unsigned)r), bias = read_float(scales_at + 4u * (unsigned)(kMaxRows + r));
@@ -201,7 +200,7 @@ __global__ __launch_bounds__(kThreadsS) __attribute__((amdgpu_waves_per_eu(2, 2)
     for (int v = 0; v < 4; ++v) {
       const int t = 16 * b + 4 * g + v;
       if (t < a.T && r < rows)
-        static_cast<S*>(a.out)[(int64_t)t * a.ldo + row0 + r] = to_out<S>(with_bias ? scaled(sum[v], xs[b][v], ws, bias) : scaled(sum[v], xs[b][v], ws));
+        static_cast<S*>(a.out)[(int64_t)t * a.ldo + row0 + r] = to_out<S>(scaled(sum[v], xs[b][v], ws, bias));
     }
   };
   int stage = 0;

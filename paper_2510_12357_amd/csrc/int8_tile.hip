@@ -74,7 +74,7 @@ __global__ __launch_bounds__(256) void int8_tile_kernel(const Int8Args a, const 
   for (int j = 0; j < 2; ++j) {
     const int n = min(n0 + n_l + j, a.N - 1);
     ws[j] = a.w_scale[n];
-    bias[j] = a.bias ? a.bias[n] : 0.f;
+    bias[j] = a.bias ? a.bias[n] : kNoBias;
   }
   const float xs = a.x_scale[min(m0 + wm * TM * 32 + lane, a.T - 1)];
 
@@ -162,7 +162,7 @@ __global__ __launch_bounds__(256) void int8_tile_kernel(const Int8Args a, const 
       const float s = __shfl(xs, r + 4 * h);
       Unaligned<S, 2> o;
 #pragma unroll
-      for (int j = 0; j < 2; ++j) o.v[j] = to_out<S>(a.bias ? scaled(acc[i][j][e], s, ws[j], bias[j]) : scaled(acc[i][j][e], s, ws[j]));
+      for (int j = 0; j < 2; ++j) o.v[j] = to_out<S>(scaled(acc[i][j][e], s, ws[j], bias[j]));
       S* const p = out0 + (int64_t)r * a.ldo + lane_off;
       if (whole) {
         *reinterpret_cast<Unaligned<S, 2>*>(p) = o;

@@ -10,6 +10,7 @@
 //     that its L2 has to fetch are the fewest so.
 //   * Codes behind K: whole vectors of 16 bytes are not loaded.  The rest of K % 16 codes is added by one k-step of its own, masked.
 #include <atomic>
+#include <type_traits>
 
 #include "internal.h"
 #include "int8_device.h"
@@ -35,6 +36,19 @@ __device__ __forceinline__ void multiply(i32x16 (&c)[4][4], const i32x4 (&fa)[4]
 #pragma unroll
     for (int j = 0; j < (TALL ? 4 : 2); ++j)
       asm volatile("s_nop 4\n\tv_mfma_i32_32x32x32_i8 %0, %1, %2, %0" : "+a"(c[i][j]) : "v"(fa[i]), "v"(fb[j]));
+}
+
+// Matrix results are readable behind this, and the compiler moves none of them in front of it.
+template <bool TALL, int NB>
+__device__ __forceinline__ void settle(i32x16 (&c)[4][4]) {
+#define SETTLE "s_nop 15\n\ts_nop 7"
+  if constexpr (TALL && NB == 4) asm volatile(SETTLE : C4(0), C4(1), C4(2), C4(3));
+  else if constexpr (TALL) asm volatile(SETTLE : C4(0), C4(1), C4(2));
+  else if constexpr (NB == 4) asm volatile(SETTLE : C1(0, 0), C1(0, 1), C1(1, 0), C1(1, 1), C1(2, 0), C1(2, 1), C1(3, 0), C1(3, 1));
+  else if constexpr (NB == 3) asm volatile(SETTLE : C1(0, 0), C1(0, 1), C1(1, 0), C1(1, 1), C1(2, 0), C1(2, 1));
+  else if constexpr (NB == 2) asm volatile(SETTLE : C1(0, 0), C1(0, 1), C1(1, 0), C1(1, 1));
+  else asm volatile(SETTLE : C1(0, 0), C1(0, 1));
+#undef SETTLE
 }
 
 template <typename S>
@@ -156,18 +170,31 @@ __global__ __launch_bounds__(kThreadsW) __attribute__((amdgpu_waves_per_eu(1, 1)
 #pragma unroll
     for (int l = 0; l < kLoads; ++l) load_one(rsA, aoff[l], ka, ldsA + slA * kSlotB + l * 1024);
     const int nk = uniform(tile_chunks((K16 + 1) / 2));
-    for (;;) {
-      // scales of this lane's outputs and of the wave's token rows (rows lane and lane + 64)
-      float ws[TN], bias[TN], xs[2];
-      const int n_l = (TALL ? wn * 128 : wn * 64) + TN * (lane & 31);
+    // Scales of this lane's outputs and of the wave's token rows (rows lane and lane + 64).  Loads end in order, so those of the next tile are issued in
+    // front of this tile's stores and awaited behind them: nowhere does a wait for them stop the loads into LDS.
+    const int n_l = (TALL ? wn * 128 : wn * 64) + TN * (lane & 31);
+    struct Scales { float w[TN], bias[TN], x[2]; };
+    auto scales_of = [&](const Tile& T) {
+      Scales s;
 #pragma unroll
       for (int j = 0; j < TN; ++j) {
-        const int n = min(cur.n0 + n_l + j, a.N - 1);
-        ws[j] = a.w_scale[n];
-        bias[j] = a.bias ? a.bias[n] : 0.f;
+        const int n = min(T.n0 + n_l + j, a.N - 1);
+        s.w[j] = a.w_scale[n];
+        s.bias[j] = a.bias ? a.bias[n] : kNoBias;
       }
 #pragma unroll
-      for (int q = 0; q < 2; ++q) xs[q] = a.x_scale[min(cur.m0 + wm * NB * 32 + q * 64 + lane, a.T - 1)];
+      for (int q = 0; q < 2; ++q) s.x[q] = a.x_scale[min(T.m0 + wm * NB * 32 + q * 64 + lane, a.T - 1)];
+      asm volatile("" ::: "memory");
+      return s;
+    };
+    auto await = [&](Scales& s) {
+#pragma unroll
+      for (int j = 0; j < TN; ++j) asm volatile("" : "+v"(s.w[j]), "+v"(s.bias[j]));
+      asm volatile("" : "+v"(s.x[0]), "+v"(s.x[1]));
+    };
+    Scales sc = scales_of(cur);
+    await(sc);
+    for (;;) {
 #pragma unroll
       for (int i = 0; i < NB; ++i)
 #pragma unroll
@@ -206,35 +233,37 @@ __global__ __launch_bounds__(kThreadsW) __attribute__((amdgpu_waves_per_eu(1, 1)
         }
         multiply<TALL, NB>(acc, ta, tb);
       }
-      asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");    // matrix results are readable
+      settle<TALL, NB>(acc);
       // ---- epilogue: accumulator v of lane l is row 8*(v/4) + 4*(l/32) + v%4, output TN*(l%32) + j ----
+      Scales next = scales_of(nx);
       const int row_w = wm * NB * 32;
       const bool whole = cur.cols == 256 && cur.rows == (TALL ? 2 : 1) * NB * 32;
-      S* const out0 = static_cast<S*>(a.out) + (int64_t)(cur.m0 + row_w) * a.ldo + cur.n0;
-      const unsigned lane_off = (unsigned)(4 * h) * (unsigned)a.ldo + (unsigned)n_l;
+      char* out_r = static_cast<char*>(a.out) + ((int64_t)(cur.m0 + row_w) * a.ldo + cur.n0) * sizeof(S);
+      const unsigned lane_off = ((unsigned)(4 * h) * (unsigned)a.ldo + (unsigned)n_l) * (unsigned)sizeof(S);
+      auto store = [&](auto whole_tag) {
 #pragma unroll
-      for (int i = 0; i < NB; ++i)
+        for (int i = 0; i < NB; ++i)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          __builtin_amdgcn_sched_barrier(0);
-          const int r = i * 32 + 8 * (v >> 2) + (v & 3);   // + 4 h
-          const float s0 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(xs[r >> 6]), r & 63));
-          const float s1 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(xs[r >> 6]), (r & 63) + 4));
-          const float s = h ? s1 : s0;
-          Unaligned<S, TN> o;
+          for (int v = 0; v < 16; ++v) {
+            __builtin_amdgcn_sched_barrier(0);
+            const int r = i * 32 + 8 * (v >> 2) + (v & 3);   // + 4 h
+            const float s0 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sc.x[r >> 6]), r & 63));
+            const float s1 = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(sc.x[r >> 6]), (r & 63) + 4));
+            const float s = h ? s1 : s0;
+            Unaligned<S, TN> o;
 #pragma unroll
-          for (int j = 0; j < TN; ++j) {
-            const int sum = acc_read(acc[i][j], v);
-            o.v[j] = to_out<S>(a.bias ? scaled(sum, s, ws[j], bias[j]) : scaled(sum, s, ws[j]));
+            for (int j = 0; j < TN; ++j) o.v[j] = to_out<S>(scaled(acc_read(acc[i][j], v), s, sc.w[j], sc.bias[j]));
+            S* const p = reinterpret_cast<S*>(out_r + (int64_t)r * a.ldo * (int)sizeof(S) + lane_off);
+            if constexpr (decltype(whole_tag)::value) {
+              *reinterpret_cast<Unaligned<S, TN>*>(p) = o;
+            } else if (row_w + r + 4 * h < cur.rows) {
+#pragma unroll
+              for (int j = 0; j < TN; ++j) if (n_l + j < cur.cols) p[j] = o.v[j];
+            }
           }
-          S* const p = out0 + (int64_t)r * a.ldo + lane_off;
-          if (whole) {
-            *reinterpret_cast<Unaligned<S, TN>*>(p) = o;
-          } else if (row_w + r + 4 * h < cur.rows) {
-#pragma unroll
-            for (int j = 0; j < TN; ++j) if (n_l + j < cur.cols) p[j] = o.v[j];
-          }
-        }
+      };
+      if (whole) { store(std::true_type{}); await(next); } else { store(std::false_type{}); await(next); }
+      sc = next;
       cur = nx;
       if (!cur.valid) break;
       nx = tile_at(ord++);
