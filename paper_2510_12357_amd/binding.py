@@ -569,45 +569,79 @@ def _torch_stream(stream) -> torch.cuda.Stream:
     return stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream))
 
 
+def _raw_stream(stream, device: int) -> int:
+    """The stream's handle as a number; None: torch's current stream of the device."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device)
+    return stream.cuda_stream if isinstance(stream, torch.cuda.Stream) else int(stream)
+
+
 class Int8Linear:
     """A projection with 8-bit weights: codes w [N, K] (rows padded to 16 bytes, as quantize_rows makes them), w_scale [N] and
     an optional bias [N] in fp32.  Calling it enqueues one product on `stream`; the workspace for float tokens is kept and
     grows with the largest call, so calls that may overlap (streams without order between them) need an object each."""
 
     def __init__(self, w: torch.Tensor, w_scale: torch.Tensor, bias: Optional[torch.Tensor] = None):
-        self.w, self.w_scale, self.bias = w, w_scale, bias
+        load_library()
+        _rows(w)
+        for name, t in (("w_scale", w_scale), ("bias", bias)):
+            assert t is None or (t.dtype == torch.float32 and tuple(t.shape) == (w.shape[0],) and t.is_contiguous()), f"{name}: [N] fp32"
+        assert w.dtype == torch.int8 and all(t is None or t.device == w.device for t in (w_scale, bias)), "int8 codes, all on one device"
+        self._w, self._w_scale, self._bias = w, w_scale, bias
         self.ws = self.ws_stream = None
+        self._calls = {}                                     # of each form of tokens and outputs: its description, workspace bytes
+
+    w, w_scale, bias = property(lambda self: self._w), property(lambda self: self._w_scale), property(lambda self: self._bias)
 
     @classmethod
     def quantize(cls, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, stream=None) -> "Int8Linear":
         """From a float weight [N, K]."""
         return cls(*quantize_rows(weight, stream), bias)
 
-    def _workspace(self, need: int, device, stream) -> torch.Tensor:
+    def _workspace(self, need: int, stream, handle: int) -> int:
         # memory belongs to the stream it was taken on: its reuse after a larger call has replaced it waits for every stream that read it
         if self.ws is None or self.ws.numel() < need:
-            self.ws_stream = _torch_stream(stream)
-            with torch.cuda.stream(self.ws_stream):
-                self.ws = torch.empty((need,), dtype=torch.uint8, device=device)
-        elif stream is not None or torch.cuda.current_stream() != self.ws_stream:
             s = _torch_stream(stream)
-            if s != self.ws_stream:
-                self.ws.record_stream(s)
-        return self.ws
+            with torch.cuda.stream(s):
+                self.ws = torch.empty((need,), dtype=torch.uint8, device=self._w.device)
+            self.ws_stream = handle
+        elif handle != self.ws_stream:
+            self.ws.record_stream(_torch_stream(stream))
+        return self.ws.data_ptr()
+
+    def _call(self, x: torch.Tensor, out: torch.Tensor):
+        """-> (description, workspace bytes) of a call with such tokens and outputs: the checks that their shapes, types and strides need."""
+        _rows(x), _rows(out)
+        assert x.device == self._w.device and out.device == self._w.device, "x, out and the weights belong on one device"
+        c = int8_config(x, self._w, out)
+        need = 0 if x.dtype == torch.int8 else moe_linear_int8_workspace_bytes(c)
+        if len(self._calls) > 256:                           # a server's batches are of any size
+            self._calls.clear()
+        return c, ctypes.byref(c), need
 
     def __call__(self, x: torch.Tensor, x_scale: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
                  stream=None) -> torch.Tensor:
         """x: float tokens [T, K], or their codes with x_scale [T].  out: [T, N] bf16 or fp32 (default: a new fp32 tensor)."""
         if out is None:
             with torch.cuda.stream(_torch_stream(stream)):
-                out = torch.empty((x.shape[0], self.w.shape[0]), dtype=torch.float32, device=x.device)
-        c = int8_config(x, self.w, out)
-        if x.dtype == torch.int8:
-            assert x_scale is not None, "codes come with their scales"
-            moe_matmul_int8(c, x, x_scale, self.w, self.w_scale, self.bias, out, stream)
-            return out
-        ws = self._workspace(moe_linear_int8_workspace_bytes(c), x.device, stream)
-        moe_linear_int8(c, x, self.w, self.w_scale, self.bias, out, ws, ws.numel(), stream)
+                out = torch.empty((x.shape[0], self._w.shape[0]), dtype=torch.float32, device=x.device)
+        key = (x.shape, x.stride(), x.dtype, x.get_device(), out.shape, out.stride(), out.dtype, out.get_device())
+        call = self._calls.get(key)
+        if call is None:
+            call = self._call(x, out)
+            self._calls[key] = call
+        _, c, need = call
+        s = _raw_stream(stream, key[3])
+        bias = None if self._bias is None else self._bias.data_ptr()
+        if x.dtype is torch.int8:
+            assert x_scale is not None and x_scale.dtype is torch.float32 and x_scale.numel() == x.shape[0] and x_scale.is_contiguous(), \
+                "codes come with their scales, [T] fp32"
+            rc = _lib.moe_matmul_int8(c, x.data_ptr(), x_scale.data_ptr(), self._w.data_ptr(), self._w_scale.data_ptr(), bias, out.data_ptr(), s)
+        else:
+            ws = self._workspace(need, stream, s)
+            rc = _lib.moe_linear_int8(c, x.data_ptr(), self._w.data_ptr(), self._w_scale.data_ptr(), bias, out.data_ptr(), ws, self.ws.numel(), s)
+        if rc:
+            _check(rc)
         return out
 
 
@@ -627,16 +661,27 @@ class LogprobBuffers:
             c = self.c[dtype] = moe_logprobs_config()
             c.T, c.V, c.dtype, c.n_given, c.n_top, c.ld = T, V, dtype, n_given, n_top, V
             need = max(need, moe_token_logprobs_workspace_bytes(c))
+        self._configs = {torch.bfloat16: (self.c[MOE_BF16], ctypes.byref(self.c[MOE_BF16])),
+                         torch.float32: (self.c[MOE_FP32], ctypes.byref(self.c[MOE_FP32]))}
         self.ws = torch.empty((need,), dtype=torch.uint8, device=device)
 
     def run(self, logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, stream=None) -> "LogprobBuffers":
         """logits [T, V] bf16 or fp32, tokens int32 [T, n_given]."""
-        assert tuple(logits.shape) == (self.T, self.V), "logits do not fit the buffers"
-        assert self.n_given == 0 or (tokens.dtype == torch.int32 and tuple(tokens.shape) == (self.T, self.n_given))
-        c = self.c[_float_type(logits)]
-        c.ld = _ld(logits)
-        moe_token_logprobs(c, logits, tokens, self.token_logp, self.entropy, self.conf, self.top_idx, self.top_logp, self.ws,
-                           self.ws.numel(), stream)
+        T, V = logits.shape
+        assert T == self.T and V == self.V, "logits do not fit the buffers"
+        step, inner = logits.stride()
+        assert inner == 1 or V == 1, "rows passed to the C ABI must be dense"
+        given = None
+        if self.n_given:
+            assert tokens.dtype is torch.int32 and tokens.shape == self.token_logp.shape and tokens.is_contiguous(), "tokens: int32 [T, n_given]"
+            given = tokens.data_ptr()
+        c, ref = self._configs[logits.dtype]
+        c.ld = step if T > 1 else max(step, V)               # a single row has no next one: torch gives such a dimension any stride
+        rc = _lib.moe_token_logprobs(ref, logits.data_ptr(), given, self.token_logp.data_ptr(), self.entropy.data_ptr(), self.conf.data_ptr(),
+                                     self.top_idx.data_ptr(), self.top_logp.data_ptr(), self.ws.data_ptr(), self.ws.numel(),
+                                     _raw_stream(stream, logits.get_device()))
+        if rc:
+            _check(rc)
         return self
 
 

@@ -62,7 +62,6 @@ struct Block { i32x4 rs_a, rs_b; unsigned a_row, b_row, a_next, b_next, to_a, to
   MF(1, 0, A, B) RA(X, 0) MF(1, 1, A, B) RA(X, 1) L1 MF(1, 2, A, B) RA(X, 2) MF(1, 3, A, B) L2 MF4(2, A, B) DONE
 #define STEP2(A, B, X, Y, k, L0, L1, L2) AT(k, ra0, rb0) MF(0, 0, A, B) RB(Y, 0) RB(Y, 1) MF(0, 1, A, B) RB(Y, 2) RB(Y, 3) MF(0, 2, A, B) RA(X, 0) L0 MF(0, 3, A, B) RA(X, 1) \
   MF(1, 0, A, B) L1 MF(1, 1, A, B) L2 MF(1, 2, A, B) MF(1, 3, A, B) DONE
-#define STEP1(A, B, X, Y, k, L0, L1, L2) AT(k, ra0, rb0) MF(0, 0, A, B) RB(Y, 0) RB(Y, 1) RB(Y, 2) RB(Y, 3) RA(X, 0) MF(0, 1, A, B) L0 MF(0, 2, A, B) L1 MF(0, 3, A, B) L2 DONE
 // the last k-step of a chunk; X, Y get the first of the next chunk
 #define LAST4(A, B, X, Y) AT(0, ran, rbn) MF4(0, A, B) BARRIER MF(1, 0, A, B) RB(Y, 0) RB(Y, 1) MF(1, 1, A, B) RB(Y, 2) RB(Y, 3) MF(1, 2, A, B) RA(X, 0) RA(X, 1) MF(1, 3, A, B) \
   RA(X, 2) RA(X, 3) MF(2, 0, A, B) LA(0) MF(2, 1, A, B) LA(1) MF(2, 2, A, B) LA(2) MF(2, 3, A, B) LA(3) MF(3, 0, A, B) LA(4) MF(3, 1, A, B) LA(5) MF(3, 2, A, B) LA(6) MF(3, 3, A, B) LA(7) DONE
@@ -70,7 +69,6 @@ struct Block { i32x4 rs_a, rs_b; unsigned a_row, b_row, a_next, b_next, to_a, to
   RA(X, 2) LA(0) LA(1) MF(2, 0, A, B) LA(2) LA(3) MF(2, 1, A, B) LA(4) MF(2, 2, A, B) LA(5) MF(2, 3, A, B) LA(6) LA(7) DONE
 #define LAST2(A, B, X, Y) AT(0, ran, rbn) MF4(0, A, B) BARRIER MF(1, 0, A, B) RB(Y, 0) RB(Y, 1) RB(Y, 2) RB(Y, 3) MF(1, 1, A, B) RA(X, 0) RA(X, 1) LA(0) LA(1) MF(1, 2, A, B) \
   LA(2) LA(3) LA(4) MF(1, 3, A, B) LA(5) LA(6) LA(7) DONE
-#define LAST1(A, B, X, Y) AT(0, ran, rbn) MF4(0, A, B) BARRIER RB(Y, 0) RB(Y, 1) RB(Y, 2) RB(Y, 3) RA(X, 0) LA(0) LA(1) LA(2) LA(3) LA(4) LA(5) LA(6) LA(7) DONE
 #define CHUNK(N) START STEP##N(p, q, u, w, 1, LB(0), LB(1), LB(2)) STEP##N(u, w, p, q, 2, LB(3), LB(4), LB(5)) STEP##N(p, q, u, w, 3, LB(6), LB(7), "") LAST##N(u, w, p, q)
 
 #define C1(i, j) [c##i##j] "+a"(c[i][j])
@@ -93,10 +91,8 @@ __device__ __forceinline__ void chunk(i32x16 (&c)[4][4], Frags& f, const unsigne
     asm volatile(CHUNK(4) : C4(0), C4(1), C4(2), C4(3), FA(0), FA(1), FA(2), FA(3), FB(0), FB(1), FB(2), FB(3), ADDRESSES : INPUTS : "memory", "scc");
   else if constexpr (NB == 3)
     asm volatile(CHUNK(3) : C4(0), C4(1), C4(2), FA(0), FA(1), FA(2), FB(0), FB(1), FB(2), FB(3), ADDRESSES : INPUTS : "memory", "scc");
-  else if constexpr (NB == 2)
-    asm volatile(CHUNK(2) : C4(0), C4(1), FA(0), FA(1), FB(0), FB(1), FB(2), FB(3), ADDRESSES : INPUTS : "memory", "scc");
   else
-    asm volatile(CHUNK(1) : C4(0), FA(0), FB(0), FB(1), FB(2), FB(3), ADDRESSES : INPUTS : "memory", "scc");
+    asm volatile(CHUNK(2) : C4(0), C4(1), FA(0), FA(1), FB(0), FB(1), FB(2), FB(3), ADDRESSES : INPUTS : "memory", "scc");
 }
 // Matrix results are readable behind this, and the compiler moves none of them in front of it.
 template <int NB>
@@ -104,8 +100,7 @@ __device__ __forceinline__ void settle(i32x16 (&c)[4][4]) {
 #define SETTLE "s_nop 15\n\ts_nop 7"
   if constexpr (NB == 4) asm volatile(SETTLE : C4(0), C4(1), C4(2), C4(3));
   else if constexpr (NB == 3) asm volatile(SETTLE : C4(0), C4(1), C4(2));
-  else if constexpr (NB == 2) asm volatile(SETTLE : C4(0), C4(1));
-  else asm volatile(SETTLE : C4(0));
+  else asm volatile(SETTLE : C4(0), C4(1));
 #undef SETTLE
 }
 // The first fragments: nothing to multiply yet.  In flight behind chunk 0: the weights of chunk 1.
@@ -117,8 +112,7 @@ __device__ __forceinline__ void first_frags(Frags& f, unsigned pa, unsigned pb) 
 #define FROM [pa] "v"(pa), [pb] "v"(pb), OFFS
   if constexpr (NB == 4) asm volatile(READS RA(p, 0) RA(p, 1) RA(p, 2) RA(p, 3) DONE : QB, PA(0), PA(1), PA(2), PA(3) : FROM : "memory");
   else if constexpr (NB == 3) asm volatile(READS RA(p, 0) RA(p, 1) RA(p, 2) DONE : QB, PA(0), PA(1), PA(2) : FROM : "memory");
-  else if constexpr (NB == 2) asm volatile(READS RA(p, 0) RA(p, 1) DONE : QB, PA(0), PA(1) : FROM : "memory");
-  else asm volatile(READS RA(p, 0) DONE : QB, PA(0) : FROM : "memory");
+  else asm volatile(READS RA(p, 0) RA(p, 1) DONE : QB, PA(0), PA(1) : FROM : "memory");
 }
 __device__ __forceinline__ void load_one(i32x4 rs, unsigned vo, unsigned so, unsigned md) {
   asm volatile("s_mov_b32 m0, %3\n\ts_nop 4\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds" :: "v"(vo), "s"(rs), "s"(so), "s"(md) : "memory");
@@ -146,7 +140,7 @@ __device__ __forceinline__ i32x4 rsrc4(const void* p, unsigned bytes) {
 // themselves (rows and columns are checked), so stating more than a short tensor has lets nothing through.
 constexpr unsigned stated(unsigned bytes) { return bytes < kMinChunks * kRowB ? kMinChunks * kRowB : bytes; }
 
-// Waves in a 2 x 2 grid, each NB blocks of 32 tokens x 128 weight rows: tiles of 64 NB tokens.
+// Waves in a 2 x 2 grid, each NB (2, 3 or 4) blocks of 32 tokens x 128 weight rows: tiles of 64 NB tokens.
 template <typename S, int NB>
 __global__ __launch_bounds__(kThreadsW) __attribute__((amdgpu_waves_per_eu(1, 1))) void int8_wide_kernel(const Int8Args a, const int mt, const int panels) {
   constexpr int kHeight = 64 * NB;
@@ -342,12 +336,8 @@ int launch_t(const Int8Args& a, hipStream_t s) {
 }
 template <typename S>
 int launch_n(const Int8Args& a, int blocks, hipStream_t s) {
-  switch (blocks) {
-    case 1: return launch_t<S, 1>(a, s);
-    case 2: return launch_t<S, 2>(a, s);
-    case 3: return launch_t<S, 3>(a, s);
-    default: return launch_t<S, 4>(a, s);
-  }
+  if (blocks == 4) return launch_t<S, 4>(a, s);
+  return blocks == 3 ? launch_t<S, 3>(a, s) : launch_t<S, 2>(a, s);
 }
 
 }  // namespace
