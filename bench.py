@@ -49,6 +49,9 @@ def parse_args():
                          "(one JSON line per point; the shapes of the paper's Tables 4 and 5)")
     ap.add_argument("--alg1-toy", action="store_true",
                     help="only the Alg. 1 loop on a toy language model made of the workload's layer; one JSON line")
+    ap.add_argument("--vocab", type=int, default=256,
+                    help="tokens of the toy language model of --alg1-toy; above 256 its head is a product of 8-bit integers and "
+                         "the confidences are read off with the log probabilities")
     ap.add_argument("--alg1-offload", action="store_true",
                     help="only the Alg. 1 loop with the experts in host memory, prefetch distance 0..3; one JSON line")
     ap.add_argument("--calibrate-copy", action="store_true",
@@ -478,15 +481,16 @@ def time_alg1_toy(mm, torch, cfg, steps: int, warmup: int, L: int = 4, V: int = 
 
     # input calibration: scale the random head so that a fraction `ratio` of the little model's
     # confidences (over the whole vocabulary as input) does not exceed gamma
-    probe = Alg1Batch(ToyLMDevice(cfg, V, embed, head32.to(dt), layers, norm=True), B, prompts, max_new=32)
-    zs = []
-    for t0 in range(0, V, B):
+    int8_head = V > 256
+    probe = Alg1Batch(ToyLMDevice(cfg, V, embed, head32.to(dt), layers, norm=True, int8_head=int8_head), B, prompts, max_new=32)
+    zs, n_probe = [], min(V, 1024)
+    for t0 in range(0, n_probe, B):
         for b in range(B):
             probe.tokens[b] = [(t0 + b) % V]
         probe.big[:] = False
         probe.step()
-        zs.append(probe.hb.logits.cpu().numpy().astype(np.float64))
-    z = np.concatenate(zs)[:V]
+        zs.append((probe.lm_logits if int8_head else probe.hb.logits).cpu().numpy().astype(np.float64))
+    z = np.concatenate(zs)[:n_probe]
 
     def frac_below(tau):
         zz = tau * z
@@ -497,7 +501,7 @@ def time_alg1_toy(mm, torch, cfg, steps: int, warmup: int, L: int = 4, V: int = 
         mid = (lo * hi) ** 0.5
         lo, hi = (mid, hi) if frac_below(mid) > ratio else (lo, mid)
     tau = hi
-    dev = ToyLMDevice(cfg, V, embed, (head32 * tau).to(dt), layers, norm=True)
+    dev = ToyLMDevice(cfg, V, embed, (head32 * tau).to(dt), layers, norm=True, int8_head=int8_head)
     del probe
 
     def timed(always_big):
@@ -512,8 +516,13 @@ def time_alg1_toy(mm, torch, cfg, steps: int, warmup: int, L: int = 4, V: int = 
         torch.cuda.synchronize()
         dt_s = time.perf_counter() - t0
         acc, fall = run.n_accepted - a0, run.n_fallbacks - f0
-        return dict(tokens_per_s=acc / dt_s, us_per_step=dt_s / (run.n_steps - n0) * 1e6, accepted_tokens=acc,
-                    fallback_ratio=fall / max(acc, 1))
+        res = dict(tokens_per_s=acc / dt_s, us_per_step=dt_s / (run.n_steps - n0) * 1e6, accepted_tokens=acc,
+                   fallback_ratio=fall / max(acc, 1))
+        if int8_head:
+            kept = [v for s in run.finished_logp + run.token_logp for v in s]
+            res["mean_log_p"] = sum(kept) / max(len(kept), 1)
+            res["mean_entropy"] = sum(v for s in run.finished_entropy + run.token_entropy for v in s) / max(len(kept), 1)
+        return res
     # each variant twice, the faster run kept: the first steps after other measurements have shown
     # launch delays that have nothing to do with the step
     def best(always_big):
@@ -523,7 +532,8 @@ def time_alg1_toy(mm, torch, cfg, steps: int, warmup: int, L: int = 4, V: int = 
     # Eq. 1 with per-slot pass times: a step costs about the same in either mode here (weights
     # resident), so T = T_b = the all-big step and T_l = a step of little passes only
     r = method["fallback_ratio"]
-    return dict(layers=L, slots=B, vocabulary=V, steps=steps, head_scale=tau, calibrated_for_ratio=ratio,
+    read_off = {k: method[k] for k in ("mean_log_p", "mean_entropy") if k in method}
+    return dict(**read_off, layers=L, slots=B, vocabulary=V, steps=steps, head_scale=tau, calibrated_for_ratio=ratio,
                 realised_fallback_ratio=r, tokens_per_s=method["tokens_per_s"],
                 us_per_step=method["us_per_step"], all_big_tokens_per_s=plain["tokens_per_s"],
                 all_big_us_per_step=plain["us_per_step"],
@@ -859,7 +869,7 @@ def main():
     if args.alg1_toy:
         L = args.layers if args.layers > 0 else 4
         res = time_alg1_toy(mm, torch, workload_config(args.workload, args.ratio), args.steps, args.warmup, L=L,
-                            ratio=args.ratio)
+                            V=args.vocab, ratio=args.ratio)
         print(json.dumps(dict(metric="Alg. 1 on a toy MoE language model: accepted tokens/s", workload=args.workload,
                               **res)))
         return

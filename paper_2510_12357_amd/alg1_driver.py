@@ -1,9 +1,11 @@
 """Alg. 1 over a batch of sequences (continuous batching) on a toy MoE language model.
 
 The method's arithmetic runs in the library's kernels: the layers are `layer_step` calls; the
-output head reuses `moe_route` with the vocabulary in the place of the experts (its logits are
-x . head^T and its rank-0 selection is the most probable token, lowest id among equals); the
-confidence is `moe_token_confidence`.  torch gathers embedding rows, optionally rescales a layer's
+output head of a small vocabulary reuses `moe_route` with the vocabulary in the place of the experts
+(its logits are x . head^T and its rank-0 selection is the most probable token, lowest id among
+equals) and the confidence is `moe_token_confidence`; a vocabulary of any size has its head in 8-bit
+integers (`moe_linear_int8`), and `moe_token_logprobs` reads the most probable token, the confidence, the
+log probability of the token and the entropy off its logits in one pass.  torch gathers embedding rows, optionally rescales a layer's
 output rows to unit RMS (the toy model's glue between layers: a stack of SwiGLU layers is quadratic
 in its input and needs it beyond a few layers) and carries a few small arrays to the host, where the
 loop of Alg. 1 takes its decisions.
@@ -43,21 +45,23 @@ class ToyLMDevice:
     the toy model does not have, for measurements that need its time."""
 
     def __init__(self, cfg: wl.LayerConfig, V: int, embed: torch.Tensor, head: torch.Tensor, layers: list,
-                 norm: bool = False, block_work=None):
-        if V > 256:
+                 norm: bool = False, block_work=None, int8_head: bool = False):
+        if V > 256 and not int8_head:
             raise ValueError("the output head runs on the router kernel: at most 256 tokens in the vocabulary")
         self.cfg, self.V, self.device = cfg, V, embed.device
         self.embed, self.head, self.layers, self.norm = embed, head, layers, norm
         self.block_work = block_work
+        # a head of codes and one scale per token, for a vocabulary of any size
+        self.int8_head = mm.Int8Linear.quantize(head) if int8_head else None
         # the head as a "router" over V outputs with one selected entry
-        self.head_cfg = wl.LayerConfig("lm_head", T=1, H=cfg.H, E=V, I=16, k_big=1, k_little=1,
+        self.head_cfg = None if int8_head else wl.LayerConfig("lm_head", T=1, H=cfg.H, E=V, I=16, k_big=1, k_little=1,
                                        dtype="fp32" if cfg.dtype == "fp32" else "bf16", gamma=cfg.gamma)
 
     @classmethod
-    def upload(cls, lm: wl.ToyLM, device="cuda") -> "ToyLMDevice":
+    def upload(cls, lm: wl.ToyLM, device="cuda", int8_head: bool = False) -> "ToyLMDevice":
         """Device copies of a workloads.ToyLM."""
         cfg = lm.cfg
-        if lm.V > 256:
+        if lm.V > 256 and not int8_head:
             raise ValueError("the output head runs on the router kernel: at most 256 tokens in the vocabulary")
         layers = []
         for l in lm.layers:
@@ -71,7 +75,7 @@ class ToyLMDevice:
                 experts=experts, table=table,
                 shared=[mm.to_device(b, cfg, device) for b in l.shared_w]))
         return cls(cfg, lm.V, mm.to_device(lm.embed, cfg, device), mm.to_device(lm.head, cfg, device), layers,
-                   lm.norm)
+                   lm.norm, int8_head=int8_head)
 
     def between_layers(self, out: torch.Tensor) -> torch.Tensor:
         """What the next layer (or the head) reads: the layer's stored output, with `norm` its rows
@@ -127,8 +131,12 @@ class Alg1Batch:
         self.prompts, self.next_prompt = np.asarray(prompts, np.int64), 0
         d = dev.device
         self.bufs = [mm.StepBuffers(dev.cfg, B, d) for _ in dev.layers]
-        self.hb = mm.StepBuffers(dev.head_cfg, B, d)
-        self.conf_out = torch.empty((B,), dtype=torch.float32, device=d)
+        if dev.int8_head is None:
+            self.hb = mm.StepBuffers(dev.head_cfg, B, d)
+            self.conf_out = torch.empty((B,), dtype=torch.float32, device=d)
+        else:
+            self.lm_logits = torch.empty((B, dev.V), dtype=torch.float32, device=d)
+            self.lp = mm.LogprobBuffers(B, 0, 1, dev.V, d)
         self.tok_dev = torch.empty((B,), dtype=torch.int64, device=d)
         self.conf_dev = torch.empty((B,), dtype=torch.float32, device=d)
         # host state of the slots
@@ -138,6 +146,10 @@ class Alg1Batch:
         self.big = np.zeros(B, bool)
         self.rejected_conf = np.zeros(B, np.float32)
         self.finished = []                  # (seq_id, tokens, from_big)
+        # with an 8-bit head: log p and entropy of every token that was kept, and those of the finished sequences
+        self.token_logp: List[List[float]] = [[] for _ in range(B)]
+        self.token_entropy: List[List[float]] = [[] for _ in range(B)]
+        self.finished_logp, self.finished_entropy = [], []
         self.n_steps = self.n_accepted = self.n_fallbacks = self.n_little = self.n_big = 0
         # offloading: the prediction made from the router logits of the rejected passes (experts per
         # layer, most likely first), and the counters
@@ -167,6 +179,7 @@ class Alg1Batch:
             self.seq_id[b] = -1
             self.tokens[b] = []
         self.from_big[b] = []
+        self.token_logp[b], self.token_entropy[b] = [], []
         self.big[b] = self.always_big
 
     def active(self) -> np.ndarray:
@@ -207,12 +220,21 @@ class Alg1Batch:
                 self.waves += waves
             x = dev.between_layers(x)
             xs.append(x)
-        hb = self.hb
-        mm.moe_route(hb.c, x, dev.head, None, None, hb.logits, False, hb.topk_idx, hb.topk_w, hb.important,
-                     hb.k_t, None)
-        mm.moe_token_confidence(hb.logits, B, dev.V, self.conf_out, None)
-        conf = self.conf_out.cpu().numpy()          # synchronises
-        top = hb.topk_idx[:, 0].cpu().numpy()
+        logp = entropy = None
+        if dev.int8_head is None:
+            hb = self.hb
+            lm_logits = hb.logits
+            mm.moe_route(hb.c, x, dev.head, None, None, hb.logits, False, hb.topk_idx, hb.topk_w, hb.important,
+                         hb.k_t, None)
+            mm.moe_token_confidence(hb.logits, B, dev.V, self.conf_out, None)
+            conf = self.conf_out.cpu().numpy()      # synchronises
+            top = hb.topk_idx[:, 0].cpu().numpy()
+        else:
+            lm_logits = self.lm_logits
+            self.lp.run(dev.int8_head(x, out=lm_logits))
+            conf = self.lp.conf.cpu().numpy()       # synchronises
+            top = self.lp.top_idx[:, 0].cpu().numpy()
+            logp, entropy = self.lp.top_logp[:, 0].cpu().numpy(), self.lp.entropy.cpu().numpy()
         if self.record is not None:
             self.record.append(dict(
                 seq_id=list(self.seq_id), pos=[len(t) for t in self.tokens], tokens_in=tok.copy(),
@@ -221,7 +243,7 @@ class Alg1Batch:
                              topk_idx=b.topk_idx.cpu().numpy(), k_t=b.k_t.cpu().numpy(),
                              important=b.important.cpu().numpy(), out=b.out.detach().cpu())
                         for xi, b in zip(xs, self.bufs)],
-                x_head=x.detach().cpu(), lm_logits=hb.logits.cpu().numpy(), conf=conf.copy(), top=top.copy()))
+                x_head=x.detach().cpu(), lm_logits=lm_logits.cpu().numpy(), conf=conf.copy(), top=top.copy()))
         self.n_steps += 1
         rejected: List[int] = []
         for b in range(B):
@@ -240,10 +262,15 @@ class Alg1Batch:
                 continue
             self.tokens[b].append(int(top[b]))
             self.from_big[b].append(bool(self.big[b]))
+            if logp is not None:
+                self.token_logp[b].append(float(logp[b]))
+                self.token_entropy[b].append(float(entropy[b]))
             self.big[b] = self.always_big
             self.n_accepted += 1
             if int(top[b]) == self.eos or len(self.from_big[b]) >= self.max_new:
                 self.finished.append((self.seq_id[b], self.tokens[b], self.from_big[b]))
+                self.finished_logp.append(self.token_logp[b])
+                self.finished_entropy.append(self.token_entropy[b])
                 self._refill(b)
         if self.caches is not None:
             self._predict(rejected)
