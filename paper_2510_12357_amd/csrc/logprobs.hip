@@ -1,17 +1,20 @@
 // Log probabilities of given tokens, entropy, confidence and most probable tokens of output distributions.
 //
 // One pass over a row.  A wave keeps the best n entries it has seen as a sorted list, entry j in lane j.  For every other entry z, with
-// d = z log2 e - c, c an fp32 number not far below the wave's largest entry times log2 e:
-//     R += 2^d,    A += 2^d d        (one fused multiply-add rounds d once; c is what it is, so nothing is lost in it).
+// d = z - ref, ref an entry not far below the wave's largest:
+//     R += e^d,    A += e^d d.
 // With m the row's largest entry, R and A of all entries but that one, and relative to m:
-//     log sum = log(1 + R),    entropy = log(1 + R) - ln 2 A / (1 + R),    log p of z = (z - m) - log(1 + R).
-// The largest entry itself is in no sum, so log p of a nearly certain token, -log(1 + R), has all digits of R.
+//     log sum = log(1 + R),    entropy = log(1 + R) - A / (1 + R),    log p of z = (z - m) - log(1 + R).
+// The largest entry itself is in no sum, so log p of a nearly certain token, -log(1 + R), has all digits of R; entries that equal it add exactly
+// one each.
 //
-// A batch of a wave (kPerLane entries per lane) is compared with the list's last entry by one maximum per lane and one ballot, on the exponents d,
-// which follow the order of the entries.  Only where one is not below it, entries go to the list, and what the list drops is summed.  A lower bound of the n-th entry is known from the
-// start: the n-th of the lanes' maxima over the first batches, which wait in registers; about n (1 + log(V / seen)) entries of a row are
-// above what is known when they come.  So the ordinary batch costs a multiply-add, an exponential and three and a half
-// further operations per entry, and nothing crosses the lanes.
+// A batch of a wave (kPerLane entries per lane) is compared with the list's last entry by one maximum per lane and one ballot, on the
+// differences d, which follow the order of the entries.  Only where one is not below it, entries go to the list, and what the list
+// drops is summed.  A lower bound of the n-th entry is known from the start: the n-th of the lanes' maxima over the first batches,
+// which wait in registers; about n (1 + log(V / seen)) entries of a row are above what is known when they come.  So the ordinary
+// batch costs a difference, a product, an exponential and three and a half further operations per entry, and nothing crosses the
+// lanes.  (One multiply-add in place of the difference and the product, on z log2 e - ref log2 e, is no faster, 182 us for 4096 rows of
+// 131072 in bf16 either way, and equal entries then add what the rounded ref log2 e makes of them.)
 // Waves of a row (and workgroups, where rows are few) take batches in turn and are joined at the end: sums by the rule of a
 // streaming softmax, lists by counting for each candidate how many come before it.  Nothing depends on which wave is first.
 #include "internal.h"
@@ -30,8 +33,7 @@ constexpr int kBatch = 64 * kPerLaneB;
 constexpr int ring(size_t bytes) { return bytes == 2 ? 4 : 2; }   // batches of a wave in registers or on their way
 constexpr int kMaxParts = 16;                              // workgroups of a row, a power of two as the waves are
 constexpr float kLead = 20.f;                              // entries may lie this far above the reference: e^20 is far from overflow
-constexpr float kLeadD = 28.f;                             // ... its exponent, less a little
-constexpr float kFloor = -200.f;                           // d is held here beside 2^d = 0
+constexpr float kFloor = -200.f;                           // d is held here beside e^d = 0
 
 struct LogprobArgs {
   const void* logits; int64_t ld;
@@ -72,32 +74,19 @@ __device__ __forceinline__ unsigned nth_bound(unsigned key, int n) {
   return t;
 }
 
-// The exponent of an entry: z scale - c.  Where z log2 e could overflow, numbers are so far apart that an entry equals the largest or
-// is nothing beside it: any small power of two does as the scale.
-struct Exponent {
-  float scale, c;
-  __device__ __forceinline__ static bool huge(float v) { return !(fabsf(v) < 1e38f); }
-  __device__ __forceinline__ static Exponent of(float ref) {
-    const float s = huge(ref) ? 0x1p-30f : 1.44269504088896341f;
-    return {s, ref * s};
-  }
-  // of ref, seen from the reference `to` >= ref
-  __device__ __forceinline__ static float between(float ref, float to) {
-    if (ref == to) return 0.f;
-    return huge(ref) || huge(to) ? kFloor : fmaxf(of(ref).c - of(to).c, kFloor);
-  }
-};
+// e^d, d = 0: exactly 1
+__device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * 1.44269504088896341f); }
 
-// Sums of everything but the entries of a list, relative to Exponent::of(ref); ref = -inf: of nothing.
+// Sums of everything but the entries of a list, relative to ref; ref = -inf: of nothing.
 struct Sums {
   float ref, R, A;
-  __device__ __forceinline__ void add(float z, Exponent x) {   // -inf adds nothing, a NaN makes R one
-    const float d = fmaf(z, x.scale, -x.c), e = __builtin_amdgcn_exp2f(d);
+  __device__ __forceinline__ void add(float z, float at) {   // -inf adds nothing, a NaN makes R one
+    const float d = z - at, e = exp_of(d);
     R += e;
     A = fmaf(e, fmaxf(d, kFloor), A);
   }
-  __device__ __forceinline__ Sums seen_from(float m) const {
-    const float d = Exponent::between(ref, m), f = __builtin_amdgcn_exp2f(d);
+  __device__ __forceinline__ Sums seen_from(float m) const {   // m >= ref
+    const float d = ref == m ? 0.f : fmaxf(ref - m, kFloor), f = exp_of(d);
     return {m, f * R, f * fmaf(d, R, A)};
   }
 };
@@ -107,24 +96,22 @@ struct Stream {
   u64 list = 0;                                            // entry j in lane j
   float last = -INFINITY;                                  // the list's n-th entry
   float ref = -INFINITY, limit = -INFINITY;                // limit: ref + kLead
-  Exponent x = {1.f, 0.f};
+  float at = 0.f;                                          // ref, or 0 while there is nothing
   float R[4] = {0.f, 0.f, 0.f, 0.f}, A[4] = {0.f, 0.f, 0.f, 0.f};   // four chains each: sums of at most V / 256 links
 
-  __device__ __forceinline__ float exponent(float z) const { return fmaf(z, x.scale, -x.c); }
   __device__ __forceinline__ void add(int chain, float d) {
-    const float e = __builtin_amdgcn_exp2f(d);
+    const float e = exp_of(d);
     float held;                                            // fmaxf would bring a signalling NaN into order first; any NaN is in R already
     asm("v_max_f32 %0, %1, %2" : "=v"(held) : "s"(kFloor), "v"(d));
     R[chain] += e;
     A[chain] = fmaf(e, held, A[chain]);
   }
   __device__ __forceinline__ void refer_to(float top) {
-    const float d = Exponent::between(ref, top), f = __builtin_amdgcn_exp2f(d);
+    const float d = fmaxf(ref - top, kFloor), f = exp_of(d);
 #pragma unroll
     for (int c = 0; c < 4; ++c) { A[c] = f * fmaf(d, R[c], A[c]); R[c] *= f; }
-    ref = top;
+    ref = at = top;
     limit = top + kLead;
-    x = Exponent::of(top);
   }
 
   // Entries of v above thr go to the list, in each turn the first lane's best one that comes before the list's last, and what the list drops to
@@ -140,11 +127,11 @@ struct Stream {
     u64 least = lane_key(list, n - 1);
 #pragma unroll 1
     while (__ballot(top > thr)) {
-      int at = 0;
+      int pos = 0;
 #pragma unroll
-      for (int j = N - 1; j > 0; --j) at = v[j] == top ? j : at;
-      at = v[0] == top ? 0 : at;
-      const u64 key = top > thr ? entry_key(top, id(at)) : 0, hit = __ballot(key > least);
+      for (int j = N - 1; j > 0; --j) pos = v[j] == top ? j : pos;
+      pos = v[0] == top ? 0 : pos;
+      const u64 key = top > thr ? entry_key(top, id(pos)) : 0, hit = __ballot(key > least);
       if (!hit) break;
       const int src = __builtin_ctzll(hit);
       const u64 k = lane_key(key, src), out = least;
@@ -154,11 +141,11 @@ struct Stream {
       if (k > list && lane < n) list = k > up ? up : k;
       least = lane_key(list, n - 1);
       if (least) thr = fmaxf(thr, below((unsigned)(least >> 32)));
-      at = lane == src ? at : -1;
+      pos = lane == src ? pos : -1;
       top = -INFINITY;
 #pragma unroll
-      for (int j = 0; j < N; ++j) { v[j] = at == j ? -INFINITY : v[j]; top = fmaxf(top, v[j]); }
-      if (out) add(0, exponent(lane == src ? entry_value(out) : -INFINITY));
+      for (int j = 0; j < N; ++j) { v[j] = pos == j ? -INFINITY : v[j]; top = fmaxf(top, v[j]); }
+      if (out) add(0, (lane == src ? entry_value(out) : -INFINITY) - at);
     }
     last = entry_value(least);
   }
@@ -180,14 +167,10 @@ __device__ __forceinline__ void write_row(const LogprobArgs& a, int64_t t, u64 l
   }
   const float m = entry_value(lane_key(list, 0));
   const bool proper = fabsf(m) < INFINITY;
-  const Exponent x = Exponent::of(proper ? m : 0.f);
   Sums rest = {m, 0.f, 0.f};
-  if (lane > 0) rest.add(entry_value(list), x);
+  if (lane > 0) rest.add(entry_value(list), proper ? m : 0.f);
   s = s.seen_from(m);
-  s.R += wave_sum(rest.R);
-  s.A += wave_sum(rest.A);
-  const float off = fmaf(proper ? m : 0.f, x.scale, -x.c), f = __builtin_amdgcn_exp2f(-off);   // from c to the largest entry itself
-  const float R = f * s.R, A = f * fmaf(-off, s.R, s.A) * 0.693147180559945309f;
+  const float R = s.R + wave_sum(rest.R), A = s.A + wave_sum(rest.A);
   const float log_sum = proper ? log1pf(R) : NAN, sum = 1.f + R;
   if (lane == 0 && a.entropy) a.entropy[t] = log_sum - A / sum;
   if (lane == 0 && a.conf) a.conf[t] = proper ? 1.f / sum : NAN;
@@ -287,8 +270,8 @@ __device__ __forceinline__ Sums join(Joint& s, int lists, int n, int tid, u64& l
     list = lane < n ? s.out[lane] : 0;
     const u64 least = lane_key(list, n - 1);
     sum.ref = entry_value(lane_key(list, 0));
-    const Exponent x = Exponent::of(sum.ref);
-    for (int i = lane; i < count; i += 64) if (s.cand[i] < least) sum.add(entry_value(s.cand[i]), x);
+    const float at = sum.ref > -INFINITY ? sum.ref : 0.f;
+    for (int i = lane; i < count; i += 64) if (s.cand[i] < least) sum.add(entry_value(s.cand[i]), at);
     if (lane < lists) {
       const Sums w = Sums{s.ref[lane], s.R[lane], s.A[lane]}.seen_from(sum.ref);
       sum.R += w.R;
@@ -343,14 +326,14 @@ __global__ __launch_bounds__(W * 64) void logprobs_kernel(const LogprobArgs a) {
   // the batch in x.  rising: its ids lie behind all that the list has
   auto process = [&](bool rising, auto id) {
     const float thr = fmaxf(rising ? st.last : below(order_key(st.last)), bound);
-    const float thr_d = fminf(thr > -INFINITY && st.ref > -INFINITY ? st.exponent(thr) : -INFINITY, kLeadD);
+    const float thr_d = fminf(thr > -INFINITY && st.ref > -INFINITY ? thr - st.at : -INFINITY, kLead);
     float d[kPerLaneB], top = -INFINITY;
 #pragma unroll
-    for (int j = 0; j < kPerLaneB; ++j) { d[j] = st.exponent(x[j]); top = fmaxf(top, d[j]); }
+    for (int j = 0; j < kPerLaneB; ++j) { d[j] = x[j] - st.at; top = fmaxf(top, d[j]); }
     if (__ballot(top >= thr_d)) {
       st.exchange(x, thr, n, lane, id);
 #pragma unroll
-      for (int j = 0; j < kPerLaneB; ++j) d[j] = st.exponent(x[j]);
+      for (int j = 0; j < kPerLaneB; ++j) d[j] = x[j] - st.at;
     }
 #pragma unroll
     for (int j = 0; j < kPerLaneB; ++j) st.add(j & 3, d[j]);
