@@ -155,16 +155,24 @@ struct Stream {
   }
 };
 
+// The given token of a lane and its entry.  Two loads that depend on each other: they are issued before the row is read and used behind it.
+template <typename S>
+struct Given {
+  int id;
+  bool in;
+  S z;
+  __device__ __forceinline__ void load_id(const LogprobArgs& a, int64_t t, int lane) {
+    id = lane < a.n_given ? a.tokens[t * a.n_given + lane] : -1;
+  }
+  __device__ __forceinline__ void load_entry(const LogprobArgs& a, const S* row) {
+    in = id >= 0 && id < a.V;
+    z = row[in ? id : 0];
+  }
+};
+
 // What is written for a row by one wave: entry j of the list in lane j, s the sums of everything else.
 template <typename S>
-__device__ __forceinline__ void write_row(const LogprobArgs& a, int64_t t, u64 list, Sums s, int lane) {
-  const S* row = static_cast<const S*>(a.logits) + t * a.ld;
-  float given = 0.f;
-  int id_given = -1;
-  if (lane < a.n_given) {
-    id_given = a.tokens[t * a.n_given + lane];
-    if (id_given >= 0 && id_given < a.V) given = to_f32(row[id_given]);
-  }
+__device__ __forceinline__ void write_row(const LogprobArgs& a, int64_t t, u64 list, Sums s, const Given<S>& given, int lane) {
   const float m = entry_value(lane_key(list, 0));
   const bool proper = fabsf(m) < INFINITY;
   Sums rest = {m, 0.f, 0.f};
@@ -174,7 +182,7 @@ __device__ __forceinline__ void write_row(const LogprobArgs& a, int64_t t, u64 l
   const float log_sum = proper ? log1pf(R) : NAN, sum = 1.f + R;
   if (lane == 0 && a.entropy) a.entropy[t] = log_sum - A / sum;
   if (lane == 0 && a.conf) a.conf[t] = proper ? 1.f / sum : NAN;
-  if (lane < a.n_given) a.token_logp[t * a.n_given + lane] = id_given >= 0 && id_given < a.V ? (float)(((double)given - m) - log_sum) : 0.f;
+  if (lane < a.n_given) a.token_logp[t * a.n_given + lane] = given.in ? (float)(((double)to_f32(given.z) - m) - log_sum) : 0.f;
   if (!a.n_top) return;
   const int found = __popcll(__ballot(lane < a.n_top && list));
   int id = entry_id(list);
@@ -200,15 +208,16 @@ __device__ __forceinline__ void write_row(const LogprobArgs& a, int64_t t, u64 l
 constexpr int kMaxLists = 16;
 constexpr int kMaxRanked = 256;
 struct Joint {
-  u64 cand[kMaxLists * kList + 8];
+  alignas(16) u64 cand[kMaxLists * kList + 8];            // eight zeros behind the last
   u64 out[kList];
   float ref[kMaxLists], R[kMaxLists], A[kMaxLists];
   int found[kMaxLists], count;
   unsigned low, bound;                                     // keys: lower bounds of the row's n-th entry
-  unsigned key[kMaxRanked];
+  alignas(16) unsigned key[kMaxRanked];
 };
 __device__ __forceinline__ void open_joint(Joint& s, int tid) {
   if (tid < kList) s.out[tid] = 0;
+  if (tid < kMaxRanked) s.key[tid] = 0;                    // no key is 0
   if (tid == 0) { s.count = 0; s.bound = 0; s.low = ~0u; }
 }
 
@@ -234,7 +243,10 @@ __device__ __forceinline__ unsigned joint_bound(Joint& s, float top, bool any, i
   if (count <= kMaxRanked && tid < count) {
     const unsigned mine = s.key[tid];
     int rank = 0;
-    for (int i = 0; i < count; ++i) rank += s.key[i] > mine || (s.key[i] == mine && i < tid);
+    for (int i = 0; i < count; i += 16) {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) rank += s.key[i + j] > mine || (s.key[i + j] == mine && i + j < tid);
+    }
     if (rank == n - 1) s.bound = mine;
   }
   __syncthreads();
@@ -250,6 +262,7 @@ __device__ __forceinline__ void put_list(Joint& s, int lists, int w, int n, int 
   const int at = wave_reduce(lane < w ? f : 0, 0, [](int x, int y) { return x + y; });
   if (lane < found) s.cand[at + lane] = list;
   if (w == lists - 1 && lane == 0) s.count = at + found;
+  if (w == lists - 1 && lane < 8) s.cand[at + found + lane] = 0;
 }
 // Candidates and sums are in place (no barrier since).  -> for the first wave: the n best, and the sums of everything else.
 __device__ __forceinline__ Sums join(Joint& s, int lists, int n, int tid, u64& list) {
@@ -260,7 +273,7 @@ __device__ __forceinline__ Sums join(Joint& s, int lists, int n, int tid, u64& l
     int rank = 0;
     for (int k = 0; k < count; k += 8) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) rank += k + i < count && s.cand[k + i] > mine;
+      for (int i = 0; i < 8; ++i) rank += s.cand[k + i] > mine;
     }
     if (rank < n) s.out[rank] = mine;
   }
@@ -307,6 +320,9 @@ __global__ __launch_bounds__(W * 64) void logprobs_kernel(const LogprobArgs a) {
 #pragma unroll
     for (int u = 0; u < U; ++u) raw[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + (unsigned)lane * 16u + u * 1024));
   };
+  Given<S> given;
+  const bool writes = a.parts == 1 && wave == 0;
+  if (W > 1 && writes) given.load_id(a, t, lane);
   float x[kPerLaneB];
   auto widen = [&](const u32x4 (&raw)[U]) {
 #pragma unroll
@@ -344,6 +360,7 @@ __global__ __launch_bounds__(W * 64) void logprobs_kernel(const LogprobArgs a) {
 #pragma unroll
     for (int i = 0; i < kRing; ++i) load(min(first + i * stride, last), raw[i]);
   }
+  if (W > 1 && writes) given.load_entry(a, row);
   if (W > 1 ? part * W < full : last >= 0) {
     float top = -INFINITY;
     if (last >= 0) {
@@ -408,7 +425,11 @@ __global__ __launch_bounds__(W * 64) void logprobs_kernel(const LogprobArgs a) {
     if (lane < n) o[2 + lane] = st.list;
     return;
   }
-  write_row<S>(a, t, st.list, sum, lane);
+  if constexpr (W == 1) {                                  // other rows' waves hide it
+    given.load_id(a, t, lane);
+    given.load_entry(a, row);
+  }
+  write_row<S>(a, t, st.list, sum, given, lane);
 }
 
 // Joins the parts of a row: one wave for each.
@@ -419,8 +440,11 @@ __global__ __launch_bounds__(kMaxParts * 64) void logprobs_join_kernel(const Log
   const int n = a.n_top > 1 ? a.n_top : 1;
   const int64_t t = blockIdx.x;
   const u64* in = a.ws + (t * a.parts + part) * partial_words(n);
+  Given<S> given;
+  if (part == 0) given.load_id(a, t, lane);
   u64 list = lane < n ? in[2 + lane] : 0;
   const u64 w0 = in[0], w1 = in[1];
+  if (part == 0) given.load_entry(a, static_cast<const S*>(a.logits) + t * a.ld);
   open_joint(s, tid);
   if (lane == 0) {
     s.ref[part] = __uint_as_float((unsigned)w0);
@@ -429,7 +453,7 @@ __global__ __launch_bounds__(kMaxParts * 64) void logprobs_join_kernel(const Log
   }
   put_list(s, a.parts, part, n, lane, list);
   const Sums sum = join(s, a.parts, n, tid, list);
-  if (tid < 64) write_row<S>(a, t, list, sum, lane);
+  if (tid < 64) write_row<S>(a, t, list, sum, given, lane);
 }
 static_assert(kMaxParts <= kMaxLists && kList <= 64, "one thread per candidate");
 
