@@ -8,18 +8,20 @@ namespace {
 // Up to 64 tokens (whose codes fit the registers of a workgroup) stream the weights: int8_stream.hip.  Beyond, tiles of 128, 192 or 256 tokens x 256 weight
 // rows, one workgroup per CU and all of a round in step (int8_wide.hip), or of 64 x 128, two workgroups per CU (int8_tile.hip): the smaller
 // estimate of time, from rounds, chunks of 128 k and what a tile costs beside them, all in us as measured.
-// us, 64 x 128 / 128 x 256 / 192 x 256 / 256 x 256: 65 x 50257 x 1971 41 / 37 / - / -, 200 x 50257 x 2048 57 / 49 / 53 / 46, 333 x 50257 x 1971 91 / 76 / 71 / 73,
-// 700 x 8192 x 2048 27 / 25 / 31 / 36, 1000 x 4096 x 4096 28 / - / 39 / 52, 1000 x 14336 x 4096 103 / - / 82 / 66, 2000 x 5000 x 1000 32 / - / 26 / 30,
-// 4096 x 600 x 1000 15 / - / 23 / 28, 4096 x 131072 x 4096 3477 / - / 1946 / 1796.
-// Two groups of waves per tile of 64 x 128 that share K: where there is no tile for every CU, and 1024 k.  us, one / two: 700 x 2048 x 5632 28 / 22, 128 x
-// 2048 x 8192 34 / 25, 300 x 4000 x 1000 10.5 / 10.3, 1500 x 1000 x 300 7.8 / 8.5, 1000 x 4096 x 4096 28 / 34.
+// us, 64 x 128 / 128 x 256 / 192 x 256 / 256 x 256: 65 x 50257 x 1971 42 / 37 / - / -, 200 x 50257 x 2048 57 / 49 / 51 / 45, 333 x 50257 x 1971 88 / 75 / 68 / 69,
+// 700 x 8192 x 2048 25 / 26 / 31 / 36, 1000 x 4096 x 4096 26 / 34 / 37 / 49, 1000 x 14336 x 4096 98 / 72 / 77 / 62, 2000 x 5000 x 1000 31 / 33 / 26 / 30,
+// 4096 x 600 x 1000 14 / 18 / 22 / 27, 4096 x 4096 x 1024 37 / 26 / 32 / 24, 4096 x 131072 x 4096 3477 / - / 1946 / 1796.
+// Two groups of waves per tile of 64 x 128 that share K: where there is no tile for every CU, and 1024 k.  us, one / two: 700 x 2048 x 5632 24 / 20, 128 x
+// 2048 x 8192 28 / 22, 65 x 2048 x 2048 10.4 / 9.4, 300 x 4000 x 1000 10.0 / 10.2, 1500 x 1000 x 300 7.8 / 8.6, 1000 x 4096 x 4096 26 / 30.
+// (Panels of 64 or 32 tokens by the streaming kernel, each reading all weights: 128 x 2048 x 8192 16.5, but 700 x 2048 x 5632 30, 200 x 8192 x 2048 19, 333 x
+// 50257 x 1971 79, and 65 tokens as tiles; not kept.)
 struct Route { int blocks; bool share_k; };              // blocks: of 64 tokens of a wide tile; 0: 64 x 128
 Route route(int T, int N, int K) {
   const int64_t cus = device_cu_count();
   const double chunks = (K + 127) / 128;
   const int64_t tiles = (int64_t)((T + 63) / 64) * ((N + 127) / 128);
   Route best = {0, tiles <= cus && chunks >= 8};
-  double least = best.share_k ? 8 + 0.42 * chunks : 4 + ((tiles + 2 * cus - 1) / (2 * cus)) * (0.73 * chunks + 3.7);
+  double least = best.share_k ? 6 + 0.3 * chunks : 4 + ((tiles + 2 * cus - 1) / (2 * cus)) * (0.73 * chunks + 3.7);
   constexpr double kChunk[5] = {0, 0, 1.0, 1.2, 1.46}, kTile[5] = {0, 0, 4.5, 6.0, 8.2};
   for (int b = 2; b <= 4; ++b) {
     const int64_t n = (int64_t)((T + 64 * b - 1) / (64 * b)) * ((N + 255) / 256);

@@ -3,9 +3,11 @@
 //
 // Four waves in a 2 x 2 grid, three stages of 128 k in LDS, filled past the registers two chunks ahead; two workgroups per CU, so that
 // one multiplies while the other waits.  Where the tiles are fewer than the CUs, eight waves: two groups with a ring each share K, and
-// their sums of integers are joined in LDS, exactly.  A chunk is one asm block: all its fragment reads are issued at once and the matrix
-// instructions of a k-step wait for those of that k-step only.  Rows of LDS, their swizzle and the order of the weight rows in them
-// as in int8_wide.hip (two neighbouring outputs per lane).
+// their sums of integers are joined in LDS, exactly.  A chunk is one asm block: matrix instructions, the fragment reads of the next k-steps and
+// the loads of the chunk after the next alternate, and the last k-step is multiplied while the first fragments of the next chunk are read
+// (all reads in front of a chunk's multiplications, behind its barrier: 700 x 2048 x 5632 21.1 us, 128 x 2048 x 8192 24.0; so 20.0 and 21.6).
+// What bounds it: LDS, 72 KB a chunk of 64 x 128 in and out, 576 cycles beside 256 of the matrix cores, and the start of a short launch.
+// Rows of LDS, their swizzle and the order of the weight rows in them as in int8_wide.hip (two neighbouring outputs per lane).
 #include <atomic>
 #include <type_traits>
 
@@ -18,30 +20,57 @@ namespace mm {
 namespace {
 
 typedef __attribute__((ext_vector_type(16))) int i32x16;
-typedef __attribute__((address_space(3))) void lds_void;
-
 constexpr int kRowBytes = 128, kTileCols = 128, kStages = 3;
 
-#define MM_WAIT_VMCNT(n) __builtin_amdgcn_s_waitcnt(0x0f70 | ((n) & 15) | (((n) >> 4) << 14))
+constexpr int kInsA = 2, kInsB = 4;     // loads of a wave per chunk: token rows, weight rows
 
-#define RD(f, p, o) "ds_read_b128 %[" #f "], %[" #p "] offset:" #o "\n\t"
-#define MUL(c, a, b) "v_mfma_i32_32x32x32_i8 %[" #c "], %[" #a "], %[" #b "], %[" #c "]\n\t"
+struct Frags { i32x4 a, b, d; };        // of a k-step: 32 token rows, two times 32 weight rows
+// What a block needs beside them.  a_row, b_row: LDS addresses of the wave's first rows in the stage of this chunk, *_next: of the next;
+// to_*: of this wave's part of the stage that is loaded; k: bytes from a row's start to the loaded chunk.
+struct Block { i32x4 rs_a, rs_b; unsigned a_row, b_row, a_next, b_next, to_a, to_b, k; };
+
 // fragments of k-step k: a block of tokens, two of weight rows, 4 KB apart
+#define AT(k, RA, RB) "v_add_u32 %[pa" #k "], %[" #RA "], %[col" #k "]\n\tv_add_u32 %[pb" #k "], %[" #RB "], %[col" #k "]\n\t"
+#define RD(f, p, o) "ds_read_b128 %[" #f "], %[" #p "] offset:" #o "\n\t"
 #define READ(k) RD(a##k, pa##k, 0) RD(b##k, pb##k, 0) RD(d##k, pb##k, 4096)
-#define MULS(k) MUL(c00, a##k, b##k) MUL(c01, a##k, d##k)
+#define MUL(c, a, b) "v_mfma_i32_32x32x32_i8 %[" #c "], %[" #a "], %[" #b "], %[" #c "]\n\t"
+#define LA(l) "s_add_u32 m0, %[ta], " #l "*1024\n\ts_nop 0\n\tbuffer_load_dwordx4 %[ao" #l "], %[ra], %[k] offen lds\n\t"
+#define LB(l) "s_add_u32 m0, %[tb], " #l "*1024\n\ts_nop 0\n\tbuffer_load_dwordx4 %[bo" #l "], %[rb], %[k] offen lds\n\t"
 #define WAIT(n) "s_waitcnt lgkmcnt(" #n ")\n\t"
-#define ADDR(k) [pa##k] "v"(pa + col[k]), [pb##k] "v"(pb + col[k])
-
-// matrix results can be read or moved: the compiler, which does not see what a block holds, may do so right behind it
+// in flight behind chunk kt + 1: chunk kt + 2
+#define BARRIER "s_waitcnt vmcnt(6)\n\ts_barrier\n\t"
+// wait states between the compiler's vector instructions and matrix instructions, and behind the last of these: the compiler, which does
+// not see what a block holds, may read or move their results right behind it
+#define START "s_nop 4\n\t"
 #define DONE "s_nop 15\n\ts_nop 1"
 
-// One chunk: tokens at LDS address pa, weight rows at pb, k-step k's 16 bytes of a lane at col[k].
-__device__ __forceinline__ void chunk(i32x16 (&c)[2], unsigned pa, unsigned pb, const unsigned (&col)[4]) {
-  i32x4 a0, a1, a2, a3, b0, b1, b2, b3, d0, d1, d2, d3;
-  asm volatile("s_nop 4\n\t" READ(0) READ(1) READ(2) READ(3) WAIT(9) MULS(0) WAIT(6) MULS(1) WAIT(3) MULS(2) WAIT(0) MULS(3) DONE
-               : [c00] "+v"(c[0]), [c01] "+v"(c[1]), [a0] "=&v"(a0), [a1] "=&v"(a1), [a2] "=&v"(a2), [a3] "=&v"(a3), [b0] "=&v"(b0), [b1] "=&v"(b1),
-                 [b2] "=&v"(b2), [b3] "=&v"(b3), [d0] "=&v"(d0), [d1] "=&v"(d1), [d2] "=&v"(d2), [d3] "=&v"(d3)
-               : ADDR(0), ADDR(1), ADDR(2), ADDR(3) : "memory");
+// One chunk: f holds the fragments of its first k-step and gets those of the next chunk's.  Chunk kt + 2 is loaded to where chunk kt - 1 was.
+__device__ __forceinline__ void chunk(i32x16 (&c)[2], Frags& f, const unsigned (&col)[4], const unsigned (&ao)[kInsA], const unsigned (&bo)[kInsB], const Block& s) {
+  Frags f1, f2, f3;
+  unsigned pa[4], pb[4];
+  asm volatile(START AT(1, row_a, row_b) AT(2, row_a, row_b) AT(3, row_a, row_b) AT(0, next_a, next_b) READ(1) MUL(c00, a0, b0) READ(2) MUL(c01, a0, d0) READ(3)
+               LA(0) LA(1) WAIT(6) MUL(c00, a1, b1) LB(0) LB(1) MUL(c01, a1, d1) LB(2) LB(3) WAIT(3) MUL(c00, a2, b2) MUL(c01, a2, d2) WAIT(0) BARRIER
+               READ(0) MUL(c00, a3, b3) MUL(c01, a3, d3) WAIT(0) DONE
+               : [c00] "+v"(c[0]), [c01] "+v"(c[1]), [a0] "+v"(f.a), [b0] "+v"(f.b), [d0] "+v"(f.d), [a1] "=&v"(f1.a), [b1] "=&v"(f1.b), [d1] "=&v"(f1.d),
+                 [a2] "=&v"(f2.a), [b2] "=&v"(f2.b), [d2] "=&v"(f2.d), [a3] "=&v"(f3.a), [b3] "=&v"(f3.b), [d3] "=&v"(f3.d),
+                 [pa0] "=&v"(pa[0]), [pa1] "=&v"(pa[1]), [pa2] "=&v"(pa[2]), [pa3] "=&v"(pa[3]), [pb0] "=&v"(pb[0]), [pb1] "=&v"(pb[1]), [pb2] "=&v"(pb[2]), [pb3] "=&v"(pb[3])
+               : [col0] "v"(col[0]), [col1] "v"(col[1]), [col2] "v"(col[2]), [col3] "v"(col[3]), [row_a] "s"(s.a_row), [row_b] "s"(s.b_row),
+                 [next_a] "s"(s.a_next), [next_b] "s"(s.b_next), [ta] "s"(s.to_a), [tb] "s"(s.to_b), [k] "s"(s.k), [ra] "s"(s.rs_a), [rb] "s"(s.rs_b),
+                 [ao0] "v"(ao[0]), [ao1] "v"(ao[1]), [bo0] "v"(bo[0]), [bo1] "v"(bo[1]), [bo2] "v"(bo[2]), [bo3] "v"(bo[3])
+               : "memory", "scc");
+}
+// The first fragments; in flight behind chunk 0: chunk 1.
+__device__ __forceinline__ void first_frags(Frags& f, unsigned pa, unsigned pb) {
+  asm volatile(BARRIER READ(0) WAIT(0) : [a0] "=&v"(f.a), [b0] "=&v"(f.b), [d0] "=&v"(f.d) : [pa0] "v"(pa), [pb0] "v"(pb) : "memory");
+}
+// one chunk into LDS without anything beside it
+__device__ __forceinline__ void load(const unsigned (&ao)[kInsA], const unsigned (&bo)[kInsB], const Block& s) {
+  asm volatile("s_nop 4\n\t" LA(0) LA(1) LB(0) LB(1) LB(2) LB(3) :: [ta] "s"(s.to_a), [tb] "s"(s.to_b), [k] "s"(s.k), [ra] "s"(s.rs_a), [rb] "s"(s.rs_b),
+               [ao0] "v"(ao[0]), [ao1] "v"(ao[1]), [bo0] "v"(bo[0]), [bo1] "v"(bo[1]), [bo2] "v"(bo[2]), [bo3] "v"(bo[3]) : "memory", "scc");
+}
+__device__ __forceinline__ i32x4 rsrc4(const void* p, unsigned bytes) {
+  const uint64_t v = (uint64_t)p;
+  return i32x4{uniform((int)(unsigned)v), uniform((int)(unsigned)(v >> 32)), uniform((int)bytes), 0x00020000};
 }
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 __device__ __forceinline__ i32x4 quarter(const i32x16& c, int q) { return i32x4{c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]}; }
@@ -50,7 +79,7 @@ __device__ __forceinline__ i32x4 quarter(const i32x16& c, int q) { return i32x4{
 template <typename S, int KG>
 __global__ __launch_bounds__(256 * KG) void int8_tile_kernel(const Int8Args a, const int mt, const int total) {
   extern __shared__ __attribute__((aligned(1024))) char s_tiles[];
-  constexpr int BM = 64, kStageBytes = (BM + kTileCols) * kRowBytes, kInsA = 2, kInsB = 4;
+  constexpr int BM = 64, kStageBytes = (BM + kTileCols) * kRowBytes;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6) & 3, group = uniform(tid >> 8), h = lane >> 5;
   const int wm = wave >> 1, wn = wave & 1;
   // an XCD has a contiguous range of the tiles; the token tiles of a panel follow each other
@@ -71,57 +100,68 @@ __global__ __launch_bounds__(256 * KG) void int8_tile_kernel(const Int8Args a, c
   }
   const float xs = a.x_scale[min(m0 + wm * 32 + lane, a.T - 1)];
 
-  const __amdgpu_buffer_rsrc_t ra = make_rsrc(a.x + (int64_t)m0 * a.ldx, (unsigned)((rows - 1) * (int)a.ldx + K16));
-  const __amdgpu_buffer_rsrc_t rb = make_rsrc(a.w + (int64_t)n0 * a.ldw, (unsigned)((cols - 1) * (int)a.ldw + K16));
   // this group's chunks; the last group may have fewer, and zeros in the place of the others
   const int nk = ((K16 + kRowBytes - 1) / kRowBytes + KG - 1) / KG, k_first = group * nk * kRowBytes;
-  char* const ring = s_tiles + group * (kStages * kStageBytes);
+  // The hardware takes the scalar offset k from the size that a descriptor states before it compares, and k runs two chunks past the end; that
+  // difference must not go below zero.  Lanes with data lie inside the tensor by themselves (rows and columns are checked), so stating more than a
+  // short tensor has lets nothing through.
+  const int k_end = k_first + (nk + 2) * kRowBytes;
+  Block s;
+  s.rs_a = rsrc4(a.x + (int64_t)m0 * a.ldx, (unsigned)max((rows - 1) * (int)a.ldx + K16, k_end));
+  s.rs_b = rsrc4(a.w + (int64_t)n0 * a.ldw, (unsigned)max((cols - 1) * (int)a.ldw + K16, k_end));
+  s.k = (unsigned)uniform(k_first);
+  const unsigned ring = (unsigned)uniform((int)(unsigned)(size_t)s_tiles + group * (kStages * kStageBytes));
   const int pc = lane & 7, sub = lane >> 3;
   unsigned aoff[kInsA], boff[kInsB];
   auto col_of = [&](int r) { return (unsigned)(pc ^ ((r >> 1) & 7)) * 16u; };
+  auto tail = [&]() {                                      // columns behind K16; kOob is the top bit
+#pragma unroll
+    for (int p = 0; p < kInsA; ++p) aoff[p] |= (unsigned)((int)(s.k + col_of((wave * kInsA + p) * 8 + sub)) >= K16) << 31;
+#pragma unroll
+    for (int p = 0; p < kInsB; ++p) boff[p] |= (unsigned)((int)(s.k + col_of((wave * kInsB + p) * 8 + sub)) >= K16) << 31;
+  };
 #pragma unroll
   for (int p = 0; p < kInsA; ++p) {
     const int r = (wave * kInsA + p) * 8 + sub;
-    aoff[p] = r < rows ? (unsigned)r * (unsigned)a.ldx + col_of(r) + (unsigned)k_first : kOob;
+    aoff[p] = ((unsigned)r * (unsigned)a.ldx + col_of(r)) | (unsigned)(r >= rows) << 31;
   }
 #pragma unroll
   for (int p = 0; p < kInsB; ++p) {
     const int r = (wave * kInsB + p) * 8 + sub, n = (r & 64) + 2 * (r & 31) + ((r >> 5) & 1);
-    boff[p] = n < cols ? (unsigned)n * (unsigned)a.ldw + col_of(r) + (unsigned)k_first : kOob;
+    boff[p] = ((unsigned)n * (unsigned)a.ldw + col_of(r)) | (unsigned)(n >= cols) << 31;
   }
-  auto issue = [&](int kt) {
-    char* const st = ring + kt % kStages * kStageBytes;
-    const int left = K16 - k_first - kt * kRowBytes;                 // columns from here on are not there
-#pragma unroll
-    for (int p = 0; p < kInsA; ++p) {
-      const unsigned off = (int)col_of((wave * kInsA + p) * 8 + sub) < left ? aoff[p] : kOob;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (lds_void*)(st + (wave * kInsA + p) * 1024), 16, (int)off, 0, 0, 0);
-      aoff[p] += kRowBytes;
-    }
-#pragma unroll
-    for (int p = 0; p < kInsB; ++p) {
-      const unsigned off = (int)col_of((wave * kInsB + p) * 8 + sub) < left ? boff[p] : kOob;
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (lds_void*)(st + BM * kRowBytes + (wave * kInsB + p) * 1024), 16, (int)off, 0, 0, 0);
-      boff[p] += kRowBytes;
-    }
+  if (K16 - (int)s.k < kRowBytes) tail();
+  auto step = [&]() {
+    s.k = (unsigned)uniform((int)s.k + kRowBytes);
+    if (K16 - (int)s.k < kRowBytes) tail();
   };
+  // LDS addresses of this wave's rows and of its part of a load; the stages of chunks kt, kt + 1, kt + 2
+  const unsigned a_at = uniform((int)ring + wm * 32 * kRowBytes), b_at = uniform((int)ring + (BM + wn * 64) * kRowBytes);
+  const unsigned a_to = uniform((int)ring + wave * (kInsA * 1024)), b_to = uniform((int)ring + BM * kRowBytes + wave * (kInsB * 1024));
+  unsigned st0 = 0, st1 = kStageBytes, st2 = 2 * kStageBytes;
+  s.to_a = a_to; s.to_b = b_to;
+  load(aoff, boff, s);
+  step();
+  s.to_a = a_to + st1; s.to_b = b_to + st1;
+  load(aoff, boff, s);
+  step();
   const unsigned fkey = (unsigned)((lane & 31) >> 1) & 7u;
-  unsigned col[4];
+  unsigned col[4];                                         // of a lane's 16 bytes of k-step k, behind the wave's first row
 #pragma unroll
   for (int k = 0; k < 4; ++k) col[k] = (unsigned)((lane & 31) * kRowBytes) + ((unsigned)(2 * k + h) ^ fkey) * 16u;
-  const unsigned lds0 = (unsigned)(size_t)ring;
-  const unsigned pa = lds0 + wm * 32 * kRowBytes, pb = lds0 + (BM + wn * 64) * kRowBytes;
+  Frags f;
+  first_frags(f, col[0] + a_at, col[0] + b_at);
   i32x16 acc[2] = {};
-#pragma unroll
-  for (int i = 0; i < kStages - 1; ++i) if (i < nk) issue(i);
   for (int kt = 0; kt < nk; ++kt) {
-    // chunk kt has landed: the loads behind it are those of chunk kt + 1
-    if (kt + 1 < nk) MM_WAIT_VMCNT(kInsA + kInsB); else MM_WAIT_VMCNT(0);
-    asm volatile("s_barrier" ::: "memory");                // ... in all waves, and all have read chunk kt - 1, whose stage chunk kt + 2 takes
-    if (kt + kStages - 1 < nk) issue(kt + kStages - 1);
-    const unsigned st = (unsigned)(kt % kStages * kStageBytes);
-    chunk(acc, pa + st, pb + st, col);
+    s.a_row = a_at + st0; s.b_row = b_at + st0;
+    s.a_next = a_at + st1; s.b_next = b_at + st1;
+    s.to_a = a_to + st2; s.to_b = b_to + st2;
+    chunk(acc, f, col, aoff, boff, s);
+    const unsigned st = st0;
+    st0 = st1; st1 = st2; st2 = st;
+    step();
   }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // the loads behind the last chunk, zeros; LDS is used again or given back
   if (a.k_tail && group == 0) {
     // the last K % 16 codes, in the lanes of the first half
     const i32x4 zero = {0, 0, 0, 0};
