@@ -457,17 +457,20 @@ __global__ __launch_bounds__(kMaxParts * 64) void logprobs_join_kernel(const Log
 }
 static_assert(kMaxParts <= kMaxLists && kList <= 64, "one thread per candidate");
 
-// Waves per row part and parts per row.  us, waves x parts: 4096 rows of 131072 bf16 1x1 208, 4x1 223; 1999 of 50257 bf16 1x1 55.3, 4x1 54.0, 8x1 64;
-// 600 of 100000 fp32 1x1 64.3, 4x1 54.5, 8x1 60.7; 300 of 50257 bf16 1x1 38.4, 4x1 21.7, 8x1 18.5, 8x2 24.0; 128 of 151001 fp32 8x1 31.5, 8x2 30.5,
-// 8x4 38.0; 64 of 131072 fp32 8x1 32.6, 8x4 24.9, 8x8 34.5; 1 of 131072 bf16 8x1 18.3, 8x4 13.0, 8x8 12.6.  Sixteen waves were slower
-// than eight everywhere.
+// Waves per row part and parts per row.  us, waves x parts: 4096 rows of 131072 bf16 1x1 206, 4x1 222; 1999 of 50257 bf16 1x1 51.2, 4x1 53.3, 8x1 63;
+// 1300 of 50257 bf16 1x1 49.3, 4x1 40.2, 8x1 46.3; 600 of 100000 fp32 1x1 69.6, 4x1 49.8, 8x1 52.6; 300 of 50257 bf16 1x1 35.7, 4x1 21.1, 8x1 18.8, 8x2
+// 24.0; 128 of 151001 fp32 8x1 31.4, 8x2 27.2, 8x4 26.8, 8x8 35.0; 64 of 131072 fp32 8x1 35.7, 8x2 27.9, 8x4 22.5, 8x8 23.2; 16 of 131072 fp32 8x1 21.4, 8x4
+// 15.0, 8x8 13.2, 8x16 13.5; 1 of 131072 bf16 8x1 16.9, 8x4 12.3, 8x8 11.6, 8x16 11.5; 8 of 50257 fp32 8x1 12.7, 8x2 12.8; 1 of 32000 fp32 8x1 8.5, 8x2
+// 10.3.  Sixteen waves were slower than eight everywhere.
+// Not kept, with eight waves: twice as many batches in registers (64 of 131072 fp32 with 20 alternatives 22.7 -> 22.0, with none 16.0 -> 16.9, 300 of
+// 50257 bf16 17.0 -> 20.0); batches through LDS, and so one copy of the code instead of one per batch in flight (0.7 to 1 us more for few rows).
 struct Split { int waves, parts; };
 Split split_of(int T, int V) {
   const int batches = V / kBatch + 1;
   if (T >= 2048 || batches < 4) return {1, 1};
   if (T >= 400 || batches < 8) return {4, 1};
   int parts = 1;
-  while (parts < kMaxParts && T * parts * 2 <= 256 && batches >= 64 * parts) parts *= 2;
+  while (parts < kMaxParts && T * parts * 2 <= 256 && batches >= (parts == 1 ? 64 : 32 * parts)) parts *= 2;
   return {8, parts};
 }
 
