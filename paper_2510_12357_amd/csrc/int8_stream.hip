@@ -50,15 +50,19 @@ __device__ __forceinline__ float read_float(unsigned at) {
   asm volatile("ds_read_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(v) : "v"(at) : "memory");
   return v;
 }
+// The sums of a block of 16 tokens: four words of 64 lanes each, one behind the other.
 // reads a sum and leaves zeros behind
 __device__ __forceinline__ i32x4 take_sum(unsigned at) {
-  i32x4 v, zero = {0, 0, 0, 0};
-  asm volatile("ds_read_b128 %0, %1\n\ts_waitcnt lgkmcnt(0)\n\tds_write_b128 %1, %2" : "=&v"(v) : "v"(at), "v"(zero) : "memory");
-  return v;
+  typedef __attribute__((ext_vector_type(2))) int i32x2;
+  i32x2 lo, hi;
+  asm volatile("ds_read2st64_b32 %0, %2 offset0:0 offset1:1\n\tds_read2st64_b32 %1, %2 offset0:2 offset1:3\n\ts_waitcnt lgkmcnt(0)\n\t"
+               "ds_write2st64_b32 %2, %3, %3 offset0:0 offset1:1\n\tds_write2st64_b32 %2, %3, %3 offset0:2 offset1:3"
+               : "=&v"(lo), "=&v"(hi) : "v"(at), "v"(0) : "memory");
+  return i32x4{lo[0], lo[1], hi[0], hi[1]};
 }
 // adds the result of a matrix instruction that may have just been issued
 __device__ __forceinline__ void add_sum(unsigned at, i32x4 v) {
-  asm volatile("s_nop 15\n\tds_add_u32 %0, %1\n\tds_add_u32 %0, %2 offset:4\n\tds_add_u32 %0, %3 offset:8\n\tds_add_u32 %0, %4 offset:12"
+  asm volatile("s_nop 15\n\tds_add_u32 %0, %1\n\tds_add_u32 %0, %2 offset:256\n\tds_add_u32 %0, %3 offset:512\n\tds_add_u32 %0, %4 offset:768"
                :: "v"(at), "v"(v[0]), "v"(v[1]), "v"(v[2]), "v"(v[3]) : "memory");
 }
 
@@ -226,7 +230,7 @@ __global__ __launch_bounds__(kThreadsS) __attribute__((amdgpu_waves_per_eu(2, 2)
     } else {
       // Two sets of sums in turn: one is finished, and left at zero, while the other is added to; the barrier of a turn is behind the
       // finishing of the one before.
-      const unsigned at = sums_at + (unsigned)(((turn & 1) * groups + group) * TB * 1024 + lane * 16);
+      const unsigned at = sums_at + (unsigned)(((turn & 1) * groups + group) * TB * 1024 + lane * 4);
       if (n > 0) {
 #pragma unroll
         for (int b = 0; b < TB; ++b) add_sum(at + b * 1024u, acc[b]);
