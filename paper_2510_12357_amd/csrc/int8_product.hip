@@ -5,28 +5,33 @@
 namespace mm {
 namespace {
 
-// Up to 64 tokens (whose codes fit the registers of a workgroup) stream the weights: int8_stream.hip.  Beyond, tiles of 128, 192 or 256 tokens x 256 weight
-// rows, one workgroup per CU and all of a round in step (int8_wide.hip), or of 64 x 128, two workgroups per CU (int8_tile.hip): the smaller
-// estimate of time, from rounds, chunks of 128 k and what a tile costs beside them, all in us as measured.
-// us, 64 x 128 / 128 x 256 / 192 x 256 / 256 x 256: 65 x 50257 x 1971 42 / 37 / - / -, 200 x 50257 x 2048 57 / 49 / 51 / 45, 333 x 50257 x 1971 88 / 75 / 68 / 69,
-// 700 x 8192 x 2048 25 / 26 / 31 / 36, 1000 x 4096 x 4096 26 / 34 / 37 / 49, 1000 x 14336 x 4096 98 / 72 / 77 / 62, 2000 x 5000 x 1000 31 / 33 / 26 / 30,
+// Up to 64 tokens (whose codes fit the registers of a workgroup) stream the weights: int8_stream.hip.  Beyond, tiles of 64 tokens x 64 or 128 weight
+// rows, two workgroups per CU or one whose two groups of waves share K (int8_tile.hip), or of 128, 192 or 256 x 256, one workgroup per CU and all of
+// a round in step (int8_wide.hip).
+// A CU for every tile of 64 x 64: these, sharing K from 13 chunks of 128 k on.  A CU for every tile of 64 x 128: the same from 13 chunks on, tiles of 64 x 64
+// without sharing below.  us, 64 x 64 shared / 64 x 64 / 64 x 128 shared / 64 x 128: 65 x 2048 x 512 5.2 / 4.7 / 6.0 / 5.8, 300 x 2048 x 1000 6.7 / 6.6 / 8.7 / 8.5,
+// 500 x 2048 x 1500 9.1 / 8.5 / 11.3 / 11.1, 65 x 2048 x 2048 7.2 / 8.0 / 9.3 / 10.4, 128 x 2048 x 8192 16.2 / 20.6 / 21.9 / 27.4; 300 x 4000 x 1000 13.1 / 9.4 / 10.1 / 9.7,
+// 700 x 2048 x 1500 15.4 / 11.2 / 11.9 / 11.3, 1024 x 2048 x 2048 14.9 / 11.7 / 11.0 / 11.7, 256 x 8192 x 4096 21.0 / 17.7 / 16.0 / 18.7, 700 x 2048 x 5632 25.8 / 20.5 / 19.9 / 22.1.
+// More tiles: the smaller estimate of time, from rounds, chunks and what a tile costs beside them, all in us as measured.
+// us, 64 x 128 / 128 x 256 / 192 x 256 / 256 x 256: 65 x 50257 x 1971 39 / 35 / - / -, 200 x 50257 x 2048 56 / 48 / 51 / 44, 333 x 50257 x 1971 85 / 73 / 67 / 70,
+// 700 x 8192 x 2048 24 / 25 / 30 / 35, 1000 x 4096 x 4096 26 / 34 / 38 / 49, 1000 x 14336 x 4096 98 / 72 / 77 / 62, 2000 x 5000 x 1000 29 / 31 / 25 / 29,
 // 4096 x 600 x 1000 14 / 18 / 22 / 27, 4096 x 4096 x 1024 37 / 26 / 32 / 24, 4096 x 131072 x 4096 3477 / - / 1946 / 1796.
-// Two groups of waves per tile of 64 x 128 that share K: where there is no tile for every CU, and 1024 k.  us, one / two: 700 x 2048 x 5632 24 / 20, 128 x
-// 2048 x 8192 28 / 22, 65 x 2048 x 2048 10.4 / 9.4, 300 x 4000 x 1000 10.0 / 10.2, 1500 x 1000 x 300 7.8 / 8.6, 1000 x 4096 x 4096 26 / 30.
-// (Panels of 64 or 32 tokens by the streaming kernel, each reading all weights: 128 x 2048 x 8192 16.5, but 700 x 2048 x 5632 30, 200 x 8192 x 2048 19, 333 x
-// 50257 x 1971 79, and 65 tokens as tiles; not kept.)
-struct Route { int blocks; bool share_k; };              // blocks: of 64 tokens of a wide tile; 0: 64 x 128
+// (Panels of 64 or 32 tokens by the streaming kernel, each reading all weights: 128 x 2048 x 8192 16.5, 700 x 2048 x 5632 30, 200 x 8192 x 2048 19, 333 x 50257 x
+// 1971 79; not kept.)
+struct Route { int blocks, cols; bool share_k; };        // blocks: of 64 tokens of a wide tile; 0: 64 x cols
 Route route(int T, int N, int K) {
-  const int64_t cus = device_cu_count();
-  const double chunks = (K + 127) / 128;
-  const int64_t tiles = (int64_t)((T + 63) / 64) * ((N + 127) / 128);
-  Route best = {0, tiles <= cus && chunks >= 8};
-  double least = best.share_k ? 6 + 0.3 * chunks : 4 + ((tiles + 2 * cus - 1) / (2 * cus)) * (0.73 * chunks + 3.7);
+  const int64_t cus = device_cu_count(), chunks = (K + 127) / 128, panels = (T + 63) / 64;
+  const bool share_k = chunks > 12;
+  if (panels * ((N + 63) / 64) <= cus) return {0, 64, share_k};
+  const int64_t tiles = panels * ((N + 127) / 128);
+  if (tiles <= cus) return {0, share_k ? 128 : 64, share_k};
+  Route best = {0, 128, false};
+  double least = 4 + (double)((tiles + 2 * cus - 1) / (2 * cus)) * (0.73 * (double)chunks + 3.7);
   constexpr double kChunk[5] = {0, 0, 1.0, 1.2, 1.46}, kTile[5] = {0, 0, 4.5, 6.0, 8.2};
   for (int b = 2; b <= 4; ++b) {
     const int64_t n = (int64_t)((T + 64 * b - 1) / (64 * b)) * ((N + 255) / 256);
-    const double t = 8 + ((n + cus - 1) / cus) * (kChunk[b] * chunks + kTile[b]);
-    if (t < least) { least = t; best = {b, false}; }
+    const double t = 8 + (double)((n + cus - 1) / cus) * (kChunk[b] * (double)chunks + kTile[b]);
+    if (t < least) { least = t; best = {b, 0, false}; }
   }
   return best;
 }
@@ -37,7 +42,7 @@ int launch_int8_product(const Int8Args& a, hipStream_t s) {
   ProfScope ps(kProfInt8Product, s);
   if (int8_streams(a.T, a.K)) return launch_int8_stream(a, s);
   const Route r = route(a.T, a.N, a.K);
-  return r.blocks ? launch_int8_wide(a, r.blocks, s) : launch_int8_tile(a, r.share_k, s);
+  return r.blocks ? launch_int8_wide(a, r.blocks, s) : launch_int8_tile(a, r.cols, r.share_k, s);
 }
 
 }  // namespace mm

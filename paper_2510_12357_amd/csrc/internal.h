@@ -171,7 +171,7 @@ struct Int8Args {
 };
 int launch_int8_product(const Int8Args& a, hipStream_t s);
 int launch_int8_wide(const Int8Args& a, int blocks, hipStream_t s);                       // token tiles of 64 blocks rows, 2 to 4
-int launch_int8_tile(const Int8Args& a, bool share_k, hipStream_t s);                     // share_k: two groups of waves a tile
+int launch_int8_tile(const Int8Args& a, int cols, bool share_k, hipStream_t s);           // tiles of 64 x cols (64, 128); share_k: two groups of waves a tile
 bool int8_streams(int T, int K);           // whether launch_int8_stream takes these sizes
 int launch_int8_stream(const Int8Args& a, hipStream_t s);
 size_t int8_lane_codes_bytes(int T, int K);

@@ -28,6 +28,19 @@ def test_product_of_codes(T, N, K, dtype, with_bias):
     assert ((got.cpu().double() - ref).abs() <= _bound(ref, part, dtype)).all()
 
 
+# tiles of 64 x 64 (a CU each, or two to a CU) and of 64 x 128, with K shared by two groups of waves or not; K below, at and behind the chunk, the ring
+# and what each group gets; last tiles of one row and one column; up to 64 tokens whose K is too long for the streaming kernel
+SMALL_TILES = [(65, 64, 128), (66, 65, 1024), (128, 1000, 1536), (193, 2050, 1537), (65, 1000, 1600), (257, 127, 2049), (300, 500, 4000), (1, 100, 20000), (33, 300, 5001),
+               (300, 4000, 500), (333, 5000, 1000), (129, 8001, 1535), (333, 5000, 1700), (129, 8065, 1541), (449, 4097, 2300), (64, 16385, 4200),
+               (333, 7000, 1111), (65, 32801, 99), (1000, 4100, 2500), (2000, 1030, 1552)]
+
+
+@pytest.mark.parametrize("T, N, K", SMALL_TILES)
+@pytest.mark.parametrize("dtype, with_bias", [(FP32, False), (BF16, True)])
+def test_product_on_small_tiles(T, N, K, dtype, with_bias):
+    test_product_of_codes(T, N, K, dtype, with_bias)
+
+
 @pytest.mark.parametrize("T, K", [(1, 1), (1, 700), (1, 16384), (2, 8192), (3, 33), (3, 5461), (4, 1000), (7, 2340), (8, 64), (8, 2048), (15, 1092), (16, 5), (16, 1024),
                                   (16, 1025), (17, 64)])
 @pytest.mark.parametrize("dtype", [BF16, FP32])
