@@ -1,7 +1,8 @@
 // Rows of floats -> 8-bit codes and one scale per row (moe_quantize_rows).
 //
-// A workgroup per row, which it holds in registers between the largest magnitude and the codes (what does not fit is read twice), so that
-// the bound is memory: each value is read once.  One wave where it holds a row by itself, four where not.
+// A workgroup per row, which it holds in registers between the largest magnitude and the codes (up to 8192 values; what does not fit is read
+// twice), so that each value is read once.  What bounds it: the launch up to some hundred rows, then memory and, with bf16, the quotients: 4096 x 4096 fp32
+// 17.2 us (4.9 TB/s), bf16 14.1 (3.6 TB/s); 4096 x 8192 fp32 33.5 (with half of a row held 39.8); 64 x 4096 bf16 3.4.
 #include "internal.h"
 #include "route_device.h"
 #include "int8_device.h"
@@ -9,7 +10,7 @@
 namespace mm {
 namespace {
 
-constexpr int kHeld = 4;                                   // vectors of 16 bytes that a thread holds
+constexpr int held(int threads, size_t bytes) { return threads == 64 || bytes == 2 ? 4 : 8; }   // vectors of 16 bytes that a thread holds
 
 template <typename X, int THREADS>
 __global__ __launch_bounds__(THREADS) void quantize_kernel(const X* __restrict__ x, int K, int64_t ldx, int8_t* __restrict__ q, int64_t ldq,
@@ -17,13 +18,14 @@ __global__ __launch_bounds__(THREADS) void quantize_kernel(const X* __restrict__
   constexpr int kVec = 16 / sizeof(X);
   __shared__ unsigned s_max[THREADS / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  constexpr int kHeld = held(THREADS, sizeof(X));
   const X* row = x + (int64_t)blockIdx.x * ldx;
-  HeldRow<X, kHeld> held;
-  held.load(row, K, tid, THREADS);
+  HeldRow<X, kHeld> in;
+  in.load(row, K, tid, THREADS);
   unsigned top = 0;
   float v[kVec];
 #pragma unroll
-  for (int u = 0; u < kHeld; ++u) { held.values(u, v); top = max(top, magnitude(v)); }
+  for (int u = 0; u < kHeld; ++u) { in.values(u, v); top = max(top, magnitude(v)); }
   for (int k = (kHeld * THREADS + tid) * kVec; k < K; k += THREADS * kVec) {
     load_floats(row, k, K, v);
     top = max(top, magnitude(v));
@@ -41,7 +43,7 @@ __global__ __launch_bounds__(THREADS) void quantize_kernel(const X* __restrict__
 #pragma unroll
   for (int u = 0; u < kHeld; ++u) {
     const int k = (u * THREADS + tid) * kVec;
-    held.values(u, v);
+    in.values(u, v);
     if (k < ldq) store_codes(out + place(k), r, v);
   }
   for (int k = (kHeld * THREADS + tid) * kVec; k < ldq; k += THREADS * kVec) {
@@ -51,10 +53,13 @@ __global__ __launch_bounds__(THREADS) void quantize_kernel(const X* __restrict__
   if (tid == 0) scale[blockIdx.x] = r.scale();
 }
 
+// One wave where it holds a row by itself, four where not, and for few rows of more than 512 bf16 values, where a wave's own time shows.  us, one / four
+// waves, bf16: 333 x 300 3.1 / 3.1, 333 x 1000 3.6 / 3.2, 333 x 1971 5.5 / 3.3, 1000 x 1500 5.4 / 4.2, 4000 x 1000 6.1 / 7.4, 4000 x 1971 10.0 / 9.4, 40000 x 1971 53 / 69;
+// fp32: 333 x 1000 2.9 / 3.0, 4000 x 1000 5.8 / 7.4.
 template <typename X>
 int launch(const void* x, int rows, int K, int64_t ldx, int8_t* q, int64_t ldq, float* scale, int lane_blocks, hipStream_t s) {
-  constexpr int kHeldByWave = 64 * kHeld * (16 / sizeof(X));
-  if (K <= kHeldByWave)
+  constexpr int kHeldByWave = 64 * held(64, sizeof(X)) * (16 / sizeof(X));
+  if (K <= kHeldByWave && !(sizeof(X) == 2 && K > 512 && rows <= 2048))
     hipLaunchKernelGGL((quantize_kernel<X, 64>), dim3((unsigned)rows), dim3(64), 0, s, static_cast<const X*>(x), K, ldx, q, ldq, scale, lane_blocks);
   else
     hipLaunchKernelGGL((quantize_kernel<X, 256>), dim3((unsigned)rows), dim3(256), 0, s, static_cast<const X*>(x), K, ldx, q, ldq, scale, lane_blocks);
