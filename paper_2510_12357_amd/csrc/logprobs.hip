@@ -119,9 +119,12 @@ struct Stream {
   // 151001 fp32 39.2, 32.4.)  id(j): of entry j, rising with j.
   template <int N, typename Id>
   __device__ __forceinline__ void exchange(float (&v)[N], float thr, int n, int lane, Id id) {
-    float top = v[0];
+    float top = -INFINITY;
 #pragma unroll
-    for (int j = 1; j < N; ++j) top = fmaxf(top, v[j]);
+    for (int j = 0; j < N; ++j) {
+      v[j] += 0.f;                                         // a maximum drops a quiet NaN, but not a signalling one
+      top = fmaxf(top, v[j]);
+    }
     if (__ballot(top > limit)) refer_to(wave_max(top));
     // many lanes (rising rows): what is below the n-th largest of the lanes' maxima need not be looked at
     if (__popcll(__ballot(top > thr)) > n) thr = fmaxf(thr, below(nth_bound(order_key(top), n)));
@@ -318,23 +321,30 @@ __global__ __launch_bounds__(W * 64) void logprobs_kernel(const LogprobArgs a) {
   const int part = a.parts > 1 ? (int)(blockIdx.x % (unsigned)a.parts) : 0;
   const int64_t t = a.parts > 1 ? blockIdx.x / (unsigned)a.parts : blockIdx.x;
   const S* row = static_cast<const S*>(a.logits) + t * a.ld;
-  // `head` entries up to the first multiple of 16 bytes, `vectors` vectors of 16 bytes in batches, the last of them not full, and `tail`
-  // entries; head and tail are one further batch at the end, one entry a lane
+  // `head` entries up to the first multiple of 16 bytes, `vectors` vectors of 16 bytes in batches, the last of them perhaps not full, and `tail`
+  // entries; head and tail are one further batch at the end, one entry a lane.  One wave for a row, many rows or short ones: the last batch
+  // and the ends are under way with the others (loaded when they are due: 3000 rows of 1500 bf16 14.3 us, so 12.1; 4096 of 2000 fp32 15.9, 14.8).  Several
+  // waves: they are loaded when they are due (otherwise, in the extra code of each copy of a batch, 1 row of 32000 8.0 us, 8.5).
+  constexpr bool kAhead = W == 1;
   const int head = min(a.V, (int)((-(uintptr_t)row & 15) / sizeof(S)));
   const int vectors = (a.V - head) / kVec, tail = (a.V - head) % kVec;
-  const int full = vectors / (64 * U), stride = W * a.parts, first = part * W + wave;
+  const int full = vectors / (64 * U), batches = kAhead ? (vectors + 64 * U - 1) / (64 * U) : full, stride = W * a.parts, first = part * W + wave;
   const char* body = reinterpret_cast<const char*>(row + head);
   constexpr unsigned kNegInf2 = sizeof(S) == 2 ? 0xff80ff80u : 0xff800000u;
-  auto load = [&](int b, u32x4 (&raw)[U]) {
+  auto load = [&](int b, u32x4 (&raw)[U]) {                // lanes behind the last vector read that one
     const char* p = body + (int64_t)b * (64 * U * 16);
+    const unsigned most = !kAhead || b < full ? ~0u : (unsigned)(vectors - 1 - b * (64 * U)) * 16u;
 #pragma unroll
-    for (int u = 0; u < U; ++u) raw[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + (unsigned)lane * 16u + u * 1024));
+    for (int u = 0; u < U; ++u) raw[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + min((unsigned)lane * 16u + u * 1024, most)));
   };
+  const int at_end = lane < head ? lane : (lane >= 32 && lane - 32 < tail ? a.V - tail + lane - 32 : -1);
+  S end = {};
+  if (kAhead && head + tail > 0) end = row[max(at_end, 0)];
   Given<S> given;
   const bool writes = a.parts == 1 && wave == 0;
   if (W > 1 && writes) given.load_id(a, t, lane);
   float x[kPerLaneB];
-  auto widen = [&](const u32x4 (&raw)[U]) {
+  auto widen = [&](const u32x4 (&raw)[U], int b) {
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -346,6 +356,10 @@ __global__ __launch_bounds__(W * 64) void logprobs_kernel(const LogprobArgs a) {
           x[u * 4 + i] = __uint_as_float(raw[u][i]);
         }
       }
+    if (kAhead && b >= full) {
+#pragma unroll
+      for (int j = 0; j < kPerLaneB; ++j) x[j] = (b * U + j / kVec) * 64 + lane < vectors ? x[j] : -INFINITY;
+    }
   };
   Stream st;
   float bound = -INFINITY;
@@ -365,29 +379,33 @@ __global__ __launch_bounds__(W * 64) void logprobs_kernel(const LogprobArgs a) {
     for (int j = 0; j < kPerLaneB; ++j) st.add(j & 3, d[j]);
   };
   u32x4 raw[kRing][U];
-  const int last = first < full ? first + (full - 1 - first) / stride * stride : -1;   // this wave's last full batch
+  const int last = first < batches ? first + (batches - 1 - first) / stride * stride : -1;   // this wave's last batch
   if (last >= 0) {
 #pragma unroll
     for (int i = 0; i < kRing; ++i) load(min(first + i * stride, last), raw[i]);
   }
   if (W > 1 && writes) given.load_entry(a, row);
-  if (W > 1 ? part * W < full : last >= 0) {
+  if (W > 1 ? part * W < batches : last >= 0) {
     float top = -INFINITY;
     if (last >= 0) {
 #pragma unroll
       for (int i = 0; i < kRing; ++i) {
-        widen(raw[i]);
+        widen(raw[i], min(first + i * stride, last));
 #pragma unroll
-        for (int j = 0; j < kPerLaneB; ++j) top = fmaxf(top, x[j]);   // a NaN is dropped; a batch that is there twice counts as one
+        for (int j = 0; j < kPerLaneB; ++j) top = fmaxf(top, x[j]);   // a batch that is there twice counts as one
       }
     }
+    // A quiet NaN is dropped, a signalling one at the end of the chain is not (earlier it takes what is in front of it along: a lower bound still).  The
+    // compiler takes neither for possible.
+    asm volatile("" : "+v"(top));
+    if (top != top) top = -INFINITY;
     if constexpr (W > 1) {
       open_joint(s_joint, tid);
       if (n == 1) {                                        // an exchange in every wave costs less than the joint bound; four (9.2 us, 12.1 so) do not
         if (last >= 0) bound = below(order_key(wave_max(top)));
       } else {
         __syncthreads();
-        bound = below(joint_bound(s_joint, top, last >= 0, min(W, full - part * W), n, tid));
+        bound = below(joint_bound(s_joint, top, last >= 0, min(W, batches - part * W), n, tid));
       }
     } else {
       bound = below(nth_bound(order_key(top), n));
@@ -400,30 +418,38 @@ __global__ __launch_bounds__(W * 64) void logprobs_kernel(const LogprobArgs a) {
     for (int i = 0; i < kRing; ++i) {
       const int at = b + i * stride;
       if (at > last) break;
-      widen(raw[i]);
+      widen(raw[i], at);
       load(min(at + kRing * stride, last), raw[i]);
       // a wave's ids rise from batch to batch, so an entry equal to its list's last comes behind it; one equal to another wave's may come before
       process(true, [&](int j) { return head + ((at * U + j / kVec) * 64 + lane) * kVec + j % kVec; });
     }
   }
-  // the batch that is not full, then head and tail
-#pragma unroll 1
-  for (int b = full + ((first - full) & (stride - 1)); b < full + 2; b += stride) {
-    const bool ends = b > full;
-    if (ends ? head + tail == 0 : vectors % (64 * U) == 0) continue;
-    u32x4 rest[U];
+  if constexpr (kAhead) {
+    if (head + tail > 0) {
+      x[0] = at_end < 0 ? -INFINITY : to_f32(end);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      rest[u] = u32x4{kNegInf2, kNegInf2, kNegInf2, kNegInf2};
-      const int v = (full * U + u) * 64 + lane;
-      if (!ends && v < vectors) rest[u] = reinterpret_cast<const u32x4*>(body)[v];
+      for (int j = 1; j < kPerLaneB; ++j) x[j] = -INFINITY;
+      process(false, [&](int) { return at_end; });
     }
-    const int at = lane < head ? lane : (lane >= 32 && lane - 32 < tail ? a.V - tail + lane - 32 : -1);
-    if (ends && at >= 0) {
-      if constexpr (sizeof(S) == 2) rest[0][0] = 0xff800000u | row[at]; else rest[0][0] = __float_as_uint(row[at]);
+  } else {
+    // the batch that is not full, then head and tail
+#pragma unroll 1
+    for (int b = full + ((first - full) & (stride - 1)); b < full + 2; b += stride) {
+      const bool ends = b > full;
+      if (ends ? head + tail == 0 : vectors % (64 * U) == 0) continue;
+      u32x4 rest[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        rest[u] = u32x4{kNegInf2, kNegInf2, kNegInf2, kNegInf2};
+        const int v = (full * U + u) * 64 + lane;
+        if (!ends && v < vectors) rest[u] = reinterpret_cast<const u32x4*>(body)[v];
+      }
+      if (ends && at_end >= 0) {
+        if constexpr (sizeof(S) == 2) rest[0][0] = 0xff800000u | row[at_end]; else rest[0][0] = __float_as_uint(row[at_end]);
+      }
+      widen(rest, full);
+      process(false, [&](int j) { return ends ? at_end : head + ((full * U + j / kVec) * 64 + lane) * kVec + j % kVec; });
     }
-    widen(rest);
-    process(false, [&](int j) { return ends ? at : head + ((full * U + j / kVec) * 64 + lane) * kVec + j % kVec; });
   }
   Sums sum = st.sums();
   if constexpr (W > 1) {

@@ -89,6 +89,25 @@ def test_nan_of_every_sign_and_kind(bits, V, T):
         assert not (b.entropy[1:].isnan().any() or b.conf[1:].isnan().any() or b.top_logp[1:].isnan().any())
 
 
+@pytest.mark.parametrize("T, V, dtype", [(300, 9000, BF16), (1100, 9000, FP32), (2100, 2500, BF16), (2100, 1300, FP32), (64, 40000, FP32), (128, 70000, BF16)])
+def test_signalling_nan_beside_the_best_tokens(T, V, dtype):
+    """In every place of a lane's entries, in front of and behind tokens that belong to the list."""
+    z = (torch.randn((T, V), generator=_gen(V)) * 3).to(dtype)
+    rows = torch.arange(T)
+    at = (rows * 37) % V
+    for step in (1, 3, 5):
+        z[rows, (at + step) % V] = 30.0 + step
+    clean = z.clone()
+    clean[rows, at] = clean[rows, (at + 4) % V] = -math.inf
+    raw, bits = (z.view(torch.int16), 0x7f81) if dtype is BF16 else (z.view(torch.int32), 0x7f800001)
+    raw[rows, at] = bits
+    raw[rows, (at + 4) % V] = bits
+    b = mm.LogprobBuffers(T, 0, 12, V).run(z.cuda())
+    assert b.conf.isnan().all() and b.entropy.isnan().all()
+    order = torch.sort(clean.float(), dim=1, descending=True, stable=True).indices[:, :12]
+    assert torch.equal(b.top_idx.cpu().long(), order)
+
+
 def test_a_row_has_the_same_bits_in_every_call():
     """The order of the sums does not depend on which wave comes first."""
     for T, V, dtype in ((1, 131072, BF16), (37, 50257, FP32), (500, 20000, BF16), (2048, 3001, FP32)):
