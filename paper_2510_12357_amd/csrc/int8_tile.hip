@@ -1,10 +1,11 @@
 // The 8-bit product on tiles of 64 tokens x 64 or 128 weight rows: more tokens than the streaming kernel takes, and too few tiles of
 // 256 x 256 to fill the chip.
 //
-// Four waves in a 2 x 2 grid; chunks of 128 k in a ring of LDS, filled past the registers: five stages of 64 x 64, three of 64 x 128.  Two workgroups
-// per CU, or one of eight waves: two groups with a ring each share K, and their sums of integers are joined in LDS, exactly.
-// What bounds it is the way of a chunk from memory: a CU has as much of it under way as its LDS holds, so that deep rings of small tiles beat the
-// lower traffic of larger ones as long as there is a CU for each tile (65 x 2048 x 2048: 64 columns 7.2 us, 128 columns 9.3; 500 x 2048 x 2048 8.4 and
+// Four waves in a 2 x 2 grid; chunks of 128 k in a ring of LDS, filled past the registers.  One workgroup per CU of eight waves: two groups with
+// a ring each share K, and their sums of integers are joined in LDS, exactly; 64 x 64 in five stages, 64 x 128 in three.  Or several workgroups per CU of
+// four: three of 64 x 64 in three stages, two of 64 x 128 in three, five of 64 x 64 in two stages where K is short.
+// What bounds it is the way of a chunk from memory: a CU has as much of it under way as its LDS holds, so that small tiles beat the lower traffic of
+// larger ones as long as all tiles are under way at once (65 x 2048 x 2048: 64 columns 7.2 us, 128 columns 9.3; 500 x 2048 x 2048 8.4 and
 // 11.0), and two groups halve the number of chunks that follow each other.
 // A chunk is one asm block: matrix instructions, the fragment reads of the next k-steps and the loads of a later chunk alternate, and the
 // last k-step is multiplied while the first fragments of the next chunk are read (all reads in front of a chunk's multiplications, behind its
@@ -25,7 +26,6 @@ typedef __attribute__((ext_vector_type(16))) int i32x16;
 constexpr int kRowBytes = 128, kTileRows = 64;
 // NJ: blocks of 32 weight rows of a wave, 1 or 2: tiles of 64 NJ weight rows.
 constexpr int stage_bytes(int nj) { return (kTileRows + 64 * nj) * kRowBytes; }
-constexpr int stages(int nj) { return nj == 1 ? 5 : 3; }
 
 constexpr int kInsA = 2;                // loads of a wave per chunk: token rows; 2 NJ of weight rows
 
@@ -43,9 +43,9 @@ struct Block { i32x4 rs_a, rs_b; unsigned a_row, b_row, a_next, b_next, to_a, to
 #define LA(l) "s_add_u32 m0, %[ta], " #l "*1024\n\ts_nop 0\n\tbuffer_load_dwordx4 %[ao" #l "], %[ra], %[k] offen lds\n\t"
 #define LB(l) "s_add_u32 m0, %[tb], " #l "*1024\n\ts_nop 0\n\tbuffer_load_dwordx4 %[bo" #l "], %[rb], %[k] offen lds\n\t"
 #define WAIT(n) "s_waitcnt lgkmcnt(" #n ")\n\t"
-// in flight behind chunk kt + 1: all later ones, stages - 2 of them
-#define BARRIER1 "s_waitcnt vmcnt(12)\n\ts_barrier\n\t"
-#define BARRIER2 "s_waitcnt vmcnt(6)\n\ts_barrier\n\t"
+// in flight behind chunk kt + 1: all later ones, ST - 2 of them
+#define BARRIER "s_waitcnt vmcnt(%[later])\n\ts_barrier\n\t"
+#define LATER [later] "n"((ST - 2) * (kInsA + 2 * NJ))
 // wait states between the compiler's vector instructions and matrix instructions, and behind the last of these: the compiler, which does
 // not see what a block holds, may read or move their results right behind it
 #define START "s_nop 4\n\t"
@@ -61,24 +61,24 @@ struct Block { i32x4 rs_a, rs_b; unsigned a_row, b_row, a_next, b_next, to_a, to
 #define LOADS1 [ta] "s"(s.to_a), [tb] "s"(s.to_b), [k] "s"(s.k), [ra] "s"(s.rs_a), [rb] "s"(s.rs_b), [ao0] "v"(ao[0]), [ao1] "v"(ao[1]), [bo0] "v"(bo[0]), [bo1] "v"(bo[1])
 #define LOADS2 LOADS1, [bo2] "v"(bo[2]), [bo3] "v"(bo[3])
 #define IN [col0] "v"(col[0]), [col1] "v"(col[1]), [col2] "v"(col[2]), [col3] "v"(col[3]), [row_a] "s"(s.a_row), [row_b] "s"(s.b_row), [next_a] "s"(s.a_next), [next_b] "s"(s.b_next)
-template <int NJ>
+template <int NJ, int ST>
 __device__ __forceinline__ void chunk(i32x16 (&c)[2], Frags& f, const unsigned (&col)[4], const unsigned (&ao)[kInsA], const unsigned (&bo)[2 * NJ], const Block& s) {
   Frags f1, f2, f3;
   unsigned pa[4], pb[4];
   if constexpr (NJ == 2)
     asm volatile(ADDRESSES READ2(1) MUL(c00, a0, b0) READ2(2) MUL(c01, a0, d0) READ2(3) LA(0) LA(1) WAIT(6) MUL(c00, a1, b1) LB(0) LB(1) MUL(c01, a1, d1) LB(2) LB(3)
-                 WAIT(3) MUL(c00, a2, b2) MUL(c01, a2, d2) WAIT(0) BARRIER2 READ2(0) MUL(c00, a3, b3) MUL(c01, a3, d3) WAIT(0) DONE : OUT2 : IN, LOADS2 : "memory", "scc");
+                 WAIT(3) MUL(c00, a2, b2) MUL(c01, a2, d2) WAIT(0) BARRIER READ2(0) MUL(c00, a3, b3) MUL(c01, a3, d3) WAIT(0) DONE : OUT2 : IN, LATER, LOADS2 : "memory", "scc");
   else
-    asm volatile(ADDRESSES READ1(1) MUL(c00, a0, b0) READ1(2) READ1(3) LA(0) LA(1) WAIT(4) MUL(c01, a1, b1) LB(0) LB(1) WAIT(2) MUL(c00, a2, b2) WAIT(0) BARRIER1
-                 READ1(0) MUL(c01, a3, b3) WAIT(0) DONE : OUT1 : IN, LOADS1 : "memory", "scc");
+    asm volatile(ADDRESSES READ1(1) MUL(c00, a0, b0) READ1(2) READ1(3) LA(0) LA(1) WAIT(4) MUL(c01, a1, b1) LB(0) LB(1) WAIT(2) MUL(c00, a2, b2) WAIT(0) BARRIER
+                 READ1(0) MUL(c01, a3, b3) WAIT(0) DONE : OUT1 : IN, LATER, LOADS1 : "memory", "scc");
 }
 // The first fragments; in flight behind chunk 0: the others that were loaded.
-template <int NJ>
+template <int NJ, int ST>
 __device__ __forceinline__ void first_frags(Frags& f, unsigned pa, unsigned pb) {
   if constexpr (NJ == 2)
-    asm volatile(BARRIER2 READ2(0) WAIT(0) : [a0] "=&v"(f.a), [b0] "=&v"(f.b), [d0] "=&v"(f.d) : [pa0] "v"(pa), [pb0] "v"(pb) : "memory");
+    asm volatile(BARRIER READ2(0) WAIT(0) : [a0] "=&v"(f.a), [b0] "=&v"(f.b), [d0] "=&v"(f.d) : [pa0] "v"(pa), [pb0] "v"(pb), LATER : "memory");
   else
-    asm volatile(BARRIER1 READ1(0) WAIT(0) : [a0] "=&v"(f.a), [b0] "=&v"(f.b) : [pa0] "v"(pa), [pb0] "v"(pb) : "memory");
+    asm volatile(BARRIER READ1(0) WAIT(0) : [a0] "=&v"(f.a), [b0] "=&v"(f.b) : [pa0] "v"(pa), [pb0] "v"(pb), LATER : "memory");
 }
 // one chunk into LDS without anything beside it
 template <int NJ>
@@ -93,11 +93,11 @@ __device__ __forceinline__ i32x4 rsrc4(const void* p, unsigned bytes) {
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 __device__ __forceinline__ i32x4 quarter(const i32x16& c, int q) { return i32x4{c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]}; }
 
-// KG: groups of four waves that share K
-template <typename S, int KG, int NJ>
+// KG: groups of four waves that share K.  ST: stages of a ring
+template <typename S, int KG, int NJ, int ST>
 __global__ __launch_bounds__(256 * KG) void int8_tile_kernel(const Int8Args a, const int mt, const int total) {
   extern __shared__ __attribute__((aligned(1024))) char s_tiles[];
-  constexpr int BM = kTileRows, BN = 64 * NJ, kStages = stages(NJ), kStageBytes = stage_bytes(NJ), kInsB = 2 * NJ;
+  constexpr int BM = kTileRows, BN = 64 * NJ, kStages = ST, kStageBytes = stage_bytes(NJ), kInsB = 2 * NJ;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6) & 3, group = uniform(tid >> 8), h = lane >> 5;
   const int wm = wave >> 1, wn = wave & 1;
   // an XCD has a contiguous range of the tiles; the token tiles of a panel follow each other
@@ -167,14 +167,14 @@ __global__ __launch_bounds__(256 * KG) void int8_tile_kernel(const Int8Args a, c
 #pragma unroll
   for (int k = 0; k < 4; ++k) col[k] = (unsigned)((lane & 31) * kRowBytes) + ((unsigned)(2 * k + h) ^ fkey) * 16u;
   Frags f;
-  first_frags<NJ>(f, col[0] + a_at, col[0] + b_at);
+  first_frags<NJ, ST>(f, col[0] + a_at, col[0] + b_at);
   i32x16 acc[2] = {};
   unsigned here = 0, next = kStageBytes, free = (kStages - 1) * kStageBytes;   // stages of chunks kt, kt + 1, kt - 1
   for (int kt = 0; kt < nk; ++kt) {
     s.a_row = a_at + here; s.b_row = b_at + here;
     s.a_next = a_at + next; s.b_next = b_at + next;
     s.to_a = a_to + free; s.to_b = b_to + free;
-    chunk<NJ>(acc, f, col, aoff, boff, s);
+    chunk<NJ, ST>(acc, f, col, aoff, boff, s);
     free = here;
     here = next;
     next = next == (kStages - 1) * kStageBytes ? 0 : next + kStageBytes;
@@ -228,32 +228,37 @@ __global__ __launch_bounds__(256 * KG) void int8_tile_kernel(const Int8Args a, c
   }
 }
 
-template <typename S, int KG, int NJ>
+template <typename S, int KG, int NJ, int ST>
 int launch_t(const Int8Args& a, hipStream_t s) {
-  constexpr int kLds = KG * stages(NJ) * stage_bytes(NJ);
+  constexpr int kLds = KG * ST * stage_bytes(NJ);
   static_assert(kLds <= 163840, "LDS of a CU");
   static std::atomic<int> ready{0};
   if (!ready.load(std::memory_order_relaxed)) {
-    if (hipFuncSetAttribute(reinterpret_cast<const void*>(&int8_tile_kernel<S, KG, NJ>), hipFuncAttributeMaxDynamicSharedMemorySize, kLds) != hipSuccess)
+    if (hipFuncSetAttribute(reinterpret_cast<const void*>(&int8_tile_kernel<S, KG, NJ, ST>), hipFuncAttributeMaxDynamicSharedMemorySize, kLds) != hipSuccess)
       return hip_fail(hipGetLastError(), "int8_tile_kernel: LDS size attribute");
     ready.store(1, std::memory_order_relaxed);
   }
   const int64_t mt = (a.T + 63) / 64, total = mt * ((a.N + 64 * NJ - 1) / (64 * NJ));
   if (total >= (int64_t)1 << 30) return fail(MOE_E_UNSUPPORTED, "8-bit product: %lld tiles", (long long)total);
-  hipLaunchKernelGGL((int8_tile_kernel<S, KG, NJ>), dim3((unsigned)(((total + 7) / 8) * 8)), dim3(256 * KG), kLds, s, a, (int)mt, (int)total);
+  hipLaunchKernelGGL((int8_tile_kernel<S, KG, NJ, ST>), dim3((unsigned)(((total + 7) / 8) * 8)), dim3(256 * KG), kLds, s, a, (int)mt, (int)total);
   return hip_fail(hipGetLastError(), "int8_tile_kernel launch");
 }
 
 template <typename S>
-int launch_s(const Int8Args& a, int cols, bool share_k, hipStream_t s) {
-  if (cols == 64) return share_k ? launch_t<S, 2, 1>(a, s) : launch_t<S, 1, 1>(a, s);
-  return share_k ? launch_t<S, 2, 2>(a, s) : launch_t<S, 1, 2>(a, s);
+int launch_s(const Int8Args& a, Int8Tile tile, hipStream_t s) {
+  switch (tile) {
+    case Int8Tile::k64Shared: return launch_t<S, 2, 1, 5>(a, s);
+    case Int8Tile::k64: return launch_t<S, 1, 1, 3>(a, s);
+    case Int8Tile::k64Short: return launch_t<S, 1, 1, 2>(a, s);
+    case Int8Tile::k128Shared: return launch_t<S, 2, 2, 3>(a, s);
+    default: return launch_t<S, 1, 2, 3>(a, s);
+  }
 }
 
 }  // namespace
 
-int launch_int8_tile(const Int8Args& a, int cols, bool share_k, hipStream_t s) {
-  return a.out_dtype == MOE_FP32 ? launch_s<float>(a, cols, share_k, s) : launch_s<uint16_t>(a, cols, share_k, s);
+int launch_int8_tile(const Int8Args& a, Int8Tile tile, hipStream_t s) {
+  return a.out_dtype == MOE_FP32 ? launch_s<float>(a, tile, s) : launch_s<uint16_t>(a, tile, s);
 }
 
 }  // namespace mm

@@ -171,7 +171,9 @@ struct Int8Args {
 };
 int launch_int8_product(const Int8Args& a, hipStream_t s);
 int launch_int8_wide(const Int8Args& a, int blocks, hipStream_t s);                       // token tiles of 64 blocks rows, 2 to 4
-int launch_int8_tile(const Int8Args& a, int cols, bool share_k, hipStream_t s);           // tiles of 64 x cols (64, 128); share_k: two groups of waves a tile
+// tiles of 64 tokens x 64 or 128 weight rows; Shared: two groups of waves share K; Short: two stages
+enum class Int8Tile { k64Shared, k64, k64Short, k128Shared, k128 };
+int launch_int8_tile(const Int8Args& a, Int8Tile tile, hipStream_t s);
 bool int8_streams(int T, int K);           // whether launch_int8_stream takes these sizes
 int launch_int8_stream(const Int8Args& a, hipStream_t s);
 size_t int8_lane_codes_bytes(int T, int K);

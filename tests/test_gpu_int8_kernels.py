@@ -34,6 +34,8 @@ SMALL_TILES = [(65, 64, 128), (66, 65, 1024), (128, 1000, 1536), (193, 2050, 153
                (300, 4000, 500), (333, 5000, 1000), (129, 8001, 1535), (333, 5000, 1700), (129, 8065, 1541), (449, 4097, 2300), (64, 16385, 4200),
                (333, 7000, 1111), (65, 32801, 99), (1000, 4100, 2500), (2000, 1030, 1552)]
 
+# more tiles than can be under way at once, short K: two stages
+SMALL_TILES += [(300, 16400, 77), (65, 40001, 128), (130, 33000, 300), (700, 7001, 513), (129, 22000, 640), (2049, 2700, 16), (100, 50000, 7)]
 
 @pytest.mark.parametrize("T, N, K", SMALL_TILES)
 @pytest.mark.parametrize("dtype, with_bias", [(FP32, False), (BF16, True)])
