@@ -245,7 +245,7 @@ __device__ __forceinline__ unsigned joint_bound(Joint& s, float top, bool any, i
   }
   __syncthreads();
   const unsigned low = s.low;
-  const bool in = any && key >= low;
+  const bool in = any && key >= low && key > kKeyNegInf;   // rows that a mask left little of: lanes without an entry are many
   const u64 mask = __ballot(in);
   int at = 0;
   if (mask && lane == 0) at = atomicAdd(&s.count, __popcll(mask));
