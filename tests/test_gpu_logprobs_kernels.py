@@ -21,6 +21,13 @@ def test_splits_of_a_row(T, V, dtype, n_top):
     _check_logprobs(z.to(dtype), _tokens(T, 2, V, T), n_top)
 
 
+# two, four, eight and sixteen workgroups a row, at the lengths where they begin
+@pytest.mark.parametrize("T, V", [(128, 64513), (64, 48129), (63, 50001), (32, 72705), (20, 80001), (16, 261121), (3, 270001)])
+@pytest.mark.parametrize("dtype, n_top", [(FP32, 5), (BF16, 1)])
+def test_parts_of_a_row(T, V, dtype, n_top):
+    test_splits_of_a_row(T, V, dtype, n_top)
+
+
 @pytest.mark.parametrize("T, V", [(1, 131072), (5, 40000), (300, 9000), (450, 4100), (2050, 2100)])
 @pytest.mark.parametrize("dtype", [FP32, BF16])
 def test_rows_in_order_and_in_steps(T, V, dtype):
