@@ -1,7 +1,7 @@
 // The 8-bit product on tiles of up to 256 tokens x 256 weight rows, for many tokens.
 //
-// What bounds it: the matrix cores (random codes draw so much power that the matrix instructions alone reach 3.3 of their 4.9 POP/s), and
-// beside them LDS: 48 KB of its 64 per 512 cycles of a k-step.  Four waves of 128 x 128 outputs, one per SIMD, so that nothing hides a stall:
+// What bounds it: the matrix cores (random codes draw so much power that the matrix instructions alone reach 3.3 of their 4.9 POP/s; LDS reads take a
+// seventh of the cycles by the counters).  Four waves of 128 x 128 outputs, one per SIMD, so that nothing hides a stall:
 // a chunk of 128 k is one asm block, in which matrix instructions, fragment reads of the next k-step, loads into LDS and the arithmetic of
 // their addresses alternate; between blocks there is what it takes to step one cursor.
 //   * LDS (all 160 KB): two slots of 256 token rows x 128 k, three of weight rows, which come from further away; rows of 128 bytes, the 16-byte

@@ -497,19 +497,21 @@ __global__ __launch_bounds__(kMaxParts * 64) void logprobs_join_kernel(const Log
 }
 static_assert(kMaxParts <= kMaxLists && kList <= 64, "one thread per candidate");
 
-// Waves per row part and parts per row.  us, waves x parts: 4096 rows of 131072 bf16 1x1 206, 4x1 222; 1999 of 50257 bf16 1x1 51.2, 4x1 53.3, 8x1 63;
-// 1300 of 50257 bf16 1x1 49.3, 4x1 40.2, 8x1 46.3; 600 of 100000 fp32 1x1 69.6, 4x1 49.8, 8x1 52.6; 300 of 50257 bf16 1x1 35.7, 4x1 21.1, 8x1 18.8, 8x2
-// 24.0; 128 of 151001 fp32 8x1 31.4, 8x2 27.2, 8x4 26.8, 8x8 35.0; 64 of 131072 fp32 8x1 35.7, 8x2 27.9, 8x4 22.5, 8x8 23.2; 16 of 131072 fp32 8x1 21.4, 8x4
-// 15.0, 8x8 13.2, 8x16 13.5; 8 of 112000 fp32 8x1 17.9, 8x4 13.5, 8x8 12.4; 1 of 131072 bf16 8x1 17.6, 8x4 12.6, 8x8 11.7, 8x16 11.5; 1 of 79984 fp32 8x1 13.2, 8x4 11.5,
-// 8x8 11.1; 32 of 50257 fp32 8x1 14.4, 8x2 14.1, 8x4 13.1; 128 of 50257 fp32 8x1 14.9, 8x2 15.7; 1 of 32000 fp32 8x1 8.2, 8x2 9.5, 8x4 8.5.  Sixteen waves were
-// slower than eight everywhere (1 of 32000 8.6, 8 of 50257 13.5 against 13.1).
+// Waves per row part and parts per row.  us, waves x parts: 4096 rows of 131072 bf16 1x1 206, 4x1 222; 3000 of 50257 bf16 1x1 66.2, 4x1
+// 72.4; 2300 of 50257 1x1 62.9, 4x1 57.0; 1999 of 50257 1x1 51.2, 4x1 51.3, 8x1 61.7, of 20000 fp32 1x1 32.0, 4x1 36.1; 1700 of 9000 bf16
+// 1x1 18.4, 4x1 23.0; 1200 of 20000 fp32 1x1 29.3, 4x1 25.1; 600 of 56585 bf16 1x1 41.1, 4x1 28.0, 8x1 29.2; 478 of 56585 bf16, 20
+// alternatives, 4x1 30.9, 8x1 26.3; 320 of it 4x1 30.0, 8x1 25.4; 300 of 50257 bf16 4x1 21.1, 8x1 18.8, 8x2 24.0; 128 of 151001 fp32 8x1
+// 31.4, 8x2 27.2, 8x4 26.8, 8x8 35.0; 64 of 131072 fp32 8x1 35.7, 8x2 27.9, 8x4 22.5, 8x8 23.2; 16 of 131072 fp32 8x1 21.4, 8x4 15.0, 8x8
+// 13.2, 8x16 13.5; 8 of 112000 fp32 8x1 17.9, 8x4 13.5, 8x8 12.4; 1 of 131072 bf16 8x1 17.6, 8x4 12.6, 8x8 11.7, 8x16 11.5; 1 of 79984 fp32
+// 8x1 13.2, 8x4 11.5, 8x8 11.1; 32 of 50257 fp32 8x1 14.4, 8x2 14.1, 8x4 13.1; 128 of 50257 fp32 8x1 14.9, 8x2 15.7; 1 of 32000 fp32 8x1
+// 8.2, 8x2 9.5, 8x4 8.5.  Sixteen waves were slower than eight everywhere (1 of 32000 8.6, 8 of 50257 13.5 against 13.1).
 // Not kept, with eight waves: twice as many batches in registers (64 of 131072 fp32 with 20 alternatives 22.7 -> 22.0, with none 16.0 -> 16.9, 300 of
 // 50257 bf16 17.0 -> 20.0); batches through LDS, and so one copy of the code instead of one per batch in flight (0.7 to 1 us more for few rows).
 struct Split { int waves, parts; };
 Split split_of(int T, int V) {
   const int batches = V / kBatch + 1;
-  if (T >= 2048 || batches < 4) return {1, 1};
-  if (T >= 400 || batches < 8) return {4, 1};
+  if (T >= 2560 || (T >= 1536 && batches < 32) || batches < 4) return {1, 1};
+  if (T > 512 || batches < 8) return {4, 1};
   int parts = 1;
   if (batches >= 64 && T * 2 <= 256) parts = 2;
   if (batches >= 48 && T * 4 <= 256) parts = 4;
