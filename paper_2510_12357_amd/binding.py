@@ -536,7 +536,15 @@ def _rows(t: Optional[torch.Tensor]):
 
 def _ld(t: torch.Tensor) -> int:
     # a single row has no next one: torch gives such a dimension any stride
-    return int(t.stride(0)) if t.shape[0] > 1 else max(int(t.stride(0)), int(t.shape[1]))
+    if t.shape[0] <= 1:
+        return max(int(t.stride(0)), int(t.shape[1]))
+    if t.stride(0) < t.shape[1]:
+        raise ValueError(_SHARED_ROWS)
+    return int(t.stride(0))
+
+
+# an expanded tensor's rows are 0 elements apart, which to the C ABI means dense rows
+_SHARED_ROWS = "rows share memory: make them dense with contiguous()"
 
 
 def _float_type(t: torch.Tensor) -> int:
@@ -676,7 +684,11 @@ class LogprobBuffers:
             assert tokens.dtype is torch.int32 and tokens.shape == self.token_logp.shape and tokens.is_contiguous(), "tokens: int32 [T, n_given]"
             given = tokens.data_ptr()
         c, ref = self._configs[logits.dtype]
-        c.ld = step if T > 1 else max(step, V)               # a single row has no next one: torch gives such a dimension any stride
+        if step < V:
+            if T > 1:
+                raise ValueError(_SHARED_ROWS)
+            step = V                                         # a single row has no next one: torch gives such a dimension any stride
+        c.ld = step
         rc = _lib.moe_token_logprobs(ref, logits.data_ptr(), given, self.token_logp.data_ptr(), self.entropy.data_ptr(), self.conf.data_ptr(),
                                      self.top_idx.data_ptr(), self.top_logp.data_ptr(), self.ws.data_ptr(), self.ws.numel(),
                                      _raw_stream(stream, logits.get_device()))

@@ -1,0 +1,49 @@
+"""What the output head's Python calls refuse of tensors before anything is enqueued (no GPU needed: each refusal comes before the library)."""
+import os
+
+import pytest
+import torch
+
+from paper_2510_12357_amd import binding as mm
+
+pytestmark = pytest.mark.skipif(not os.path.exists(mm.LIB_PATH), reason="libmobile_moe.so not built")
+
+
+def _codes(rows, K=64):
+    return torch.ones((rows, K), dtype=torch.int8)
+
+
+# ------------------------------------------------------------------------------------ rows that lie on each other
+@pytest.mark.parametrize("step", [0, 1, 63])
+def test_rows_of_one_place_are_not_dense_rows(step):
+    """A distance of 0 means "dense" to the C calls, so rows that share memory (expanded tensors) must not reach them."""
+    x, w, out = torch.zeros((4, 64)), _codes(8), torch.zeros((4, 8))
+    lie = lambda t: t.reshape(-1).as_strided(t.shape, (min(step, t.shape[1] - 1), 1))  # noqa: E731
+    assert mm.int8_config(x, w, out).ldx == 64
+    for a in ((lie(x), w, out), (x, lie(w), out), (x, w, lie(out))):
+        with pytest.raises(ValueError, match="rows"):
+            mm.int8_config(*a)
+    with pytest.raises(ValueError, match="rows"):
+        mm.moe_quantize_rows(lie(x), _codes(4), torch.zeros(4))
+    with pytest.raises(ValueError, match="rows"):
+        mm.LogprobBuffers(4, 0, 1, 64, device="cpu").run(lie(x))
+
+
+def test_expanded_rows():
+    x, w = torch.zeros((1, 64)).expand(4, 64), _codes(1).expand(8, 64)
+    for a in ((x, _codes(8), torch.zeros((4, 8))), (torch.zeros((4, 64)), w, torch.zeros((4, 8))),
+              (torch.zeros((4, 64)), _codes(8), torch.zeros((1, 8)).expand(4, 8))):
+        with pytest.raises(ValueError, match="rows"):
+            mm.int8_config(*a)
+    for z in (torch.zeros((1, 5)).expand(3, 5), torch.zeros((1, 1)).expand(3, 1)):
+        with pytest.raises(ValueError, match="rows"):
+            mm.LogprobBuffers(3, 0, 1, z.shape[1], device="cpu").run(z)
+
+
+def test_a_single_row_may_have_any_stride():
+    """A dimension of one row has no distance to a next one."""
+    for step in (0, 1, 64, 80):
+        c = mm.int8_config(torch.zeros(80).as_strided((1, 64), (step, 1)), _codes(8), torch.zeros((1, 8)).as_strided((1, 8), (step, 1)))
+        assert c.ldx >= 64 and c.ldo >= 8
+    c = mm.int8_config(torch.zeros((0, 64)), _codes(8), torch.zeros((0, 8)))
+    assert (c.T, c.ldx, c.ldo) == (0, 64, 8)
