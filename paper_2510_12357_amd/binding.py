@@ -587,7 +587,9 @@ def _raw_stream(stream, device: int) -> int:
 class Int8Linear:
     """A projection with 8-bit weights: codes w [N, K] (rows padded to 16 bytes, as quantize_rows makes them), w_scale [N] and
     an optional bias [N] in fp32.  Calling it enqueues one product on `stream`; the workspace for float tokens is kept and
-    grows with the largest call, so calls that may overlap (streams without order between them) need an object each."""
+    grows with the largest call, so calls that may overlap (streams without order between them, a graph's replay among them) need
+    an object each.  A captured graph reads the weights and a workspace of its object, which has to live as long as the graph; larger
+    calls in between do not matter to it."""
 
     def __init__(self, w: torch.Tensor, w_scale: torch.Tensor, bias: Optional[torch.Tensor] = None):
         load_library()
@@ -597,6 +599,7 @@ class Int8Linear:
         assert w.dtype == torch.int8 and all(t is None or t.device == w.device for t in (w_scale, bias)), "int8 codes, all on one device"
         self._w, self._w_scale, self._bias = w, w_scale, bias
         self.ws = self.ws_stream = None
+        self._outgrown = []                                  # workspaces of smaller calls: captured graphs have their addresses
         self._calls = {}                                     # of each form of tokens and outputs: its description, workspace bytes
 
     w, w_scale, bias = property(lambda self: self._w), property(lambda self: self._w_scale), property(lambda self: self._bias)
@@ -607,10 +610,12 @@ class Int8Linear:
         return cls(*quantize_rows(weight, stream), bias)
 
     def _workspace(self, need: int, stream, handle: int) -> int:
-        # memory belongs to the stream it was taken on: its reuse after a larger call has replaced it waits for every stream that read it
+        # memory belongs to the stream it was taken on: its reuse after the object's end waits for every stream that read it
         if self.ws is None or self.ws.numel() < need:
-            s = _torch_stream(stream)
-            with torch.cuda.stream(s):
+            if self.ws is not None:                          # twice as large at least: what is kept stays below the one in use
+                need = max(need, 2 * self.ws.numel())
+                self._outgrown.append(self.ws)
+            with torch.cuda.stream(_torch_stream(stream)):
                 self.ws = torch.empty((need,), dtype=torch.uint8, device=self._w.device)
             self.ws_stream = handle
         elif handle != self.ws_stream:

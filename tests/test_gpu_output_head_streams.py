@@ -1,0 +1,45 @@
+"""The output head's Python objects in graphs and on several streams: memory that a graph or another stream still uses is not given away."""
+import pytest
+import torch
+
+from paper_2510_12357_amd import binding as mm
+
+pytestmark = pytest.mark.gpu
+BF16, FP32 = torch.bfloat16, torch.float32
+
+
+def _gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+@pytest.mark.parametrize("T, K", [(40, 512), (100, 333)])
+def test_a_graph_outlives_larger_calls_of_its_object(T, K):
+    """Captured with few tokens, then eager prompts on the same object and tensors that take whatever memory is free: the replays write over
+    none of them and are right."""
+    N = 700
+    weight = torch.randn((N, K), generator=_gen(1)).cuda()
+    lin, other = mm.Int8Linear.quantize(weight), mm.Int8Linear.quantize(weight)
+    x = torch.zeros((T, K), dtype=BF16, device="cuda")
+    out = torch.empty((T, N), dtype=FP32, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        lin(x, out=out)
+    torch.cuda.synchronize()
+    size = lin.ws.numel()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lin(x, out=out)
+    for i in range(4):
+        prompt = torch.randn((T * (i + 2) ** 2, K), generator=_gen(i)).cuda()
+        assert torch.equal(lin(prompt), other(prompt))
+        assert lin.ws.numel() > size
+        with torch.cuda.stream(side):
+            there = [torch.full((size,), 7, dtype=torch.uint8, device="cuda") for _ in range(40)]
+        here = [torch.full((size,), 9, dtype=torch.uint8, device="cuda") for _ in range(40)]
+        torch.cuda.synchronize()
+        x.copy_(torch.randn((T, K), generator=_gen(10 + i)).to(BF16))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, other(x))
+        assert all((t == 7).all() for t in there) and all((t == 9).all() for t in here)

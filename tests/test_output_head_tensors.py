@@ -1,5 +1,7 @@
 """What the output head's Python calls refuse of tensors before anything is enqueued (no GPU needed: each refusal comes before the library)."""
+import contextlib
 import os
+import weakref
 
 import pytest
 import torch
@@ -47,3 +49,21 @@ def test_a_single_row_may_have_any_stride():
         assert c.ldx >= 64 and c.ldo >= 8
     c = mm.int8_config(torch.zeros((0, 64)), _codes(8), torch.zeros((0, 8)))
     assert (c.T, c.ldx, c.ldo) == (0, 64, 8)
+
+
+# ------------------------------------------------------------------------------------ workspaces
+def test_a_workspace_lives_as_long_as_its_object(monkeypatch):
+    """A captured graph holds the address of the workspace that its call had, so a larger call must not give that memory back; and what is
+    kept stays below what the largest call took."""
+    monkeypatch.setattr(mm, "_torch_stream", lambda stream: None)
+    monkeypatch.setattr(torch.cuda, "stream", lambda stream: contextlib.nullcontext())
+    lin = mm.Int8Linear(_codes(8), torch.ones(8))
+    held, largest = [], 0
+    for need in list(range(256, 40000, 256)) + [100, 5000, 10 ** 6, 512]:
+        address = lin._workspace(need, None, 7)
+        largest = max(largest, need)
+        assert lin.ws.data_ptr() == address and lin.ws.numel() >= need
+        if not any(h() is lin.ws for h in held):
+            held.append(weakref.ref(lin.ws))
+    assert len(held) > 2 and all(h() is not None for h in held)
+    assert sum(h().numel() for h in held) <= 4 * largest
