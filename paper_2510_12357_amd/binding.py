@@ -497,11 +497,13 @@ def moe_prefetcher_advance(p: int, layer: int, distance: int, n_layers: int, str
 def moe_quantize_rows(x, q, scale, stream=None) -> None:
     """x: [rows, K] float rows; q: int8 [rows, ldq] whole rows, ldq >= K a multiple of 16; scale: [rows] fp32."""
     assert q.shape[0] == x.shape[0] and q.is_contiguous()
-    _check(load_library().moe_quantize_rows(_rows(x), _float_type(x), x.shape[0], x.shape[1], _ld(x), _ptr(q), q.shape[1], _ptr(scale),
-                                            _stream(stream)))
+    args = _rows(x), _float_type(x), x.shape[0], x.shape[1], _ld(x), _ptr(q), q.shape[1], _ptr(scale)
+    _on_one_gpu(x, q, scale)
+    _check(load_library().moe_quantize_rows(*args, _stream(stream)))
 
 
 def moe_matmul_int8(cfg: moe_int8_config, x, x_scale, w, w_scale, bias, out, stream=None) -> None:
+    _on_one_gpu(x, x_scale, w, w_scale, bias, out)
     _check(load_library().moe_matmul_int8(ctypes.byref(cfg), _rows(x), _ptr(x_scale), _rows(w), _ptr(w_scale), _ptr(bias), _rows(out),
                                           _stream(stream)))
 
@@ -511,6 +513,7 @@ def moe_linear_int8_workspace_bytes(cfg: moe_int8_config) -> int:
 
 
 def moe_linear_int8(cfg: moe_int8_config, x, w, w_scale, bias, out, ws, ws_bytes: int, stream=None) -> None:
+    _on_one_gpu(x, w, w_scale, bias, out, ws)
     _check(load_library().moe_linear_int8(ctypes.byref(cfg), _rows(x), _rows(w), _ptr(w_scale), _ptr(bias), _rows(out), _ptr(ws),
                                           ws_bytes, _stream(stream)))
 
@@ -521,6 +524,7 @@ def moe_token_logprobs_workspace_bytes(cfg: moe_logprobs_config) -> int:
 
 def moe_token_logprobs(cfg: moe_logprobs_config, logits, tokens, token_logp, entropy, conf, top_idx, top_logp, ws, ws_bytes: int,
                        stream=None) -> None:
+    _on_one_gpu(logits, tokens, token_logp, entropy, conf, top_idx, top_logp, ws)
     _check(load_library().moe_token_logprobs(ctypes.byref(cfg), _rows(logits), _ptr(tokens), _ptr(token_logp), _ptr(entropy), _ptr(conf),
                                              _ptr(top_idx), _ptr(top_logp), _ptr(ws), ws_bytes, _stream(stream)))
 
@@ -532,6 +536,16 @@ def _rows(t: Optional[torch.Tensor]):
         return None
     assert t.dim() == 2 and (t.shape[1] <= 1 or t.stride(1) == 1), "rows passed to the C ABI must be dense"
     return ctypes.c_void_p(t.data_ptr())
+
+
+_DEVICES = "tensors on more than one device, or not on a GPU"
+
+
+def _on_one_gpu(*tensors: Optional[torch.Tensor]) -> None:
+    """The kernels take addresses as they are."""
+    devices = {t.device for t in tensors if t is not None}
+    if len(devices) != 1 or devices.pop().type != "cuda":
+        raise ValueError(_DEVICES)
 
 
 def _ld(t: torch.Tensor) -> int:
@@ -625,7 +639,7 @@ class Int8Linear:
     def _call(self, x: torch.Tensor, out: torch.Tensor):
         """-> (description, workspace bytes) of a call with such tokens and outputs: the checks that their shapes, types and strides need."""
         _rows(x), _rows(out)
-        assert x.device == self._w.device and out.device == self._w.device, "x, out and the weights belong on one device"
+        _on_one_gpu(x, out, self._w)
         c = int8_config(x, self._w, out)
         need = 0 if x.dtype == torch.int8 else moe_linear_int8_workspace_bytes(c)
         if len(self._calls) > 256:                           # a server's batches are of any size
@@ -649,6 +663,8 @@ class Int8Linear:
         if x.dtype is torch.int8:
             assert x_scale is not None and x_scale.dtype is torch.float32 and x_scale.numel() == x.shape[0] and x_scale.is_contiguous(), \
                 "codes come with their scales, [T] fp32"
+            if x_scale.get_device() != key[3]:
+                raise ValueError(_DEVICES)
             rc = _lib.moe_matmul_int8(c, x.data_ptr(), x_scale.data_ptr(), self._w.data_ptr(), self._w_scale.data_ptr(), bias, out.data_ptr(), s)
         else:
             ws = self._workspace(need, stream, s)
@@ -677,6 +693,7 @@ class LogprobBuffers:
         self._configs = {torch.bfloat16: (self.c[MOE_BF16], ctypes.byref(self.c[MOE_BF16])),
                          torch.float32: (self.c[MOE_FP32], ctypes.byref(self.c[MOE_FP32]))}
         self.ws = torch.empty((need,), dtype=torch.uint8, device=device)
+        self._device = self.ws.get_device()                  # -1: not a GPU's
 
     def run(self, logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, stream=None) -> "LogprobBuffers":
         """logits [T, V] bf16 or fp32, tokens int32 [T, n_given]."""
@@ -684,8 +701,10 @@ class LogprobBuffers:
         assert T == self.T and V == self.V, "logits do not fit the buffers"
         step, inner = logits.stride()
         assert inner == 1 or V == 1, "rows passed to the C ABI must be dense"
-        given = None
+        given, device = None, logits.get_device()
         if self.n_given:
+            if tokens is None:
+                raise ValueError("the buffers are for given tokens, of which there are none")
             assert tokens.dtype is torch.int32 and tokens.shape == self.token_logp.shape and tokens.is_contiguous(), "tokens: int32 [T, n_given]"
             given = tokens.data_ptr()
         c, ref = self._configs[logits.dtype]
@@ -694,9 +713,11 @@ class LogprobBuffers:
                 raise ValueError(_SHARED_ROWS)
             step = V                                         # a single row has no next one: torch gives such a dimension any stride
         c.ld = step
+        if device < 0 or device != self._device or (given is not None and tokens.get_device() != device):
+            raise ValueError(_DEVICES)
         rc = _lib.moe_token_logprobs(ref, logits.data_ptr(), given, self.token_logp.data_ptr(), self.entropy.data_ptr(), self.conf.data_ptr(),
                                      self.top_idx.data_ptr(), self.top_logp.data_ptr(), self.ws.data_ptr(), self.ws.numel(),
-                                     _raw_stream(stream, logits.get_device()))
+                                     _raw_stream(stream, device))
         if rc:
             _check(rc)
         return self

@@ -67,3 +67,26 @@ def test_a_workspace_lives_as_long_as_its_object(monkeypatch):
             held.append(weakref.ref(lin.ws))
     assert len(held) > 2 and all(h() is not None for h in held)
     assert sum(h().numel() for h in held) <= 4 * largest
+
+
+# ------------------------------------------------------------------------------------ devices
+def test_host_tensors_are_refused():
+    """A kernel would take a host address as it is."""
+    lin = mm.Int8Linear(_codes(8), torch.ones(8))
+    for x, scale in ((torch.zeros((2, 64)), None), (_codes(2), torch.ones(2)), (_codes(2), torch.ones(2, device="meta"))):
+        with pytest.raises(ValueError, match="device"):
+            lin(x, x_scale=scale, out=torch.zeros((2, 8)))
+    for n, tokens in ((0, None), (1, torch.zeros((2, 1), dtype=torch.int32)), (1, torch.zeros((2, 1), dtype=torch.int32, device="meta"))):
+        with pytest.raises(ValueError, match="device"):
+            mm.LogprobBuffers(2, n, 1, 64, device="cpu").run(torch.zeros((2, 64)), tokens)
+
+
+def test_host_tensors_are_refused_by_every_call():
+    x, w, out, f = torch.zeros((2, 64)), _codes(8), torch.zeros((2, 8)), torch.zeros(8)
+    b = mm.LogprobBuffers(2, 0, 1, 64, device="cpu")
+    for call in (lambda: mm.moe_quantize_rows(x, _codes(2), f[:2]), lambda: mm.quantize_rows(x),
+                 lambda: mm.moe_matmul_int8(mm.int8_config(_codes(2), w, out), _codes(2), f[:2], w, f, None, out),
+                 lambda: mm.moe_linear_int8(mm.int8_config(x, w, out), x, w, f, f, out, torch.zeros(512, dtype=torch.uint8), 512),
+                 lambda: mm.moe_token_logprobs(b.c[mm.MOE_FP32], x, None, None, b.entropy, b.conf, b.top_idx, b.top_logp, b.ws, 0)):
+        with pytest.raises(ValueError, match="device"):
+            call()
