@@ -577,10 +577,13 @@ def int8_config(x: torch.Tensor, w: torch.Tensor, out: torch.Tensor) -> moe_int8
 
 
 def quantize_rows(x: torch.Tensor, stream=None):
-    """-> (codes int8 [rows, K], a view of rows padded to 16 bytes; scales fp32 [rows]) of float rows [rows, K]."""
+    """-> (codes int8 [rows, K], a view of rows padded to 16 bytes; scales fp32 [rows]) of float rows [rows, K].  They belong to `stream`: what reads
+    them on another one has to be ordered behind it."""
     rows, K = x.shape
-    q = torch.empty((rows, (K + 15) // 16 * 16), dtype=torch.int8, device=x.device)
-    scale = torch.empty((rows,), dtype=torch.float32, device=x.device)
+    _on_one_gpu(x)
+    with torch.cuda.stream(_torch_stream(stream)):
+        q = torch.empty((rows, (K + 15) // 16 * 16), dtype=torch.int8, device=x.device)
+        scale = torch.empty((rows,), dtype=torch.float32, device=x.device)
     moe_quantize_rows(x, q, scale, stream)
     return q[:, :K], scale
 

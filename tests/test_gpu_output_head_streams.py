@@ -43,3 +43,22 @@ def test_a_graph_outlives_larger_calls_of_its_object(T, K):
         torch.cuda.synchronize()
         assert torch.equal(out, other(x))
         assert all((t == 7).all() for t in there) and all((t == 9).all() for t in here)
+
+
+def test_codes_made_on_another_stream_take_no_memory_of_this_one():
+    """A tensor that this stream still has to read, given back already: its memory is not what a side stream's codes are written to."""
+    rows, K = 64, 1024
+    x = torch.randn((rows, K), generator=_gen(0)).cuda()
+    want = mm.quantize_rows(x)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        last = [torch.full((rows * K,), 77, dtype=torch.int8, device="cuda") for _ in range(20)]
+        torch.cuda._sleep(20_000_000)
+        copies = [t.clone() for t in last]
+        del last
+        q, s = mm.quantize_rows(x, stream=side)
+        lin = mm.Int8Linear.quantize(x, stream=side)
+        torch.cuda.synchronize()
+        assert all((t == 77).all() for t in copies)
+        assert torch.equal(q, want[0]) and torch.equal(s, want[1]) and torch.equal(lin.w, q) and torch.equal(lin.w_scale, s)

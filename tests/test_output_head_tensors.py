@@ -90,3 +90,24 @@ def test_host_tensors_are_refused_by_every_call():
                  lambda: mm.moe_token_logprobs(b.c[mm.MOE_FP32], x, None, None, b.entropy, b.conf, b.top_idx, b.top_logp, b.ws, 0)):
         with pytest.raises(ValueError, match="device"):
             call()
+
+
+# ------------------------------------------------------------------------------------ streams
+def test_codes_are_allocated_on_the_stream_that_writes_them(monkeypatch):
+    """Memory of another stream may still be read there by earlier work."""
+    stack, places, empty = ["current"], [], torch.empty
+
+    @contextlib.contextmanager
+    def on(stream):
+        stack.append(stream)
+        yield
+        stack.pop()
+    monkeypatch.setattr(mm, "_on_one_gpu", lambda *tensors: None)
+    monkeypatch.setattr(mm, "_torch_stream", lambda stream: stream)
+    monkeypatch.setattr(torch.cuda, "stream", on)
+    monkeypatch.setattr(mm, "moe_quantize_rows", lambda x, q, scale, stream: places.append(stream))
+    monkeypatch.setattr(torch, "empty", lambda *a, **k: (places.append(stack[-1]), empty(*a, **k))[1])
+    for make in (lambda s: mm.quantize_rows(torch.zeros((3, 20)), s), lambda s: mm.Int8Linear.quantize(torch.zeros((3, 20)), stream=s)):
+        places.clear()
+        make("side")
+        assert places == ["side"] * 3
