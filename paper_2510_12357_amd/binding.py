@@ -615,7 +615,8 @@ class Int8Linear:
             assert t is None or (t.dtype == torch.float32 and tuple(t.shape) == (w.shape[0],) and t.is_contiguous()), f"{name}: [N] fp32"
         assert w.dtype == torch.int8 and all(t is None or t.device == w.device for t in (w_scale, bias)), "int8 codes, all on one device"
         self._w, self._w_scale, self._bias = w, w_scale, bias
-        self.ws = self.ws_stream = None
+        self.ws = None
+        self._streams = set()
         self._outgrown = []                                  # workspaces of smaller calls: captured graphs have their addresses
         self._calls = {}                                     # of each form of tokens and outputs: its description, workspace bytes
 
@@ -626,18 +627,23 @@ class Int8Linear:
         """From a float weight [N, K]."""
         return cls(*quantize_rows(weight, stream), bias)
 
-    def _workspace(self, need: int, stream, handle: int) -> int:
-        # memory belongs to the stream it was taken on: its reuse after the object's end waits for every stream that read it
+    def _workspace(self, need: int, stream) -> int:
         if self.ws is None or self.ws.numel() < need:
             if self.ws is not None:                          # twice as large at least: what is kept stays below the one in use
                 need = max(need, 2 * self.ws.numel())
                 self._outgrown.append(self.ws)
             with torch.cuda.stream(_torch_stream(stream)):
                 self.ws = torch.empty((need,), dtype=torch.uint8, device=self._w.device)
-            self.ws_stream = handle
-        elif handle != self.ws_stream:
-            self.ws.record_stream(_torch_stream(stream))
+            self._streams.clear()
         return self.ws.data_ptr()
+
+    def _used_on(self, stream, handle: int) -> None:
+        """Memory belongs to the stream it was taken on: its reuse after the object's end waits for every other one that was here."""
+        if handle not in self._streams:
+            for t in (self._w, self._w_scale, self._bias, self.ws):
+                if t is not None:
+                    t.record_stream(_torch_stream(stream))
+            self._streams.add(handle)
 
     def _call(self, x: torch.Tensor, out: torch.Tensor):
         """-> (description, workspace bytes) of a call with such tokens and outputs: the checks that their shapes, types and strides need."""
@@ -663,6 +669,9 @@ class Int8Linear:
         _, c, need = call
         s = _raw_stream(stream, key[3])
         bias = None if self._bias is None else self._bias.data_ptr()
+        ws = None if x.dtype is torch.int8 else self._workspace(need, stream)
+        if s not in self._streams:
+            self._used_on(stream, s)
         if x.dtype is torch.int8:
             assert x_scale is not None and x_scale.dtype is torch.float32 and x_scale.numel() == x.shape[0] and x_scale.is_contiguous(), \
                 "codes come with their scales, [T] fp32"
@@ -670,7 +679,6 @@ class Int8Linear:
                 raise ValueError(_DEVICES)
             rc = _lib.moe_matmul_int8(c, x.data_ptr(), x_scale.data_ptr(), self._w.data_ptr(), self._w_scale.data_ptr(), bias, out.data_ptr(), s)
         else:
-            ws = self._workspace(need, stream, s)
             rc = _lib.moe_linear_int8(c, x.data_ptr(), self._w.data_ptr(), self._w_scale.data_ptr(), bias, out.data_ptr(), ws, self.ws.numel(), s)
         if rc:
             _check(rc)
@@ -697,6 +705,14 @@ class LogprobBuffers:
                          torch.float32: (self.c[MOE_FP32], ctypes.byref(self.c[MOE_FP32]))}
         self.ws = torch.empty((need,), dtype=torch.uint8, device=device)
         self._device = self.ws.get_device()                  # -1: not a GPU's
+        self._streams = set()
+
+    def _used_on(self, stream, handle: int) -> None:
+        """Memory belongs to the stream it was taken on: its reuse after the object's end waits for every other one that was here."""
+        if handle not in self._streams:
+            for t in (self.token_logp, self.entropy, self.conf, self.top_idx, self.top_logp, self.ws):
+                t.record_stream(_torch_stream(stream))
+            self._streams.add(handle)
 
     def run(self, logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, stream=None) -> "LogprobBuffers":
         """logits [T, V] bf16 or fp32, tokens int32 [T, n_given]."""
@@ -718,9 +734,11 @@ class LogprobBuffers:
         c.ld = step
         if device < 0 or device != self._device or (given is not None and tokens.get_device() != device):
             raise ValueError(_DEVICES)
+        s = _raw_stream(stream, device)
+        if s not in self._streams:
+            self._used_on(stream, s)
         rc = _lib.moe_token_logprobs(ref, logits.data_ptr(), given, self.token_logp.data_ptr(), self.entropy.data_ptr(), self.conf.data_ptr(),
-                                     self.top_idx.data_ptr(), self.top_logp.data_ptr(), self.ws.data_ptr(), self.ws.numel(),
-                                     _raw_stream(stream, device))
+                                     self.top_idx.data_ptr(), self.top_logp.data_ptr(), self.ws.data_ptr(), self.ws.numel(), s)
         if rc:
             _check(rc)
         return self

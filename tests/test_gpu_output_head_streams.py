@@ -62,3 +62,46 @@ def test_codes_made_on_another_stream_take_no_memory_of_this_one():
         torch.cuda.synchronize()
         assert all((t == 77).all() for t in copies)
         assert torch.equal(q, want[0]) and torch.equal(s, want[1]) and torch.equal(lin.w, q) and torch.equal(lin.w_scale, s)
+
+
+@pytest.mark.parametrize("T, V", [(3, 131072), (300, 4000)])
+def test_buffers_given_back_while_another_stream_fills_them(T, V):
+    """Dropped right after the call, which still waits on its stream: tensors made meanwhile keep what is in them."""
+    z = (torch.randn((T, V), generator=_gen(0)) * 3).cuda()
+    tokens = torch.zeros((T, 2), dtype=torch.int32, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        b = mm.LogprobBuffers(T, 2, 20, V)
+        kinds = [(t.numel(), t.dtype) for t in (b.token_logp, b.entropy, b.conf, b.top_idx, b.top_logp, b.ws)]
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)
+        b.run(z, tokens, stream=side)
+        del b
+        made = [torch.full((n,), 55, dtype=dtype, device="cuda") for n, dtype in kinds for _ in range(4)]
+        torch.cuda.synchronize()
+        assert all((t == 55).all() for t in made)
+
+
+def test_weights_given_back_while_another_stream_reads_them():
+    """The same of a projection: its codes, scales, bias and workspace."""
+    N, K, T = 4000, 1000, 70
+    x = torch.randn((T, K), generator=_gen(1)).cuda()
+    weight, bias = torch.randn((N, K), generator=_gen(2)).cuda(), torch.randn((N,), generator=_gen(3)).cuda()
+    want = mm.Int8Linear.quantize(weight, bias)(x)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        lin = mm.Int8Linear.quantize(weight, bias.clone())
+        lin(x)                                               # the workspace belongs to this stream
+        kinds = [t.untyped_storage().nbytes() for t in (lin.w, lin.w_scale, lin.bias, lin.ws)]
+        out = torch.empty((T, N), device="cuda")
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)
+        lin(x, out=out, stream=side)
+        del lin
+        made = [torch.full((n,), 55, dtype=torch.uint8, device="cuda") for n in kinds for _ in range(4)]
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and all((t == 55).all() for t in made)

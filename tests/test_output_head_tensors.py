@@ -60,7 +60,7 @@ def test_a_workspace_lives_as_long_as_its_object(monkeypatch):
     lin = mm.Int8Linear(_codes(8), torch.ones(8))
     held, largest = [], 0
     for need in list(range(256, 40000, 256)) + [100, 5000, 10 ** 6, 512]:
-        address = lin._workspace(need, None, 7)
+        address = lin._workspace(need, None)
         largest = max(largest, need)
         assert lin.ws.data_ptr() == address and lin.ws.numel() >= need
         if not any(h() is lin.ws for h in held):
@@ -111,3 +111,28 @@ def test_codes_are_allocated_on_the_stream_that_writes_them(monkeypatch):
         places.clear()
         make("side")
         assert places == ["side"] * 3
+
+
+def test_logprob_buffers_are_known_to_every_stream_that_uses_them(monkeypatch):
+    """Once per stream: their memory must not be given away while that stream still works on it."""
+    b = mm.LogprobBuffers(3, 2, 4, 131072, device="cpu")
+    seen = []
+    monkeypatch.setattr(mm, "_torch_stream", lambda stream: stream)
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, stream: seen.append((t.data_ptr(), stream)))
+    for handle, stream in ((5, "a"), (5, "a"), (6, "b"), (5, "a")):
+        b._used_on(stream, handle)
+    tensors = {t.data_ptr() for t in (b.token_logp, b.entropy, b.conf, b.top_idx, b.top_logp, b.ws)}
+    assert len(tensors) == 6 and sorted(seen) == sorted((t, s) for t in tensors for s in ("a", "b"))
+
+
+def test_weights_and_workspace_are_known_to_every_stream_that_uses_them(monkeypatch):
+    lin, seen = mm.Int8Linear(_codes(8), torch.ones(8), torch.ones(8)), []
+    monkeypatch.setattr(mm, "_torch_stream", lambda stream: stream)
+    monkeypatch.setattr(torch.cuda, "stream", lambda stream: contextlib.nullcontext())
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, stream: seen.append((t.data_ptr(), stream)))
+    for need in (512, 4096):                                 # a larger workspace is another tensor
+        seen.clear()
+        tensors = {t.data_ptr() for t in (lin.w, lin.w_scale, lin.bias)} | {lin._workspace(need, "a")}
+        for handle, stream in ((5, "a"), (5, "a"), (6, "b"), (5, "a")):
+            lin._used_on(stream, handle)
+        assert sorted(seen) == sorted((t, s) for t in tensors for s in ("a", "b"))
