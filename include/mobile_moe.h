@@ -492,7 +492,8 @@ int moe_prefetcher_advance(moe_prefetcher_t* p, int32_t layer, int32_t distance,
  *
  * moe_quantize_rows   codes and scales of `rows` rows of K values; for weights once, for tokens that several
  *                     products read.
- *   x      device [rows, ldx] dtype (MOE_BF16 or MOE_FP32), ldx >= K elements from row to row; any alignment of elements
+ *   x      device [rows, ldx] dtype (MOE_BF16 or MOE_FP32), ldx >= K elements from row to row, below 2^22 as ldq; any
+ *          alignment of elements
  *   q      device [rows, ldq] int8, ldq >= K and a multiple of 16, 16-byte aligned; the columns K .. ldq get zeros
  *   scale  device [rows] fp32
  * moe_matmul_int8     x device [T, ldx] int8, x_scale device [T] fp32, w device [N, ldw] int8, w_scale device [N] fp32,
@@ -511,7 +512,8 @@ typedef struct moe_int8_config {
   int32_t x_dtype;   /* MOE_BF16 | MOE_FP32: tokens of moe_linear_int8 (moe_matmul_int8 ignores it) */
   int32_t out_dtype; /* MOE_BF16 | MOE_FP32                                                  */
   int32_t reserved;  /* 0                                                                    */
-  int64_t ldx, ldw, ldo; /* elements from row to row of x, w, out; below 2^22 each (0 = dense) */
+  int64_t ldx, ldw, ldo; /* elements from row to row of x, w, out (0 = dense); below 2^22 each, but for the float tokens
+                          * of moe_linear_int8, which may lie any distance apart (the last positions of a batch of prompts) */
 } moe_int8_config;
 #define MOE_INT8_MAX_K 131071
 int moe_quantize_rows(const void* x, int32_t dtype, int32_t rows, int32_t K, int64_t ldx, int8_t* q, int64_t ldq,
@@ -533,7 +535,8 @@ int moe_linear_int8(const moe_int8_config* cfg, const void* x, const int8_t* w, 
  * A row without a distribution (all entries -inf, a NaN or a +inf among them) gives NaN for every number but those
  * of padding ids; top_idx follows the order above all the same.
  * The sum beside the largest entry is kept apart from it, so that log p of a nearly certain token keeps its digits.
- * logits     device [T, ld] dtype (MOE_FP32 or MOE_BF16), ld >= V elements from row to row (0 = V), any alignment of elements
+ * logits     device [T, ld] dtype (MOE_FP32 or MOE_BF16), ld >= V elements from row to row (0 = V), below 2^22; any alignment
+ *            of elements
  * tokens     device [T, n_given] int32 (NULL if n_given == 0)        token_logp device [T, n_given] fp32
  * entropy, conf device [T] fp32, either may be NULL                  top_idx [T, n_top] int32, top_logp [T, n_top] fp32
  * ws         device scratch of moe_token_logprobs_workspace_bytes(cfg) bytes, 256-byte aligned (a size of 0: NULL will do)

@@ -497,8 +497,9 @@ def moe_prefetcher_advance(p: int, layer: int, distance: int, n_layers: int, str
 def moe_quantize_rows(x, q, scale, stream=None) -> None:
     """x: [rows, K] float rows; q: int8 [rows, ldq] whole rows, ldq >= K a multiple of 16; scale: [rows] fp32."""
     assert q.shape[0] == x.shape[0] and q.is_contiguous()
+    _ld(x), _on_one_gpu(x, q, scale)
+    x = _near_rows(x, stream)
     args = _rows(x), _float_type(x), x.shape[0], x.shape[1], _ld(x), _ptr(q), q.shape[1], _ptr(scale)
-    _on_one_gpu(x, q, scale)
     _check(load_library().moe_quantize_rows(*args, _stream(stream)))
 
 
@@ -548,17 +549,26 @@ def _on_one_gpu(*tensors: Optional[torch.Tensor]) -> None:
         raise ValueError(_DEVICES)
 
 
-def _ld(t: torch.Tensor) -> int:
-    # a single row has no next one: torch gives such a dimension any stride
-    if t.shape[0] <= 1:
-        return max(int(t.stride(0)), int(t.shape[1]))
-    if t.stride(0) < t.shape[1]:
-        raise ValueError(_SHARED_ROWS)
-    return int(t.stride(0))
-
-
 # an expanded tensor's rows are 0 elements apart, which to the C ABI means dense rows
 _SHARED_ROWS = "rows share memory: make them dense with contiguous()"
+_MAX_LD = 1 << 22                                            # distances of rows that most calls stay below
+
+
+def _ld(t: torch.Tensor) -> int:
+    step, n = int(t.stride(0)), int(t.shape[1])
+    if t.shape[0] <= 1:                                      # there is no next row: torch gives such a dimension any stride
+        return max(step, n) if step < _MAX_LD else (n + 15) // 16 * 16
+    if step < n:
+        raise ValueError(_SHARED_ROWS)
+    return step
+
+
+def _near_rows(t: torch.Tensor, stream) -> torch.Tensor:
+    """Rows that lie too far apart for a call (logits[:, -1] of a batch of prompts) as a dense copy, made on the stream that reads it."""
+    if t.shape[0] <= 1 or t.stride(0) < _MAX_LD:
+        return t
+    with torch.cuda.stream(_torch_stream(stream)):
+        return t.contiguous()
 
 
 def _float_type(t: torch.Tensor) -> int:
@@ -727,13 +737,15 @@ class LogprobBuffers:
             assert tokens.dtype is torch.int32 and tokens.shape == self.token_logp.shape and tokens.is_contiguous(), "tokens: int32 [T, n_given]"
             given = tokens.data_ptr()
         c, ref = self._configs[logits.dtype]
-        if step < V:
-            if T > 1:
-                raise ValueError(_SHARED_ROWS)
-            step = V                                         # a single row has no next one: torch gives such a dimension any stride
-        c.ld = step
+        if T <= 1:
+            step = V                                         # there is no next row: torch gives such a dimension any stride
+        elif step < V:
+            raise ValueError(_SHARED_ROWS)
         if device < 0 or device != self._device or (given is not None and tokens.get_device() != device):
             raise ValueError(_DEVICES)
+        if step >= _MAX_LD:
+            logits, step = _near_rows(logits, stream), V
+        c.ld = step
         s = _raw_stream(stream, device)
         if s not in self._streams:
             self._used_on(stream, s)

@@ -6,11 +6,12 @@ namespace mm {
 namespace {
 
 constexpr int64_t kMaxLd = 1 << 22;      // rows of a tile stay below 2 GiB, so that 32 bits address them
+constexpr int64_t kAnyLd = INT64_MAX;    // float tokens are read row by row, in 64 bits
 
-int check_ld(const char* what, int64_t ld, int64_t least, int64_t multiple) {
+int check_ld(const char* what, int64_t ld, int64_t least, int64_t multiple, int64_t most = kMaxLd) {
   if (ld < least) return fail(MOE_E_SHAPE, "%s = %lld is below the row length %lld", what, (long long)ld, (long long)least);
   if (ld % multiple) return fail(MOE_E_UNSUPPORTED, "%s = %lld must be a multiple of %lld", what, (long long)ld, (long long)multiple);
-  if (ld >= kMaxLd) return fail(MOE_E_UNSUPPORTED, "%s = %lld reaches %lld", what, (long long)ld, (long long)kMaxLd);
+  if (ld >= most) return fail(MOE_E_UNSUPPORTED, "%s = %lld reaches %lld", what, (long long)ld, (long long)most);
   return MOE_OK;
 }
 bool float_type(int dtype) { return dtype == MOE_BF16 || dtype == MOE_FP32; }
@@ -29,7 +30,7 @@ int resolve(const moe_int8_config* cfg, bool codes, moe_int8_config* c) {
   if (!c->ldx) c->ldx = c->K;
   if (!c->ldw) c->ldw = c->K;
   if (!c->ldo) c->ldo = c->N;
-  int rc = check_ld("ldx", c->ldx, c->K, codes ? 16 : 1);
+  int rc = check_ld("ldx", c->ldx, c->K, codes ? 16 : 1, codes ? kMaxLd : kAnyLd);
   if (!rc) rc = check_ld("ldw", c->ldw, c->K, 16);
   if (!rc) rc = check_ld("ldo", c->ldo, c->N, 1);
   return rc;

@@ -1,5 +1,6 @@
 """What the output head's Python calls refuse of tensors before anything is enqueued (no GPU needed: each refusal comes before the library)."""
 import contextlib
+import ctypes
 import os
 import weakref
 
@@ -136,3 +137,44 @@ def test_weights_and_workspace_are_known_to_every_stream_that_uses_them(monkeypa
         for handle, stream in ((5, "a"), (5, "a"), (6, "b"), (5, "a")):
             lin._used_on(stream, handle)
         assert sorted(seen) == sorted((t, s) for t in tensors for s in ("a", "b"))
+
+
+# ------------------------------------------------------------------------------------ rows far apart
+def _far(rows, n, step, dtype=torch.float32):
+    """Shape and strides of such rows, without their memory."""
+    return torch.empty_strided((rows, n), (step, 1), dtype=dtype, device="meta")
+
+
+@pytest.mark.parametrize("step", [1 << 22, 1024 * 4096 + 3, 1 << 33])
+def test_float_tokens_lie_as_far_apart_as_they_like(step):
+    """hidden[:, -1] of a batch of prompts: only rows of codes, weights and outputs have to be near each other."""
+    c = mm.int8_config(_far(4, 64, step), _codes(8), torch.zeros((4, 8)))
+    assert c.ldx == step and mm.moe_linear_int8_workspace_bytes(c) > 0
+    P = 1 << 20                                               # an address that passes the alignment checks and is never read
+    lib = mm.load_library()
+    assert lib.moe_linear_int8(ctypes.byref(c), P, P, P, None, P, None, 0, None) == -6      # MOE_E_WORKSPACE: all else is as it should be
+    assert lib.moe_matmul_int8(ctypes.byref(c), P, P, P, P, None, P, None) == -3            # MOE_E_UNSUPPORTED as codes
+
+
+@pytest.mark.parametrize("step", [1 << 22, 1 << 33])
+def test_one_row_has_no_next_one(step):
+    """The only row of a tensor whose strides are those of a larger one."""
+    c = mm.int8_config(_far(1, 60, step, torch.int8), _far(1, 60, step, torch.int8), _far(1, 1, step))
+    assert mm.load_library().moe_matmul_int8(ctypes.byref(c), None, None, None, None, None, None, None) == -1   # past the checks of distances
+    assert "x is NULL" in mm.moe_last_error()
+
+
+def test_rows_far_apart_are_made_dense_for_the_calls_that_need_it():
+    near = _far(4, 64, 4096)
+    assert mm._near_rows(near, None) is near and mm._near_rows(_far(1, 64, 1 << 30), None).shape == (1, 64)
+
+
+def test_dense_copies_of_rows_far_apart(monkeypatch):
+    streams = []
+    monkeypatch.setattr(mm, "_torch_stream", lambda stream: stream)
+    monkeypatch.setattr(torch.cuda, "stream", lambda stream: (streams.append(stream), contextlib.nullcontext())[1])
+    mem = torch.zeros((1 << 22) + 10)
+    mem[0], mem[1 << 22] = 1.0, 2.0
+    z = mem.as_strided((2, 10), (1 << 22, 1))
+    dense = mm._near_rows(z, "side")
+    assert torch.equal(dense, z) and dense.is_contiguous() and streams == ["side"]
