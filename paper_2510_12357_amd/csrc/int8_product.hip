@@ -1,5 +1,7 @@
 // Which kernel computes an 8-bit product.  All end with the same arithmetic on an exact sum (scaled in int8_device.h), so the choice does not
 // show in the result.
+#include <algorithm>
+
 #include "internal.h"
 
 namespace mm {
@@ -43,11 +45,20 @@ Route route(int T, int N, int K) {
 
 }  // namespace
 
-int launch_int8_product(const Int8Args& a, hipStream_t s) {
+int launch_int8_product(const Int8Args& all, hipStream_t s) {
   ProfScope ps(kProfInt8Product, s);
-  if (int8_streams(a.T, a.K)) return launch_int8_stream(a, s);
-  const Route r = route(a.T, a.N, a.K);
-  return r.blocks ? launch_int8_wide(a, r.blocks, s) : launch_int8_tile(a, r.tile, s);
+  if (int8_streams(all.T, all.K)) return launch_int8_stream(all, s);
+  int rc = MOE_OK;
+  for (int64_t t = 0; t < all.T && !rc; t += kLaunchRows) {
+    Int8Args a = all;
+    a.T = (int)std::min<int64_t>(all.T - t, kLaunchRows);
+    a.x += t * a.ldx;
+    a.x_scale += t;
+    a.out = static_cast<char*>(a.out) + t * a.ldo * (a.out_dtype == MOE_FP32 ? 4 : 2);
+    const Route r = route(a.T, a.N, a.K);
+    rc = r.blocks ? launch_int8_wide(a, r.blocks, s) : launch_int8_tile(a, r.tile, s);
+  }
+  return rc;
 }
 
 }  // namespace mm

@@ -3,6 +3,8 @@
 // A workgroup per row, which it holds in registers between the largest magnitude and the codes (up to 8192 values; what does not fit is read
 // twice), so that each value is read once.  What bounds it: the launch up to some hundred rows, then memory and, with bf16, the quotients: 4096 x 4096 fp32
 // 17.2 us (4.9 TB/s), bf16 14.1 (3.6 TB/s); 4096 x 8192 fp32 33.5 (with half of a row held 39.8); 64 x 4096 bf16 3.4.
+#include <algorithm>
+
 #include "internal.h"
 #include "route_device.h"
 #include "int8_device.h"
@@ -59,11 +61,18 @@ __global__ __launch_bounds__(THREADS) void quantize_kernel(const X* __restrict__
 template <typename X>
 int launch(const void* x, int rows, int K, int64_t ldx, int8_t* q, int64_t ldq, float* scale, int lane_blocks, hipStream_t s) {
   constexpr int kHeldByWave = 64 * held(64, sizeof(X)) * (16 / sizeof(X));
-  if (K <= kHeldByWave && !(sizeof(X) == 2 && K > 512 && rows <= 2048))
-    hipLaunchKernelGGL((quantize_kernel<X, 64>), dim3((unsigned)rows), dim3(64), 0, s, static_cast<const X*>(x), K, ldx, q, ldq, scale, lane_blocks);
-  else
-    hipLaunchKernelGGL((quantize_kernel<X, 256>), dim3((unsigned)rows), dim3(256), 0, s, static_cast<const X*>(x), K, ldx, q, ldq, scale, lane_blocks);
-  return hip_fail(hipGetLastError(), "quantize_kernel launch");
+  const bool one_wave = K <= kHeldByWave && !(sizeof(X) == 2 && K > 512 && rows <= 2048);
+  for (int64_t r = 0; r < rows; r += kLaunchRows) {        // more than one: rows of codes, for lane_blocks are of 64 tokens at most
+    const dim3 grid((unsigned)std::min<int64_t>(rows - r, kLaunchRows));
+    const X* xr = static_cast<const X*>(x) + r * ldx;
+    if (one_wave)
+      hipLaunchKernelGGL((quantize_kernel<X, 64>), grid, dim3(64), 0, s, xr, K, ldx, q + r * ldq, ldq, scale + r, lane_blocks);
+    else
+      hipLaunchKernelGGL((quantize_kernel<X, 256>), grid, dim3(256), 0, s, xr, K, ldx, q + r * ldq, ldq, scale + r, lane_blocks);
+    const int rc = hip_fail(hipGetLastError(), "quantize_kernel launch");
+    if (rc) return rc;
+  }
+  return MOE_OK;
 }
 
 }  // namespace

@@ -239,7 +239,7 @@ int launch_t(const Int8Args& a, hipStream_t s) {
     ready.store(1, std::memory_order_relaxed);
   }
   const int64_t mt = (a.T + 63) / 64, total = mt * ((a.N + 64 * NJ - 1) / (64 * NJ));
-  if (total >= (int64_t)1 << 30) return fail(MOE_E_UNSUPPORTED, "8-bit product: %lld tiles", (long long)total);
+  if (total >= (int64_t)1 << 23) return fail(MOE_E_UNSUPPORTED, "8-bit product: %lld tiles", (long long)total);   // of 2^32 threads in a grid
   hipLaunchKernelGGL((int8_tile_kernel<S, KG, NJ, ST>), dim3((unsigned)(((total + 7) / 8) * 8)), dim3(256 * KG), kLds, s, a, (int)mt, (int)total);
   return hip_fail(hipGetLastError(), "int8_tile_kernel launch");
 }

@@ -157,6 +157,8 @@ int launch_combine_add(const moe_config& c, const float* y, const float* w, cons
                        const int32_t* k_t, int j_lo, void* out, hipStream_t s);
 
 // ---- the output head: 8-bit product and log probabilities (head_api.hip resolves the dense leading dimensions) -----
+// Rows that one launch takes, further ones by further launches: a grid of 2^32 threads and more would run as what is left of it modulo 2^32.
+constexpr int kLaunchRows = 1 << 22;
 // Where the codes of a row go: one after the other (lane_blocks 0); or to the lane that needs them in a matrix instruction of 16 x 16 x 64, lane l the
 // 16 codes from 16 (l / 16) on of row l % 16, for each 64 k the blocks of 16 rows one after the other (lane_blocks: as many).
 int launch_quantize_rows(const void* x, int dtype, int rows, int K, int64_t ldx, int8_t* q, int64_t ldq, float* scale, int lane_blocks, hipStream_t s);

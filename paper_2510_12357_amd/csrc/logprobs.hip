@@ -19,6 +19,8 @@
 // streaming softmax, lists by counting for each candidate how many come before it.  Nothing depends on which wave is first.
 // Measured: 4096 rows of 131072 bf16 with 8 alternatives 180 - 191 us (5.6 - 6.0 TB/s; a plain read gets 6.9, and the vector unit issues 0.9 of the time),
 // 1999 of 50257 bf16 49 (4.1), 64 of 131072 fp32 with 20 alternatives 20.5 (15.2 with one), one row of 32000 fp32 8.0.
+#include <algorithm>
+
 #include "internal.h"
 #include "int8_device.h"
 #include "route_device.h"
@@ -523,7 +525,7 @@ Split split_of(int T, int V) {
 }
 
 template <typename S>
-int launch(const LogprobArgs& a, int T, int waves, hipStream_t s) {
+int launch_rows(const LogprobArgs& a, int T, int waves, hipStream_t s) {
   const dim3 grid((unsigned)T * (unsigned)a.parts);
   switch (waves) {
     case 1: hipLaunchKernelGGL((logprobs_kernel<S, 1>), grid, dim3(64), 0, s, a); break;
@@ -534,6 +536,24 @@ int launch(const LogprobArgs& a, int T, int waves, hipStream_t s) {
   if (rc || a.parts == 1) return rc;
   hipLaunchKernelGGL(logprobs_join_kernel<S>, dim3((unsigned)T), dim3((unsigned)(a.parts * 64)), 0, s, a);
   return hip_fail(hipGetLastError(), "logprobs_join_kernel launch");
+}
+template <typename S>
+int launch(const LogprobArgs& all, int T, int waves, hipStream_t s) {
+  int rc = MOE_OK;
+  for (int64_t t = 0; t < T && !rc; t += kLaunchRows) {     // more than one: a wave per row, no workspace
+    LogprobArgs a = all;
+    if (t) {
+      a.logits = static_cast<const S*>(a.logits) + t * a.ld;
+      a.tokens += t * a.n_given;                           // 0 where there is none
+      a.token_logp += t * a.n_given;
+      a.top_idx += t * a.n_top;
+      a.top_logp += t * a.n_top;
+      if (a.entropy) a.entropy += t;
+      if (a.conf) a.conf += t;
+    }
+    rc = launch_rows<S>(a, (int)std::min<int64_t>(T - t, kLaunchRows), waves, s);
+  }
+  return rc;
 }
 
 }  // namespace
