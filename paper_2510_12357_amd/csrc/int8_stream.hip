@@ -25,13 +25,11 @@ namespace {
 
 typedef __attribute__((address_space(3))) void lds_void;
 
-constexpr int kWavesS = 8, kThreadsS = kWavesS * 64;
-constexpr int kRing = 4, kRowBytes = 256, kStage = 16 * kRowBytes, kRingBytes = kWavesS * kRing * kStage;
+constexpr int kWavesS = kStreamWaves, kThreadsS = kWavesS * 64;
+constexpr int kRing = 4, kRowBytes = kStreamChunk, kStage = 16 * kRowBytes, kRingBytes = kWavesS * kRing * kStage;
 constexpr int kSteps = kRowBytes / 64;                     // matrix instructions (16 x 16 x 64) of a chunk
 constexpr int kMaxRows = 512;                              // weight rows of a workgroup: their scales and biases are kept in LDS
 constexpr int kScaleBytes = 2 * kMaxRows * 4;
-constexpr int max_chunks(int TB) { return 8 / TB; }        // chunks of a wave's part of K: 128 registers of codes
-constexpr int kMaxFused = 16384;                           // elements of float tokens that every workgroup quantises
 constexpr int code_pitch(int K) { return ((K + 15) / 16 | 1) * 16; }   // bytes of a token's codes in LDS: 16 tokens start at 16 different banks
 constexpr int code_bytes(int T, int K) { return T * code_pitch(K) + kRowBytes; }   // a chunk may reach behind the last token's
 constexpr int sum_bytes(int TB, int split) { return split > 1 ? 2 * (kWavesS / split) * TB * 1024 : 0; }
@@ -72,7 +70,7 @@ __device__ __forceinline__ void add_sum(unsigned at, i32x4 v) {
 template <typename S, Tokens FROM, typename X, int TB>
 __global__ __launch_bounds__(kThreadsS) __attribute__((amdgpu_waves_per_eu(2, 2))) void int8_stream_kernel(const Int8Args a, const FloatTokens f, const int split,
                                                                                                           const int turns) {
-  constexpr int kChunks = max_chunks(TB);
+  constexpr int kChunks = stream_chunks(TB);
   extern __shared__ __attribute__((aligned(1024))) char s_mem[];   // the rings, scales and biases, sums, codes of float tokens
   __shared__ unsigned s_max[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
@@ -252,7 +250,7 @@ Shape shape_of(int T, int N, int K) {
   const int tb = T <= 16 ? 1 : (T <= 32 ? 2 : 4);
   const int blocks = (N + 15) / 16, chunks = (K + kRowBytes - 1) / kRowBytes, cus = device_cu_count();
   int split = 1;
-  while (split * max_chunks(tb) < chunks) split *= 2;
+  while (split * stream_chunks(tb) < chunks) split *= 2;
   while (split < kWavesS && split < chunks && (int64_t)blocks * split < (int64_t)cus * kWavesS) split *= 2;
   if (tb == 4 && split == 2) split = 4;                    // the sums of four groups of 64 tokens have no room in LDS
   const int groups = kWavesS / split;
@@ -292,10 +290,8 @@ int launch_x(const Int8Args& a, const FloatTokens& f, hipStream_t s) {
 
 }  // namespace
 
-bool int8_streams(int T, int K) { return T <= 64 && (K + kRowBytes - 1) / kRowBytes <= kWavesS * max_chunks(T <= 16 ? 1 : (T <= 32 ? 2 : 4)); }
 int launch_int8_stream(const Int8Args& a, hipStream_t s) { return a.out_dtype == MOE_FP32 ? launch_s<float>(a, s) : launch_s<uint16_t>(a, s); }
 
-bool int8_quantises_itself(int T, int K) { return T <= 16 && (int64_t)T * K <= kMaxFused; }
 size_t int8_lane_codes_bytes(int T, int K) { return (size_t)((T + 15) / 16 * 16) * ((K + kRowBytes - 1) / kRowBytes * kRowBytes); }
 
 int launch_int8_stream_float(const Int8Args& a, const void* x, int x_dtype, int64_t ldx, hipStream_t s) {

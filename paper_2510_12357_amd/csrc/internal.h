@@ -6,6 +6,7 @@
 
 #include "mobile_moe.h"
 #include "ffn_route.h"
+#include "int8_route.h"
 
 namespace mm {
 
@@ -173,14 +174,10 @@ struct Int8Args {
 };
 int launch_int8_product(const Int8Args& a, hipStream_t s);
 int launch_int8_wide(const Int8Args& a, int blocks, hipStream_t s);                       // token tiles of 64 blocks rows, 2 to 4
-// tiles of 64 tokens x 64 or 128 weight rows; Shared: two groups of waves share K; Short: two stages
-enum class Int8Tile { k64Shared, k64, k64Short, k128Shared, k128 };
 int launch_int8_tile(const Int8Args& a, Int8Tile tile, hipStream_t s);
-bool int8_streams(int T, int K);           // whether launch_int8_stream takes these sizes
 int launch_int8_stream(const Int8Args& a, hipStream_t s);
 size_t int8_lane_codes_bytes(int T, int K);
 // the same on float tokens, quantised by every workgroup; where int8_quantises_itself says so
-bool int8_quantises_itself(int T, int K);
 int launch_int8_stream_float(const Int8Args& a, const void* x, int x_dtype, int64_t ldx, hipStream_t s);
 int launch_logprobs(const moe_logprobs_config& c, const void* logits, const int32_t* tokens, float* token_logp, float* entropy, float* conf,
                     int32_t* top_idx, float* top_logp, void* ws, hipStream_t s);
