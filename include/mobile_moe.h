@@ -535,6 +535,8 @@ int moe_linear_int8(const moe_int8_config* cfg, const void* x, const int8_t* w, 
  * A row without a distribution (all entries -inf, a NaN or a +inf among them) gives NaN for every number but those
  * of padding ids; top_idx follows the order above all the same.
  * The sum beside the largest entry is kept apart from it, so that log p of a nearly certain token keeps its digits.
+ * Sums are in fp32, in an order that goes by T, V, n_top and the row's address within 16 bytes: the same call has the same bits
+ * again, and the same row in another batch may differ in the last bits of its numbers (not in top_idx).
  * logits     device [T, ld] dtype (MOE_FP32 or MOE_BF16), ld >= V elements from row to row (0 = V), below 2^22; any alignment
  *            of elements
  * tokens     device [T, n_given] int32 (NULL if n_given == 0)        token_logp device [T, n_given] fp32

@@ -5,8 +5,10 @@
 //     R += e^d,    A += e^d d.
 // With m the row's largest entry, R and A of all entries but that one, and relative to m:
 //     log sum = log(1 + R),    entropy = log(1 + R) - A / (1 + R),    log p of z = (z - m) - log(1 + R).
-// The largest entry itself is in no sum, so log p of a nearly certain token, -log(1 + R), has all digits of R; entries that equal it add exactly
-// one each.
+// The largest entry itself is in no sum, so log p of a nearly certain token, -log(1 + R), has all digits of R.  Entries that equal a wave's
+// reference add exactly one each.  Entries that come later may lie up to kLead above it before it moves: each adds e^d with an error of 3 d 2^-24,
+// and the sum is brought to m by e^(ref - m) with as much again, 120 2^-24 at most; A is then a difference, A + (ref - m) R, with that error of
+// either.  (A row that is constant but for lower first batches; ordinary rows have their largest entry at most a few units above the reference.)
 //
 // A batch of a wave (kPerLane entries per lane) is compared with the list's last entry by one maximum per lane and one ballot, on the
 // differences d, which follow the order of the entries.  Only where one is not below it, entries go to the list, and what the list
@@ -14,7 +16,7 @@
 // which wait in registers; about n (1 + log(V / seen)) entries of a row are above what is known when they come.  So the ordinary
 // batch costs a difference, a product, an exponential and three and a half further operations per entry, and nothing crosses the
 // lanes.  (One multiply-add in place of the difference and the product, on z log2 e - ref log2 e, is no faster, 182 us for 4096 rows of
-// 131072 in bf16 either way, and equal entries then add what the rounded ref log2 e makes of them.)
+// 131072 in bf16 either way, and entries that equal the reference then add what the rounded ref log2 e makes of them.)
 // Waves of a row (and workgroups, where rows are few) take batches in turn and are joined at the end: sums by the rule of a
 // streaming softmax, lists by counting for each candidate how many come before it.  Nothing depends on which wave is first.
 // Measured: 4096 rows of 131072 bf16 with 8 alternatives 180 - 191 us (5.6 - 6.0 TB/s; a plain read gets 6.9, and the vector unit issues 0.9 of the time),
