@@ -1,8 +1,9 @@
 // Rows of floats -> 8-bit codes and one scale per row (moe_quantize_rows).
 //
 // A workgroup per row, which it holds in registers between the largest magnitude and the codes (up to 8192 values; what does not fit is read
-// twice), so that each value is read once.  What bounds it: the launch up to some hundred rows, then memory and, with bf16, the quotients: 4096 x 4096 fp32
-// 17.2 us (4.9 TB/s), bf16 14.1 (3.6 TB/s); 4096 x 8192 fp32 33.5 (with half of a row held 39.8); 64 x 4096 bf16 3.4.
+// twice), so that each value is read once.  What bounds it: the launch up to some hundred rows, then memory and the vector unit, which quotients and codes
+// take 19 instructions an element, 20 thousand cycles a SIMD for 4096 x 4096 of either type, 0.76 of its busy cycles with bf16 and 0.60 with fp32 (counters).
+// 4096 x 4096 fp32 17.2 us (4.9 TB/s), bf16 14.1 (3.6 TB/s); 4096 x 8192 fp32 33.5 (with half of a row held 39.8); 64 x 4096 bf16 3.4.
 #include <algorithm>
 
 #include "internal.h"

@@ -9,6 +9,11 @@ namespace mm {
 
 bool int8_streams(int T, int K) { return T <= 64 && (K + kStreamChunk - 1) / kStreamChunk <= kStreamWaves * stream_chunks(T <= 16 ? 1 : (T <= 32 ? 2 : 4)); }
 
+// Wherever their codes fit beside the rings: a launch in front of the product costs a caller 3.7 us (eager, from Python), and the GPU, in a graph, us inside / in a
+// launch of its own on 2048 | 32000 outputs: bf16 1 x 2048 5.5 / 6.5 | 14.5 / 16.3, 1 x 16384 12.1 / 18.4 | 84 / 90, 4 x 4096 7.4 / 8.1 | 25.5 / 27.0, 8 x 2048 6.7 / 7.0 |
+// 16.1 / 16.6, 16 x 1024 6.7 / 6.9 | 11.6 / 12.1; fp32 1 x 16384 13.7 / 20.3 | 87 / 93, 2 x 8192 10.7 / 11.8 | 46.8 / 48.4, 8 x 1024 6.3 / 6.9 | 10.7 / 11.6, 16 x 512 6.2 / 6.5 |
+// 8.8 / 9.1.  The other way round where more than two rows are longer than their threads hold, and so are read twice: fp32 4 x 4096 8.8 / 8.4 | 27.6 / 27.4,
+// 8 x 2048 8.0 / 7.3 | 17.9 / 16.7, 16 x 1024 8.0 / 6.9 | 13.2 / 12.0, bf16 12 x 1344 7.8 / 6.7 | 15.2 / 14.5, 9 x 1792 8.2 / 6.8 | 16.7 / 15.4.
 bool int8_quantises_itself(int T, int K) { return T <= 16 && (int64_t)T * K <= kMaxFused; }
 
 // Up to 64 tokens (whose codes fit the registers of a workgroup) stream the weights: int8_stream.hip.  Beyond, tiles of 64 tokens x 64 or 128 weight

@@ -8,7 +8,7 @@ namespace mm {
 constexpr int kStreamWaves = 8;                            // of a workgroup
 constexpr int kStreamChunk = 256;                          // k of a chunk
 constexpr int stream_chunks(int TB) { return 8 / TB; }     // chunks of a wave's part of K with TB blocks of 16 tokens: 128 registers of codes
-constexpr int kMaxFused = 16384;                           // elements of float tokens that every workgroup quantises
+constexpr int kMaxFused = 16384;                           // elements of float tokens that every workgroup quantises: codes of more have no room in LDS
 bool int8_streams(int T, int K);
 // whether moe_linear_int8 leaves the quantisation to the product's workgroups
 bool int8_quantises_itself(int T, int K);

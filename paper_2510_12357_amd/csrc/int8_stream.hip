@@ -10,8 +10,8 @@
 // Measured: 64 x 131072 x 4096 102 us (5.5 TB/s of weights and outputs), 16 x 131072 x 4096 91 (5.9), 8 x 131072 x 16384 332 (6.5), 1 x 32000 x 2048 with its
 // quantisation 13.4 (4.9), 8 x 2048 x 2048 6.5; a plain read gets 6.9.
 // Where the codes come from: the caller's rows; the workspace of moe_linear_int8, in the order of the matrix instruction's lanes, so that a load is
-// 1 KB in one piece; or float tokens that every workgroup quantises for itself, up to a size where that costs less than a launch in
-// front of this one.
+// 1 KB in one piece; or float tokens that every workgroup quantises for itself, which saves a launch in front of this one
+// (both ways measured: int8_route.cpp).
 #include <atomic>
 #include <type_traits>
 
