@@ -7,11 +7,11 @@ from test_gpu_output_head import BF16, FP32, _bound, _gen, _operands, _product, 
 
 pytestmark = pytest.mark.gpu
 
-# tiles of 256 x 256: heights 32 to 256, several tiles per workgroup, last tiles of one row and one column, K below, at and behind the
-# vector, the chunk and the ring
+# large outputs: last tiles of one row and one column, K below, at and behind the vector, the chunk and the ring.  Most of these sizes run on tiles of
+# 64 x 64 in two stages, four on those of 128, 192 or 256 x 256, which test_gpu_int8_routes.py has by kernel
 WIDE = [(65, 33000, 77), (97, 32800, 16), (128, 33025, 400), (129, 32769, 33), (192, 33000, 129), (193, 32770, 1000), (256, 33000, 7), (257, 16640, 128),
         (300, 20000, 1000), (513, 11009, 640), (700, 12000, 15), (2049, 20001, 200), (1100, 16384, 2000), (640, 9000, 385)]
-# tiles of 64 and 128 tokens x 128 weight rows
+# few outputs or tokens: tiles of 64 x 64
 TILE = [(65, 128, 128), (65, 1, 1), (127, 129, 255), (128, 1000, 2048), (130, 127, 384), (191, 640, 100), (333, 2000, 1111), (700, 2048, 512), (1000, 130, 4097),
         (4096, 129, 64)]
 # up to 64 tokens: 1 to 4 blocks of 16, K split over waves or not, the last step whole, in part and alone
