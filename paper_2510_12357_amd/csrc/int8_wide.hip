@@ -1,5 +1,5 @@
 // The 8-bit product on tiles of up to 256 tokens x 256 weight rows, for many tokens.  4096 x 131072 x 4096 1745 - 1870 us (2.35 - 2.5 POP/s, by the card),
-// 4096 x 14336 x 4096 201 - 215 (3.5 rounds of tiles, which take four), 333 x 50257 x 1971 61.
+// 4096 x 14336 x 4096 201 - 215 (3.5 rounds of tiles, which take four), 333 x 50257 x 1971 61 - 65.
 //
 // What bounds it: the matrix cores (random codes draw so much power that the matrix instructions alone reach 3.3 of their 4.9 POP/s; LDS reads take a
 // seventh of the cycles by the counters).  Four waves of 128 x 128 outputs, one per SIMD, so that nothing hides a stall:
