@@ -496,7 +496,10 @@ def moe_prefetcher_advance(p: int, layer: int, distance: int, n_layers: int, str
 
 def moe_quantize_rows(x, q, scale, stream=None) -> None:
     """x: [rows, K] float rows; q: int8 [rows, ldq] whole rows, ldq >= K a multiple of 16; scale: [rows] fp32."""
-    assert q.shape[0] == x.shape[0] and q.is_contiguous()
+    if q.dim() != 2 or q.shape[0] != x.shape[0] or q.dtype != torch.int8 or not q.is_contiguous():
+        raise ValueError("codes: int8 [rows, ldq], dense")
+    if scale.dtype != torch.float32 or scale.numel() != x.shape[0]:
+        raise ValueError("scales: fp32 [rows]")
     _ld(x), _on_one_gpu(x, q, scale)
     x = _near_rows(x, stream)
     args = _rows(x), _float_type(x), x.shape[0], x.shape[1], _ld(x), _ptr(q), q.shape[1], _ptr(scale)

@@ -178,3 +178,15 @@ def test_dense_copies_of_rows_far_apart(monkeypatch):
     z = mem.as_strided((2, 10), (1 << 22, 1))
     dense = mm._near_rows(z, "side")
     assert torch.equal(dense, z) and dense.is_contiguous() and streams == ["side"]
+
+
+# ------------------------------------------------------------------------------------ codes and scales of other forms
+@pytest.mark.parametrize("q, scale", [(torch.zeros((4, 64)), torch.zeros(4)), (torch.zeros((4, 64), dtype=torch.int8), torch.zeros(3)),
+                                      (torch.zeros((4, 64), dtype=torch.int8), torch.zeros(4, dtype=torch.bfloat16)),
+                                      (torch.zeros((4, 64), dtype=torch.int8), torch.zeros(4, dtype=torch.float64)),
+                                      (torch.zeros(4 * 64, dtype=torch.int8).reshape(4, 8, 8), torch.zeros(4)),
+                                      (torch.zeros((3, 64), dtype=torch.int8), torch.zeros(4))])
+def test_codes_and_scales_have_a_place_each(q, scale):
+    """The kernel writes a scale of fp32 per row and rows of q.shape[1] codes, whatever stands there."""
+    with pytest.raises(ValueError, match="codes|scales"):
+        mm.moe_quantize_rows(torch.zeros((4, 60)), q, scale)
