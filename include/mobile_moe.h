@@ -557,6 +557,89 @@ int moe_token_logprobs(const moe_logprobs_config* cfg, const void* logits, const
                        float* entropy, float* conf, int32_t* top_idx, float* top_logp, void* ws, size_t ws_bytes,
                        void* stream);
 
+/* ------------------------------------------------------------------------------------------
+ * The attention step of a decoder around the layer (not in the paper, which only notes that the big pass of a rejected token shares the
+ * little pass's key-value cache: it writes the same position again).  A step of generation is, per layer, one moe_kv_append (queries turned,
+ * keys turned and stored, values stored) and one moe_paged_attention.
+ *
+ * Rotary positions: the first `rotary_dim` channels of a head are pairs (a, b), the channels (i, i + rotary_dim / 2) with MOE_ROPE_HALF, (2i, 2i + 1)
+ * with MOE_ROPE_INTERLEAVED, i < rotary_dim / 2, and
+ *     a' = m (a cos t - b sin t),   b' = m (b cos t + a sin t),   t = pos * freq[i],
+ * the other channels stay.  `freq` is in radians per position, so that any scaling for long contexts is a list of frequencies and a factor m
+ * (mscale).  The angle is taken in 64 bits, so that far positions lose nothing; sine, cosine and the rotation are in fp32, rounded once to the output
+ * type.  inverse != 0 turns back (by -t), which is also the rotation of gradients.
+ *
+ * The cache of one layer: pages of page_size positions, rows of D channels per key head and position, keys and values alike.  dtype MOE_BF16, MOE_FP32,
+ * or MOE_E4M3: rows of OCP E4M3 codes with one fp32 scale per row; scale = max |x| / 448 and the code nearest (ties to even) to 448 x / max |x|, in
+ * fp32; a row of zeros has scale 0, a row with a NaN or an infinity has scale NaN and codes 0.
+ * Position p of sequence s is in page table[s][p / page_size]; sequences may share pages that no call writes.
+ *
+ * moe_rope      x -> out, [T, heads, D] of cfg.dtype; they may be the same memory (and else must not overlap).
+ *   pos device [T] int32; freq device [rotary_dim / 2] fp64
+ * moe_kv_append k, v [T, cache.heads, D] and q [T, heads, D] of cfg.dtype; q -> q_out as moe_rope does (heads == 0: neither is used; q_out may be q).
+ *   k turned and v go to position pos[t] of sequence seq[t] (seq NULL: sequence t).  A position below 0 is padding: nothing of k and v is stored, and
+ *   its q is turned all the same.  A token whose sequence is outside [0, n_seqs), whose position lies behind its table row or whose page number is outside [0, n_pages) is
+ *   not stored either.  rotary_dim == 0 turns nothing (freq may be NULL).  Two tokens of a call must not have the same position of the same page.
+ * moe_paged_attention   one new token per sequence: of the positions j, max(0, length - window) <= j < length (window 0: all), with
+ *     s_j = scale q . k_j, with softcap > 0 instead softcap tanh(scale q . k_j / softcap):
+ *     out = sum_j exp(s_j) v_j / sum_j exp(s_j),   lse = log sum_j exp(s_j).
+ *   Query heads h use key head h / (heads / cache.heads).  q, out [B, heads, D] of cfg.dtype; lse device [B, heads] fp32 or NULL; table device
+ *   [B, table_ld] int32, of which table_len count; lengths device [B] int32.  Length 0, or scores that are all -inf: zeros, lse -inf.  max_len bounds the lengths (it sizes the
+ *   grid): a sequence whose length is negative, above max_len or behind its table row, or that sees a page outside [0, n_pages), has NaN everywhere.  Nothing
+ *   of the cache behind the length or before the window is used, whatever it holds.  A NaN or an infinity in a key or value that is seen gives NaN.
+ *   Scores, softmax and sums are in fp32; the same call has the same bits again.
+ *   ws: device scratch of moe_paged_attention_workspace_bytes(cfg, cache) bytes, 256-byte aligned (a size of 0: NULL will do).
+ *
+ * Strides are in elements, 0 = dense; the last dimension is dense always, and heads and tokens do not overlap.  1 <= D <= 256; D and rotary_dim even; D a multiple of 16 in
+ * a cache, whose memory is 16-byte aligned with strides of whole 16 bytes (scales: [n_pages, heads, page_size] dense).  page_size: a power of two from 4 to 2^20.
+ * Other tensors have any alignment of elements.  T, B == 0 are legal: nothing is enqueued. */
+#define MOE_E4M3 4
+#define MOE_ROPE_HALF 0
+#define MOE_ROPE_INTERLEAVED 1
+#define MOE_MAX_HEAD_DIM 256
+typedef struct moe_rope_config {
+  int32_t T, heads, D, rotary_dim;
+  int32_t dtype;     /* MOE_BF16 | MOE_FP32 */
+  int32_t layout;    /* MOE_ROPE_HALF | MOE_ROPE_INTERLEAVED */
+  int32_t inverse;   /* 0 | 1 */
+  float mscale;
+  int64_t x_token, x_head, out_token, out_head;
+} moe_rope_config;
+int moe_rope(const moe_rope_config* cfg, const void* x, const int32_t* pos, const double* freq, void* out, void* stream);
+
+typedef struct moe_kv_cache {
+  int32_t n_pages, page_size, heads, D;
+  int32_t dtype;     /* MOE_BF16 | MOE_FP32 | MOE_E4M3 */
+  int32_t reserved;  /* 0 */
+  int64_t page, head, row;      /* strides from page to page, head to head, position to position of k and v; dense: pages of [heads, page_size, D] */
+  void* k; void* v;
+  float* k_scale; float* v_scale; /* MOE_E4M3, else not used */
+} moe_kv_cache;
+typedef struct moe_append_config {
+  int32_t T, heads, rotary_dim;
+  int32_t dtype;     /* MOE_BF16 | MOE_FP32, of q, k and v */
+  int32_t layout;
+  int32_t n_seqs;    /* rows of the table */
+  int32_t table_len; /* entries of a table row */
+  float mscale;
+  int64_t table_ld;  /* elements from table row to table row (0 = table_len) */
+  int64_t q_token, q_head, k_token, k_head, v_token, v_head, out_token, out_head;
+} moe_append_config;
+int moe_kv_append(const moe_append_config* cfg, const moe_kv_cache* cache, const void* q, const void* k, const void* v, const int32_t* pos,
+                  const int32_t* seq, const int32_t* table, const double* freq, void* q_out, void* stream);
+
+typedef struct moe_attention_config {
+  int32_t B, heads;
+  int32_t dtype;     /* MOE_BF16 | MOE_FP32, of q and out */
+  int32_t max_len, window, table_len;
+  float scale, softcap;
+  int64_t table_ld;
+  int64_t q_token, q_head, out_token, out_head;
+} moe_attention_config;
+size_t moe_paged_attention_workspace_bytes(const moe_attention_config* cfg, const moe_kv_cache* cache); /* 0 on a bad config too */
+int moe_paged_attention(const moe_attention_config* cfg, const moe_kv_cache* cache, const void* q, const int32_t* table, const int32_t* lengths,
+                        void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -8,6 +8,7 @@ there is no fallback: if the HIP library is missing, loading fails with an error
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from typing import Optional, Sequence
 
@@ -22,6 +23,9 @@ MOE_BF16, MOE_FP32, MOE_BF16_W8, MOE_BF16_MXFP4 = 0, 1, 2, 3
 MOE_FETCH_DEMAND, MOE_FETCH_PREFETCH = 0, 1
 MOE_MAX_SHARED = 4
 MOE_INT8_MAX_K, MOE_MAX_ALTERNATIVES, MOE_MAX_GIVEN = 131071, 32, 64
+MOE_E4M3 = 4
+MOE_ROPE_HALF, MOE_ROPE_INTERLEAVED = 0, 1
+MOE_MAX_HEAD_DIM = 256
 MOE_OK = 0
 ERRORS = {-1: "MOE_E_BADARG", -2: "MOE_E_SHAPE", -3: "MOE_E_UNSUPPORTED", -4: "MOE_E_HIP",
           -5: "MOE_E_CACHE_FULL", -6: "MOE_E_WORKSPACE"}
@@ -36,7 +40,8 @@ EXPORTS = ("moe_last_error", "moe_device_info", "moe_profile_enable", "moe_profi
            "moe_cache_set_prefetch_limit", "moe_cache_emulate_link", "moe_prefetcher_create", "moe_prefetcher_destroy",
            "moe_prefetcher_set_in_flight_limit", "moe_prefetcher_set_yield_to_demand", "moe_prefetcher_predict", "moe_prefetcher_predicted",
            "moe_prefetcher_advance", "moe_quantize_rows", "moe_matmul_int8", "moe_linear_int8_workspace_bytes", "moe_linear_int8",
-           "moe_token_logprobs_workspace_bytes", "moe_token_logprobs")
+           "moe_token_logprobs_workspace_bytes", "moe_token_logprobs", "moe_rope", "moe_kv_append",
+           "moe_paged_attention_workspace_bytes", "moe_paged_attention")
 
 
 class MoeError(RuntimeError):
@@ -66,6 +71,26 @@ class moe_int8_config(ctypes.Structure):
 
 class moe_logprobs_config(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("T", "V", "dtype", "n_given", "n_top", "reserved")] + [("ld", ctypes.c_int64)]
+
+
+class moe_rope_config(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("T", "heads", "D", "rotary_dim", "dtype", "layout", "inverse")] + [("mscale", ctypes.c_float)] + [
+        (n, ctypes.c_int64) for n in ("x_token", "x_head", "out_token", "out_head")]
+
+
+class moe_kv_cache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_pages", "page_size", "heads", "D", "dtype", "reserved")] + [
+        (n, ctypes.c_int64) for n in ("page", "head", "row")] + [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale")]
+
+
+class moe_append_config(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("T", "heads", "rotary_dim", "dtype", "layout", "n_seqs", "table_len")] + [("mscale", ctypes.c_float)] + [
+        (n, ctypes.c_int64) for n in ("table_ld", "q_token", "q_head", "k_token", "k_head", "v_token", "v_head", "out_token", "out_head")]
+
+
+class moe_attention_config(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "heads", "dtype", "max_len", "window", "table_len")] + [
+        ("scale", ctypes.c_float), ("softcap", ctypes.c_float)] + [(n, ctypes.c_int64) for n in ("table_ld", "q_token", "q_head", "out_token", "out_head")]
 
 
 class moe_fetch_stats(ctypes.Structure):
@@ -174,7 +199,13 @@ def load_library() -> ctypes.CDLL:
     lib.moe_token_logprobs_workspace_bytes.argtypes = [ctypes.POINTER(moe_logprobs_config)]
     lib.moe_token_logprobs_workspace_bytes.restype = sz
     lib.moe_token_logprobs.argtypes = [ctypes.POINTER(moe_logprobs_config)] + [vp] * 8 + [sz, vp]
-    for name in ("moe_quantize_rows", "moe_matmul_int8", "moe_linear_int8", "moe_token_logprobs"):
+    kvp = ctypes.POINTER(moe_kv_cache)
+    lib.moe_rope.argtypes = [ctypes.POINTER(moe_rope_config)] + [vp] * 5
+    lib.moe_kv_append.argtypes = [ctypes.POINTER(moe_append_config), kvp] + [vp] * 9
+    lib.moe_paged_attention_workspace_bytes.argtypes = [ctypes.POINTER(moe_attention_config), kvp]
+    lib.moe_paged_attention_workspace_bytes.restype = sz
+    lib.moe_paged_attention.argtypes = [ctypes.POINTER(moe_attention_config), kvp] + [vp] * 6 + [sz, vp]
+    for name in ("moe_quantize_rows", "moe_matmul_int8", "moe_linear_int8", "moe_token_logprobs", "moe_rope", "moe_kv_append", "moe_paged_attention"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -533,7 +564,36 @@ def moe_token_logprobs(cfg: moe_logprobs_config, logits, tokens, token_logp, ent
                                              _ptr(top_idx), _ptr(top_logp), _ptr(ws), ws_bytes, _stream(stream)))
 
 
+def moe_rope(cfg: moe_rope_config, x, pos, freq, out, stream=None) -> None:
+    _on_one_gpu(x, pos, freq, out)
+    _check(load_library().moe_rope(ctypes.byref(cfg), _heads_ptr(x), _ptr(pos), _ptr(freq), _heads_ptr(out), _stream(stream)))
+
+
+def moe_kv_append(cfg: moe_append_config, cache: moe_kv_cache, q, k, v, pos, seq, table, freq, q_out, stream=None) -> None:
+    _on_one_gpu(q, k, v, pos, seq, table, freq, q_out)
+    _check(load_library().moe_kv_append(ctypes.byref(cfg), ctypes.byref(cache), _heads_ptr(q), _heads_ptr(k), _heads_ptr(v), _ptr(pos), _ptr(seq),
+                                        _rows(table), _ptr(freq), _heads_ptr(q_out), _stream(stream)))
+
+
+def moe_paged_attention_workspace_bytes(cfg: moe_attention_config, cache: moe_kv_cache) -> int:
+    return int(load_library().moe_paged_attention_workspace_bytes(ctypes.byref(cfg), ctypes.byref(cache)))
+
+
+def moe_paged_attention(cfg: moe_attention_config, cache: moe_kv_cache, q, table, lengths, out, lse, ws, ws_bytes: int, stream=None) -> None:
+    _on_one_gpu(q, table, lengths, out, lse, ws)
+    _check(load_library().moe_paged_attention(ctypes.byref(cfg), ctypes.byref(cache), _heads_ptr(q), _rows(table), _ptr(lengths), _heads_ptr(out),
+                                              _ptr(lse), _ptr(ws), ws_bytes, _stream(stream)))
+
+
 # ------------------------------------------------------------------------------ plumbing helpers
+def _heads_ptr(t: Optional[torch.Tensor]):
+    """Address of [tokens, heads, channels] whose channels are dense."""
+    if t is None:
+        return None
+    assert t.dim() == 3 and (t.shape[2] <= 1 or t.stride(2) == 1), "channels passed to the C ABI must be dense"
+    return ctypes.c_void_p(t.data_ptr())
+
+
 def _rows(t: Optional[torch.Tensor]):
     """Address of a matrix whose rows are dense and may lie apart."""
     if t is None:
@@ -757,6 +817,322 @@ class LogprobBuffers:
         if rc:
             _check(rc)
         return self
+
+
+# ------------------------------------------------------------------------------ the attention step
+def _strides(t: torch.Tensor, what: str):
+    """Strides of [tokens, heads, channels] as the C ABI takes them: 0 (dense) where there is no next one, whose stride torch leaves open."""
+    if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError(f"{what}: [tokens, heads, channels] with dense channels")
+    token, head = (0 if n <= 1 else s for n, s in zip(t.shape[:2], t.stride()[:2]))
+    if (t.shape[0] > 1 and token == 0) or (t.shape[1] > 1 and head == 0):
+        raise ValueError(f"{what}: {_SHARED_ROWS}")
+    return token, head
+
+
+def _integers(t: torch.Tensor, what: str, shape) -> None:
+    if t.dtype is not torch.int32 or t.dim() != len(shape) or any(n >= 0 and n != m for n, m in zip(shape, t.shape)):
+        raise ValueError(f"{what}: int32 {[('any' if n < 0 else n) for n in shape]}")
+    if (not t.is_contiguous()) if len(shape) == 1 else (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what}: dense rows")
+
+
+def _table_ld(table: torch.Tensor) -> int:
+    if table.shape[0] <= 1:
+        return 0
+    if table.stride(0) < table.shape[1]:
+        raise ValueError(f"table: {_SHARED_ROWS}")
+    return table.stride(0)
+
+
+class _Owner:
+    """Of device memory: its reuse after the object's end waits for every stream that used it."""
+
+    def __init__(self):
+        self._streams = set()
+
+    def _memory(self):
+        return ()
+
+    def _used_on(self, stream, handle: int) -> None:
+        if handle not in self._streams:
+            for t in self._memory():
+                if t is not None:
+                    t.record_stream(_torch_stream(stream))
+            self._streams.add(handle)
+
+
+def _call_on(device: int, function, *args) -> None:
+    """A C call with the tensors' device as the current one."""
+    if torch.cuda.current_device() == device:
+        rc = function(*args)
+    else:
+        with torch.cuda.device(device):
+            rc = function(*args)
+    if rc:
+        _check(rc)
+
+
+class Rotary(_Owner):
+    """Rotary positions: freq is fp64 [rotary_dim / 2] on the GPU, radians per position of each pair of channels; layout "half" (pairs i, i + rotary_dim / 2)
+    or "interleaved" (pairs 2i, 2i + 1); mscale multiplies what is turned."""
+
+    LAYOUTS = {"half": MOE_ROPE_HALF, "interleaved": MOE_ROPE_INTERLEAVED}
+
+    def __init__(self, freq: torch.Tensor, layout: str = "half", mscale: float = 1.0):
+        super().__init__()
+        load_library()
+        if freq.dtype != torch.float64 or freq.dim() != 1 or not freq.is_contiguous() or freq.numel() == 0:
+            raise ValueError("freq: fp64 [rotary_dim / 2], dense")
+        if layout not in self.LAYOUTS:
+            raise ValueError(f"layout {layout!r}: one of {sorted(self.LAYOUTS)}")
+        _on_one_gpu(freq)
+        self._freq, self.layout, self.mscale = freq, layout, float(mscale)
+        self.rotary_dim = 2 * freq.numel()
+        self._key = (self.rotary_dim, self.LAYOUTS[layout], self.mscale)
+        self._calls = {}
+
+    freq = property(lambda self: self._freq)
+
+    @classmethod
+    def scaled(cls, rotary_dim: int, base: float = 10000.0, layout: str = "half", factor: float = 1.0, trained: int = 0, slow: float = 1.0,
+               fast: float = 32.0, mscale: float = 1.0, device="cuda") -> "Rotary":
+        """Frequencies base^(-2i / rotary_dim), slowed for contexts `factor` times as long: all of them, or with `trained` positions those that turn at
+        most `slow` times over them, those between `slow` and `fast` in proportion, faster ones not."""
+        if rotary_dim < 2 or rotary_dim % 2 or not factor > 0 or trained < 0 or not fast > slow:
+            raise ValueError(f"rotary_dim={rotary_dim} factor={factor} trained={trained} slow={slow} fast={fast}")
+        freq = []
+        for i in range(rotary_dim // 2):
+            f = base ** (-2.0 * i / rotary_dim)
+            keep = 0.0 if not trained else min(1.0, max(0.0, (trained * f / (2.0 * math.pi) - slow) / (fast - slow)))
+            freq.append(f if factor == 1.0 else f * (keep + (1.0 - keep) / factor))
+        return cls(torch.tensor(freq, dtype=torch.float64, device=device), layout, mscale)
+
+    def _memory(self):
+        return (self._freq,)
+
+    def _call(self, x: torch.Tensor, out: torch.Tensor):
+        c = moe_rope_config()
+        if x.shape != out.shape or x.dtype != out.dtype:
+            raise ValueError("out: shape and type of x")
+        (c.x_token, c.x_head), (c.out_token, c.out_head) = _strides(x, "x"), _strides(out, "out")
+        c.T, c.heads, c.D = x.shape
+        c.rotary_dim, c.layout, c.mscale = self._key
+        c.dtype = _float_type(x)
+        if len(self._calls) > 256:                           # a server's batches are of any size
+            self._calls.clear()
+        return c, ctypes.byref(c)
+
+    def __call__(self, x: torch.Tensor, pos: torch.Tensor, out: Optional[torch.Tensor] = None, inverse: bool = False, stream=None) -> torch.Tensor:
+        """x [tokens, heads, channels] bf16 or fp32 at positions pos int32 [tokens] -> out (default: a new tensor; x itself: in place).  inverse: turned back."""
+        if out is None:
+            with torch.cuda.stream(_torch_stream(stream)):
+                out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        key = (x.shape, x.stride(), x.dtype, out.shape, out.stride(), out.dtype)
+        call = self._calls.get(key)
+        if call is None:
+            call = self._calls[key] = self._call(x, out)
+        c, ref = call
+        device = x.get_device()
+        if device < 0 or device != self._freq.get_device() or device != out.get_device() or device != pos.get_device():
+            raise ValueError(_DEVICES)
+        _integers(pos, "pos", x.shape[:1])
+        c.inverse = 1 if inverse else 0
+        s = _raw_stream(stream, device)
+        if s not in self._streams:
+            self._used_on(stream, s)
+        _call_on(device, _lib.moe_rope, ref, x.data_ptr(), pos.data_ptr(), self._freq.data_ptr(), out.data_ptr(), s)
+        return out
+
+
+class KvCache(_Owner):
+    """The paged keys and values of one layer: k, v [pages, key heads, positions of a page, channels] bf16, fp32 or, with scales [pages, key heads, positions]
+    fp32, float8_e4m3fn.  Which pages a sequence has is in the page table of each call: int32 [sequences, entries], positions p of a sequence in
+    page table[s, p // page_size]."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None):
+        super().__init__()
+        load_library()
+        kinds = {torch.bfloat16: MOE_BF16, torch.float32: MOE_FP32, torch.float8_e4m3fn: MOE_E4M3}
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.dtype not in kinds or k.stride(3) != 1 or v.stride(3) != 1:
+            raise ValueError("k, v: [pages, key heads, positions, channels] of one type (bf16, fp32, float8_e4m3fn), with dense channels")
+        steps = [0 if n <= 1 else s for n, s in zip(k.shape[:3], k.stride())]
+        if steps != [0 if n <= 1 else s for n, s in zip(v.shape[:3], v.stride())]:
+            raise ValueError("k and v have different strides")
+        if any(n > 1 and s == 0 for n, s in zip(k.shape[:3], steps)):
+            raise ValueError(_SHARED_ROWS)
+        codes = k.dtype is torch.float8_e4m3fn
+        for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+            if codes != (t is not None) or (codes and (t.dtype != torch.float32 or t.shape != k.shape[:3] or not t.is_contiguous())):
+                raise ValueError(f"{name}: fp32 [pages, key heads, positions] with float8_e4m3fn rows, None with others")
+        _on_one_gpu(k, v, k_scale, v_scale)
+        self._k, self._v, self._k_scale, self._v_scale = k, v, k_scale, v_scale
+        self.n_pages, self.n_heads, self.page_size, self.head_dim = k.shape
+        self._device = k.get_device()
+        c = self.c = moe_kv_cache()
+        c.n_pages, c.heads, c.page_size, c.D = k.shape
+        c.dtype = kinds[k.dtype]
+        c.page, c.head, c.row = steps
+        c.k, c.v = k.data_ptr(), v.data_ptr()
+        if codes:
+            c.k_scale, c.v_scale = k_scale.data_ptr(), v_scale.data_ptr()
+        self._ref = ctypes.byref(c)
+        self._calls = {}
+
+    k, v = property(lambda self: self._k), property(lambda self: self._v)
+    k_scale, v_scale = property(lambda self: self._k_scale), property(lambda self: self._v_scale)
+
+    @classmethod
+    def empty(cls, n_pages: int, page_size: int, n_heads: int, head_dim: int, dtype: torch.dtype = torch.bfloat16, device="cuda") -> "KvCache":
+        """A cache of dense pages; what is in them does not matter until it is written."""
+        k, v = (torch.empty((n_pages, n_heads, page_size, head_dim), dtype=dtype, device=device) for _ in range(2))
+        if dtype is not torch.float8_e4m3fn:
+            return cls(k, v)
+        return cls(k, v, *(torch.empty((n_pages, n_heads, page_size), dtype=torch.float32, device=device) for _ in range(2)))
+
+    def _memory(self):
+        return self._k, self._v, self._k_scale, self._v_scale
+
+    def _call(self, k, v, q, q_out, table, rotary):
+        c = moe_append_config()
+        if k.dim() != 3 or k.shape != v.shape or k.dtype != v.dtype or tuple(k.shape[1:]) != (self.n_heads, self.head_dim):
+            raise ValueError(f"k, v: [tokens, {self.n_heads}, {self.head_dim}] of one type")
+        (c.k_token, c.k_head), (c.v_token, c.v_head) = _strides(k, "k"), _strides(v, "v")
+        c.T, c.dtype = k.shape[0], _float_type(k)
+        if q is not None:
+            if q.dim() != 3 or q.shape[0] != k.shape[0] or q.shape[2] != self.head_dim or q.dtype != k.dtype or q_out.shape != q.shape or q_out.dtype != q.dtype:
+                raise ValueError(f"q, q_out: [tokens, heads, {self.head_dim}] of the keys' type")
+            (c.q_token, c.q_head), (c.out_token, c.out_head) = _strides(q, "q"), _strides(q_out, "q_out")
+            c.heads = q.shape[1]
+        _integers(table, "table", (-1, -1))
+        c.n_seqs, c.table_len = table.shape
+        c.table_ld = _table_ld(table)
+        c.mscale = 1.0
+        if rotary is not None:
+            c.rotary_dim, c.layout, c.mscale = rotary._key
+        if len(self._calls) > 256:                           # a server's batches are of any size
+            self._calls.clear()
+        return c, ctypes.byref(c)
+
+    def append(self, k: torch.Tensor, v: torch.Tensor, pos: torch.Tensor, table: torch.Tensor, seq: Optional[torch.Tensor] = None,
+               rotary: Optional[Rotary] = None, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+               stream=None) -> Optional[torch.Tensor]:
+        """Stores keys (turned, with `rotary`) and values [tokens, key heads, channels] at positions pos int32 [tokens] of sequences seq int32 [tokens] (None:
+        token t is of sequence t); positions below 0 are padding.  With queries q [tokens, heads, channels]: -> q_out (default: a new tensor; q itself: in
+        place), turned."""
+        if q is None:
+            if q_out is not None:
+                raise ValueError("q_out without q")
+            key = (k.shape, k.stride(), k.dtype, v.shape, v.stride(), v.dtype, table.shape, table.stride(), table.dtype, rotary and rotary._key)
+        else:
+            if q_out is None:
+                with torch.cuda.stream(_torch_stream(stream)):
+                    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            key = (k.shape, k.stride(), k.dtype, v.shape, v.stride(), v.dtype, table.shape, table.stride(), table.dtype, rotary and rotary._key,
+                   q.shape, q.stride(), q.dtype, q_out.shape, q_out.stride(), q_out.dtype)
+        call = self._calls.get(key)
+        if call is None:
+            call = self._calls[key] = self._call(k, v, q, q_out, table, rotary)
+        device = self._device
+        for t in (k, v, pos, table):
+            if t.get_device() != device:
+                raise ValueError(_DEVICES)
+        for t in (seq, q, q_out, rotary and rotary._freq):
+            if t is not None and t.get_device() != device:
+                raise ValueError(_DEVICES)
+        _integers(pos, "pos", k.shape[:1])
+        if seq is not None:
+            _integers(seq, "seq", k.shape[:1])
+        s = _raw_stream(stream, device)
+        if s not in self._streams:
+            self._used_on(stream, s)
+        if rotary is not None and s not in rotary._streams:
+            rotary._used_on(stream, s)
+        _call_on(device, _lib.moe_kv_append, call[1], self._ref, None if q is None else q.data_ptr(), k.data_ptr(), v.data_ptr(), pos.data_ptr(),
+                 None if seq is None else seq.data_ptr(), table.data_ptr(), None if rotary is None else rotary._freq.data_ptr(),
+                 None if q is None else q_out.data_ptr(), s)
+        return q_out
+
+
+class DecodeAttention(_Owner):
+    """Attention of one new token per sequence over a cache.  Calling it enqueues it on `stream`; its workspace is kept and grows with the largest call, so
+    calls that may overlap (streams without order between them, a graph's replay among them) need an object each.  A captured graph reads the cache and a
+    workspace of its object, which has to live as long as the graph; larger calls in between do not matter to it."""
+
+    def __init__(self, cache: KvCache, n_heads: int, scale: Optional[float] = None, window: int = 0, softcap: float = 0.0):
+        super().__init__()
+        if n_heads <= 0 or n_heads % cache.n_heads:
+            raise ValueError(f"{n_heads} query heads on {cache.n_heads} key heads")
+        self.cache, self.n_heads = cache, n_heads
+        self.scale = 1.0 / math.sqrt(cache.head_dim) if scale is None else float(scale)
+        self.window, self.softcap = int(window), float(softcap)
+        self.ws = None
+        self._outgrown = []                                  # workspaces of smaller calls: captured graphs have their addresses
+        self._calls = {}
+
+    def _memory(self):
+        return (self.ws,)
+
+    def _workspace(self, need: int, stream) -> None:
+        if self.ws is not None:                              # twice as large at least: what is kept stays below the one in use
+            need = max(need, 2 * self.ws.numel())
+            self._outgrown.append(self.ws)
+        with torch.cuda.stream(_torch_stream(stream)):
+            self.ws = torch.empty((need,), dtype=torch.uint8, device=self.cache.k.device)
+        self._streams.clear()
+
+    def _call(self, q, out, table):
+        c = moe_attention_config()
+        if q.dim() != 3 or tuple(q.shape[1:]) != (self.n_heads, self.cache.head_dim) or out.shape != q.shape or out.dtype != q.dtype:
+            raise ValueError(f"q, out: [sequences, {self.n_heads}, {self.cache.head_dim}] of one type")
+        (c.q_token, c.q_head), (c.out_token, c.out_head) = _strides(q, "q"), _strides(out, "out")
+        c.B, c.heads, c.dtype = q.shape[0], self.n_heads, _float_type(q)
+        _integers(table, "table", (q.shape[0], -1))
+        c.table_len, c.table_ld = table.shape[1], _table_ld(table)
+        c.window, c.scale, c.softcap = self.window, self.scale, self.softcap
+        if len(self._calls) > 256:                           # a server's batches are of any size
+            self._calls.clear()
+        return [c, ctypes.byref(c), 0, None]
+
+    def __call__(self, q: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, max_len: int, out: Optional[torch.Tensor] = None,
+                 lse: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """q [sequences, heads, channels] bf16 or fp32, lengths int32 [sequences] (the new token's position is length - 1) of at most max_len -> out (default: a new
+        tensor); lse: fp32 [sequences, heads], filled where it is given."""
+        if out is None:
+            with torch.cuda.stream(_torch_stream(stream)):
+                out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        key = (q.shape, q.stride(), q.dtype, out.shape, out.stride(), out.dtype, table.shape, table.stride(), table.dtype)
+        call = self._calls.get(key)
+        if call is None:
+            call = self._calls[key] = self._call(q, out, table)
+        cache = self.cache
+        device = cache._device
+        for t in (q, table, lengths, out):
+            if t.get_device() != device:
+                raise ValueError(_DEVICES)
+        _integers(lengths, "lengths", q.shape[:1])
+        if lse is not None:
+            if lse.get_device() != device:
+                raise ValueError(_DEVICES)
+            if lse.dtype is not torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous():
+                raise ValueError("lse: fp32 [sequences, heads], dense")
+        c, ref, need, bound = call
+        if bound != max_len:
+            if not 0 <= max_len < 2 ** 31:
+                raise ValueError(f"max_len {max_len}")
+            c.max_len = call[3] = max_len
+            need = call[2] = int(_lib.moe_paged_attention_workspace_bytes(ref, cache._ref))
+        if need and (self.ws is None or self.ws.numel() < need):
+            self._workspace(need, stream)
+        s = _raw_stream(stream, device)
+        if s not in self._streams:
+            self._used_on(stream, s)
+        if s not in cache._streams:
+            cache._used_on(stream, s)
+        ws = self.ws
+        _call_on(device, _lib.moe_paged_attention, ref, cache._ref, q.data_ptr(), table.data_ptr(), lengths.data_ptr(), out.data_ptr(),
+                 None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), s)
+        return out
 
 
 def torch_dtype(cfg: LayerConfig):

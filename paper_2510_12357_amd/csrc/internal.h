@@ -7,6 +7,7 @@
 #include "mobile_moe.h"
 #include "ffn_route.h"
 #include "int8_route.h"
+#include "attention_plan.h"
 
 namespace mm {
 
@@ -24,7 +25,7 @@ int validate_config(const moe_config* cfg);
 // ---- optional per-kernel timing (moe_profile_*): an event pair around each launch site -------
 enum ProfKind { kProfRouterGemm = 0, kProfRouteTopk, kProfDispatch, kProfFfnGateUp, kProfFfnDown,
                 kProfCombine, kProfConfidence, kProfDecodeStep, kProfQuantize, kProfInt8Product, kProfLogprobs,
-                kProfKinds };
+                kProfRotary, kProfAttention, kProfKinds };
 void prof_mark(int kind, bool begin, hipStream_t s);
 struct ProfScope {
   int kind; hipStream_t s;
@@ -182,5 +183,34 @@ int launch_int8_stream_float(const Int8Args& a, const void* x, int x_dtype, int6
 int launch_logprobs(const moe_logprobs_config& c, const void* logits, const int32_t* tokens, float* token_logp, float* entropy, float* conf,
                     int32_t* top_idx, float* top_logp, void* ws, hipStream_t s);
 size_t logprobs_workspace_bytes(const moe_logprobs_config& c);
+
+// ---- the attention step (attention_api.hip resolves the dense strides and checks everything) -----------------------
+// What a rotation reads and writes per head: `heads` query heads in front, then, with a cache, its key heads and value heads.
+struct RotaryArgs {
+  int T, heads, kv_heads, D, rotary_dim, layout;
+  float mscale, sign;                    // sign -1: turned back
+  const void *q, *k, *v; void* q_out;
+  int64_t q_token, q_head, k_token, k_head, v_token, v_head, out_token, out_head;
+  const int32_t *pos, *seq, *table;
+  const double* freq;
+  int n_seqs, table_len, n_pages, shift, cache_dtype;
+  int64_t table_ld;
+  int64_t page, head, row;               // strides of the cache in its elements
+  void *k_cache, *v_cache; float *k_scale, *v_scale;
+};
+int launch_rotary(const RotaryArgs& a, int dtype, hipStream_t s);
+struct AttentionArgs {
+  int B, heads, kv_heads, group, D, dtype, cache_dtype;
+  int max_len, window, table_len, n_pages, shift, split, parts;
+  int64_t table_ld;
+  float scale, softcap;
+  int64_t q_token, q_head, out_token, out_head;
+  int64_t page, head, row;
+  const void* q; const int32_t *table, *lengths;
+  const void *k, *v; const float *k_scale, *v_scale;
+  void* out; float* lse;
+  float *part_out, *part_stat;           // [B, parts, heads, D] and [B, parts, heads, 2] where there is more than one part
+};
+int launch_attention(const AttentionArgs& a, hipStream_t s);
 
 }  // namespace mm
