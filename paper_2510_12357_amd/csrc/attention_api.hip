@@ -91,7 +91,7 @@ int resolve(const char* call, const moe_attention_config* cfg, const moe_kv_cach
   if (span < c->max_len) c->max_len = (int)span;           // longer sequences are behind their table row
   *plan = plan_splits(c->B, cache.heads, c->heads / cache.heads, c->max_len, c->window, device_cu_count());
   const int64_t tiles = (int64_t)cache.heads * ((c->heads / cache.heads + kHeadTile - 1) / kHeadTile);
-  if ((double)c->B * tiles * plan->parts >= (double)(1 << 22)) return fail(MOE_E_UNSUPPORTED, "%s: %d sequences of %d positions on %lld heads are too many workgroups", call, c->B, c->max_len, (long long)tiles);
+  if ((double)c->B * tiles * plan->parts >= (double)(1 << 20)) return fail(MOE_E_UNSUPPORTED, "%s: %d sequences of %d positions on %lld heads are too many workgroups", call, c->B, c->max_len, (long long)tiles);
   return MOE_OK;
 }
 size_t part_floats(const moe_attention_config& c, const moe_kv_cache& cache, const SplitPlan& p) {

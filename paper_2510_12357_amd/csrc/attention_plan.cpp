@@ -9,7 +9,7 @@ SplitPlan plan_splits(int sequences, int kv_heads, int group, int max_len, int w
   // a window that starts inside a block of 64 positions reaches over one more of them
   const int64_t span = std::max<int64_t>(1, window > 0 && window < max_len ? (int64_t)window + 63 : max_len);
   const int64_t blocks = (span + 63) / 64, tiles = (group + kHeadTile - 1) / kHeadTile;
-  const int64_t units = std::max<int64_t>(1, (int64_t)sequences * kv_heads * tiles), wanted = 4 * (int64_t)device_cus;
+  const int64_t units = std::max<int64_t>(1, (int64_t)sequences * kv_heads * tiles), wanted = 16 * (int64_t)device_cus;
   const int64_t most = kMaxSplit / 64;
   int64_t each = std::min(most, std::max<int64_t>(blocks * units / wanted, 8));      // blocks of a part
   each = std::min(each, blocks);

@@ -8,6 +8,8 @@
 // maxima nor rescale.  Waves' sums are joined in LDS, parts' sums by a second kernel, both in a fixed order.
 #include <math.h>
 
+#include <type_traits>
+
 #include "internal.h"
 #include "groups.h"
 
@@ -44,24 +46,24 @@ __device__ __forceinline__ Eight zeros(Eight) { return {zeros(f32x4{}), zeros(f3
 
 template <typename C, int N>
 __device__ __forceinline__ float element(const typename Raw<C, N>::type& v, int j) {
-  if constexpr (sizeof(C) == 2) {
-    const unsigned d = (unsigned)dword(v, j / 2);
-    return __uint_as_float(j & 1 ? d & 0xffff0000u : d << 16);
-  } else if constexpr (sizeof(C) == 1) {
-    switch (j & 3) {                                        // the byte is part of the instruction
-      case 0: return __builtin_amdgcn_cvt_f32_fp8(dword(v, j / 4), 0);
-      case 1: return __builtin_amdgcn_cvt_f32_fp8(dword(v, j / 4), 1);
-      case 2: return __builtin_amdgcn_cvt_f32_fp8(dword(v, j / 4), 2);
-      default: return __builtin_amdgcn_cvt_f32_fp8(dword(v, j / 4), 3);
-    }
-  } else if constexpr (N == 8) {
-    return j < 4 ? v.lo[j & 3] : v.hi[j & 3];
-  } else {
-    return v[j];
-  }
+  if constexpr (N == 8) return j < 4 ? v.lo[j & 3] : v.hi[j & 3];
+  else return v[j];
 }
-__device__ __forceinline__ bf16x8 as_bf16(const i32x4& v) { return __builtin_bit_cast(bf16x8, v); }
-__device__ __forceinline__ bf16x8 as_bf16(const i32x2& v) { return widen_e4m3(v[0], v[1]); }
+// Element `at` of the operands of four channels from channel j on: bf16 values, or E4M3 codes widened exactly
+template <typename C, typename R>
+__device__ __forceinline__ void widen_four(const R& v, int j, int at, bool there, bf16x8* to) {
+  typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+  bf16x2 a, b;
+  if constexpr (sizeof(C) == 2) {
+    a = __builtin_bit_cast(bf16x2, there ? dword(v, j / 2) : 0);
+    b = __builtin_bit_cast(bf16x2, there ? dword(v, j / 2 + 1) : 0);
+  } else {
+    const unsigned d = there ? (unsigned)dword(v, j / 4) : 0u;
+    a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(d, 1.f, false);
+    b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(d, 1.f, true);
+  }
+  to[0][at] = a[0]; to[1][at] = a[1]; to[2][at] = b[0]; to[3][at] = b[1];
+}
 
 __device__ __forceinline__ float lane_max(float v) {        // over the four lanes of a column
   v = fmaxf(v, __shfl_xor(v, 16));
@@ -79,51 +81,75 @@ __device__ __forceinline__ void store_out(const AttentionArgs& a, int64_t at, fl
   else static_cast<__bf16*>(a.out)[at] = (__bf16)v;
 }
 
+// A wave's block of positions, and what its lanes load of it: values of positions 4 g .. 4 g + 3 of a tile, as the product with them wants them, and keys by whole
+// rows, 16 bytes a lane, which go through LDS to the lane that has their position in the product with the queries.
+template <typename C, int VW, int CHUNKS>
+struct Block {
+  static constexpr bool kF32 = sizeof(C) == 4, kCodes = sizeof(C) == 1;
+  static constexpr int kDims = 16 * VW * CHUNKS;            // channels that registers are for
+  static constexpr int kTiles = kF32 || kDims > 128 ? 1 : 2;     // tiles of 16 positions
+  static constexpr int kPositions = 16 * kTiles;
+  static constexpr int kVec = 16 / sizeof(C);               // channels of 16 bytes
+  static constexpr int kRowLanes = kDims / kVec;            // lanes of a row of keys
+  static constexpr int kLoads = kRowLanes / 4;              // rows of a tile that a lane loads of, and its vectors in the product
+  static constexpr int kKeyBytes = kPositions * kRowLanes * 16;
+  typedef typename Raw<C, VW>::type RawV;
+  typedef typename std::conditional<kF32, f32x4, i32x4>::type RawK;
+  RawK k[kTiles][kLoads];
+  RawV v[kTiles][4][CHUNKS];
+  f32x4 ks[kCodes ? kTiles : 1], vs[kCodes ? kTiles : 1];
+  // where vector c of row r of a tile is in LDS: eight rows' vectors of the same c fall on different banks
+  static __device__ __forceinline__ int place(int r, int c) {
+    constexpr int kRows = kRowLanes < 16 ? 16 / kRowLanes : 1;        // of 256 bytes, all banks
+    return (r * kRowLanes + (c ^ (r / kRows & (kRowLanes < 16 ? kRowLanes - 1 : 15)))) * 16;
+  }
+};
+// loads past the caches: keys and values are read once
+template <typename T>
+__device__ __forceinline__ T load_once(const T* p) { return __builtin_nontemporal_load(p); }
+__device__ __forceinline__ Eight load_once(const Eight* p) { return {load_once(&p->lo), load_once(&p->hi)}; }
+
+// Waves of a SIMD that the registers are shared by: as many as need no spills.
+constexpr int waves_per_simd(size_t bytes, int dims, int parts) {
+  if (dims > 128) return bytes < 4 && parts == 1 ? 2 : 1;
+  if (dims > 64) return parts == 1 ? 3 : 2;
+  return parts == 1 ? 4 : 3;
+}
+
 // C: type of the cache's rows.  A row of the head is CHUNKS chunks of 16 VW channels, VW of them a lane (D below that: RAGGED).  PARTS: bf16 terms of a query,
 // 1 of a bf16 one and 3 of an fp32 one, exact; keys of fp32 are multiplied in fp32.
 template <typename C, int VW, int CHUNKS, int PARTS, bool RAGGED>
-__global__ __launch_bounds__(kThreads) void attention_kernel(const AttentionArgs a) {
-  constexpr bool kF32 = sizeof(C) == 4, kCodes = sizeof(C) == 1;
-  constexpr int kDims = 16 * VW * CHUNKS;                   // channels that registers are for
-  constexpr int kTiles = kF32 || kDims > 128 ? 1 : 2;       // tiles of 16 positions of a block
-  constexpr int kBlock = 16 * kTiles;
+__global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNKS, PARTS)) void attention_kernel(const AttentionArgs a) {
+  typedef Block<C, VW, CHUNKS> Blk;
+  constexpr bool kF32 = Blk::kF32, kCodes = Blk::kCodes;
+  constexpr int kDims = Blk::kDims, kTiles = Blk::kTiles, kBlock = Blk::kPositions, kVec = Blk::kVec, kLoads = Blk::kLoads;
   constexpr int kSteps = kDims / 32;                        // of the scores' contraction: 32 channels, 8 a lane
-  typedef typename Raw<C, VW>::type RawV;
-  typedef typename Raw<C, 8>::type RawK;
   __shared__ int s_page[kMaxPages];
-  __shared__ __attribute__((aligned(16))) float s_out[kWaves][16][16 * VW];
+  // keys of the waves' blocks, in the end their sums
+  constexpr int kOutBytes = 16 * 16 * VW * 4, kWaveBytes = Blk::kKeyBytes > kOutBytes ? Blk::kKeyBytes : kOutBytes;
+  __shared__ __attribute__((aligned(16))) char s_mem[kWaves * kWaveBytes];
   __shared__ float s_max[kWaves][16], s_sum[kWaves][16];
   __shared__ int s_bad;
+  fetch_arguments<sizeof(AttentionArgs)>();
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), n = lane & 15, g = lane >> 4;
+  // workgroups of the same keys and values (tiles of a large group) follow each other on one XCD, of which there are 8
   const int tiles = (a.group + kHeadTile - 1) / kHeadTile;
-  int at = blockIdx.x;
-  const int tile = at % tiles; at /= tiles;
+  const int units = a.B * a.parts * a.kv_heads;
+  int at = blockIdx.x, tile = 0;
+  if (tiles > 1) {
+    const int eighth = at / 8, full = units / 8 * 8;
+    if (at < full * tiles) { tile = eighth % tiles; at = eighth / tiles * 8 + at % 8; }
+    else { const int rest = at - full * tiles; tile = rest % tiles; at = full + rest / tiles; }
+  }
   const int kvh = at % a.kv_heads; at /= a.kv_heads;
   const int part = at % a.parts, b = at / a.parts;
-
-  const Seen seen = seen_by(a.lengths[b], a.max_len, a.window, a.table_len, a.shift);
-  const Part p = part_of(seen, a.split, part);
-  if (a.parts > 1 && p.begin >= p.end) return;
   const int heads = min(kHeadTile, a.group - tile * kHeadTile), head0 = kvh * a.group + tile * kHeadTile;
 
-  // ---- pages of the part; a number outside the cache spoils the sequence ----
-  const int entry0 = p.begin >> a.shift;
-  if (tid == 0) s_bad = seen.bad;
-  __syncthreads();
-  if (p.begin < p.end) {
-    const int entries = ((p.begin + a.split - 1) >> a.shift) - entry0 + 1;
-    const int32_t* row = a.table + b * a.table_ld;
-    for (int i = tid; i < entries; i += kThreads) {
-      const int64_t from = (int64_t)(entry0 + i) << a.shift;
-      int page = 0;                                         // of positions that are not seen: any
-      if (from < p.end && from + ((int64_t)1 << a.shift) > max(p.begin, seen.first)) page = page_of(row, a.table_len, a.n_pages, a.shift, from);
-      if (page < 0) { s_bad = 1; page = 0; }
-      s_page[i] = page;
-    }
-  }
-
-  // ---- queries ----
+  // ---- loads that depend on nothing: queries, and without a window the first pages' numbers ----
+  const int32_t* const row = a.table + b * a.table_ld;
+  int early = -1;
+  if (a.window == 0) early = row[min((int)(((int64_t)part * a.split) >> a.shift) + tid, a.table_len - 1)];
   bf16x8 qf[kF32 ? 1 : PARTS][kSteps];
   float q32[kF32 ? kDims / 4 : 1];
   {
@@ -139,7 +165,7 @@ __global__ __launch_bounds__(kThreads) void attention_kernel(const AttentionArgs
       for (int s = 0; s < kSteps; ++s)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const int d = 32 * s + 8 * g + e;
+          const int d = kCodes ? 64 * (s / 2) + 16 * g + 8 * (s % 2) + e : 32 * s + 8 * g + e;      // the order of the keys' loads
           float q = n < heads && (!RAGGED || d < a.D) ? load_query(a, q_at + d) : 0.f;
 #pragma unroll
           for (int t = 0; t < PARTS; ++t) {
@@ -150,6 +176,30 @@ __global__ __launch_bounds__(kThreads) void attention_kernel(const AttentionArgs
         }
     }
   }
+
+  const Seen seen = seen_by(a.lengths[b], a.max_len, a.window, a.table_len, a.shift);
+  const Part p = part_of(seen, a.split, part);
+  if (a.parts > 1 && p.begin >= p.end) return;
+  const int first = max(seen.first, p.begin);
+
+  // ---- pages of the part; a number outside the cache spoils the sequence ----
+  const int entry0 = p.begin >> a.shift;
+  if (tid == 0) s_bad = seen.bad;
+  __syncthreads();
+  if (p.begin < p.end) {
+    const int entries = ((p.begin + a.split - 1) >> a.shift) - entry0 + 1;
+    for (int i = tid; i < entries; i += kThreads) {
+      const int64_t from = (int64_t)(entry0 + i) << a.shift;
+      int page = 0;                                         // of positions that are not seen: any
+      if (from < p.end && from + ((int64_t)1 << a.shift) > first) {
+        if (a.window == 0 && i == tid) page = entry0 + i < a.table_len && early >= 0 && early < a.n_pages ? early : -1;
+        else page = page_of(row, a.table_len, a.n_pages, a.shift, from);
+      }
+      if (page < 0) { s_bad = 1; page = 0; }
+      s_page[i] = page;
+    }
+  }
+
   const float to_log2 = a.softcap > 0.f ? a.softcap * kLog2e : a.scale * kLog2e, in_cap = a.softcap > 0.f ? a.scale / a.softcap : 0.f;
   const C* const kbase = static_cast<const C*>(a.k) + (int64_t)kvh * a.head;
   const C* const vbase = static_cast<const C*>(a.v) + (int64_t)kvh * a.head;
@@ -163,74 +213,96 @@ __global__ __launch_bounds__(kThreads) void attention_kernel(const AttentionArgs
     for (int j = 0; j < VW; ++j) acc[c][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   __syncthreads();
 
-  const int first = max(seen.first, p.begin);
-  for (int t0 = p.begin + (first - p.begin) / kBlock * kBlock + wave * kBlock; t0 < p.end; t0 += kWaves * kBlock) {
-    const bool whole = t0 >= first && t0 + kBlock <= p.end;
-    // ---- loads ----
-    RawK kr[kTiles][kF32 ? kDims / 8 : kSteps];
-    RawV vr[kTiles][4][CHUNKS];
-    f32x4 ks[kTiles], vs[kTiles];
+  Blk r;
+  char* const keys = s_mem + wave * kWaveBytes;
+  auto load_keys = [&](int t0) {
 #pragma unroll
     for (int u = 0; u < kTiles; ++u) {
-      const int tk = t0 + 16 * u + n;
-      const C* krow = kbase + (int64_t)s_page[(tk >> a.shift) - entry0] * a.page + (int64_t)(tk & mask) * a.row;
-      if constexpr (kF32) {
 #pragma unroll
-        for (int i = 0; i < kDims / 16; ++i) {
-          const int d = 16 * i + 4 * g;
-          const f32x4 x = !RAGGED || d < a.D ? *reinterpret_cast<const f32x4*>(krow + d) : f32x4{0.f, 0.f, 0.f, 0.f};
-          if (i % 2) kr[u][i / 2].hi = x; else kr[u][i / 2].lo = x;
-        }
-      } else {
+      for (int s = 0; s < kLoads; s += kLoads < 4 ? kLoads : 4) {
+        const int tk = t0 + 16 * u + lane / Blk::kRowLanes * kLoads + s, c = lane % Blk::kRowLanes * kVec;
+        const C* krow = kbase + (int64_t)s_page[(tk >> a.shift) - entry0] * a.page + (int64_t)(tk & mask) * a.row + c;
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-          const int d = 32 * s + 8 * g;
-          kr[u][s] = !RAGGED || d < a.D ? *reinterpret_cast<const RawK*>(krow + d) : zeros(RawK{});
-        }
+        for (int i = 0; i < (kLoads < 4 ? kLoads : 4); ++i)
+          r.k[u][s + i] = !RAGGED || c < a.D ? load_once(reinterpret_cast<const typename Blk::RawK*>(krow + i * a.row)) : typename Blk::RawK{0, 0, 0, 0};
       }
+      if constexpr (kCodes) {
+        const int ts = t0 + 16 * u + 4 * g;
+        r.ks[u] = *reinterpret_cast<const f32x4*>(a.k_scale + ((((int64_t)s_page[(ts >> a.shift) - entry0] * a.kv_heads + kvh) << a.shift) + (ts & mask)));
+      }
+    }
+  };
+  auto load_values = [&](int t0) {
+#pragma unroll
+    for (int u = 0; u < kTiles; ++u) {
       const int tv = t0 + 16 * u + 4 * g, page = s_page[(tv >> a.shift) - entry0];
-      const C* vrow = vbase + (int64_t)page * a.page + (int64_t)(tv & mask) * a.row;
+      const C* vrow = vbase + (int64_t)page * a.page + (int64_t)(tv & mask) * a.row + VW * n;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
-          const int d = 16 * VW * c + VW * n;
-          vr[u][i][c] = !RAGGED || d < a.D ? *reinterpret_cast<const RawV*>(vrow + (int64_t)i * a.row + d) : zeros(RawV{});
+          const int d = 16 * VW * c;
+          r.v[u][i][c] = !RAGGED || d + VW * n < a.D ? load_once(reinterpret_cast<const typename Blk::RawV*>(vrow + i * a.row + d)) : zeros(typename Blk::RawV{});
         }
-      if constexpr (kCodes) {
-        const int64_t sc = (((int64_t)page * a.kv_heads + kvh) << a.shift) + (tv & mask);
-        ks[u] = *reinterpret_cast<const f32x4*>(a.k_scale + sc);
-        vs[u] = *reinterpret_cast<const f32x4*>(a.v_scale + sc);
-      }
+      if constexpr (kCodes) r.vs[u] = *reinterpret_cast<const f32x4*>(a.v_scale + ((((int64_t)page * a.kv_heads + kvh) << a.shift) + (tv & mask)));
     }
+  };
+  auto use = [&](int t0, int next) {
     // ---- scores, in units of log 2 ----
+    const bool whole = t0 >= first && t0 + kBlock <= p.end;
+#pragma unroll
+    for (int u = 0; u < kTiles; ++u)
+#pragma unroll
+      for (int s = 0; s < kLoads; ++s) *reinterpret_cast<typename Blk::RawK*>(keys + u * 16 * Blk::kRowLanes * 16 + Blk::place(lane / Blk::kRowLanes * kLoads + s, lane % Blk::kRowLanes)) = r.k[u][s];
+    float ks[kTiles][4];
+    if constexpr (kCodes) {
+#pragma unroll
+      for (int u = 0; u < kTiles; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ks[u][i] = r.ks[u][i];
+    }
+    if (next < p.end) load_keys(next);
     float x[kTiles][4];
-    bool there[kTiles][4];
     float most = -INFINITY;
 #pragma unroll
     for (int u = 0; u < kTiles; ++u) {
       f32x4 z = {0.f, 0.f, 0.f, 0.f};
+      typename Blk::RawK kf[kLoads];
+#pragma unroll
+      for (int s = 0; s < kLoads; ++s) kf[s] = *reinterpret_cast<const typename Blk::RawK*>(keys + u * 16 * Blk::kRowLanes * 16 + Blk::place(n, 4 * s + g));
       if constexpr (kF32) {
 #pragma unroll
-        for (int i = 0; i < kDims / 4; ++i)
-          z = __builtin_amdgcn_mfma_f32_16x16x4f32(i % 8 < 4 ? kr[u][i / 8].lo[i % 4] : kr[u][i / 8].hi[i % 4], q32[i], z, 0, 0, 0);
+        for (int i = 0; i < kDims / 4; ++i) z = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[i / 4][i % 4], q32[i], z, 0, 0, 0);
       } else {
 #pragma unroll
         for (int t = PARTS - 1; t >= 0; --t)                // small terms first
 #pragma unroll
-          for (int s = 0; s < kSteps; ++s) z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16(kr[u][s]), qf[t][s], z, 0, 0, 0);
+          for (int s = 0; s < kSteps; ++s) {
+            bf16x8 key;
+            if constexpr (kCodes) key = widen_e4m3(kf[s / 2][s % 2 * 2], kf[s / 2][s % 2 * 2 + 1]);
+            else key = __builtin_bit_cast(bf16x8, kf[s]);
+            z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(key, qf[t][s], z, 0, 0, 0);
+          }
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float v = z[i];
         if constexpr (kCodes) v *= ks[u][i];
         if (a.softcap > 0.f) v = tanhf(v * in_cap);
-        const int t = t0 + 16 * u + 4 * g + i;
-        there[u][i] = whole || (t >= first && t < p.end);
-        x[u][i] = v;
-        most = fmaxf(most, there[u][i] ? v * to_log2 : -INFINITY);
+        x[u][i] = v * to_log2;
       }
     }
+    auto hidden = [&](int u, int i) { const int t = t0 + 16 * u + 4 * g + i; return t < first || t >= p.end; };
+    if (!whole) {                                           // what is not seen counts as nothing, whatever it is
+#pragma unroll
+      for (int u = 0; u < kTiles; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[u][i] = hidden(u, i) ? -INFINITY : x[u][i];
+    }
+#pragma unroll
+    for (int u = 0; u < kTiles; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) most = fmaxf(most, x[u][i]);
     if (__any(most > top + kSlack)) {
       const float now = lane_max(fmaxf(top, most));
       const float alpha = top == -INFINITY ? 0.f : exp2f(top - now);
@@ -242,22 +314,78 @@ __global__ __launch_bounds__(kThreads) void attention_kernel(const AttentionArgs
         for (int j = 0; j < VW; ++j) acc[c][j] *= alpha;
     }
     const float base = top == -INFINITY ? 0.f : top;
+    float e[kTiles][4];
 #pragma unroll
     for (int u = 0; u < kTiles; ++u)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        float e = there[u][i] ? __builtin_amdgcn_exp2f(fmaf(x[u][i], to_log2, -base)) : 0.f;
-        sum += e;
-        if constexpr (kCodes) e = there[u][i] ? e * vs[u][i] : 0.f;
-        // ---- values: what stands behind the sequence counts as zero, whatever it is ----
+        e[u][i] = __builtin_amdgcn_exp2f(x[u][i] - base);
+        sum += e[u][i];
+      }
+    if (!whole) {
 #pragma unroll
-        for (int c = 0; c < CHUNKS; ++c) {
-          const RawV v = there[u][i] ? vr[u][i][c] : zeros(RawV{});
+      for (int u = 0; u < kTiles; ++u)
 #pragma unroll
-          for (int j = 0; j < VW; ++j) acc[c][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(element<C, VW>(v, j), e, acc[c][j], 0, 0, 0);
+        for (int i = 0; i < 4; ++i) {
+          const bool no = hidden(u, i);
+          if constexpr (kCodes) r.vs[u][i] = no ? 0.f : r.vs[u][i];
+#pragma unroll
+          for (int c = 0; c < CHUNKS; ++c) r.v[u][i][c] = no ? zeros(typename Blk::RawV{}) : r.v[u][i][c];
+        }
+    }
+    if constexpr (kCodes) {
+#pragma unroll
+      for (int u = 0; u < kTiles; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) e[u][i] *= r.vs[u][i];
+    }
+    // ---- values ----
+    if constexpr (kF32) {
+#pragma unroll
+      for (int u = 0; u < kTiles; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+            for (int j = 0; j < VW; ++j)
+              acc[c][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(element<C, VW>(r.v[u][i][c], j), e[u][i], acc[c][j], 0, 0, 0);
+    } else {
+      // position 4 g + i of tile u is operand element 4 u + i of lane group g in both; probabilities in two bf16 terms, 2^-17 of them off
+      bf16x8 hi, lo;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float w = u < kTiles ? e[u < kTiles ? u : 0][i] : 0.f;
+          hi[4 * u + i] = (__bf16)w;
+          lo[4 * u + i] = (__bf16)(w - (float)hi[4 * u + i]);
+        }
+#pragma unroll
+      for (int c = 0; c < CHUNKS; ++c) {
+#pragma unroll
+        for (int j = 0; j < VW; j += 4) {
+          bf16x8 value[4];
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) widen_four<C>(r.v[u < kTiles ? u : 0][i][c], j, 4 * u + i, u < kTiles, value);
+#pragma unroll
+          for (int o = 0; o < 4; ++o) {
+            acc[c][j + o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(value[o], lo, acc[c][j + o], 0, 0, 0);
+            acc[c][j + o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(value[o], hi, acc[c][j + o], 0, 0, 0);
+          }
         }
       }
-  }
+    }
+    if (next < p.end) load_values(next);
+  };
+
+  // ---- the part's blocks in turn over the waves; keys of the next one are loaded as soon as this one's are used, and values ----
+  constexpr int kStride = kWaves * kBlock;
+  int t0 = p.begin + (first - p.begin) / kBlock * kBlock + wave * kBlock;
+  if (t0 < p.end) { load_keys(t0); load_values(t0); }
+  for (; t0 < p.end; t0 += kStride) use(t0, t0 + kStride);
 
   // ---- join the waves ----
   sum = lane_sum(sum);
@@ -284,15 +412,15 @@ __global__ __launch_bounds__(kThreads) void attention_kernel(const AttentionArgs
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int j = 0; j < VW; j += 4)
-        *reinterpret_cast<f32x4*>(&s_out[wave][n][VW * (4 * g + i) + j]) =
+        *reinterpret_cast<f32x4*>(keys + 4 * (n * 16 * VW + VW * (4 * g + i) + j)) =
             f32x4{acc[c][j][i], acc[c][j + 1][i], acc[c][j + 2][i], acc[c][j + 3][i]} * weight;
     __syncthreads();
     for (int o = tid; o < 16 * 16 * VW / 4; o += kThreads) {
       const int head = o / (4 * VW), d = o % (4 * VW) * 4, channel = 16 * VW * c + d;
       if (head >= heads || channel >= a.D) continue;
-      f32x4 v = *reinterpret_cast<const f32x4*>(&s_out[0][head][d]);
+      f32x4 v = *reinterpret_cast<const f32x4*>(s_mem + 4 * (head * 16 * VW + d));
 #pragma unroll
-      for (int w = 1; w < kWaves; ++w) v += *reinterpret_cast<const f32x4*>(&s_out[w][head][d]);
+      for (int w = 1; w < kWaves; ++w) v += *reinterpret_cast<const f32x4*>(s_mem + w * kWaveBytes + 4 * (head * 16 * VW + d));
       joined(head, &m, &l);
       if (bad) l = nan;
       if (a.parts > 1) {
@@ -312,33 +440,45 @@ __global__ __launch_bounds__(kThreads) void attention_kernel(const AttentionArgs
   }
 }
 
-// The parts of a row (sequence, head), one wave a row.
-__global__ __launch_bounds__(64) void join_kernel(const AttentionArgs a) {
-  const int row = blockIdx.x, lane = threadIdx.x, b = row / a.heads, head = row - b * a.heads;
+// The parts of a row (sequence, head): four channels a thread, the parts in turn over the threads of a channel; first the largest maximum.
+__global__ __launch_bounds__(kThreads) void join_kernel(const AttentionArgs a) {
+  __shared__ float s_top[kWaves];
+  __shared__ __attribute__((aligned(16))) f32x4 s_v[kThreads];
+  __shared__ float s_l[kThreads];
+  const int row = blockIdx.x, tid = threadIdx.x, b = row / a.heads, head = row - b * a.heads;
   const Seen seen = seen_by(a.lengths[b], a.max_len, a.window, a.table_len, a.shift);
   const int parts = (seen.end - seen.first / 64 * 64 + a.split - 1) / a.split;
   const int64_t first = (int64_t)b * a.parts * a.heads + head;
   const float* stat = a.part_stat + 2 * first;
-  float m = -INFINITY, l = 0.f;
-  for (int i = lane; i < parts; i += 64) m = fmaxf(m, stat[2 * (int64_t)i * a.heads]);
+  const int64_t step = 2 * (int64_t)a.heads;
+  float m = -INFINITY;
+  for (int i = tid; i < parts; i += kThreads) m = fmaxf(m, stat[i * step]);
   for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-  auto weight = [&](int i) {
-    const float pm = stat[2 * (int64_t)i * a.heads];
-    return pm == -INFINITY ? 0.f : exp2f(pm - m);
-  };
-  for (int i = lane; i < parts; i += 64) l += weight(i) == 0.f ? 0.f : weight(i) * stat[2 * (int64_t)i * a.heads + 1];
-  for (int o = 32; o; o >>= 1) l += __shfl_xor(l, o);
+  if ((tid & 63) == 0) s_top[tid >> 6] = m;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) m = fmaxf(m, s_top[w]);
+  const int vecs = a.D / 4, turns = kThreads / vecs, turn = tid / vecs, d = tid % vecs * 4;
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  float l = 0.f;
+  if (turn < turns) {
+#pragma unroll 4
+    for (int i = turn; i < parts; i += turns) {
+      const float pm = stat[i * step], w = pm == -INFINITY ? 0.f : exp2f(pm - m);
+      l += w * stat[i * step + 1];
+      v += w * *reinterpret_cast<const f32x4*>(a.part_out + (first + (int64_t)i * a.heads) * a.D + d);
+    }
+  }
+  s_v[tid] = v;
+  s_l[tid] = l;
+  __syncthreads();
+  if (tid >= vecs) return;
+  for (int t = 1; t < turns; ++t) { v += s_v[t * vecs + tid]; l += s_l[t * vecs + tid]; }
   if (seen.bad) l = __uint_as_float(0x7fc00000u);
   const float over = l == 0.f ? 0.f : 1.f / l;
-  for (int d = lane; d < a.D; d += 64) {
-    float v = 0.f;
-    for (int i = 0; i < parts; ++i) {
-      const float w = weight(i);
-      if (w != 0.f) v = fmaf(w, a.part_out[(first + (int64_t)i * a.heads) * a.D + d], v);
-    }
-    store_out(a, (int64_t)b * a.out_token + (int64_t)head * a.out_head + d, v * over);
-  }
-  if (a.lse && lane == 0) a.lse[row] = l == 0.f ? -INFINITY : fmaf(m, kLn2, logf(l));
+#pragma unroll
+  for (int e = 0; e < 4; ++e) store_out(a, (int64_t)b * a.out_token + (int64_t)head * a.out_head + d + e, v[e] * over);
+  if (a.lse && tid == 0) a.lse[row] = l == 0.f ? -INFINITY : fmaf(m, kLn2, logf(l));
 }
 
 template <typename C, int VW, int CHUNKS, int PARTS>
@@ -368,7 +508,7 @@ int launch_attention(const AttentionArgs& a, hipStream_t s) {
   else if (a.cache_dtype == MOE_E4M3) rc = launch_cache<uint8_t>(a, blocks, s);
   else rc = launch_cache<__bf16>(a, blocks, s);
   if (rc || a.parts == 1) return rc;
-  join_kernel<<<a.B * a.heads, 64, 0, s>>>(a);
+  join_kernel<<<a.B * a.heads, kThreads, 0, s>>>(a);
   return hip_fail(hipGetLastError(), "join_kernel");
 }
 
