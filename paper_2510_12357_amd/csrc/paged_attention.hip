@@ -8,6 +8,7 @@
 // maxima nor rescale.  Waves' sums are joined in LDS, parts' sums by a second kernel, both in a fixed order.
 #include <math.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "internal.h"
@@ -81,13 +82,21 @@ __device__ __forceinline__ void store_out(const AttentionArgs& a, int64_t at, fl
   else static_cast<__bf16*>(a.out)[at] = (__bf16)v;
 }
 
+// Tiles of 16 positions of a wave's block, and waves of a SIMD that the registers are shared by.
+constexpr int block_tiles(size_t bytes, int dims) { return std::clamp(512 / (int)(dims * bytes), 1, 2); }
+constexpr int waves_per_simd(size_t bytes, int dims, int parts) {
+  if (dims > 128) return bytes < 4 && parts == 1 ? 2 : 1;
+  if (dims > 64) return parts == 1 && bytes < 4 ? 3 : 2;
+  return parts == 1 && bytes == 2 ? 4 : 3;
+}
+
 // A wave's block of positions, and what its lanes load of it: values of positions 4 g .. 4 g + 3 of a tile, as the product with them wants them, and keys by whole
 // rows, 16 bytes a lane, which go through LDS to the lane that has their position in the product with the queries.
 template <typename C, int VW, int CHUNKS>
 struct Block {
   static constexpr bool kF32 = sizeof(C) == 4, kCodes = sizeof(C) == 1;
   static constexpr int kDims = 16 * VW * CHUNKS;            // channels that registers are for
-  static constexpr int kTiles = kF32 || kDims > 128 ? 1 : 2;     // tiles of 16 positions
+  static constexpr int kTiles = block_tiles(sizeof(C), kDims);      // tiles of 16 positions: 16 KB of keys and values up to 512 bytes a row
   static constexpr int kPositions = 16 * kTiles;
   static constexpr int kVec = 16 / sizeof(C);               // channels of 16 bytes
   static constexpr int kRowLanes = kDims / kVec;            // lanes of a row of keys
@@ -97,7 +106,7 @@ struct Block {
   typedef typename std::conditional<kF32, f32x4, i32x4>::type RawK;
   RawK k[kTiles][kLoads];
   RawV v[kTiles][4][CHUNKS];
-  f32x4 ks[kCodes ? kTiles : 1], vs[kCodes ? kTiles : 1];
+  float scale;                                              // of a key (lanes below 32) or value: position lane % 32
   // where vector c of row r of a tile is in LDS: eight rows' vectors of the same c fall on different banks
   static __device__ __forceinline__ int place(int r, int c) {
     constexpr int kRows = kRowLanes < 16 ? 16 / kRowLanes : 1;        // of 256 bytes, all banks
@@ -108,13 +117,6 @@ struct Block {
 template <typename T>
 __device__ __forceinline__ T load_once(const T* p) { return __builtin_nontemporal_load(p); }
 __device__ __forceinline__ Eight load_once(const Eight* p) { return {load_once(&p->lo), load_once(&p->hi)}; }
-
-// Waves of a SIMD that the registers are shared by: as many as need no spills.
-constexpr int waves_per_simd(size_t bytes, int dims, int parts) {
-  if (dims > 128) return bytes < 4 && parts == 1 ? 2 : 1;
-  if (dims > 64) return parts == 1 ? 3 : 2;
-  return parts == 1 ? 4 : 3;
-}
 
 // C: type of the cache's rows.  A row of the head is CHUNKS chunks of 16 VW channels, VW of them a lane (D below that: RAGGED).  PARTS: bf16 terms of a query,
 // 1 of a bf16 one and 3 of an fp32 one, exact; keys of fp32 are multiplied in fp32.
@@ -129,11 +131,12 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNK
   constexpr int kOutBytes = 16 * 16 * VW * 4, kWaveBytes = Blk::kKeyBytes > kOutBytes ? Blk::kKeyBytes : kOutBytes;
   __shared__ __attribute__((aligned(16))) char s_mem[kWaves * kWaveBytes];
   __shared__ float s_max[kWaves][16], s_sum[kWaves][16];
+  __shared__ __attribute__((aligned(16))) float s_scale[kCodes ? kWaves : 1][2][32];
   __shared__ int s_bad;
   fetch_arguments<sizeof(AttentionArgs)>();
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), n = lane & 15, g = lane >> 4;
-  // workgroups of the same keys and values (tiles of a large group) follow each other on one XCD, of which there are 8
+  // Workgroups of the same keys and values (tiles of a large group) follow each other on one XCD, of which there are 8 that take workgroups in turn.
   const int tiles = (a.group + kHeadTile - 1) / kHeadTile;
   const int units = a.B * a.parts * a.kv_heads;
   int at = blockIdx.x, tile = 0;
@@ -200,7 +203,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNK
     }
   }
 
-  const float to_log2 = a.softcap > 0.f ? a.softcap * kLog2e : a.scale * kLog2e, in_cap = a.softcap > 0.f ? a.scale / a.softcap : 0.f;
+  const float to_log2 = a.scale * kLog2e;
   const C* const kbase = static_cast<const C*>(a.k) + (int64_t)kvh * a.head;
   const C* const vbase = static_cast<const C*>(a.v) + (int64_t)kvh * a.head;
   const int mask = (1 << a.shift) - 1;
@@ -215,28 +218,33 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNK
 
   Blk r;
   char* const keys = s_mem + wave * kWaveBytes;
+  // Behind the part's end every lane reads the first row: a load in a branch would make each wait behind it one for all loads on their way.
   auto load_keys = [&](int t0) {
+    const bool any = t0 < p.end;
 #pragma unroll
     for (int u = 0; u < kTiles; ++u) {
 #pragma unroll
       for (int s = 0; s < kLoads; s += kLoads < 4 ? kLoads : 4) {
         const int tk = t0 + 16 * u + lane / Blk::kRowLanes * kLoads + s, c = lane % Blk::kRowLanes * kVec;
-        const C* krow = kbase + (int64_t)s_page[(tk >> a.shift) - entry0] * a.page + (int64_t)(tk & mask) * a.row + c;
+        const C* krow = kbase + (any ? (int64_t)s_page[any ? (tk >> a.shift) - entry0 : 0] * a.page + (int64_t)(tk & mask) * a.row + c : 0);
 #pragma unroll
         for (int i = 0; i < (kLoads < 4 ? kLoads : 4); ++i)
           r.k[u][s + i] = !RAGGED || c < a.D ? load_once(reinterpret_cast<const typename Blk::RawK*>(krow + i * a.row)) : typename Blk::RawK{0, 0, 0, 0};
       }
-      if constexpr (kCodes) {
-        const int ts = t0 + 16 * u + 4 * g;
-        r.ks[u] = *reinterpret_cast<const f32x4*>(a.k_scale + ((((int64_t)s_page[(ts >> a.shift) - entry0] * a.kv_heads + kvh) << a.shift) + (ts & mask)));
-      }
+    }
+    if constexpr (kCodes) {
+      const int ts = t0 + lane % kBlock;
+      const int64_t at = any ? (((int64_t)s_page[(ts >> a.shift) - entry0] * a.kv_heads + kvh) << a.shift) + (ts & mask) : 0;
+      r.scale = load_once((lane < 32 ? a.k_scale : a.v_scale) + at);
     }
   };
   auto load_values = [&](int t0) {
+    const bool any = t0 < p.end;
 #pragma unroll
     for (int u = 0; u < kTiles; ++u) {
-      const int tv = t0 + 16 * u + 4 * g, page = s_page[(tv >> a.shift) - entry0];
-      const C* vrow = vbase + (int64_t)page * a.page + (int64_t)(tv & mask) * a.row + VW * n;
+      const int tv = t0 + 16 * u + 4 * g;
+      const int64_t page = s_page[any ? (tv >> a.shift) - entry0 : 0];
+      const C* vrow = vbase + (any ? page * a.page + (int64_t)(tv & mask) * a.row + VW * n : 0);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -244,7 +252,6 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNK
           const int d = 16 * VW * c;
           r.v[u][i][c] = !RAGGED || d + VW * n < a.D ? load_once(reinterpret_cast<const typename Blk::RawV*>(vrow + i * a.row + d)) : zeros(typename Blk::RawV{});
         }
-      if constexpr (kCodes) r.vs[u] = *reinterpret_cast<const f32x4*>(a.v_scale + ((((int64_t)page * a.kv_heads + kvh) << a.shift) + (tv & mask)));
     }
   };
   auto use = [&](int t0, int next) {
@@ -254,14 +261,16 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNK
     for (int u = 0; u < kTiles; ++u)
 #pragma unroll
       for (int s = 0; s < kLoads; ++s) *reinterpret_cast<typename Blk::RawK*>(keys + u * 16 * Blk::kRowLanes * 16 + Blk::place(lane / Blk::kRowLanes * kLoads + s, lane % Blk::kRowLanes)) = r.k[u][s];
-    float ks[kTiles][4];
+    f32x4 ks[kTiles], vs[kTiles];
     if constexpr (kCodes) {
+      s_scale[wave][lane / 32][lane % 32] = r.scale;
 #pragma unroll
-      for (int u = 0; u < kTiles; ++u)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) ks[u][i] = r.ks[u][i];
+      for (int u = 0; u < kTiles; ++u) {
+        ks[u] = *reinterpret_cast<const f32x4*>(&s_scale[wave][0][16 * u + 4 * g]);
+        vs[u] = *reinterpret_cast<const f32x4*>(&s_scale[wave][1][16 * u + 4 * g]);
+      }
     }
-    if (next < p.end) load_keys(next);
+    load_keys(next);
     float x[kTiles][4];
     float most = -INFINITY;
 #pragma unroll
@@ -288,9 +297,15 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNK
       for (int i = 0; i < 4; ++i) {
         float v = z[i];
         if constexpr (kCodes) v *= ks[u][i];
-        if (a.softcap > 0.f) v = tanhf(v * in_cap);
         x[u][i] = v * to_log2;
       }
+    }
+    if (a.softcap > 0.f) {                                  // cap tanh(s / cap) = cap - 2 cap / (1 + e^(2 s / cap)), off by 2^-22 of the cap
+      const float cap = a.softcap * kLog2e, twice = 2.f / a.softcap;
+#pragma unroll
+      for (int u = 0; u < kTiles; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[u][i] = cap - 2.f * cap / (1.f + __builtin_amdgcn_exp2f(x[u][i] * twice));
     }
     auto hidden = [&](int u, int i) { const int t = t0 + 16 * u + 4 * g + i; return t < first || t >= p.end; };
     if (!whole) {                                           // what is not seen counts as nothing, whatever it is
@@ -305,7 +320,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNK
       for (int i = 0; i < 4; ++i) most = fmaxf(most, x[u][i]);
     if (__any(most > top + kSlack)) {
       const float now = lane_max(fmaxf(top, most));
-      const float alpha = top == -INFINITY ? 0.f : exp2f(top - now);
+      const float alpha = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - now);
       top = now;
       sum *= alpha;
 #pragma unroll
@@ -328,7 +343,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNK
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const bool no = hidden(u, i);
-          if constexpr (kCodes) r.vs[u][i] = no ? 0.f : r.vs[u][i];
+          if constexpr (kCodes) vs[u][i] = no ? 0.f : vs[u][i];
 #pragma unroll
           for (int c = 0; c < CHUNKS; ++c) r.v[u][i][c] = no ? zeros(typename Blk::RawV{}) : r.v[u][i][c];
         }
@@ -337,7 +352,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNK
 #pragma unroll
       for (int u = 0; u < kTiles; ++u)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) e[u][i] *= r.vs[u][i];
+        for (int i = 0; i < 4; ++i) e[u][i] *= vs[u][i];
     }
     // ---- values ----
     if constexpr (kF32) {
@@ -351,34 +366,36 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNK
             for (int j = 0; j < VW; ++j)
               acc[c][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(element<C, VW>(r.v[u][i][c], j), e[u][i], acc[c][j], 0, 0, 0);
     } else {
-      // position 4 g + i of tile u is operand element 4 u + i of lane group g in both; probabilities in two bf16 terms, 2^-17 of them off
-      bf16x8 hi, lo;
+      // position 4 g + i of tile u is operand element 4 (u % 2) + i of lane group g in both; probabilities in two bf16 terms, 2^-17 of them off
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int u0 = 0; u0 < kTiles; u0 += 2) {
+        bf16x8 hi, lo;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float w = u < kTiles ? e[u < kTiles ? u : 0][i] : 0.f;
-          hi[4 * u + i] = (__bf16)w;
-          lo[4 * u + i] = (__bf16)(w - (float)hi[4 * u + i]);
-        }
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int c = 0; c < CHUNKS; ++c) {
-#pragma unroll
-        for (int j = 0; j < VW; j += 4) {
-          bf16x8 value[4];
-#pragma unroll
-          for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) widen_four<C>(r.v[u < kTiles ? u : 0][i][c], j, 4 * u + i, u < kTiles, value);
-#pragma unroll
-          for (int o = 0; o < 4; ++o) {
-            acc[c][j + o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(value[o], lo, acc[c][j + o], 0, 0, 0);
-            acc[c][j + o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(value[o], hi, acc[c][j + o], 0, 0, 0);
+          for (int i = 0; i < 4; ++i) {
+            const float w = u0 + u < kTiles ? e[u0 + u < kTiles ? u0 + u : 0][i] : 0.f;
+            hi[4 * u + i] = (__bf16)w;
+            lo[4 * u + i] = (__bf16)(w - (float)hi[4 * u + i]);
           }
-        }
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+          for (int j = 0; j < VW; j += 4) {
+            bf16x8 value[4];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) widen_four<C>(r.v[u0 + u < kTiles ? u0 + u : 0][i][c], j, 4 * u + i, u0 + u < kTiles, value);
+#pragma unroll
+            for (int o = 0; o < 4; ++o) {
+              acc[c][j + o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(value[o], lo, acc[c][j + o], 0, 0, 0);
+              acc[c][j + o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(value[o], hi, acc[c][j + o], 0, 0, 0);
+            }
+          }
       }
     }
-    if (next < p.end) load_values(next);
+    load_values(next);
   };
 
   // ---- the part's blocks in turn over the waves; keys of the next one are loaded as soon as this one's are used, and values ----
