@@ -589,6 +589,8 @@ int moe_token_logprobs(const moe_logprobs_config* cfg, const void* logits, const
  *   of the cache behind the length or before the window is used, whatever it holds.  A NaN or an infinity in a key or value that is seen gives NaN.
  *   Scores, softmax and sums are in fp32; the same call has the same bits again.
  *   ws: device scratch of moe_paged_attention_workspace_bytes(cfg, cache) bytes, 256-byte aligned (a size of 0: NULL will do).
+ *   counters: device, MOE_ATTENTION_COUNTERS bytes, zero before the first call; every call leaves them so.  With them, sequences of a few parts are joined by
+ *   the launch that computes the parts; NULL: a second one joins them.  Calls that may overlap need a workspace and counters each.
  *
  * Strides are in elements, 0 = dense; the last dimension is dense always, and heads and tokens do not overlap.  1 <= D <= 256; D and rotary_dim even; D a multiple of 16 in
  * a cache, whose memory is 16-byte aligned with strides of whole 16 bytes (scales: [n_pages, heads, page_size] dense).  page_size: a power of two from 4 to 2^20.
@@ -597,6 +599,7 @@ int moe_token_logprobs(const moe_logprobs_config* cfg, const void* logits, const
 #define MOE_ROPE_HALF 0
 #define MOE_ROPE_INTERLEAVED 1
 #define MOE_MAX_HEAD_DIM 256
+#define MOE_ATTENTION_COUNTERS 65536
 typedef struct moe_rope_config {
   int32_t T, heads, D, rotary_dim;
   int32_t dtype;     /* MOE_BF16 | MOE_FP32 */
@@ -638,7 +641,7 @@ typedef struct moe_attention_config {
 } moe_attention_config;
 size_t moe_paged_attention_workspace_bytes(const moe_attention_config* cfg, const moe_kv_cache* cache); /* 0 on a bad config too */
 int moe_paged_attention(const moe_attention_config* cfg, const moe_kv_cache* cache, const void* q, const int32_t* table, const int32_t* lengths,
-                        void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+                        void* out, float* lse, void* ws, size_t ws_bytes, int32_t* counters, void* stream);
 
 #ifdef __cplusplus
 }

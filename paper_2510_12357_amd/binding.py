@@ -25,7 +25,7 @@ MOE_MAX_SHARED = 4
 MOE_INT8_MAX_K, MOE_MAX_ALTERNATIVES, MOE_MAX_GIVEN = 131071, 32, 64
 MOE_E4M3 = 4
 MOE_ROPE_HALF, MOE_ROPE_INTERLEAVED = 0, 1
-MOE_MAX_HEAD_DIM = 256
+MOE_MAX_HEAD_DIM, MOE_ATTENTION_COUNTERS = 256, 65536
 MOE_OK = 0
 ERRORS = {-1: "MOE_E_BADARG", -2: "MOE_E_SHAPE", -3: "MOE_E_UNSUPPORTED", -4: "MOE_E_HIP",
           -5: "MOE_E_CACHE_FULL", -6: "MOE_E_WORKSPACE"}
@@ -204,7 +204,7 @@ def load_library() -> ctypes.CDLL:
     lib.moe_kv_append.argtypes = [ctypes.POINTER(moe_append_config), kvp] + [vp] * 9
     lib.moe_paged_attention_workspace_bytes.argtypes = [ctypes.POINTER(moe_attention_config), kvp]
     lib.moe_paged_attention_workspace_bytes.restype = sz
-    lib.moe_paged_attention.argtypes = [ctypes.POINTER(moe_attention_config), kvp] + [vp] * 6 + [sz, vp]
+    lib.moe_paged_attention.argtypes = [ctypes.POINTER(moe_attention_config), kvp] + [vp] * 6 + [sz, vp, vp]
     for name in ("moe_quantize_rows", "moe_matmul_int8", "moe_linear_int8", "moe_token_logprobs", "moe_rope", "moe_kv_append", "moe_paged_attention"):
         getattr(lib, name).restype = ctypes.c_int
     _lib = lib
@@ -579,10 +579,10 @@ def moe_paged_attention_workspace_bytes(cfg: moe_attention_config, cache: moe_kv
     return int(load_library().moe_paged_attention_workspace_bytes(ctypes.byref(cfg), ctypes.byref(cache)))
 
 
-def moe_paged_attention(cfg: moe_attention_config, cache: moe_kv_cache, q, table, lengths, out, lse, ws, ws_bytes: int, stream=None) -> None:
-    _on_one_gpu(q, table, lengths, out, lse, ws)
+def moe_paged_attention(cfg: moe_attention_config, cache: moe_kv_cache, q, table, lengths, out, lse, ws, ws_bytes: int, counters=None, stream=None) -> None:
+    _on_one_gpu(q, table, lengths, out, lse, ws, counters)
     _check(load_library().moe_paged_attention(ctypes.byref(cfg), ctypes.byref(cache), _heads_ptr(q), _rows(table), _ptr(lengths), _heads_ptr(out),
-                                              _ptr(lse), _ptr(ws), ws_bytes, _stream(stream)))
+                                              _ptr(lse), _ptr(ws), ws_bytes, _ptr(counters), _stream(stream)))
 
 
 # ------------------------------------------------------------------------------ plumbing helpers
@@ -1066,12 +1066,17 @@ class DecodeAttention(_Owner):
         self.cache, self.n_heads = cache, n_heads
         self.scale = 1.0 / math.sqrt(cache.head_dim) if scale is None else float(scale)
         self.window, self.softcap = int(window), float(softcap)
+        if torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("made while a graph is captured: its counters have to be zero before")
+        # zero before any stream's first call, and after each call again
+        self.counters = torch.zeros((MOE_ATTENTION_COUNTERS // 4,), dtype=torch.int32, device=cache.k.device)
+        torch.cuda.current_stream(cache.k.device).synchronize()
         self.ws = None
         self._outgrown = []                                  # workspaces of smaller calls: captured graphs have their addresses
         self._calls = {}
 
     def _memory(self):
-        return (self.ws,)
+        return self.ws, self.counters
 
     def _workspace(self, need: int, stream) -> None:
         if self.ws is not None:                              # twice as large at least: what is kept stays below the one in use
@@ -1131,7 +1136,7 @@ class DecodeAttention(_Owner):
             cache._used_on(stream, s)
         ws = self.ws
         _call_on(device, _lib.moe_paged_attention, ref, cache._ref, q.data_ptr(), table.data_ptr(), lengths.data_ptr(), out.data_ptr(),
-                 None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), s)
+                 None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), self.counters.data_ptr(), s)
         return out
 
 

@@ -94,6 +94,7 @@ int resolve(const char* call, const moe_attention_config* cfg, const moe_kv_cach
   if ((double)c->B * tiles * plan->parts >= (double)(1 << 20)) return fail(MOE_E_UNSUPPORTED, "%s: %d sequences of %d positions on %lld heads are too many workgroups", call, c->B, c->max_len, (long long)tiles);
   return MOE_OK;
 }
+static_assert(kCounters * sizeof(int32_t) == MOE_ATTENTION_COUNTERS, "the header's size");
 size_t part_floats(const moe_attention_config& c, const moe_kv_cache& cache, const SplitPlan& p) {
   return p.parts > 1 ? (size_t)c.B * p.parts * c.heads * cache.D : 0;
 }
@@ -182,7 +183,7 @@ extern "C" size_t moe_paged_attention_workspace_bytes(const moe_attention_config
 }
 
 extern "C" int moe_paged_attention(const moe_attention_config* cfg, const moe_kv_cache* cache, const void* q, const int32_t* table,
-                                   const int32_t* lengths, void* out, float* lse, void* ws, size_t ws_bytes, void* stream) {
+                                   const int32_t* lengths, void* out, float* lse, void* ws, size_t ws_bytes, int32_t* counters, void* stream) {
   const char* call = "moe_paged_attention";
   moe_kv_cache kv;
   moe_attention_config c;
@@ -197,6 +198,8 @@ extern "C" int moe_paged_attention(const moe_attention_config* cfg, const moe_kv
   if (!rc) rc = check_aligned(call, "out", out, type_bytes(c.dtype));
   if (!rc && lse) rc = check_aligned(call, "lse", lse, 4);
   if (rc) return rc;
+  if (counters) rc = check_aligned(call, "counters", counters, 4);
+  if (rc) return rc;
   const size_t need = workspace(c, kv, p);
   if (need && (!ws || ((uintptr_t)ws & 255) || ws_bytes < need))
     return fail(MOE_E_WORKSPACE, "%s: workspace %p of %zu bytes (need %zu, 256-byte aligned)", call, ws, ws_bytes, need);
@@ -209,6 +212,7 @@ extern "C" int moe_paged_attention(const moe_attention_config* cfg, const moe_kv
   a.q = q; a.table = table; a.lengths = lengths; a.k = kv.k; a.v = kv.v; a.k_scale = kv.k_scale; a.v_scale = kv.v_scale;
   a.out = out; a.lse = lse;
   if (need) {
+    if (joins_inside(c.B, kv.heads, c.heads / kv.heads, p, device_cu_count())) a.counters = counters;
     a.part_out = static_cast<float*>(ws);
     a.part_stat = reinterpret_cast<float*>(static_cast<char*>(ws) + align256(part_floats(c, kv, p) * sizeof(float)));
   }

@@ -16,4 +16,10 @@ SplitPlan plan_splits(int sequences, int kv_heads, int group, int max_len, int w
   return {(int)(each * 64), (int)((blocks + each - 1) / each)};
 }
 
+// Few workgroups: waiting until what they hand over has arrived costs each of them less than a second launch costs the call.
+bool joins_inside(int sequences, int kv_heads, int group, const SplitPlan& p, int device_cus) {
+  const int64_t units = (int64_t)sequences * kv_heads * ((group + kHeadTile - 1) / kHeadTile);
+  return p.parts <= 32 && units <= kCounters && units * p.parts <= 3 * (int64_t)device_cus;
+}
+
 }  // namespace mm

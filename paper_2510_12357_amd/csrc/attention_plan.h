@@ -46,8 +46,16 @@ MM_BOTH Part part_of(const Seen& v, int split, int s) {
   return {(int)(b < v.end ? b : v.end), (int)(e < v.end ? e : v.end)};
 }
 
+// How many parts a sequence has.
+MM_BOTH int parts_of(const Seen& v, int split) {
+  const int64_t n = (int64_t)v.end - v.first / 64 * 64;
+  return (int)((n + split - 1) / split);
+}
+
 // The split of a call: positions of a part and how many there are at most.
 struct SplitPlan { int split, parts; };
+constexpr int kCounters = 16384;         // of workgroups' ends, one per sequence, key head and head tile
+bool joins_inside(int sequences, int kv_heads, int group, const SplitPlan& p, int device_cus);
 SplitPlan plan_splits(int sequences, int kv_heads, int group, int max_len, int window, int device_cus);
 
 }  // namespace mm

@@ -210,6 +210,7 @@ struct AttentionArgs {
   const void *k, *v; const float *k_scale, *v_scale;
   void* out; float* lse;
   float *part_out, *part_stat;           // [B, parts, heads, D] and [B, parts, heads, 2] where there is more than one part
+  int32_t* counters;                     // of the parts that have ended, zero between calls; NULL: a second kernel joins the parts
 };
 int launch_attention(const AttentionArgs& a, hipStream_t s);
 

@@ -5,7 +5,8 @@
 // product with the values wants the probabilities: nothing moves between lanes.  That product runs on fp32 matrix instructions, whose operands hold one position a lane: values
 // are used as their rows lie in memory, and probabilities are not rounded.
 // The maximum that exponentials are taken against follows the scores only when one is 2^8 above it: sums stay far below fp32's range, and most blocks neither exchange
-// maxima nor rescale.  Waves' sums are joined in LDS, parts' sums by a second kernel, both in a fixed order.
+// maxima nor rescale.  Waves' sums are joined in LDS, parts' sums by the last of a sequence's workgroups or, where they are many, by a second
+// kernel, all in a fixed order.
 #include <math.h>
 
 #include <algorithm>
@@ -13,6 +14,7 @@
 
 #include "internal.h"
 #include "groups.h"
+#include "unaligned.h"
 
 namespace mm {
 namespace {
@@ -77,9 +79,18 @@ __device__ __forceinline__ float lane_sum(float v) {
 __device__ __forceinline__ float load_query(const AttentionArgs& a, int64_t at) {
   return a.dtype == MOE_FP32 ? static_cast<const float*>(a.q)[at] : (float)static_cast<const __bf16*>(a.q)[at];
 }
-__device__ __forceinline__ void store_out(const AttentionArgs& a, int64_t at, float v) {
-  if (a.dtype == MOE_FP32) static_cast<float*>(a.out)[at] = v;
-  else static_cast<__bf16*>(a.out)[at] = (__bf16)v;
+// Four channels of a result: sums v, the maximum m (log2) that they are taken against and the sum l of the exponentials; without any, zeros.
+__device__ __forceinline__ void store_row(const AttentionArgs& a, int b, int head, int channel, f32x4 v, float m, float l) {
+  const float over = l == 0.f ? 0.f : 1.f / l;
+  const int64_t at = (int64_t)b * a.out_token + (int64_t)head * a.out_head + channel;
+  v *= over;
+  if (a.dtype == MOE_FP32) {
+    store_unaligned(static_cast<float*>(a.out) + at, v);
+  } else {
+    typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+    store_unaligned(static_cast<__bf16*>(a.out) + at, __builtin_convertvector(v, bf16x4));
+  }
+  if (a.lse && channel == 0) a.lse[(int64_t)b * a.heads + head] = l == 0.f ? -INFINITY : fmaf(m, kLn2, logf(l));
 }
 
 // Tiles of 16 positions of a wave's block, and waves of a SIMD that the registers are shared by.
@@ -118,6 +129,14 @@ template <typename T>
 __device__ __forceinline__ T load_once(const T* p) { return __builtin_nontemporal_load(p); }
 __device__ __forceinline__ Eight load_once(const Eight* p) { return {load_once(&p->lo), load_once(&p->hi)}; }
 
+// What workgroups hand to each other through memory goes past their XCDs' caches.
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+__device__ __forceinline__ void hand_over(float* p, f32x2 v) {
+  __hip_atomic_store(reinterpret_cast<uint64_t*>(p), __builtin_bit_cast(uint64_t, v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ f32x2 taken_over(const float* p) {
+  return __builtin_bit_cast(f32x2, __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
 // C: type of the cache's rows.  A row of the head is CHUNKS chunks of 16 VW channels, VW of them a lane (D below that: RAGGED).  PARTS: bf16 terms of a query,
 // 1 of a bf16 one and 3 of an fp32 one, exact; keys of fp32 are multiplied in fp32.
 template <typename C, int VW, int CHUNKS, int PARTS, bool RAGGED>
@@ -182,7 +201,8 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNK
 
   const Seen seen = seen_by(a.lengths[b], a.max_len, a.window, a.table_len, a.shift);
   const Part p = part_of(seen, a.split, part);
-  if (a.parts > 1 && p.begin >= p.end) return;
+  const int parts = parts_of(seen, a.split);                // of the sequence; without any, or with one, its first workgroup has the result
+  if (part > 0 && part >= parts) return;
   const int first = max(seen.first, p.begin);
 
   // ---- pages of the part; a number outside the cache spoils the sequence ----
@@ -262,8 +282,8 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNK
 #pragma unroll
       for (int s = 0; s < kLoads; ++s) *reinterpret_cast<typename Blk::RawK*>(keys + u * 16 * Blk::kRowLanes * 16 + Blk::place(lane / Blk::kRowLanes * kLoads + s, lane % Blk::kRowLanes)) = r.k[u][s];
     f32x4 ks[kTiles], vs[kTiles];
+    if constexpr (kCodes) s_scale[wave][lane / 32][lane % 32] = r.scale;
     if constexpr (kCodes) {
-      s_scale[wave][lane / 32][lane % 32] = r.scale;
 #pragma unroll
       for (int u = 0; u < kTiles; ++u) {
         ks[u] = *reinterpret_cast<const f32x4*>(&s_scale[wave][0][16 * u + 4 * g]);
@@ -408,19 +428,20 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNK
   sum = lane_sum(sum);
   if (g == 0) { s_max[wave][n] = top; s_sum[wave][n] = sum; }
   __syncthreads();
+  const float nan = __uint_as_float(0x7fc00000u);
+  const bool bad = s_bad;
   auto joined = [&](int head, float* m, float* l) {
     *m = s_max[0][head];
 #pragma unroll
     for (int w = 1; w < kWaves; ++w) *m = fmaxf(*m, s_max[w][head]);
     *l = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) *l += s_max[w][head] == -INFINITY ? s_sum[w][head] : s_sum[w][head] * exp2f(s_max[w][head] - *m);
+    for (int w = 0; w < kWaves; ++w) *l += s_max[w][head] == -INFINITY ? s_sum[w][head] : s_sum[w][head] * __builtin_amdgcn_exp2f(s_max[w][head] - *m);
+    if (bad) *l = nan;
   };
   float m, l;
   joined(n, &m, &l);
-  const float weight = top == -INFINITY ? (sum == 0.f ? 0.f : sum) : exp2f(top - m);     // a sum without a maximum is NaN
-  const bool bad = s_bad;
-  const float nan = __uint_as_float(0x7fc00000u);
+  const float weight = top == -INFINITY ? (sum == 0.f ? 0.f : sum) : __builtin_amdgcn_exp2f(top - m);     // a sum without a maximum is NaN
   const int64_t part_row = ((int64_t)b * a.parts + part) * a.heads + head0;
 #pragma unroll
   for (int c = 0; c < CHUNKS; ++c) {
@@ -439,49 +460,85 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNK
 #pragma unroll
       for (int w = 1; w < kWaves; ++w) v += *reinterpret_cast<const f32x4*>(s_mem + w * kWaveBytes + 4 * (head * 16 * VW + d));
       joined(head, &m, &l);
-      if (bad) l = nan;
-      if (a.parts > 1) {
-        *reinterpret_cast<f32x4*>(a.part_out + (part_row + head) * a.D + channel) = v;
-        if (channel == 0) {
-          a.part_stat[2 * (part_row + head)] = l == l ? m : nan;      // a sum that is none spoils the whole row
-          a.part_stat[2 * (part_row + head) + 1] = l;
+      if (parts > 1) {
+        float* to = a.part_out + (part_row + head) * a.D + channel;
+        const f32x2 stat = {l == l ? m : nan, l};           // a sum that is none spoils the whole row
+        if (a.counters) {
+          hand_over(to, f32x2{v[0], v[1]});
+          hand_over(to + 2, f32x2{v[2], v[3]});
+          if (channel == 0) hand_over(a.part_stat + 2 * (part_row + head), stat);
+        } else {
+          *reinterpret_cast<f32x4*>(to) = v;
+          if (channel == 0) *reinterpret_cast<f32x2*>(a.part_stat + 2 * (part_row + head)) = stat;
         }
       } else {
-        const float over = l == 0.f ? 0.f : 1.f / l;
-        const int64_t to = (int64_t)b * a.out_token + (int64_t)(head0 + head) * a.out_head + channel;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) store_out(a, to + e, v[e] * over);
-        if (a.lse && channel == 0) a.lse[(int64_t)b * a.heads + head0 + head] = l == 0.f ? -INFINITY : fmaf(m, kLn2, logf(l));
+        store_row(a, b, head0 + head, channel, v, m, l);
       }
     }
   }
+  if (parts == 1 || !a.counters) return;
+
+  // ---- the last of a sequence's parts to end joins them, in their order ----
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");          // what was handed over is there
+  __syncthreads();
+  if (tid == 0) {
+    int* counter = a.counters + (b * a.kv_heads + kvh) * tiles + tile;
+    const int before = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (before == parts - 1) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);      // as the next call finds it
+    s_bad = before == parts - 1;
+  }
+  __syncthreads();
+  if (!s_bad) return;
+  const float* const stat = a.part_stat + 2 * ((int64_t)b * a.parts * a.heads + head0);
+  f32x2* const s_stat = reinterpret_cast<f32x2*>(s_mem);    // [heads][parts]: maximum, sum
+  for (int i = tid; i < heads * parts; i += kThreads) s_stat[i] = taken_over(stat + 2 * ((int64_t)(i % parts) * a.heads + i / parts));
+  __syncthreads();
+  const int vecs = a.D / 4;
+  for (int o = tid; o < heads * vecs; o += kThreads) {
+    const int head = o / vecs, channel = o % vecs * 4;
+    const f32x2* const st = s_stat + head * parts;
+    float most = -INFINITY, l = 0.f;
+    for (int i = 0; i < parts; ++i) most = fmaxf(most, st[i][0]);
+    const float* from = a.part_out + ((int64_t)b * a.parts * a.heads + head0 + head) * a.D + channel;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int i = 0; i < parts; ++i) {
+      const float w = st[i][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st[i][0] - most);
+      const f32x2 lo = taken_over(from + (int64_t)i * a.heads * a.D), hi = taken_over(from + (int64_t)i * a.heads * a.D + 2);
+      l += w * st[i][1];
+      v += w * f32x4{lo[0], lo[1], hi[0], hi[1]};
+    }
+    store_row(a, b, head0 + head, channel, v, most, l);
+  }
 }
 
-// The parts of a row (sequence, head): four channels a thread, the parts in turn over the threads of a channel; first the largest maximum.
-__global__ __launch_bounds__(kThreads) void join_kernel(const AttentionArgs a) {
-  __shared__ float s_top[kWaves];
-  __shared__ __attribute__((aligned(16))) f32x4 s_v[kThreads];
-  __shared__ float s_l[kThreads];
+// The same of sequences of many parts, a workgroup for each row (sequence, head): four channels a thread, the parts in turn over the threads of a channel.
+template <int kJoinThreads>
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(const AttentionArgs a) {
+  __shared__ float s_top[kJoinThreads / 64];
+  __shared__ __attribute__((aligned(16))) f32x4 s_v[kJoinThreads];
+  __shared__ float s_l[kJoinThreads];
   const int row = blockIdx.x, tid = threadIdx.x, b = row / a.heads, head = row - b * a.heads;
   const Seen seen = seen_by(a.lengths[b], a.max_len, a.window, a.table_len, a.shift);
-  const int parts = (seen.end - seen.first / 64 * 64 + a.split - 1) / a.split;
+  const int parts = parts_of(seen, a.split);
+  if (parts <= 1) return;
   const int64_t first = (int64_t)b * a.parts * a.heads + head;
   const float* stat = a.part_stat + 2 * first;
   const int64_t step = 2 * (int64_t)a.heads;
   float m = -INFINITY;
-  for (int i = tid; i < parts; i += kThreads) m = fmaxf(m, stat[i * step]);
+  for (int i = tid; i < parts; i += kJoinThreads) m = fmaxf(m, stat[i * step]);
   for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
   if ((tid & 63) == 0) s_top[tid >> 6] = m;
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) m = fmaxf(m, s_top[w]);
-  const int vecs = a.D / 4, turns = kThreads / vecs, turn = tid / vecs, d = tid % vecs * 4;
+  for (int w = 0; w < kJoinThreads / 64; ++w) m = fmaxf(m, s_top[w]);
+  const int vecs = a.D / 4, turns = kJoinThreads / vecs, turn = tid / vecs, d = tid % vecs * 4;
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
   float l = 0.f;
   if (turn < turns) {
-#pragma unroll 4
+#pragma unroll 8
     for (int i = turn; i < parts; i += turns) {
-      const float pm = stat[i * step], w = pm == -INFINITY ? 0.f : exp2f(pm - m);
+      const float pm = stat[i * step], w = pm == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(pm - m);
       l += w * stat[i * step + 1];
       v += w * *reinterpret_cast<const f32x4*>(a.part_out + (first + (int64_t)i * a.heads) * a.D + d);
     }
@@ -491,11 +548,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(const AttentionArgs a) {
   __syncthreads();
   if (tid >= vecs) return;
   for (int t = 1; t < turns; ++t) { v += s_v[t * vecs + tid]; l += s_l[t * vecs + tid]; }
-  if (seen.bad) l = __uint_as_float(0x7fc00000u);
-  const float over = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) store_out(a, (int64_t)b * a.out_token + (int64_t)head * a.out_head + d + e, v[e] * over);
-  if (a.lse && tid == 0) a.lse[row] = l == 0.f ? -INFINITY : fmaf(m, kLn2, logf(l));
+  store_row(a, b, head, d, v, m, l);
 }
 
 template <typename C, int VW, int CHUNKS, int PARTS>
@@ -524,8 +577,9 @@ int launch_attention(const AttentionArgs& a, hipStream_t s) {
   if (a.cache_dtype == MOE_FP32) rc = launch_parts<float, 1>(a, blocks, s);
   else if (a.cache_dtype == MOE_E4M3) rc = launch_cache<uint8_t>(a, blocks, s);
   else rc = launch_cache<__bf16>(a, blocks, s);
-  if (rc || a.parts == 1) return rc;
-  join_kernel<<<a.B * a.heads, kThreads, 0, s>>>(a);
+  if (rc || a.parts == 1 || a.counters) return rc;
+  if (a.parts > 64) join_kernel<1024><<<a.B * a.heads, 1024, 0, s>>>(a);
+  else join_kernel<256><<<a.B * a.heads, 256, 0, s>>>(a);
   return hip_fail(hipGetLastError(), "join_kernel");
 }
 

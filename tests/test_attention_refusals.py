@@ -54,8 +54,8 @@ def append(c, cache, q=P, k=P, v=P, pos=P, seq=None, table=P, freq=P, q_out=P2):
     return mm.load_library().moe_kv_append(_ref(c), _ref(cache), q, k, v, pos, seq, table, freq, q_out, None)
 
 
-def attend(c, cache, q=P, table=P, lengths=P, out=P2, lse=None, ws=None, ws_bytes=0):
-    return mm.load_library().moe_paged_attention(_ref(c), _ref(cache), q, table, lengths, out, lse, ws, ws_bytes, None)
+def attend(c, cache, q=P, table=P, lengths=P, out=P2, lse=None, ws=None, ws_bytes=0, counters=None):
+    return mm.load_library().moe_paged_attention(_ref(c), _ref(cache), q, table, lengths, out, lse, ws, ws_bytes, counters, None)
 
 
 NAN, INF = float("nan"), float("inf")
@@ -135,7 +135,7 @@ def test_attention_configs(change, code):
 
 
 @pytest.mark.parametrize("arg, value", [("q", None), ("q", P + 1), ("table", None), ("table", P + 2), ("lengths", None), ("lengths", P + 1), ("out", None),
-                                        ("out", P2 + 1), ("lse", P + 2)])
+                                        ("out", P2 + 1), ("lse", P + 2), ("counters", P + 2)])
 def test_attention_pointers(arg, value):
     assert attend(_attention(), _cache(), **{arg: value}) == BADARG and arg in mm.moe_last_error()
 
