@@ -587,7 +587,8 @@ int moe_token_logprobs(const moe_logprobs_config* cfg, const void* logits, const
  *   [B, table_ld] int32, of which table_len count; lengths device [B] int32.  Length 0, or scores that are all -inf: zeros, lse -inf.  max_len bounds the lengths (it sizes the
  *   grid): a sequence whose length is negative, above max_len or behind its table row, or that sees a page outside [0, n_pages), has NaN everywhere.  Nothing
  *   of the cache behind the length or before the window is used, whatever it holds.  A NaN or an infinity in a key or value that is seen gives NaN.
- *   Scores, softmax and sums are in fp32; the same call has the same bits again.
+ *   Scores, softmax and sums are in fp32, in an order that goes by the lengths of the whole batch: the same call has the same bits again, and the same
+ *   sequence in another batch may differ in the last bits.
  *   ws: device scratch of moe_paged_attention_workspace_bytes(cfg, cache) bytes, 256-byte aligned (a size of 0: NULL will do).
  *   counters: device, MOE_ATTENTION_COUNTERS bytes, zero before the first call; every call leaves them so.  With them, sequences of a few parts are joined by
  *   the launch that computes the parts; NULL: a second one joins them.  Calls that may overlap need a workspace and counters each.
@@ -599,7 +600,7 @@ int moe_token_logprobs(const moe_logprobs_config* cfg, const void* logits, const
 #define MOE_ROPE_HALF 0
 #define MOE_ROPE_INTERLEAVED 1
 #define MOE_MAX_HEAD_DIM 256
-#define MOE_ATTENTION_COUNTERS 65536
+#define MOE_ATTENTION_COUNTERS 16384
 typedef struct moe_rope_config {
   int32_t T, heads, D, rotary_dim;
   int32_t dtype;     /* MOE_BF16 | MOE_FP32 */

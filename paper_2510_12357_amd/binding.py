@@ -25,7 +25,7 @@ MOE_MAX_SHARED = 4
 MOE_INT8_MAX_K, MOE_MAX_ALTERNATIVES, MOE_MAX_GIVEN = 131071, 32, 64
 MOE_E4M3 = 4
 MOE_ROPE_HALF, MOE_ROPE_INTERLEAVED = 0, 1
-MOE_MAX_HEAD_DIM, MOE_ATTENTION_COUNTERS = 256, 65536
+MOE_MAX_HEAD_DIM, MOE_ATTENTION_COUNTERS = 256, 16384
 MOE_OK = 0
 ERRORS = {-1: "MOE_E_BADARG", -2: "MOE_E_SHAPE", -3: "MOE_E_UNSUPPORTED", -4: "MOE_E_HIP",
           -5: "MOE_E_CACHE_FULL", -6: "MOE_E_WORKSPACE"}

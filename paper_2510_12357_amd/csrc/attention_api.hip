@@ -75,32 +75,35 @@ int check_cache_pointers(const char* call, const moe_kv_cache& c) {
   return rc;
 }
 
-int resolve(const char* call, const moe_attention_config* cfg, const moe_kv_cache& cache, moe_attention_config* c, SplitPlan* plan) {
+int resolve(const char* call, const moe_attention_config* cfg, const moe_kv_cache& cache, moe_attention_config* c, AttentionPlan* plan) {
   if (!cfg) return fail(MOE_E_BADARG, "%s: config is NULL", call);
   *c = *cfg;
   if (c->B < 0 || c->heads <= 0) return fail(MOE_E_SHAPE, "%s: B=%d heads=%d", call, c->B, c->heads);
   if (c->heads % cache.heads) return fail(MOE_E_SHAPE, "%s: %d query heads on %d key heads", call, c->heads, cache.heads);
   if (!float_type(c->dtype)) return fail(MOE_E_BADARG, "%s: dtype %d", call, c->dtype);
   if (c->max_len < 0 || c->window < 0) return fail(MOE_E_BADARG, "%s: max_len=%d window=%d", call, c->max_len, c->window);
-  if (c->max_len > INT32_MAX - 2 * kMaxSplit) return fail(MOE_E_UNSUPPORTED, "%s: max_len=%d", call, c->max_len);
+  if (c->max_len > INT32_MAX - 2 * kMaxPiece) return fail(MOE_E_UNSUPPORTED, "%s: max_len=%d", call, c->max_len);
   if (!isfinite(c->scale) || !isfinite(c->softcap) || c->softcap < 0) return fail(MOE_E_BADARG, "%s: scale %g softcap %g", call, c->scale, c->softcap);
   if (int rc = resolve_table(call, c->B, c->table_len, &c->table_ld)) return rc;
   if (int rc = resolve_strides(call, "q", c->B, c->heads, cache.D, &c->q_token, &c->q_head)) return rc;
   if (int rc = resolve_strides(call, "out", c->B, c->heads, cache.D, &c->out_token, &c->out_head)) return rc;
   const int64_t span = (int64_t)c->table_len << page_shift(cache.page_size);
   if (span < c->max_len) c->max_len = (int)span;           // longer sequences are behind their table row
-  *plan = plan_splits(c->B, cache.heads, c->heads / cache.heads, c->max_len, c->window, device_cu_count());
-  const int64_t tiles = (int64_t)cache.heads * ((c->heads / cache.heads + kHeadTile - 1) / kHeadTile);
-  if ((double)c->B * tiles * plan->parts >= (double)(1 << 20)) return fail(MOE_E_UNSUPPORTED, "%s: %d sequences of %d positions on %lld heads are too many workgroups", call, c->B, c->max_len, (long long)tiles);
+  *plan = plan_attention(c->B, cache.heads, c->heads / cache.heads, c->max_len, c->window, attention_slots(cache.dtype, cache.D, c->dtype));
+  if (!plan->fits) return fail(MOE_E_UNSUPPORTED, "%s: %d sequences of up to %d positions on %d heads are too many", call, c->B, c->max_len, c->heads);
   return MOE_OK;
 }
-static_assert(kCounters * sizeof(int32_t) == MOE_ATTENTION_COUNTERS, "the header's size");
-size_t part_floats(const moe_attention_config& c, const moe_kv_cache& cache, const SplitPlan& p) {
-  return p.parts > 1 ? (size_t)c.B * p.parts * c.heads * cache.D : 0;
-}
-size_t workspace(const moe_attention_config& c, const moe_kv_cache& cache, const SplitPlan& p) {
-  return p.parts > 1 ? align256(part_floats(c, cache, p) * sizeof(float)) + align256((size_t)c.B * p.parts * c.heads * 2 * sizeof(float)) : 0;
-}
+static_assert(kMostWorkgroups * sizeof(int32_t) == MOE_ATTENTION_COUNTERS, "the header's size");
+// Workspace: of each workgroup two segments' sums and their statistics, and what the second kernel needs.
+struct Workspace {
+  size_t stat, started, bytes;
+  Workspace(const moe_attention_config& c, const moe_kv_cache& cache, const AttentionPlan& p) {
+    const size_t rows = (size_t)p.workgroups * 2 * (c.heads / cache.heads < kHeadTile ? c.heads / cache.heads : kHeadTile);
+    stat = align256(rows * cache.D * sizeof(float));
+    started = stat + align256(rows * 2 * sizeof(float));
+    bytes = p.split && p.workgroups > 1 ? started + align256((size_t)p.workgroups * 4 * sizeof(int32_t)) : 0;
+  }
+};
 
 }  // namespace
 }  // namespace mm
@@ -177,9 +180,9 @@ extern "C" size_t moe_paged_attention_workspace_bytes(const moe_attention_config
   const char* call = "moe_paged_attention_workspace_bytes";
   moe_kv_cache kv;
   moe_attention_config c;
-  SplitPlan p;
+  AttentionPlan p;
   if (resolve(call, cache, &kv) || resolve(call, cfg, kv, &c, &p)) return 0;
-  return workspace(c, kv, p);
+  return Workspace(c, kv, p).bytes;
 }
 
 extern "C" int moe_paged_attention(const moe_attention_config* cfg, const moe_kv_cache* cache, const void* q, const int32_t* table,
@@ -187,7 +190,7 @@ extern "C" int moe_paged_attention(const moe_attention_config* cfg, const moe_kv
   const char* call = "moe_paged_attention";
   moe_kv_cache kv;
   moe_attention_config c;
-  SplitPlan p;
+  AttentionPlan p;
   int rc = resolve(call, cache, &kv);
   if (!rc) rc = resolve(call, cfg, kv, &c, &p);
   if (rc || c.B == 0) return rc;
@@ -200,21 +203,24 @@ extern "C" int moe_paged_attention(const moe_attention_config* cfg, const moe_kv
   if (rc) return rc;
   if (counters) rc = check_aligned(call, "counters", counters, 4);
   if (rc) return rc;
-  const size_t need = workspace(c, kv, p);
+  const Workspace w(c, kv, p);
+  const size_t need = w.bytes;
   if (need && (!ws || ((uintptr_t)ws & 255) || ws_bytes < need))
     return fail(MOE_E_WORKSPACE, "%s: workspace %p of %zu bytes (need %zu, 256-byte aligned)", call, ws, ws_bytes, need);
   AttentionArgs a = {};
   a.B = c.B; a.heads = c.heads; a.kv_heads = kv.heads; a.group = c.heads / kv.heads; a.D = kv.D; a.dtype = c.dtype; a.cache_dtype = kv.dtype;
   a.max_len = c.max_len; a.window = c.window; a.table_len = c.table_len; a.table_ld = c.table_ld; a.n_pages = kv.n_pages; a.shift = page_shift(kv.page_size);
-  a.split = p.split; a.parts = p.parts; a.scale = c.scale; a.softcap = c.softcap;
+  a.workgroups = p.workgroups; a.scale = c.scale; a.softcap = c.softcap;
   a.q_token = c.q_token; a.q_head = c.q_head; a.out_token = c.out_token; a.out_head = c.out_head;
   a.page = kv.page; a.head = kv.head; a.row = kv.row;
   a.q = q; a.table = table; a.lengths = lengths; a.k = kv.k; a.v = kv.v; a.k_scale = kv.k_scale; a.v_scale = kv.v_scale;
   a.out = out; a.lse = lse;
   if (need) {
-    if (joins_inside(c.B, kv.heads, c.heads / kv.heads, p, device_cu_count())) a.counters = counters;
+    char* const at = static_cast<char*>(ws);
     a.part_out = static_cast<float*>(ws);
-    a.part_stat = reinterpret_cast<float*>(static_cast<char*>(ws) + align256(part_floats(c, kv, p) * sizeof(float)));
+    a.part_stat = reinterpret_cast<float*>(at + w.stat);
+    if (p.few_parts) a.counters = counters;
+    if (!a.counters) a.started = reinterpret_cast<int32_t*>(at + w.started);
   }
   return launch_attention(a, static_cast<hipStream_t>(stream));
 }

@@ -13,7 +13,8 @@
 namespace mm {
 
 constexpr int kMinPage = 4;              // four neighbouring positions that start at a multiple of four are in one page
-constexpr int kMaxSplit = 4096;          // positions of a workgroup: its pages' numbers stay in LDS
+constexpr int kSpan = 64;                // positions of the blocks that work is counted in
+constexpr int kMaxPiece = 4096;          // positions whose pages' numbers a workgroup has in LDS at once
 constexpr int kHeadTile = 16;            // query heads of a workgroup, the columns of a matrix instruction
 
 // log2 of the page size; -1 where it is none of 4, 8, 16 ..
@@ -39,23 +40,47 @@ MM_BOTH Seen seen_by(int length, int max_len, int window, int table_len, int shi
   return {window > 0 && length > window ? length - window : 0, length, false};
 }
 
-// Part s of what a token sees, in positions: parts are `split` long (a multiple of 64) and start at multiples of 64.
-struct Part { int begin, end; };
-MM_BOTH Part part_of(const Seen& v, int split, int s) {
-  const int64_t base = v.first / 64 * 64, b = base + (int64_t)s * split, e = b + split;
-  return {(int)(b < v.end ? b : v.end), (int)(e < v.end ? e : v.end)};
+// Its blocks, of which the first one may begin before what is seen.
+MM_BOTH int blocks_of(const Seen& v) { return (int)(((int64_t)v.end - v.first / kSpan * kSpan + kSpan - 1) / kSpan); }
+
+// All work of a call is a line of blocks: sequence by sequence, of each its units (a tile of query heads on a key head), of each unit kSetup blocks that stand for what it takes
+// to begin and end one, and its own.  Workgroup w has the blocks [w each, (w + 1) each) of the line, a row of segments, each of one unit.  A unit whose own blocks lie in
+// several workgroups has its parts joined.
+constexpr int kSetup = 4;
+MM_BOTH int line_blocks(int n) { return n > 0 ? n + kSetup : 0; }
+MM_BOTH int blocks_each(int total, int workgroups, int least) {
+  const int n = (int)(((int64_t)total + workgroups - 1) / workgroups);
+  return n > least ? n : least;
+}
+struct Segment {
+  int unit;                              // of the sequence
+  int length;                            // on the line
+  int block, blocks;                     // of the unit's own, from where on, and how many
+  int workgroup, parts;                  // that has the unit's first block, and how many have any
+};
+// The segment at place `at` of the line for a workgroup whose share ends at `end`; the sequence begins at `line` and has n > 0 blocks a unit.
+MM_BOTH Segment segment_at(int line, int n, int at, int end, int each) {
+  Segment s;
+  s.unit = (at - line) / (n + kSetup);
+  const int begin = line + s.unit * (n + kSetup), own = begin + kSetup, behind = own + n;
+  const int stop = behind < end ? behind : end, start = at > own ? at : own;
+  s.length = stop - at;
+  s.block = start - own;
+  s.blocks = stop > start ? stop - start : 0;
+  s.workgroup = own / each;
+  s.parts = (behind - 1) / each - s.workgroup + 1;
+  return s;
 }
 
-// How many parts a sequence has.
-MM_BOTH int parts_of(const Seen& v, int split) {
-  const int64_t n = (int64_t)v.end - v.first / 64 * 64;
-  return (int)((n + split - 1) / split);
-}
-
-// The split of a call: positions of a part and how many there are at most.
-struct SplitPlan { int split, parts; };
-constexpr int kCounters = 16384;         // of workgroups' ends, one per sequence, key head and head tile
-bool joins_inside(int sequences, int kv_heads, int group, const SplitPlan& p, int device_cus);
-SplitPlan plan_splits(int sequences, int kv_heads, int group, int max_len, int window, int device_cus);
+// What the host knows of a call.
+constexpr int kLeastBlocks = 8;          // of a workgroup, on the line
+constexpr int kMostWorkgroups = 4096;
+struct AttentionPlan {
+  bool fits;                             // the line's length in 31 bits
+  int workgroups;
+  bool split;                            // a unit may lie in several workgroups
+  bool few_parts;                        // units are expected to lie in so few that the last one to end joins them; else a second kernel
+};
+AttentionPlan plan_attention(int sequences, int kv_heads, int group, int max_len, int window, int slots);
 
 }  // namespace mm

@@ -201,7 +201,7 @@ struct RotaryArgs {
 int launch_rotary(const RotaryArgs& a, int dtype, hipStream_t s);
 struct AttentionArgs {
   int B, heads, kv_heads, group, D, dtype, cache_dtype;
-  int max_len, window, table_len, n_pages, shift, split, parts;
+  int max_len, window, table_len, n_pages, shift, workgroups;
   int64_t table_ld;
   float scale, softcap;
   int64_t q_token, q_head, out_token, out_head;
@@ -209,9 +209,11 @@ struct AttentionArgs {
   const void* q; const int32_t *table, *lengths;
   const void *k, *v; const float *k_scale, *v_scale;
   void* out; float* lse;
-  float *part_out, *part_stat;           // [B, parts, heads, D] and [B, parts, heads, 2] where there is more than one part
+  float *part_out, *part_stat;           // [workgroups, 2, tile heads, D] and [workgroups, 2, tile heads, 2]: a workgroup's first segment, and its last one
   int32_t* counters;                     // of the parts that have ended, zero between calls; NULL: a second kernel joins the parts
+  int32_t* started;                      // [workgroups, 4] for it: sequence, unit and parts of the unit that begins in a workgroup and ends in another one
 };
+int attention_slots(int cache_dtype, int D, int dtype);      // workgroups that the device runs at once
 int launch_attention(const AttentionArgs& a, hipStream_t s);
 
 }  // namespace mm

@@ -1,6 +1,7 @@
 // Attention of one new token per sequence over a paged cache (moe_paged_attention).
 //
-// A workgroup has a part of a sequence's positions, one key head and up to 16 of its query heads; its waves take blocks of the part's positions in turn.
+// The positions that all sequences' tokens see, for each key head and up to 16 of its query heads, are a line of blocks that workgroups share equally, as many as run at once
+// (attention_plan.h); of a workgroup's segments, each of one sequence and key head, its waves take blocks in turn.
 // Scores are the product of a tile of keys (rows: positions) and the queries (columns: heads), so that a lane has four positions of one head, which is where the
 // product with the values wants the probabilities: nothing moves between lanes.  That product runs on fp32 matrix instructions, whose operands hold one position a lane: values
 // are used as their rows lie in memory, and probabilities are not rounded.
@@ -22,7 +23,7 @@ namespace {
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 constexpr float kSlack = 8.f;                               // how far (log2) scores may be above the maximum in use
-constexpr int kMaxPages = kMaxSplit / kMinPage;
+constexpr int kMaxPages = kMaxPiece / kMinPage;
 
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) int i32x4;
@@ -68,6 +69,17 @@ __device__ __forceinline__ void widen_four(const R& v, int j, int at, bool there
   to[0][at] = a[0]; to[1][at] = a[1]; to[2][at] = b[0]; to[3][at] = b[1];
 }
 
+// Sums over a wave's lanes up to each, and over all, on the data-parallel primitives: rows of 16, lane 15 of a row into the next one, lane 31 into rows 2 and 3.
+__device__ __forceinline__ int wave_sums(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);
+  return v + __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+}
+__device__ __forceinline__ int wave_total(int v) { return __builtin_amdgcn_readlane(wave_sums(v), 63); }
+
 __device__ __forceinline__ float lane_max(float v) {        // over the four lanes of a column
   v = fmaxf(v, __shfl_xor(v, 16));
   return fmaxf(v, __shfl_xor(v, 32));
@@ -76,9 +88,19 @@ __device__ __forceinline__ float lane_sum(float v) {
   v += __shfl_xor(v, 16);
   return v + __shfl_xor(v, 32);
 }
-__device__ __forceinline__ float load_query(const AttentionArgs& a, int64_t at) {
-  return a.dtype == MOE_FP32 ? static_cast<const float*>(a.q)[at] : (float)static_cast<const __bf16*>(a.q)[at];
+typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+typedef __attribute__((ext_vector_type(8))) float f32x8;
+template <typename V>
+__device__ __forceinline__ V load_queries(const AttentionArgs& a, int64_t at) {
+  if (a.dtype == MOE_FP32) return load_unaligned<V>(static_cast<const float*>(a.q) + at);
+  return __builtin_convertvector(load_unaligned<bf16x4>(static_cast<const __bf16*>(a.q) + at), V);
 }
+// The first head's row of what a workgroup has of a unit that lies in several: of the one that begins there, its last segment, or else of its first one.
+__device__ __forceinline__ int64_t part_at(const AttentionArgs& a, int workgroup, bool begins) {
+  return (2 * (int64_t)workgroup + begins) * min(a.group, kHeadTile);
+}
+__device__ __forceinline__ int line_place(int block, int) { return block; }
+
 // Four channels of a result: sums v, the maximum m (log2) that they are taken against and the sum l of the exponentials; without any, zeros.
 __device__ __forceinline__ void store_row(const AttentionArgs& a, int b, int head, int channel, f32x4 v, float m, float l) {
   const float over = l == 0.f ? 0.f : 1.f / l;
@@ -87,7 +109,6 @@ __device__ __forceinline__ void store_row(const AttentionArgs& a, int b, int hea
   if (a.dtype == MOE_FP32) {
     store_unaligned(static_cast<float*>(a.out) + at, v);
   } else {
-    typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
     store_unaligned(static_cast<__bf16*>(a.out) + at, __builtin_convertvector(v, bf16x4));
   }
   if (a.lse && channel == 0) a.lse[(int64_t)b * a.heads + head] = l == 0.f ? -INFINITY : fmaf(m, kLn2, logf(l));
@@ -97,8 +118,8 @@ __device__ __forceinline__ void store_row(const AttentionArgs& a, int b, int hea
 constexpr int block_tiles(size_t bytes, int dims) { return std::clamp(512 / (int)(dims * bytes), 1, 2); }
 constexpr int waves_per_simd(size_t bytes, int dims, int parts) {
   if (dims > 128) return bytes < 4 && parts == 1 ? 2 : 1;
-  if (dims > 64) return parts == 1 && bytes < 4 ? 3 : 2;
-  return parts == 1 && bytes == 2 ? 4 : 3;
+  if (dims > 64) return parts == 1 && bytes == 1 ? 3 : 2;
+  return parts == 1 && bytes <= 2 ? 4 : 3;
 }
 
 // A wave's block of positions, and what its lanes load of it: values of positions 4 g .. 4 g + 3 of a tile, as the product with them wants them, and keys by whole
@@ -151,82 +172,101 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNK
   __shared__ __attribute__((aligned(16))) char s_mem[kWaves * kWaveBytes];
   __shared__ float s_max[kWaves][16], s_sum[kWaves][16];
   __shared__ __attribute__((aligned(16))) float s_scale[kCodes ? kWaves : 1][2][32];
-  __shared__ int s_bad;
+  __shared__ int s_bad, s_last;
   fetch_arguments<sizeof(AttentionArgs)>();
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), n = lane & 15, g = lane >> 4;
-  // Workgroups of the same keys and values (tiles of a large group) follow each other on one XCD, of which there are 8 that take workgroups in turn.
-  const int tiles = (a.group + kHeadTile - 1) / kHeadTile;
-  const int units = a.B * a.parts * a.kv_heads;
-  int at = blockIdx.x, tile = 0;
-  if (tiles > 1) {
-    const int eighth = at / 8, full = units / 8 * 8;
-    if (at < full * tiles) { tile = eighth % tiles; at = eighth / tiles * 8 + at % 8; }
-    else { const int rest = at - full * tiles; tile = rest % tiles; at = full + rest / tiles; }
-  }
-  const int kvh = at % a.kv_heads; at /= a.kv_heads;
-  const int part = at % a.parts, b = at / a.parts;
-  const int heads = min(kHeadTile, a.group - tile * kHeadTile), head0 = kvh * a.group + tile * kHeadTile;
+  const int tiles = (a.group + kHeadTile - 1) / kHeadTile, units = a.kv_heads * tiles;
+  const int workgroup = line_place(blockIdx.x, a.workgroups);
+  auto seen_with = [&](int length) { return seen_by(length, a.max_len, a.window, a.table_len, a.shift); };
+  auto seen_of = [&](int b) { return seen_with(uniform(a.lengths[b])); };       // b: the same in all lanes
 
-  // ---- loads that depend on nothing: queries, and without a window the first pages' numbers ----
+  // ---- the line: its length, and the sequence in which this workgroup's share begins; every wave by itself ----
+  int cursor, finish, each, b = 0, line = 0;
+  {
+    const int lane = threadIdx.x & 63;
+    auto on_line = [&](int i) { return i < a.B ? line_blocks(blocks_of(seen_with(a.lengths[i]))) * units : 0; };
+    const int first_64 = on_line(lane);
+    int total = first_64;
+    for (int i = lane + 64; i < a.B; i += 64) total += on_line(i);
+    total = wave_total(total);
+    each = blocks_each(total, a.workgroups, kLeastBlocks);
+    cursor = min(total, workgroup * each);
+    finish = min(total, cursor + each);
+    if (cursor < finish)
+      for (;; b += 64) {                                    // ends at the sequence that holds the place
+        const int n = b ? on_line(b + lane) : first_64, upto = line + wave_sums(n);
+        const uint64_t behind = __ballot(cursor < upto);
+        if (behind) {
+          const int at = __builtin_ctzll(behind);
+          line = __builtin_amdgcn_readlane(upto - n, at);
+          b += at;
+          break;
+        }
+        line = __builtin_amdgcn_readlane(upto, 63);
+      }
+  }
+  // ---- sequences without anything to see, or of a length that there is not ----
+  for (int e = blockIdx.x; e < a.B; e += a.workgroups) {
+    const Seen v = seen_of(e);
+    if (v.first < v.end) continue;
+    const float l = v.bad ? __uint_as_float(0x7fc00000u) : 0.f;
+    for (int i = threadIdx.x; i < a.heads * a.D / 4; i += kThreads)
+      store_row(a, e, i / (a.D / 4), i % (a.D / 4) * 4, f32x4{0.f, 0.f, 0.f, 0.f}, -INFINITY, l);
+  }
+  if (a.started && threadIdx.x < 4) a.started[4 * workgroup + threadIdx.x] = 0;
+  if (cursor >= finish) return;
+  int length = uniform(a.lengths[b]);
+  int listed_b = -1, listed_from = 0, listed_to = 0;        // whose pages' numbers are in LDS
+
+  // ================= the segments of the share =================
+  while (true) {
+  // what follows from the lane is worked out anew for each segment: held over all of them it would not leave registers enough
+  const int wave = uniform(threadIdx.x >> 6);
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));
+  const int lane = tid & 63, n = lane & 15, g = lane >> 4;
+  const Seen seen = seen_with(length);
+  const int next_length = a.lengths[min(b + 1, a.B - 1)];   // on its way meanwhile
+  const Segment seg = segment_at(line, blocks_of(seen), cursor, finish, each);
+  if (seg.blocks) {
+  const int tile = seg.unit % tiles, kvh = seg.unit / tiles;
+  const int heads = min(kHeadTile, a.group - tile * kHeadTile), head0 = kvh * a.group + tile * kHeadTile;
   const int32_t* const row = a.table + b * a.table_ld;
-  int early = -1;
-  if (a.window == 0) early = row[min((int)(((int64_t)part * a.split) >> a.shift) + tid, a.table_len - 1)];
   bf16x8 qf[kF32 ? 1 : PARTS][kSteps];
   float q32[kF32 ? kDims / 4 : 1];
   {
     const int64_t q_at = (int64_t)b * a.q_token + (int64_t)(head0 + min(n, heads - 1)) * a.q_head;
     if constexpr (kF32) {
 #pragma unroll
-      for (int i = 0; i < kDims / 4; ++i) {
-        const int d = 16 * (i / 4) + 4 * g + i % 4;
-        q32[i] = n < heads && (!RAGGED || d < a.D) ? load_query(a, q_at + d) : 0.f;
+      for (int i = 0; i < kDims / 4; i += 4) {
+        const int d = 4 * i + 4 * g;
+        const f32x4 q = n < heads && (!RAGGED || d < a.D) ? load_queries<f32x4>(a, q_at + d) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) q32[i + e] = q[e];
       }
     } else {
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int d = kCodes ? 64 * (s / 2) + 16 * g + 8 * (s % 2) + e : 32 * s + 8 * g + e;      // the order of the keys' loads
-          float q = n < heads && (!RAGGED || d < a.D) ? load_query(a, q_at + d) : 0.f;
+      for (int s = 0; s < kSteps; ++s) {
+        const int d = kCodes ? 64 * (s / 2) + 16 * g + 8 * (s % 2) : 32 * s + 8 * g;      // the order of the keys' vectors
+        const bool there = n < heads && (!RAGGED || d < a.D);
+        if constexpr (PARTS == 1) {
+          qf[0][s] = there ? load_unaligned<bf16x8>(static_cast<const __bf16*>(a.q) + q_at + d) : bf16x8{};
+        } else {
+          f32x8 q = there ? load_unaligned<f32x8>(static_cast<const float*>(a.q) + q_at + d) : f32x8{};
 #pragma unroll
           for (int t = 0; t < PARTS; ++t) {
-            const __bf16 r = (__bf16)q;
-            qf[t][s][e] = r;
-            q -= (float)r;
+            qf[t][s] = __builtin_convertvector(q, bf16x8);
+            q -= __builtin_convertvector(qf[t][s], f32x8);
           }
         }
-    }
-  }
-
-  const Seen seen = seen_by(a.lengths[b], a.max_len, a.window, a.table_len, a.shift);
-  const Part p = part_of(seen, a.split, part);
-  const int parts = parts_of(seen, a.split);                // of the sequence; without any, or with one, its first workgroup has the result
-  if (part > 0 && part >= parts) return;
-  const int first = max(seen.first, p.begin);
-
-  // ---- pages of the part; a number outside the cache spoils the sequence ----
-  const int entry0 = p.begin >> a.shift;
-  if (tid == 0) s_bad = seen.bad;
-  __syncthreads();
-  if (p.begin < p.end) {
-    const int entries = ((p.begin + a.split - 1) >> a.shift) - entry0 + 1;
-    for (int i = tid; i < entries; i += kThreads) {
-      const int64_t from = (int64_t)(entry0 + i) << a.shift;
-      int page = 0;                                         // of positions that are not seen: any
-      if (from < p.end && from + ((int64_t)1 << a.shift) > first) {
-        if (a.window == 0 && i == tid) page = entry0 + i < a.table_len && early >= 0 && early < a.n_pages ? early : -1;
-        else page = page_of(row, a.table_len, a.n_pages, a.shift, from);
       }
-      if (page < 0) { s_bad = 1; page = 0; }
-      s_page[i] = page;
     }
   }
-
   const float to_log2 = a.scale * kLog2e;
   const C* const kbase = static_cast<const C*>(a.k) + (int64_t)kvh * a.head;
   const C* const vbase = static_cast<const C*>(a.v) + (int64_t)kvh * a.head;
   const int mask = (1 << a.shift) - 1;
+  char* const keys = s_mem + wave * kWaveBytes;
 
   float top = -INFINITY, sum = 0.f;
   f32x4 acc[CHUNKS][VW];
@@ -234,10 +274,40 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNK
   for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
     for (int j = 0; j < VW; ++j) acc[c][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  bool bad = false;
+
+  // ---- pieces of the segment, as long as LDS has room for their pages' numbers ----
+  const int segment_begin = (seen.first / kSpan + seg.block) * kSpan, segment_end = (int)min((int64_t)seen.end, (int64_t)segment_begin + (int64_t)seg.blocks * kSpan);
+  for (int piece = segment_begin; piece < segment_end; piece += kMaxPiece) {
+  const struct { int begin, end; } p = {piece, (int)min((int64_t)segment_end, (int64_t)piece + kMaxPiece)};
+  const int first = max(seen.first, p.begin), entry0 = p.begin >> a.shift, entries = (((p.end - 1) | (kSpan - 1)) >> a.shift) - entry0 + 1;
   __syncthreads();
+  if (b != listed_b || p.begin != listed_from || p.end != listed_to) {      // the next key head's are the same
+  listed_b = b; listed_from = p.begin; listed_to = p.end;
+  if (tid == 0) s_bad = 0;
+  __syncthreads();
+  for (int i = tid; i < entries; i += kThreads) {
+    const int64_t from = (int64_t)(entry0 + i) << a.shift;
+    int page = 0;                                           // of positions that are not seen: any
+    if (from < p.end && from + ((int64_t)1 << a.shift) > first) page = page_of(row, a.table_len, a.n_pages, a.shift, from);
+    if (page < 0) { s_bad = 1; page = 0; }                  // a number outside the cache spoils the sequence
+    s_page[i] = page;
+  }
+  __syncthreads();
+  }
+  bad |= s_bad;
 
   Blk r;
-  char* const keys = s_mem + wave * kWaveBytes;
+  // The queries are here before the loop begins, so that no wait for them stands in it.
+  if constexpr (kF32) {
+#pragma unroll
+    for (int i = 0; i < kDims / 4; ++i) asm volatile("" : "+v"(q32[i]));
+  } else {
+#pragma unroll
+    for (int t = 0; t < PARTS; ++t)
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) asm volatile("" : "+v"(qf[t][s]));
+  }
   // Behind the part's end every lane reads the first row: a load in a branch would make each wait behind it one for all loads on their way.
   auto load_keys = [&](int t0) {
     const bool any = t0 < p.end;
@@ -418,18 +488,22 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNK
     load_values(next);
   };
 
-  // ---- the part's blocks in turn over the waves; keys of the next one are loaded as soon as this one's are used, and values ----
+  // ---- the piece's blocks in turn over the waves; keys of the next one are loaded as soon as this one's are used, and values ----
   constexpr int kStride = kWaves * kBlock;
   int t0 = p.begin + (first - p.begin) / kBlock * kBlock + wave * kBlock;
   if (t0 < p.end) { load_keys(t0); load_values(t0); }
   for (; t0 < p.end; t0 += kStride) use(t0, t0 + kStride);
+  }
 
   // ---- join the waves ----
+  {
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));
+  const int lane = tid & 63, n = lane & 15, g = lane >> 4;
   sum = lane_sum(sum);
   if (g == 0) { s_max[wave][n] = top; s_sum[wave][n] = sum; }
   __syncthreads();
   const float nan = __uint_as_float(0x7fc00000u);
-  const bool bad = s_bad;
   auto joined = [&](int head, float* m, float* l) {
     *m = s_max[0][head];
 #pragma unroll
@@ -442,7 +516,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNK
   float m, l;
   joined(n, &m, &l);
   const float weight = top == -INFINITY ? (sum == 0.f ? 0.f : sum) : __builtin_amdgcn_exp2f(top - m);     // a sum without a maximum is NaN
-  const int64_t part_row = ((int64_t)b * a.parts + part) * a.heads + head0;
+  const int64_t part_row = part_at(a, workgroup, seg.block == 0);
 #pragma unroll
   for (int c = 0; c < CHUNKS; ++c) {
     if (c) __syncthreads();
@@ -460,7 +534,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNK
 #pragma unroll
       for (int w = 1; w < kWaves; ++w) v += *reinterpret_cast<const f32x4*>(s_mem + w * kWaveBytes + 4 * (head * 16 * VW + d));
       joined(head, &m, &l);
-      if (parts > 1) {
+      if (seg.parts > 1) {
         float* to = a.part_out + (part_row + head) * a.D + channel;
         const f32x2 stat = {l == l ? m : nan, l};           // a sum that is none spoils the whole row
         if (a.counters) {
@@ -476,57 +550,82 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNK
       }
     }
   }
-  if (parts == 1 || !a.counters) return;
-
-  // ---- the last of a sequence's parts to end joins them, in their order ----
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");          // what was handed over is there
-  __syncthreads();
-  if (tid == 0) {
-    int* counter = a.counters + (b * a.kv_heads + kvh) * tiles + tile;
-    const int before = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (before == parts - 1) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);      // as the next call finds it
-    s_bad = before == parts - 1;
-  }
-  __syncthreads();
-  if (!s_bad) return;
-  const float* const stat = a.part_stat + 2 * ((int64_t)b * a.parts * a.heads + head0);
-  f32x2* const s_stat = reinterpret_cast<f32x2*>(s_mem);    // [heads][parts]: maximum, sum
-  for (int i = tid; i < heads * parts; i += kThreads) s_stat[i] = taken_over(stat + 2 * ((int64_t)(i % parts) * a.heads + i / parts));
-  __syncthreads();
-  const int vecs = a.D / 4;
-  for (int o = tid; o < heads * vecs; o += kThreads) {
-    const int head = o / vecs, channel = o % vecs * 4;
-    const f32x2* const st = s_stat + head * parts;
-    float most = -INFINITY, l = 0.f;
-    for (int i = 0; i < parts; ++i) most = fmaxf(most, st[i][0]);
-    const float* from = a.part_out + ((int64_t)b * a.parts * a.heads + head0 + head) * a.D + channel;
-    f32x4 v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-    for (int i = 0; i < parts; ++i) {
-      const float w = st[i][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st[i][0] - most);
-      const f32x2 lo = taken_over(from + (int64_t)i * a.heads * a.D), hi = taken_over(from + (int64_t)i * a.heads * a.D + 2);
-      l += w * st[i][1];
-      v += w * f32x4{lo[0], lo[1], hi[0], hi[1]};
+  if (seg.parts > 1 && a.counters) {
+    // ---- the last of a unit's parts to end joins them, in their order ----
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");        // what was handed over is there
+    __syncthreads();
+    if (tid == 0) {
+      int* counter = a.counters + seg.workgroup;
+      const int ended = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1;
+      if (ended == seg.parts) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);     // as the next call finds it
+      s_last = ended == seg.parts;
     }
-    store_row(a, b, head0 + head, channel, v, most, l);
+    __syncthreads();
+    if (s_last) {
+      const int vecs = a.D / 4;
+      for (int o = tid; o < heads * vecs; o += kThreads) {
+        const int head = o / vecs, channel = o % vecs * 4;
+        float most = -INFINITY, l = 0.f;
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+        constexpr int kAhead = 8;
+        for (int i0 = 0; i0 < seg.parts; i0 += kAhead) {
+          f32x2 st[kAhead], lo[kAhead], hi[kAhead];
+#pragma unroll
+          for (int i = 0; i < kAhead; ++i) {
+            const int part = min(i0 + i, seg.parts - 1);
+            const int64_t at = part_at(a, seg.workgroup + part, part == 0) + head;
+            st[i] = taken_over(a.part_stat + 2 * at);
+            lo[i] = taken_over(a.part_out + at * a.D + channel);
+            hi[i] = taken_over(a.part_out + at * a.D + channel + 2);
+          }
+          float now = most;
+#pragma unroll
+          for (int i = 0; i < kAhead; ++i) now = fmaxf(now, st[i][0]);
+          const float alpha = most == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(most - now);
+          most = now;
+          l = l == l ? l * alpha : l;
+          v *= alpha;
+#pragma unroll
+          for (int i = 0; i < kAhead; ++i) {
+            const float w = i0 + i >= seg.parts || st[i][0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st[i][0] - most);
+            if (i0 + i < seg.parts) l += w * st[i][1];
+            v += w * f32x4{lo[i][0], lo[i][1], hi[i][0], hi[i][1]};
+          }
+        }
+        store_row(a, b, head0 + head, channel, v, most, l);
+      }
+    }
+  }
+  if (seg.parts > 1 && seg.block == 0 && a.started && tid < 4) a.started[4 * workgroup + tid] = tid == 0 ? seg.parts : tid == 1 ? b : tid == 2 ? seg.unit : 0;
+  }
+
+  __syncthreads();
+  }
+  cursor += seg.length;
+  if (cursor >= finish) break;
+  const int behind = line + line_blocks(blocks_of(seen)) * units;
+  if (cursor >= behind) {
+    line = behind;
+    ++b;
+    length = uniform(next_length);
+    while (blocks_of(seen_with(length)) == 0) length = uniform(a.lengths[++b]);
+  }
   }
 }
 
-// The same of sequences of many parts, a workgroup for each row (sequence, head): four channels a thread, the parts in turn over the threads of a channel.
+// The same of units of many parts: a workgroup for each workgroup of the first kernel in which a unit begins that ends in another one, and for each of its heads; four channels
+// a thread, the parts in turn over the threads of a channel.
 template <int kJoinThreads>
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(const AttentionArgs a) {
   __shared__ float s_top[kJoinThreads / 64];
   __shared__ __attribute__((aligned(16))) f32x4 s_v[kJoinThreads];
   __shared__ float s_l[kJoinThreads];
-  const int row = blockIdx.x, tid = threadIdx.x, b = row / a.heads, head = row - b * a.heads;
-  const Seen seen = seen_by(a.lengths[b], a.max_len, a.window, a.table_len, a.shift);
-  const int parts = parts_of(seen, a.split);
-  if (parts <= 1) return;
-  const int64_t first = (int64_t)b * a.parts * a.heads + head;
-  const float* stat = a.part_stat + 2 * first;
-  const int64_t step = 2 * (int64_t)a.heads;
+  const int tid = threadIdx.x, workgroup = blockIdx.x, parts = a.started[4 * workgroup], b = a.started[4 * workgroup + 1], unit = a.started[4 * workgroup + 2];
+  const int tiles = (a.group + kHeadTile - 1) / kHeadTile, tile = unit % tiles, h = blockIdx.y, head = unit / tiles * a.group + tile * kHeadTile + h;
+  if (parts == 0 || h >= a.group - tile * kHeadTile) return;
+  auto at = [&](int part) { return part_at(a, workgroup + part, part == 0) + h; };
   float m = -INFINITY;
-  for (int i = tid; i < parts; i += kJoinThreads) m = fmaxf(m, stat[i * step]);
+  for (int i = tid; i < parts; i += kJoinThreads) m = fmaxf(m, a.part_stat[2 * at(i)]);
   for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
   if ((tid & 63) == 0) s_top[tid >> 6] = m;
   __syncthreads();
@@ -538,9 +637,10 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const AttentionArgs 
   if (turn < turns) {
 #pragma unroll 8
     for (int i = turn; i < parts; i += turns) {
-      const float pm = stat[i * step], w = pm == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(pm - m);
-      l += w * stat[i * step + 1];
-      v += w * *reinterpret_cast<const f32x4*>(a.part_out + (first + (int64_t)i * a.heads) * a.D + d);
+      const f32x2 st = *reinterpret_cast<const f32x2*>(a.part_stat + 2 * at(i));
+      const float w = st[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st[0] - m);
+      l += w * st[1];
+      v += w * *reinterpret_cast<const f32x4*>(a.part_out + at(i) * a.D + d);
     }
   }
   s_v[tid] = v;
@@ -552,34 +652,37 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const AttentionArgs 
 }
 
 template <typename C, int VW, int CHUNKS, int PARTS>
-int launch_dims(const AttentionArgs& a, int blocks, hipStream_t s) {
-  if (a.D < 16 * VW * CHUNKS) attention_kernel<C, VW, CHUNKS, PARTS, true><<<blocks, kThreads, 0, s>>>(a);
-  else attention_kernel<C, VW, CHUNKS, PARTS, false><<<blocks, kThreads, 0, s>>>(a);
+int launch_dims(const AttentionArgs& a, hipStream_t s) {
+  if (a.D < 16 * VW * CHUNKS) attention_kernel<C, VW, CHUNKS, PARTS, true><<<a.workgroups, kThreads, 0, s>>>(a);
+  else attention_kernel<C, VW, CHUNKS, PARTS, false><<<a.workgroups, kThreads, 0, s>>>(a);
   return hip_fail(hipGetLastError(), "attention_kernel");
 }
 template <typename C, int PARTS>
-int launch_parts(const AttentionArgs& a, int blocks, hipStream_t s) {
-  if (a.D <= 64) return launch_dims<C, 4, 1, PARTS>(a, blocks, s);
-  if (a.D <= 128) return launch_dims<C, 8, 1, PARTS>(a, blocks, s);
-  return launch_dims<C, 8, 2, PARTS>(a, blocks, s);
+int launch_parts(const AttentionArgs& a, hipStream_t s) {
+  if (a.D <= 64) return launch_dims<C, 4, 1, PARTS>(a, s);
+  if (a.D <= 128) return launch_dims<C, 8, 1, PARTS>(a, s);
+  return launch_dims<C, 8, 2, PARTS>(a, s);
 }
 template <typename C>
-int launch_cache(const AttentionArgs& a, int blocks, hipStream_t s) {
-  return a.dtype == MOE_FP32 ? launch_parts<C, 3>(a, blocks, s) : launch_parts<C, 1>(a, blocks, s);
+int launch_cache(const AttentionArgs& a, hipStream_t s) {
+  return a.dtype == MOE_FP32 ? launch_parts<C, 3>(a, s) : launch_parts<C, 1>(a, s);
 }
 
 }  // namespace
 
+int attention_slots(int cache_dtype, int D, int dtype) {
+  const size_t bytes = cache_dtype == MOE_FP32 ? 4 : cache_dtype == MOE_E4M3 ? 1 : 2;
+  return device_cu_count() * waves_per_simd(bytes, D <= 64 ? 64 : D <= 128 ? 128 : 256, bytes == 4 || dtype == MOE_BF16 ? 1 : 3);
+}
+
 int launch_attention(const AttentionArgs& a, hipStream_t s) {
   ProfScope prof(kProfAttention, s);
-  const int blocks = a.B * a.parts * a.kv_heads * ((a.group + kHeadTile - 1) / kHeadTile);
   int rc;
-  if (a.cache_dtype == MOE_FP32) rc = launch_parts<float, 1>(a, blocks, s);
-  else if (a.cache_dtype == MOE_E4M3) rc = launch_cache<uint8_t>(a, blocks, s);
-  else rc = launch_cache<__bf16>(a, blocks, s);
-  if (rc || a.parts == 1 || a.counters) return rc;
-  if (a.parts > 64) join_kernel<1024><<<a.B * a.heads, 1024, 0, s>>>(a);
-  else join_kernel<256><<<a.B * a.heads, 256, 0, s>>>(a);
+  if (a.cache_dtype == MOE_FP32) rc = launch_parts<float, 1>(a, s);
+  else if (a.cache_dtype == MOE_E4M3) rc = launch_cache<uint8_t>(a, s);
+  else rc = launch_cache<__bf16>(a, s);
+  if (rc || !a.started) return rc;
+  join_kernel<1024><<<dim3(a.workgroups, std::min(a.group, kHeadTile)), 1024, 0, s>>>(a);
   return hip_fail(hipGetLastError(), "join_kernel");
 }
 

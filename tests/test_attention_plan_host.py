@@ -9,7 +9,7 @@ import pytest
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 CSRC = os.path.join(ROOT, "paper_2510_12357_amd", "csrc")
-CUS, MOST = 256, 2 ** 31 - 1 - 2 * 4096                       # the longest bound that a call takes
+SETUP, MOST = 4, 2 ** 31 - 1 - 2 * 4096                       # the longest bound that a call takes
 
 
 @pytest.fixture(scope="module")
@@ -55,44 +55,63 @@ def test_what_a_token_sees(ask):
         for max_len in (0, 1, 64, 1000, MOST):
             for window in (0, 1, 63, 64, 65, 2 ** 31 - 1):
                 for shift, entries in ((2, 1), (4, 4), (4, 63), (20, 2048), (20, 2 ** 31 - 1)):
-                    lines.append(f"seen {length} {max_len} {window} {entries} {shift} 64 0")
+                    lines.append(f"seen {length} {max_len} {window} {entries} {shift}")
                     bad = length < 0 or length > max_len or length > entries << shift
                     first = max(0, length - window) if window else 0
-                    want.append((0, 0, 1) if bad else (0, 0, 0) if length == 0 else (first, length, 0))
-    assert [g[:3] for g in ask(lines)] == want
+                    want.append((0, 0, 1, 0) if bad else (0, 0, 0, 0) if length == 0 else (first, length, 0, -(-(length - first // 64 * 64) // 64)))
+    assert ask(lines) == want
 
 
-def test_parts_cover_what_is_seen_once(ask):
+def _line(ask, workgroups, least, units, blocks):
+    (got,) = ask([f"line {workgroups} {least} {units} " + " ".join(map(str, blocks))])
+    assert got[-1] == -1 and len(got) % 7 == 1
+    return [got[i:i + 7] for i in range(0, len(got) - 1, 7)]
+
+
+def test_every_block_belongs_to_one_workgroup(ask):
+    """Shares are equal, in the order of the line; a workgroup has at most two units in part, its first and its last; parts of a unit know each other."""
     rng = random.Random(1)
-    cases = []
-    for _ in range(400):
-        max_len = rng.choice([1, 2, 64, 65, rng.randint(1, 10000), rng.randint(1, 2 ** 22), MOST])
-        window = rng.choice([0, 0, 1, 63, 64, 65, rng.randint(1, 5000), rng.randint(1, max_len)])
-        cases.append((rng.choice([1, 2, rng.randint(1, 500)]), rng.choice([1, 2, 8, 16]), rng.choice([1, 4, 16, 17, 71]), max_len, window))
-    plans = ask([f"plan {b} {h} {g} {m} {w} {CUS}" for b, h, g, m, w in cases])
-    lines, which = [], []
-    for (b, h, g, max_len, window), (split, parts) in zip(cases, plans):
-        assert split % 64 == 0 and 64 <= split <= 4096 and parts >= 1
-        for length in {0, 1, max_len, max_len // 2, max(0, max_len - 63), min(max_len, window), min(max_len, window + 1), rng.randint(0, max_len)}:
-            some = range(parts) if parts < 40 else sorted({0, 1, parts - 1} | {rng.randrange(parts) for _ in range(10)})
-            for s in some:
-                lines.append(f"seen {length} {max_len} {window} {2 ** 29} 4 {split} {s}")
-                which.append((length, split, parts, s))
-    ends = {}
-    for (length, split, parts, s), (first, end, bad, begin, stop) in zip(which, ask(lines)):
-        assert not bad and begin <= stop <= end and stop - begin <= split
-        if begin < stop:
-            assert begin % 64 == 0 and begin == first // 64 * 64 + s * split
-            assert stop == end or stop == begin + split
-            # its pages' numbers fit, and so does the sum of positions
-            assert ((begin + split - 1) >> 2) - (begin >> 2) + 1 <= 1024 and begin + split + 4096 < 2 ** 31
-        if s == 0 and length:
-            assert begin <= first < stop
-        if s == parts - 1:
-            assert first // 64 * 64 + (s + 1) * split >= end     # nothing is left behind the last part
-        ends[(length, split, s)] = (begin, stop)
+    for turn in range(300):
+        workgroups, least, units = rng.choice([1, 2, 7, 64, 512, 768, 1024]), rng.choice([1, 4, 8]), rng.choice([1, 2, 8, 5, 40])
+        kind = rng.randrange(4)
+        blocks = [rng.choice([0, 1, 2, rng.randint(0, 130)]) if kind else rng.randint(100, 3000) for _ in range(rng.choice([1, 2, 3, 30, 300]))]
+        if kind == 3:
+            blocks[rng.randrange(len(blocks))] = 2048
+        total = sum(n + SETUP for n in blocks if n) * units
+        got = _line(ask, workgroups, least, units, blocks)
+        each = max(least, -(-total // workgroups))
+        # the line, unit by unit: SETUP places, then the blocks
+        place, line = {}, 0
+        for b, n in enumerate(blocks):
+            for unit in range(units if n else 0):
+                place[b, unit] = line + SETUP
+                line += n + SETUP
+        at, parts = -1, {}
+        for w, b, unit, block, n, first, count in got:
+            begin = place[b, unit]
+            assert n >= 1 and block >= 0 and block + n <= blocks[b] and begin + block > at
+            assert w * each <= begin + block and begin + block + n <= (w + 1) * each
+            at = begin + block + n - 1
+            parts.setdefault((b, unit), []).append((w, block, n))
+            assert first == begin // each and count == (begin + blocks[b] - 1) // each - first + 1
+        assert set(parts) == set(place)
+        slots = {}
+        for (b, unit), p in parts.items():
+            assert [w for w, _, _ in p] == list(range(p[0][0], p[0][0] + len(p)))
+            assert [block for _, block, _ in p] == [sum(n for _, _, n in p[:i]) for i in range(len(p))] and sum(n for _, _, n in p) == blocks[b]
+            for w, block, _ in p if len(p) > 1 else []:
+                key = (w, block == 0)                        # where its sums go
+                assert key not in slots
+                slots[key] = (b, unit)
 
 
-def test_few_long_sequences_are_split_and_full_batches_less(ask):
-    (one,), (many,), (short,) = (ask([f"plan {b} 8 4 {m} 0 {CUS}"]) for b, m in ((1, 131072), (256, 131072), (1, 200)))
-    assert one[1] * 8 >= CUS and many[0] >= one[0] and short[1] == 1
+def test_plans(ask):
+    cases = [(1, 8, 4, 131072, 0), (64, 8, 4, 8192, 0), (1, 16, 1, 200, 0), (33, 1, 71, 5000, 1000), (1, 1, 1, 0, 0), (1, 1, 1, 1, 1), (0, 8, 4, 100, 0),
+             (4096, 16, 24, MOST, 0), (256, 8, 8, 131072, 0), (1, 1, 16, MOST, 0)]
+    plans = ask([f"plan {b} {h} {g} {m} {w} 768" for b, h, g, m, w in cases])
+    for (b, h, g, m, w), (fits, workgroups, split, few) in zip(cases, plans):
+        span = min(m, w + 63) if 0 < w < m else m
+        total = b * h * -(-g // 16) * (-(-span // 64) + SETUP)
+        assert fits == (total < 2 ** 30) and workgroups == min(768, max(1, -(-total // 8)))
+    fits, workgroups, split, few = zip(*plans)
+    assert few[:4] == (0, 1, 1, 1) and split[4:6] == (0, 0)

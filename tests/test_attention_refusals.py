@@ -127,7 +127,7 @@ def test_append_empty_calls():
     (dict(B=-1), SHAPE), (dict(heads=0), SHAPE), (dict(heads=5), SHAPE), (dict(dtype=4), BADARG), (dict(max_len=-1), BADARG), (dict(window=-1), BADARG),
     (dict(table_len=0), SHAPE), (dict(table_ld=1), SHAPE), (dict(max_len=2 ** 31 - 100), UNSUPPORTED), (dict(scale=NAN), BADARG), (dict(scale=-INF), BADARG),
     (dict(softcap=-1.0), BADARG), (dict(softcap=INF), BADARG), (dict(q_head=63), SHAPE), (dict(out_token=-1), BADARG),
-    (dict(B=1 << 22, heads=64), UNSUPPORTED),
+    (dict(B=1 << 30, heads=64), UNSUPPORTED),
 ])
 def test_attention_configs(change, code):
     assert attend(_attention(**change), _cache()) == code and mm.moe_last_error()
