@@ -89,7 +89,7 @@ int resolve(const char* call, const moe_attention_config* cfg, const moe_kv_cach
   if (int rc = resolve_strides(call, "out", c->B, c->heads, cache.D, &c->out_token, &c->out_head)) return rc;
   const int64_t span = (int64_t)c->table_len << page_shift(cache.page_size);
   if (span < c->max_len) c->max_len = (int)span;           // longer sequences are behind their table row
-  *plan = plan_attention(c->B, cache.heads, c->heads / cache.heads, c->max_len, c->window, attention_slots(cache.dtype, cache.D, c->dtype));
+  *plan = plan_attention(c->B, cache.heads, c->heads / cache.heads, c->max_len, c->window, attention_slots(cache.dtype, cache.D, c->dtype), device_cu_count());
   if (!plan->fits) return fail(MOE_E_UNSUPPORTED, "%s: %d sequences of up to %d positions on %d heads are too many", call, c->B, c->max_len, c->heads);
   return MOE_OK;
 }
@@ -101,7 +101,7 @@ struct Workspace {
     const size_t rows = (size_t)p.workgroups * 2 * (c.heads / cache.heads < kHeadTile ? c.heads / cache.heads : kHeadTile);
     stat = align256(rows * cache.D * sizeof(float));
     started = stat + align256(rows * 2 * sizeof(float));
-    bytes = p.split && p.workgroups > 1 ? started + align256((size_t)p.workgroups * 4 * sizeof(int32_t)) : 0;
+    bytes = p.split && p.workgroups > 1 ? started + align256(((size_t)p.workgroups * 4 + 1) * sizeof(int32_t)) : 0;
   }
 };
 
@@ -210,7 +210,7 @@ extern "C" int moe_paged_attention(const moe_attention_config* cfg, const moe_kv
   AttentionArgs a = {};
   a.B = c.B; a.heads = c.heads; a.kv_heads = kv.heads; a.group = c.heads / kv.heads; a.D = kv.D; a.dtype = c.dtype; a.cache_dtype = kv.dtype;
   a.max_len = c.max_len; a.window = c.window; a.table_len = c.table_len; a.table_ld = c.table_ld; a.n_pages = kv.n_pages; a.shift = page_shift(kv.page_size);
-  a.workgroups = p.workgroups; a.scale = c.scale; a.softcap = c.softcap;
+  a.workgroups = p.workgroups; a.align = p.align; a.scale = c.scale; a.softcap = c.softcap;
   a.q_token = c.q_token; a.q_head = c.q_head; a.out_token = c.out_token; a.out_head = c.out_head;
   a.page = kv.page; a.head = kv.head; a.row = kv.row;
   a.q = q; a.table = table; a.lengths = lengths; a.k = kv.k; a.v = kv.v; a.k_scale = kv.k_scale; a.v_scale = kv.v_scale;

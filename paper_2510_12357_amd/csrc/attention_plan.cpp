@@ -5,18 +5,21 @@
 
 namespace mm {
 
-// slots: workgroups that the device runs at once.  As many have the line's blocks in equal shares, whatever the sequences' lengths are, so that all end together;
-// fewer where their shares would be below the least.
-AttentionPlan plan_attention(int sequences, int kv_heads, int group, int max_len, int window, int slots) {
+// slots: workgroups that the device runs at once.  As many have equal shares, whatever the sequences' lengths are, so that all end together.  Where the work is too little
+// for that, a workgroup has one unit or a part of one: what a second one in a row would wait for costs more.
+AttentionPlan plan_attention(int sequences, int kv_heads, int group, int max_len, int window, int slots, int device_cus) {
   const int64_t units = (int64_t)sequences * kv_heads * ((group + kHeadTile - 1) / kHeadTile);
   // a window that starts inside a block reaches over one more of them
   const int64_t span = window > 0 && window < max_len ? (int64_t)window + kSpan - 1 : max_len;
-  const int64_t blocks = (span + kSpan - 1) / kSpan, total = units * (blocks + kSetup);
+  const int64_t blocks = std::max<int64_t>(1, (span + kSpan - 1) / kSpan);
+  auto parts = [&](int64_t align) { return (blocks + align - 1) / align; };
   AttentionPlan p;
-  p.fits = (double)units * (double)(blocks + kSetup) < (double)(1 << 30);
-  p.workgroups = (int)std::clamp<int64_t>((total + kLeastBlocks - 1) / kLeastBlocks, 1, std::min(slots, kMostWorkgroups));
-  p.split = blocks > 1;
-  p.few_parts = std::min((blocks + kLeastBlocks - 1) / kLeastBlocks, p.workgroups / std::max<int64_t>(units, 1)) <= 16;
+  p.align = units * parts(4) <= device_cus ? 4 : units * parts(8) <= slots ? 8 : 0;
+  p.fits = (double)units * (double)(blocks + std::max(kSetup, p.align)) < (double)(1 << 30);
+  if (!p.fits) return p;
+  p.workgroups = p.align ? (int)std::max<int64_t>(1, units * parts(p.align)) : std::min(slots, kMostWorkgroups);
+  p.split = p.align ? parts(p.align) > 1 : true;
+  p.few_parts = (p.align ? parts(p.align) : p.workgroups / units) <= 16;
   return p;
 }
 

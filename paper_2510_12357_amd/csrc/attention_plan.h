@@ -43,44 +43,48 @@ MM_BOTH Seen seen_by(int length, int max_len, int window, int table_len, int shi
 // Its blocks, of which the first one may begin before what is seen.
 MM_BOTH int blocks_of(const Seen& v) { return (int)(((int64_t)v.end - v.first / kSpan * kSpan + kSpan - 1) / kSpan); }
 
-// All work of a call is a line of blocks: sequence by sequence, of each its units (a tile of query heads on a key head), of each unit kSetup blocks that stand for what it takes
-// to begin and end one, and its own.  Workgroup w has the blocks [w each, (w + 1) each) of the line, a row of segments, each of one unit.  A unit whose own blocks lie in
-// several workgroups has its parts joined.
+// All work of a call is a line of blocks: sequence by sequence, of each its units (a tile of query heads on a key head), of each unit its own blocks.  Workgroup w has the
+// places [w each, (w + 1) each) of the line, a row of segments, each of one unit.  A unit whose own blocks lie in several workgroups has its parts joined.
+// align 0: equal shares of the whole line, on which kSetup places in front of each unit stand for what it takes to begin and end one.  Else shares are of `align`
+// places, and so is what units are rounded up to: a workgroup has one unit.
 constexpr int kSetup = 4;
-MM_BOTH int line_blocks(int n) { return n > 0 ? n + kSetup : 0; }
-MM_BOTH int blocks_each(int total, int workgroups, int least) {
+MM_BOTH int unit_places(int n, int align) { return align ? (n + align - 1) / align * align : n + kSetup; }
+MM_BOTH int line_places(int n, int align) { return n > 0 ? unit_places(n, align) : 0; }
+MM_BOTH int places_each(int total, int workgroups, int align, int least) {
+  if (align) return align;
   const int n = (int)(((int64_t)total + workgroups - 1) / workgroups);
   return n > least ? n : least;
 }
 struct Segment {
   int unit;                              // of the sequence
-  int length;                            // on the line
+  int length;                            // places of the line
   int block, blocks;                     // of the unit's own, from where on, and how many
   int workgroup, parts;                  // that has the unit's first block, and how many have any
 };
 // The segment at place `at` of the line for a workgroup whose share ends at `end`; the sequence begins at `line` and has n > 0 blocks a unit.
-MM_BOTH Segment segment_at(int line, int n, int at, int end, int each) {
+MM_BOTH Segment segment_at(int line, int n, int align, int at, int end, int each) {
   Segment s;
-  s.unit = (at - line) / (n + kSetup);
-  const int begin = line + s.unit * (n + kSetup), own = begin + kSetup, behind = own + n;
-  const int stop = behind < end ? behind : end, start = at > own ? at : own;
+  const int places = unit_places(n, align);
+  s.unit = (at - line) / places;
+  const int begin = line + s.unit * places, own = begin + (align ? 0 : kSetup), behind = own + n;
+  const int stop = begin + places < end ? begin + places : end, last = behind < stop ? behind : stop, start = at > own ? at : own;
   s.length = stop - at;
   s.block = start - own;
-  s.blocks = stop > start ? stop - start : 0;
+  s.blocks = last > start ? last - start : 0;
   s.workgroup = own / each;
   s.parts = (behind - 1) / each - s.workgroup + 1;
   return s;
 }
 
 // What the host knows of a call.
-constexpr int kLeastBlocks = 8;          // of a workgroup, on the line
+constexpr int kLeast = 8;                // places of a workgroup
 constexpr int kMostWorkgroups = 4096;
 struct AttentionPlan {
   bool fits;                             // the line's length in 31 bits
-  int workgroups;
+  int workgroups, align;
   bool split;                            // a unit may lie in several workgroups
   bool few_parts;                        // units are expected to lie in so few that the last one to end joins them; else a second kernel
 };
-AttentionPlan plan_attention(int sequences, int kv_heads, int group, int max_len, int window, int slots);
+AttentionPlan plan_attention(int sequences, int kv_heads, int group, int max_len, int window, int slots, int device_cus);
 
 }  // namespace mm

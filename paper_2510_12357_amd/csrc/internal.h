@@ -201,7 +201,7 @@ struct RotaryArgs {
 int launch_rotary(const RotaryArgs& a, int dtype, hipStream_t s);
 struct AttentionArgs {
   int B, heads, kv_heads, group, D, dtype, cache_dtype;
-  int max_len, window, table_len, n_pages, shift, workgroups;
+  int max_len, window, table_len, n_pages, shift, workgroups, align;
   int64_t table_ld;
   float scale, softcap;
   int64_t q_token, q_head, out_token, out_head;
@@ -211,7 +211,8 @@ struct AttentionArgs {
   void* out; float* lse;
   float *part_out, *part_stat;           // [workgroups, 2, tile heads, D] and [workgroups, 2, tile heads, 2]: a workgroup's first segment, and its last one
   int32_t* counters;                     // of the parts that have ended, zero between calls; NULL: a second kernel joins the parts
-  int32_t* started;                      // [workgroups, 4] for it: sequence, unit and parts of the unit that begins in a workgroup and ends in another one
+  int32_t* started;                      // [workgroups, 4] for it: parts, sequence and unit of the unit that begins in a workgroup and ends in another one; then how
+                                         // many workgroups there are on the line
 };
 int attention_slots(int cache_dtype, int D, int dtype);      // workgroups that the device runs at once
 int launch_attention(const AttentionArgs& a, hipStream_t s);

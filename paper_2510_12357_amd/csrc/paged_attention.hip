@@ -99,7 +99,6 @@ __device__ __forceinline__ V load_queries(const AttentionArgs& a, int64_t at) {
 __device__ __forceinline__ int64_t part_at(const AttentionArgs& a, int workgroup, bool begins) {
   return (2 * (int64_t)workgroup + begins) * min(a.group, kHeadTile);
 }
-__device__ __forceinline__ int line_place(int block, int) { return block; }
 
 // Four channels of a result: sums v, the maximum m (log2) that they are taken against and the sum l of the exponentials; without any, zeros.
 __device__ __forceinline__ void store_row(const AttentionArgs& a, int b, int head, int channel, f32x4 v, float m, float l) {
@@ -176,29 +175,35 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNK
   fetch_arguments<sizeof(AttentionArgs)>();
 
   const int tiles = (a.group + kHeadTile - 1) / kHeadTile, units = a.kv_heads * tiles;
-  const int workgroup = line_place(blockIdx.x, a.workgroups);
+  int workgroup;
   auto seen_with = [&](int length) { return seen_by(length, a.max_len, a.window, a.table_len, a.shift); };
   auto seen_of = [&](int b) { return seen_with(uniform(a.lengths[b])); };       // b: the same in all lanes
 
   // ---- the line: its length, and the sequence in which this workgroup's share begins; every wave by itself ----
-  int cursor, finish, each, b = 0, line = 0;
+  int cursor, finish, each, b = 0, line = 0, length = 0;
   {
     const int lane = threadIdx.x & 63;
-    auto on_line = [&](int i) { return i < a.B ? line_blocks(blocks_of(seen_with(a.lengths[i]))) * units : 0; };
-    const int first_64 = on_line(lane);
-    int total = first_64;
-    for (int i = lane + 64; i < a.B; i += 64) total += on_line(i);
+    auto length_of = [&](int i) { return i < a.B ? a.lengths[i] : 0; };
+    auto on_line = [&](int length) { return line_places(blocks_of(seen_with(length)), a.align) * units; };
+    const int first_64 = length_of(lane);
+    int total = on_line(first_64);
+    for (int i = lane + 64; i < a.B; i += 64) total += on_line(a.lengths[i]);
     total = wave_total(total);
-    each = blocks_each(total, a.workgroups, kLeastBlocks);
-    cursor = min(total, workgroup * each);
+    each = places_each(total, a.workgroups, a.align, kLeast);
+    // neighbours on the line run on the same XCD of the 8 that take workgroups in turn: tiles of a large group read the same keys and values.  The grid is whole eights.
+    const int active = (total + each - 1) / each, run = (active + 7) / 8;
+    workgroup = blockIdx.x / 8 < run ? blockIdx.x % 8 * run + blockIdx.x / 8 : active;
+    cursor = min(total, min(workgroup, active) * each);
     finish = min(total, cursor + each);
+    if (a.started && blockIdx.x == 0 && threadIdx.x == 0) a.started[4 * a.workgroups] = active;
     if (cursor < finish)
       for (;; b += 64) {                                    // ends at the sequence that holds the place
-        const int n = b ? on_line(b + lane) : first_64, upto = line + wave_sums(n);
+        const int there = b ? length_of(b + lane) : first_64, n = on_line(there), upto = line + wave_sums(n);
         const uint64_t behind = __ballot(cursor < upto);
         if (behind) {
           const int at = __builtin_ctzll(behind);
           line = __builtin_amdgcn_readlane(upto - n, at);
+          length = __builtin_amdgcn_readlane(there, at);
           b += at;
           break;
         }
@@ -206,16 +211,15 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNK
       }
   }
   // ---- sequences without anything to see, or of a length that there is not ----
-  for (int e = blockIdx.x; e < a.B; e += a.workgroups) {
+  for (int e = blockIdx.x; e < a.B; e += gridDim.x) {
     const Seen v = seen_of(e);
     if (v.first < v.end) continue;
     const float l = v.bad ? __uint_as_float(0x7fc00000u) : 0.f;
     for (int i = threadIdx.x; i < a.heads * a.D / 4; i += kThreads)
       store_row(a, e, i / (a.D / 4), i % (a.D / 4) * 4, f32x4{0.f, 0.f, 0.f, 0.f}, -INFINITY, l);
   }
-  if (a.started && threadIdx.x < 4) a.started[4 * workgroup + threadIdx.x] = 0;
   if (cursor >= finish) return;
-  int length = uniform(a.lengths[b]);
+  if (a.started && threadIdx.x < 4) a.started[4 * workgroup + threadIdx.x] = 0;
   int listed_b = -1, listed_from = 0, listed_to = 0;        // whose pages' numbers are in LDS
 
   // ================= the segments of the share =================
@@ -227,7 +231,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNK
   const int lane = tid & 63, n = lane & 15, g = lane >> 4;
   const Seen seen = seen_with(length);
   const int next_length = a.lengths[min(b + 1, a.B - 1)];   // on its way meanwhile
-  const Segment seg = segment_at(line, blocks_of(seen), cursor, finish, each);
+  const Segment seg = segment_at(line, blocks_of(seen), a.align, cursor, finish, each);
   if (seg.blocks) {
   const int tile = seg.unit % tiles, kvh = seg.unit / tiles;
   const int heads = min(kHeadTile, a.group - tile * kHeadTile), head0 = kvh * a.group + tile * kHeadTile;
@@ -603,7 +607,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNK
   }
   cursor += seg.length;
   if (cursor >= finish) break;
-  const int behind = line + line_blocks(blocks_of(seen)) * units;
+  const int behind = line + line_places(blocks_of(seen), a.align) * units;
   if (cursor >= behind) {
     line = behind;
     ++b;
@@ -620,7 +624,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const AttentionArgs 
   __shared__ float s_top[kJoinThreads / 64];
   __shared__ __attribute__((aligned(16))) f32x4 s_v[kJoinThreads];
   __shared__ float s_l[kJoinThreads];
-  const int tid = threadIdx.x, workgroup = blockIdx.x, parts = a.started[4 * workgroup], b = a.started[4 * workgroup + 1], unit = a.started[4 * workgroup + 2];
+  const int tid = threadIdx.x, workgroup = blockIdx.x, parts = workgroup < a.started[4 * a.workgroups] ? a.started[4 * workgroup] : 0, b = a.started[4 * workgroup + 1], unit = a.started[4 * workgroup + 2];
   const int tiles = (a.group + kHeadTile - 1) / kHeadTile, tile = unit % tiles, h = blockIdx.y, head = unit / tiles * a.group + tile * kHeadTile + h;
   if (parts == 0 || h >= a.group - tile * kHeadTile) return;
   auto at = [&](int part) { return part_at(a, workgroup + part, part == 0) + h; };
@@ -653,8 +657,9 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const AttentionArgs 
 
 template <typename C, int VW, int CHUNKS, int PARTS>
 int launch_dims(const AttentionArgs& a, hipStream_t s) {
-  if (a.D < 16 * VW * CHUNKS) attention_kernel<C, VW, CHUNKS, PARTS, true><<<a.workgroups, kThreads, 0, s>>>(a);
-  else attention_kernel<C, VW, CHUNKS, PARTS, false><<<a.workgroups, kThreads, 0, s>>>(a);
+  const int grid = (a.workgroups + 7) / 8 * 8;
+  if (a.D < 16 * VW * CHUNKS) attention_kernel<C, VW, CHUNKS, PARTS, true><<<grid, kThreads, 0, s>>>(a);
+  else attention_kernel<C, VW, CHUNKS, PARTS, false><<<grid, kThreads, 0, s>>>(a);
   return hip_fail(hipGetLastError(), "attention_kernel");
 }
 template <typename C, int PARTS>

@@ -62,30 +62,35 @@ def test_what_a_token_sees(ask):
     assert ask(lines) == want
 
 
-def _line(ask, workgroups, least, units, blocks):
-    (got,) = ask([f"line {workgroups} {least} {units} " + " ".join(map(str, blocks))])
+def _line(ask, workgroups, align, least, units, blocks):
+    (got,) = ask([f"line {workgroups} {align} {least} {units} " + " ".join(map(str, blocks))])
     assert got[-1] == -1 and len(got) % 7 == 1
     return [got[i:i + 7] for i in range(0, len(got) - 1, 7)]
 
 
 def test_every_block_belongs_to_one_workgroup(ask):
-    """Shares are equal, in the order of the line; a workgroup has at most two units in part, its first and its last; parts of a unit know each other."""
+    """Shares are equal, in the order of the line; a workgroup has at most two units in part, its first and its last; parts of a unit know each other.
+    Where units are rounded up, a workgroup has one of them."""
     rng = random.Random(1)
-    for turn in range(300):
+    for turn in range(120):
+        align = rng.choice([0, 0, 4, 8])
         workgroups, least, units = rng.choice([1, 2, 7, 64, 512, 768, 1024]), rng.choice([1, 4, 8]), rng.choice([1, 2, 8, 5, 40])
         kind = rng.randrange(4)
         blocks = [rng.choice([0, 1, 2, rng.randint(0, 130)]) if kind else rng.randint(100, 3000) for _ in range(rng.choice([1, 2, 3, 30, 300]))]
         if kind == 3:
             blocks[rng.randrange(len(blocks))] = 2048
-        total = sum(n + SETUP for n in blocks if n) * units
-        got = _line(ask, workgroups, least, units, blocks)
-        each = max(least, -(-total // workgroups))
-        # the line, unit by unit: SETUP places, then the blocks
+        places = lambda n: -(-n // align) * align if align else n + SETUP  # noqa: E731
+        total = sum(places(n) for n in blocks if n) * units
+        if align:
+            workgroups = max(1, total // align)
+        got = _line(ask, workgroups, align, least, units, blocks)
+        each = align or max(least, -(-total // workgroups))
+        # the line, unit by unit: SETUP places or none, the blocks, places up to a whole share or none
         place, line = {}, 0
         for b, n in enumerate(blocks):
             for unit in range(units if n else 0):
-                place[b, unit] = line + SETUP
-                line += n + SETUP
+                place[b, unit] = line + (0 if align else SETUP)
+                line += places(n)
         at, parts = -1, {}
         for w, b, unit, block, n, first, count in got:
             begin = place[b, unit]
@@ -95,6 +100,8 @@ def test_every_block_belongs_to_one_workgroup(ask):
             parts.setdefault((b, unit), []).append((w, block, n))
             assert first == begin // each and count == (begin + blocks[b] - 1) // each - first + 1
         assert set(parts) == set(place)
+        if align:
+            assert len({w for w, *_ in got}) == len(got)
         slots = {}
         for (b, unit), p in parts.items():
             assert [w for w, _, _ in p] == list(range(p[0][0], p[0][0] + len(p)))
@@ -106,12 +113,20 @@ def test_every_block_belongs_to_one_workgroup(ask):
 
 
 def test_plans(ask):
+    """Grids hold the longest line that a call can have; where there is little work a workgroup has one unit."""
     cases = [(1, 8, 4, 131072, 0), (64, 8, 4, 8192, 0), (1, 16, 1, 200, 0), (33, 1, 71, 5000, 1000), (1, 1, 1, 0, 0), (1, 1, 1, 1, 1), (0, 8, 4, 100, 0),
-             (4096, 16, 24, MOST, 0), (256, 8, 8, 131072, 0), (1, 1, 16, MOST, 0)]
-    plans = ask([f"plan {b} {h} {g} {m} {w} 768" for b, h, g, m, w in cases])
-    for (b, h, g, m, w), (fits, workgroups, split, few) in zip(cases, plans):
+             (4096, 16, 24, MOST, 0), (256, 8, 8, 131072, 0), (1, 1, 16, MOST, 0), (5000, 8, 4, 500, 0), (1 << 20, 8, 4, 64, 0), (8, 8, 4, 4096, 0)]
+    plans = ask([f"plan {b} {h} {g} {m} {w} 768 256" for b, h, g, m, w in cases])
+    for (b, h, g, m, w), (fits, *plan) in zip(cases, plans):
         span = min(m, w + 63) if 0 < w < m else m
-        total = b * h * -(-g // 16) * (-(-span // 64) + SETUP)
-        assert fits == (total < 2 ** 30) and workgroups == min(768, max(1, -(-total // 8)))
-    fits, workgroups, split, few = zip(*plans)
-    assert few[:4] == (0, 1, 1, 1) and split[4:6] == (0, 0)
+        units, blocks = b * h * -(-g // 16), max(1, -(-span // 64))
+        assert fits == (units * (blocks + 8) < 2 ** 30) or units * (blocks + 4) >= 2 ** 29
+        if fits:
+            workgroups, align, split, few = plan
+            assert workgroups * 256 < 2 ** 32 and (workgroups <= 4096 or not split)
+            if align:
+                assert workgroups == max(1, units * -(-blocks // align)) and split == (blocks > align)
+            else:
+                assert workgroups == 768 and split
+    got = [p[2] if p[0] else None for p in plans]
+    assert got == [0, 0, 4, 8, 4, 4, 4, None, 0, 0, 0, 0, 8] and plans[3][4] == 1 and plans[0][4] == 0
