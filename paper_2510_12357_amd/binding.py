@@ -831,6 +831,8 @@ def _strides(t: torch.Tensor, what: str):
 
 
 def _integers(t: torch.Tensor, what: str, shape) -> None:
+    if t.dtype is torch.int32 and t.shape == shape and t.is_contiguous():        # as nearly every call has them
+        return
     if t.dtype is not torch.int32 or t.dim() != len(shape) or any(n >= 0 and n != m for n, m in zip(shape, t.shape)):
         raise ValueError(f"{what}: int32 {[('any' if n < 0 else n) for n in shape]}")
     if (not t.is_contiguous()) if len(shape) == 1 else (t.shape[1] > 1 and t.stride(1) != 1):
@@ -864,7 +866,7 @@ class _Owner:
 
 def _call_on(device: int, function, *args) -> None:
     """A C call with the tensors' device as the current one."""
-    if torch.cuda.current_device() == device:
+    if torch._C._cuda_getDevice() == device:
         rc = function(*args)
     else:
         with torch.cuda.device(device):

@@ -193,7 +193,7 @@ struct RotaryArgs {
   int64_t q_token, q_head, k_token, k_head, v_token, v_head, out_token, out_head;
   const int32_t *pos, *seq, *table;
   const double* freq;
-  int n_seqs, table_len, n_pages, shift, cache_dtype;
+  int n_seqs, table_len, n_pages, shift, cache_dtype, first_seq;        // first_seq: of token 0 where there is no seq
   int64_t table_ld;
   int64_t page, head, row;               // strides of the cache in its elements
   void *k_cache, *v_cache; float *k_scale, *v_scale;

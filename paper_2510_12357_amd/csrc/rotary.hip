@@ -1,7 +1,7 @@
 // Rotary positions (moe_rope), and new keys and values stored in a paged cache with the rotation on the way (moe_kv_append).
 //
-// Pairs of channels (a, b) turn by t = pos freq: a' = m (a cos t - b sin t), b' = m (b cos t + a sin t).  A group of lanes takes a token: a lane has
-// V pairs of channels, computes their sines and cosines once and turns them in several heads.
+// Pairs of channels (a, b) turn by t = pos freq: a' = m (a cos t - b sin t), b' = m (b cos t + a sin t).  A workgroup has a few tokens, works out their sines and cosines
+// once, one a thread, into LDS, and turns V pairs a lane of head after head; of a row's lanes each has the same pairs in all heads, so that they stay in registers.
 #include <algorithm>
 
 #include "internal.h"
@@ -44,8 +44,8 @@ __device__ __forceinline__ float widen(X x) { return (float)x; }
 template <typename X, int N>
 struct Chunk {
   typedef X type __attribute__((ext_vector_type(N)));
-  static __device__ __forceinline__ void load(const X* p, float* v) {
-    const type x = load_unaligned<type>(p);
+  static __device__ __forceinline__ type load(const X* p) { return load_unaligned<type>(p); }
+  static __device__ __forceinline__ void widened(const type& x, float* v) {
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = widen<X>(x[i]);
   }
@@ -58,7 +58,9 @@ struct Chunk {
 };
 template <typename X>
 struct Chunk<X, 1> {
-  static __device__ __forceinline__ void load(const X* p, float* v) { v[0] = widen<X>(*p); }
+  typedef X type;
+  static __device__ __forceinline__ type load(const X* p) { return *p; }
+  static __device__ __forceinline__ void widened(const type& x, float* v) { v[0] = widen<X>(x); }
   static __device__ __forceinline__ void store(X* p, const float* v) { *p = (X)v[0]; }
 };
 template <int N>
@@ -76,62 +78,79 @@ __device__ __forceinline__ void store_codes(uint8_t* p, const float* v) {
   }
 }
 
-// X: type of queries, keys and values; V: pairs of a unit, which divides a row's pairs that turn and those that do not; UNITS: units of a lane, a token's lanes
-// apart.  C: type of the cache's rows.
+// X: type of queries, keys and values; V: pairs of a unit, which divides a row's pairs that turn and those that do not; UNITS: units of a lane, a row's lanes
+// apart.  C: type of the cache's rows.  A workgroup has `tokens` tokens (a power of two) and of each the heads of its part of the grid's second dimension.
+constexpr int kAngles = 256;               // of a workgroup
+constexpr int kAhead = 4;                  // heads whose loads are on their way together
 template <typename X, typename C, int V, int UNITS, bool HALF>
-__global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a, const int lanes_log, const int slices) {
+__global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a, const int lanes_log, const int tokens, const int heads_each) {
   constexpr bool kCodes = sizeof(C) == 1;
-  const int lanes = 1 << lanes_log, j = threadIdx.x & (lanes - 1);
+  typedef Chunk<X, V> Ch;
+  __shared__ __attribute__((aligned(16))) float s_cos[kAngles], s_sin[kAngles];
+  const int lanes = 1 << lanes_log, j = threadIdx.x & (lanes - 1), row = threadIdx.x >> lanes_log, rows = (kThreads >> lanes_log) / tokens;
   const int units = a.D / (2 * V), half = a.rotary_dim / 2, turning = half / V;
-  const unsigned step = gridDim.x * (kThreads >> lanes_log), groups = (unsigned)a.T * (unsigned)slices;      // below 2^31, so that no sum passes 2^32
-  for (unsigned at = blockIdx.x * (kThreads >> lanes_log) + (threadIdx.x >> lanes_log); at < groups; at += step) {
-    const int t = (int)(at / (unsigned)slices), slice = (int)at - t * slices;
-    const int pos = a.pos[t];
-    // where the key and value of this token go
-    int64_t slot = -1, row = 0;
-    if (a.kv_heads && pos >= 0) {
-      const int seq = a.seq ? a.seq[t] : t;
-      const int page = seq >= 0 && seq < a.n_seqs ? page_of(a.table + seq * a.table_ld, a.table_len, a.n_pages, a.shift, pos) : -1;
-      row = pos & ((1 << a.shift) - 1);
-      slot = page;
-    }
-    const int heads = slot >= 0 ? a.heads + 2 * a.kv_heads : a.heads;
-    if (slice >= heads) continue;
-    float c[UNITS][V], s[UNITS][V];
-    int o0[UNITS], o1[UNITS];
-    bool turns[UNITS], there[UNITS];
+  const int t0 = blockIdx.x * tokens, local = row / rows, t = t0 + local;
+  for (int i = threadIdx.x; i < tokens * half; i += kThreads) {
+    const int token = i / half;
+    float c = 1.f, s = 0.f;
+    if (t0 + token < a.T) turn((double)a.pos[t0 + token] * (a.freq[i - token * half] * 0.15915494309189533577), &c, &s);
+    s_cos[i] = c * a.mscale;
+    s_sin[i] = s * (a.mscale * a.sign);
+  }
+  // where the key and value of this token go
+  int64_t page = -1, slot = 0;
+  if (a.kv_heads && t < a.T) {
+    const int pos = a.pos[t], seq = a.seq ? a.seq[t] : a.first_seq + t;
+    if (pos >= 0 && seq >= 0 && seq < a.n_seqs) page = page_of(a.table + seq * a.table_ld, a.table_len, a.n_pages, a.shift, pos);
+    slot = pos & ((1 << a.shift) - 1);
+  }
+  __syncthreads();
+  const int first = blockIdx.y * heads_each, heads = t < a.T ? min(page >= 0 ? a.heads + 2 * a.kv_heads : a.heads, first + heads_each) : 0;
+  float c[UNITS][V], s[UNITS][V];
+  int o0[UNITS], o1[UNITS];
+  bool turns[UNITS], there[UNITS];
 #pragma unroll
-    for (int k = 0; k < UNITS; ++k) {
-      const int u = j + k * lanes;
-      there[k] = u < units;
-      turns[k] = u < turning;
-      o0[k] = turns[k] ? (HALF ? u * V : 2 * u * V) : 2 * u * V;
-      o1[k] = turns[k] && HALF ? half + u * V : o0[k] + V;
+  for (int k = 0; k < UNITS; ++k) {
+    const int u = j + k * lanes;
+    there[k] = u < units;
+    turns[k] = u < turning;
+    o0[k] = turns[k] && HALF ? u * V : 2 * u * V;
+    o1[k] = turns[k] && HALF ? half + u * V : o0[k] + V;
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        c[k][e] = 1.f; s[k][e] = 0.f;
-        if (turns[k]) {
-          turn((double)pos * (a.freq[u * V + e] * 0.15915494309189533577), &c[k][e], &s[k][e]);
-          c[k][e] *= a.mscale; s[k][e] *= a.mscale * a.sign;
-        }
-      }
+    for (int e = 0; e < V; ++e) {
+      c[k][e] = turns[k] ? s_cos[local * half + u * V + e] : 1.f;
+      s[k][e] = turns[k] ? s_sin[local * half + u * V + e] : 0.f;
     }
-    for (int h = slice; h < heads; h += slices) {
-      const int kv = h - a.heads;
-      const bool value = kv >= a.kv_heads;
+  }
+  for (int h0 = first + row % rows; h0 < heads; h0 += kAhead * rows) {
+    typename Ch::type x0[kAhead][UNITS], x1[kAhead][UNITS];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int h = h0 + i * rows, kv = h - a.heads;
+      if (h >= heads) continue;
       const X* from = kv < 0 ? static_cast<const X*>(a.q) + t * a.q_token + h * a.q_head
-                      : value ? static_cast<const X*>(a.v) + t * a.v_token + (kv - a.kv_heads) * a.v_head
-                              : static_cast<const X*>(a.k) + t * a.k_token + kv * a.k_head;
-      float x[UNITS][2 * V], y[UNITS][2 * V];
+                      : kv >= a.kv_heads ? static_cast<const X*>(a.v) + t * a.v_token + (kv - a.kv_heads) * a.v_head
+                                         : static_cast<const X*>(a.k) + t * a.k_token + kv * a.k_head;
+#pragma unroll
+      for (int k = 0; k < UNITS; ++k)
+        if (there[k]) { x0[i][k] = Ch::load(from + o0[k]); x1[i][k] = Ch::load(from + o1[k]); }
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int h = h0 + i * rows, kv = h - a.heads;
+      if (h >= heads) continue;
+      const bool value = kv >= a.kv_heads;
+      float y[UNITS][2 * V];
 #pragma unroll
       for (int k = 0; k < UNITS; ++k) {
         if (!there[k]) continue;
-        Chunk<X, V>::load(from + o0[k], x[k]);
-        Chunk<X, V>::load(from + o1[k], x[k] + V);
+        float x[2 * V];
+        Ch::widened(x0[i][k], x);
+        Ch::widened(x1[i][k], x + V);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
           const int ia = HALF ? e : 2 * e, ib = HALF ? V + e : 2 * e + 1;
-          const float p = x[k][ia], q = x[k][ib];
+          const float p = x[ia], q = x[ib];
           const bool moves = turns[k] && !value;
           y[k][ia] = moves ? fmaf(p, c[k][e], -(q * s[k][e])) : p;
           y[k][ib] = moves ? fmaf(q, c[k][e], p * s[k][e]) : q;
@@ -142,13 +161,13 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a, co
 #pragma unroll
         for (int k = 0; k < UNITS; ++k) {
           if (!there[k]) continue;
-          Chunk<X, V>::store(to + o0[k], y[k]);
-          Chunk<X, V>::store(to + o1[k], y[k] + V);
+          Ch::store(to + o0[k], y[k]);
+          Ch::store(to + o1[k], y[k] + V);
         }
         continue;
       }
       const int head = value ? kv - a.kv_heads : kv;
-      C* to = static_cast<C*>(value ? a.v_cache : a.k_cache) + slot * a.page + head * a.head + row * a.row;
+      C* to = static_cast<C*>(value ? a.v_cache : a.k_cache) + page * a.page + head * a.head + slot * a.row;
       if constexpr (kCodes) {
         unsigned top = 0;
 #pragma unroll
@@ -162,13 +181,18 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a, co
         const float most = __uint_as_float(top);
         if (j == 0) {
           float* scales = value ? a.v_scale : a.k_scale;
-          scales[((int64_t)slot * a.kv_heads + head) * ((int64_t)1 << a.shift) + row] = finite ? most / kCodeMax : __uint_as_float(0x7fc00000u);
+          scales[((page * a.kv_heads + head) << a.shift) + slot] = finite ? most / kCodeMax : __uint_as_float(0x7fc00000u);
         }
+        // quotients by the reciprocal and one step that takes the rest into account; rows of the smallest numbers times 2^64, exactly, so that it is finite
+        const float lift = most < 1e-30f ? 18446744073709551616.f : 1.f, divisor = most * lift, over = 1.f / divisor, by = kCodeMax * lift;
 #pragma unroll
         for (int k = 0; k < UNITS; ++k) {
           if (!there[k]) continue;
 #pragma unroll
-          for (int e = 0; e < 2 * V; ++e) y[k][e] = finite && top ? kCodeMax * y[k][e] / most : 0.f;
+          for (int e = 0; e < 2 * V; ++e) {
+            const float n = by * y[k][e], q = n * over;
+            y[k][e] = finite && top ? fmaf(fmaf(-q, divisor, n), over, q) : 0.f;
+          }
           store_codes<V>((uint8_t*)to + o0[k], y[k]);
           store_codes<V>((uint8_t*)to + o1[k], y[k] + V);
         }
@@ -186,15 +210,31 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a, co
 
 template <typename X, typename C, int V, int UNITS>
 int launch_units(const RotaryArgs& a, hipStream_t s) {
-  const int units = a.D / (2 * V), rows = a.heads + 2 * a.kv_heads;
+  const int units = a.D / (2 * V), heads = a.heads + 2 * a.kv_heads, half = a.rotary_dim / 2;
   int lanes_log = 0;
   while ((UNITS << lanes_log) < units) ++lanes_log;
-  const int slices = (int)std::min<int64_t>(rows, std::max<int64_t>(1, (int64_t)(1 << 19) / ((int64_t)a.T << lanes_log)));
-  const int per = kThreads >> lanes_log;
-  const int blocks = (int)std::min<int64_t>(((int64_t)a.T * slices + per - 1) / per, 1 << 16);
+  const int slots = kThreads >> lanes_log;
+  int tokens = 1;
+  while (2 * tokens <= slots && 2 * tokens * half <= kAngles && a.T / (2 * tokens) >= 1024) tokens *= 2;
+  // few tokens: their heads over more workgroups
+  const int rows = slots / tokens, blocks = (a.T + tokens - 1) / tokens;
+  const int turns = (heads + rows - 1) / rows, parts = std::max(1, std::min(turns, 1024 / blocks));
+  const int heads_each = (turns + parts - 1) / parts * rows;
   ProfScope prof(kProfRotary, s);
-  if (a.layout == MOE_ROPE_HALF) rotary_kernel<X, C, V, UNITS, true><<<blocks, kThreads, 0, s>>>(a, lanes_log, slices);
-  else rotary_kernel<X, C, V, UNITS, false><<<blocks, kThreads, 0, s>>>(a, lanes_log, slices);
+  // a grid of 2^32 threads and more would run as what is left of it modulo 2^32
+  for (int64_t t = 0; t < a.T; t += (int64_t)tokens << 20) {
+    RotaryArgs p = a;
+    p.T = (int)std::min<int64_t>(a.T - t, (int64_t)tokens << 20);
+    const int64_t x = t * (int64_t)sizeof(X);
+    auto moved = [](const void* q, int64_t bytes) { return q ? static_cast<const char*>(q) + bytes : nullptr; };
+    p.q = moved(a.q, x * a.q_token); p.k = moved(a.k, x * a.k_token); p.v = moved(a.v, x * a.v_token); p.q_out = const_cast<char*>(moved(a.q_out, x * a.out_token));
+    p.pos = a.pos + t;
+    p.seq = a.seq ? a.seq + t : nullptr;
+    p.first_seq = (int)t;
+    const dim3 grid((p.T + tokens - 1) / tokens, (heads + heads_each - 1) / heads_each);
+    if (a.layout == MOE_ROPE_HALF) rotary_kernel<X, C, V, UNITS, true><<<grid, kThreads, 0, s>>>(p, lanes_log, tokens, heads_each);
+    else rotary_kernel<X, C, V, UNITS, false><<<grid, kThreads, 0, s>>>(p, lanes_log, tokens, heads_each);
+  }
   return hip_fail(hipGetLastError(), "rotary_kernel");
 }
 
@@ -202,7 +242,8 @@ template <typename X, typename C>
 int launch_typed(const RotaryArgs& a, hipStream_t s) {
   // units of V pairs that divide the pairs that turn and those that do not
   const int both = a.rotary_dim / 2 | (a.D - a.rotary_dim) / 2;
-  if (both % 8 == 0 && sizeof(X) == 2) return launch_units<X, C, 8, 1>(a, s);
+  if constexpr (sizeof(X) == 2)
+    if (both % 8 == 0) return launch_units<X, C, 8, 1>(a, s);
   if (both % 4 == 0) return launch_units<X, C, 4, 1>(a, s);
   if (both % 2 == 0) return launch_units<X, C, 2, 1>(a, s);
   return launch_units<X, C, 1, 2>(a, s);
