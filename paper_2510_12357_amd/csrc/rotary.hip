@@ -81,10 +81,11 @@ __device__ __forceinline__ void store_codes(uint8_t* p, const float* v) {
 // X: type of queries, keys and values; V: pairs of a unit, which divides a row's pairs that turn and those that do not; UNITS: units of a lane, a row's lanes
 // apart.  C: type of the cache's rows.  A workgroup has `tokens` tokens (a power of two) and of each the heads of its part of the grid's second dimension.
 constexpr int kAngles = 256;               // of a workgroup
-constexpr int kAhead = 4;                  // heads whose loads are on their way together
 template <typename X, typename C, int V, int UNITS, bool HALF>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a, const int lanes_log, const int tokens, const int heads_each) {
   constexpr bool kCodes = sizeof(C) == 1;
+  constexpr int kAhead = sizeof(X) == 4 || kCodes ? 2 : 4;  // heads whose loads are on their way together: registers for more cost waves
+  constexpr bool kApart = !HALF && V > 1;                   // a lane's two chunks are half a row apart, each of whole pairs, so that lanes' are neighbours
   typedef Chunk<X, V> Ch;
   __shared__ __attribute__((aligned(16))) float s_cos[kAngles], s_sin[kAngles];
   const int lanes = 1 << lanes_log, j = threadIdx.x & (lanes - 1), row = threadIdx.x >> lanes_log, rows = (kThreads >> lanes_log) / tokens;
@@ -108,18 +109,26 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a, co
   const int first = blockIdx.y * heads_each, heads = t < a.T ? min(page >= 0 ? a.heads + 2 * a.kv_heads : a.heads, first + heads_each) : 0;
   float c[UNITS][V], s[UNITS][V];
   int o0[UNITS], o1[UNITS];
-  bool turns[UNITS], there[UNITS];
+  bool turns[UNITS][2], there[UNITS];                       // the first half of a lane's pairs, the others
 #pragma unroll
   for (int k = 0; k < UNITS; ++k) {
     const int u = j + k * lanes;
     there[k] = u < units;
-    turns[k] = u < turning;
-    o0[k] = turns[k] && HALF ? u * V : 2 * u * V;
-    o1[k] = turns[k] && HALF ? half + u * V : o0[k] + V;
+    turns[k][0] = turns[k][1] = u < turning;
+    o0[k] = HALF && u < turning ? u * V : 2 * u * V;
+    o1[k] = HALF && u < turning ? half + u * V : o0[k] + V;
+    if constexpr (kApart) {
+      o0[k] = u * V;
+      o1[k] = (units + u) * V;
+      turns[k][0] = o0[k] < a.rotary_dim;
+      turns[k][1] = there[k] && o1[k] < a.rotary_dim;
+    }
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-      c[k][e] = turns[k] ? s_cos[local * half + u * V + e] : 1.f;
-      s[k][e] = turns[k] ? s_sin[local * half + u * V + e] : 0.f;
+      const bool turned = turns[k][2 * e >= V];
+      const int angle = local * half + (!kApart ? u * V + e : 2 * e < V ? o0[k] / 2 + e : o1[k] / 2 + e - V / 2);
+      c[k][e] = turned ? s_cos[angle] : 1.f;
+      s[k][e] = turned ? s_sin[angle] : 0.f;
     }
   }
   for (int h0 = first + row % rows; h0 < heads; h0 += kAhead * rows) {
@@ -151,7 +160,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a, co
         for (int e = 0; e < V; ++e) {
           const int ia = HALF ? e : 2 * e, ib = HALF ? V + e : 2 * e + 1;
           const float p = x[ia], q = x[ib];
-          const bool moves = turns[k] && !value;
+          const bool moves = turns[k][2 * e >= V] && !value;
           y[k][ia] = moves ? fmaf(p, c[k][e], -(q * s[k][e])) : p;
           y[k][ib] = moves ? fmaf(q, c[k][e], p * s[k][e]) : q;
         }
@@ -215,7 +224,7 @@ int launch_units(const RotaryArgs& a, hipStream_t s) {
   while ((UNITS << lanes_log) < units) ++lanes_log;
   const int slots = kThreads >> lanes_log;
   int tokens = 1;
-  while (2 * tokens <= slots && 2 * tokens * half <= kAngles && a.T / (2 * tokens) >= 1024) tokens *= 2;
+  while (2 * tokens <= slots && 2 * tokens * half <= kAngles && 2 * tokens <= a.T && (a.T / (2 * tokens) >= 1024 || slots / (2 * tokens) >= heads)) tokens *= 2;
   // few tokens: their heads over more workgroups
   const int rows = slots / tokens, blocks = (a.T + tokens - 1) / tokens;
   const int turns = (heads + rows - 1) / rows, parts = std::max(1, std::min(turns, 1024 / blocks));
