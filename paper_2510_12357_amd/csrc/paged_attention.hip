@@ -29,6 +29,14 @@ typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) int i32x4;
 typedef __attribute__((ext_vector_type(2))) int i32x2;
 
+// tanh: below 1 by Lambert's continued fraction to its sixth term (2^-29 off), beyond by 1 - 2 / (1 + e^2y).
+__device__ __forceinline__ float capped(float y) {
+  const float z = y * y;
+  const float p = y * fmaf(z, fmaf(z, 21.f, 1260.f), 10395.f), q = fmaf(z, fmaf(z, z + 210.f, 4725.f), 10395.f);
+  const float near = p * __builtin_amdgcn_rcpf(q), far = 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(y * (2.f * kLog2e)));
+  return fabsf(y) < 1.f ? near : far;
+}
+
 // N neighbouring elements of a row of the cache, as they lie there and in fp32
 template <typename C, int N> struct Raw;
 template <> struct Raw<__bf16, 8> { typedef i32x4 type; };
@@ -394,12 +402,12 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNK
         x[u][i] = v * to_log2;
       }
     }
-    if (a.softcap > 0.f) {                                  // cap tanh(s / cap) = cap - 2 cap / (1 + e^(2 s / cap)), off by 2^-22 of the cap
-      const float cap = a.softcap * kLog2e, twice = 2.f / a.softcap;
+    if (a.softcap > 0.f) {
+      const float cap = a.softcap * kLog2e, per = 1.f / cap;
 #pragma unroll
       for (int u = 0; u < kTiles; ++u)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[u][i] = cap - 2.f * cap / (1.f + __builtin_amdgcn_exp2f(x[u][i] * twice));
+        for (int i = 0; i < 4; ++i) x[u][i] = cap * capped(x[u][i] * per);
     }
     auto hidden = [&](int u, int i) { const int t = t0 + 16 * u + 4 * g + i; return t < first || t >= p.end; };
     if (!whole) {                                           // what is not seen counts as nothing, whatever it is
@@ -460,18 +468,22 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNK
             for (int j = 0; j < VW; ++j)
               acc[c][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(element<C, VW>(r.v[u][i][c], j), e[u][i], acc[c][j], 0, 0, 0);
     } else {
-      // position 4 g + i of tile u is operand element 4 (u % 2) + i of lane group g in both; probabilities in two bf16 terms, 2^-17 of them off
+      // position 4 g + i of tile u is operand element 4 (u % 2) + i of lane group g in both; probabilities in two bf16 terms, 2^-17
+      // of them off, which bf16 results do not show, in three for fp32 ones
 #pragma unroll
       for (int u0 = 0; u0 < kTiles; u0 += 2) {
-        bf16x8 hi, lo;
+        constexpr int kTerms = PARTS == 1 ? 2 : 3;
+        f32x8 w;
+        bf16x8 term[kTerms];
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float w = u0 + u < kTiles ? e[u0 + u < kTiles ? u0 + u : 0][i] : 0.f;
-            hi[4 * u + i] = (__bf16)w;
-            lo[4 * u + i] = (__bf16)(w - (float)hi[4 * u + i]);
-          }
+          for (int i = 0; i < 4; ++i) w[4 * u + i] = u0 + u < kTiles ? e[u0 + u < kTiles ? u0 + u : 0][i] : 0.f;
+#pragma unroll
+        for (int t = 0; t < kTerms; ++t) {
+          term[t] = __builtin_convertvector(w, bf16x8);
+          w -= __builtin_convertvector(term[t], f32x8);
+        }
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
@@ -482,10 +494,9 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNK
 #pragma unroll
               for (int i = 0; i < 4; ++i) widen_four<C>(r.v[u0 + u < kTiles ? u0 + u : 0][i][c], j, 4 * u + i, u0 + u < kTiles, value);
 #pragma unroll
-            for (int o = 0; o < 4; ++o) {
-              acc[c][j + o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(value[o], lo, acc[c][j + o], 0, 0, 0);
-              acc[c][j + o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(value[o], hi, acc[c][j + o], 0, 0, 0);
-            }
+            for (int t = kTerms - 1; t >= 0; --t)           // small terms first
+#pragma unroll
+              for (int o = 0; o < 4; ++o) acc[c][j + o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(value[o], term[t], acc[c][j + o], 0, 0, 0);
           }
       }
     }
