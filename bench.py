@@ -52,6 +52,8 @@ def parse_args():
     ap.add_argument("--vocab", type=int, default=256,
                     help="tokens of the toy language model of --alg1-toy; above 256 its head is a product of 8-bit integers and "
                          "the confidences are read off with the log probabilities")
+    ap.add_argument("--attention", action="store_true",
+                    help="the toy language model of --alg1-toy has attention over a paged key-value cache in front of every layer")
     ap.add_argument("--alg1-offload", action="store_true",
                     help="only the Alg. 1 loop with the experts in host memory, prefetch distance 0..3; one JSON line")
     ap.add_argument("--calibrate-copy", action="store_true",
@@ -462,13 +464,13 @@ def time_offload_eq1(mm, torch, cfg, steps: int, warmup: int, n_slots: int = 16,
     return out
 
 
-def time_alg1_toy(mm, torch, cfg, steps: int, warmup: int, L: int = 4, V: int = 256, ratio: float = 0.2):
+def time_alg1_toy(mm, torch, cfg, steps: int, warmup: int, L: int = 4, V: int = 256, ratio: float = 0.2, attention: bool = False):
     """Alg. 1 over many decoding steps on a toy language model of L layers of shape `cfg` (continuous
     batching, cfg.T slots): accepted tokens per second and the realised fallback ratio, against the
     same model without the method (every pass a big pass) and against Eq. 1's estimate."""
     import numpy as np
     from paper_2510_12357_amd import workloads as wl
-    from paper_2510_12357_amd.alg1_driver import Alg1Batch, ToyLMDevice
+    from paper_2510_12357_amd.alg1_driver import Alg1Batch, ToyAttention, ToyLMDevice
     B = cfg.T
     dl = DeviceLayers(cfg, L, seed=7)
     g = torch.Generator(device="cuda")
@@ -482,7 +484,11 @@ def time_alg1_toy(mm, torch, cfg, steps: int, warmup: int, L: int = 4, V: int = 
     # input calibration: scale the random head so that a fraction `ratio` of the little model's
     # confidences (over the whole vocabulary as input) does not exceed gamma
     int8_head = V > 256
-    probe = Alg1Batch(ToyLMDevice(cfg, V, embed, head32.to(dt), layers, norm=True, int8_head=int8_head), B, prompts, max_new=32)
+    more = dict(norm=True, int8_head=int8_head)
+    if attention:                                            # heads of 128 channels, four of them to a key head
+        n = max(4, cfg.H // 128 // 4 * 4)
+        more["attention"] = ToyAttention.random(cfg, L, n, n // 4, 128, seed=78)
+    probe = Alg1Batch(ToyLMDevice(cfg, V, embed, head32.to(dt), layers, **more), B, prompts, max_new=32)
     zs, n_probe = [], min(V, 1024)
     for t0 in range(0, n_probe, B):
         for b in range(B):
@@ -501,7 +507,7 @@ def time_alg1_toy(mm, torch, cfg, steps: int, warmup: int, L: int = 4, V: int = 
         mid = (lo * hi) ** 0.5
         lo, hi = (mid, hi) if frac_below(mid) > ratio else (lo, mid)
     tau = hi
-    dev = ToyLMDevice(cfg, V, embed, (head32 * tau).to(dt), layers, norm=True, int8_head=int8_head)
+    dev = ToyLMDevice(cfg, V, embed, (head32 * tau).to(dt), layers, **more)
     del probe
 
     def timed(always_big):
@@ -869,7 +875,7 @@ def main():
     if args.alg1_toy:
         L = args.layers if args.layers > 0 else 4
         res = time_alg1_toy(mm, torch, workload_config(args.workload, args.ratio), args.steps, args.warmup, L=L,
-                            V=args.vocab, ratio=args.ratio)
+                            V=args.vocab, ratio=args.ratio, attention=args.attention)
         print(json.dumps(dict(metric="Alg. 1 on a toy MoE language model: accepted tokens/s", workload=args.workload,
                               **res)))
         return

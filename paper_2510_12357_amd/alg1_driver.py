@@ -18,6 +18,11 @@ runs all slots together as one mixed batch: the per-token confidence handed to t
 big-mode slots, so that the layer kernels see exactly the mixed k of the paper's method.  A
 finished sequence (<eos> or the length cap) is replaced by the next prompt at once.
 
+Attention (optional, `ToyAttention`; not in the paper): every layer looks back at its sequence's earlier tokens first.  Its keys and
+values lie in pages that a slot takes as its sequence grows and gives back at its end; the step is one `KvCache.append` (queries and keys
+turned by their positions, keys and values stored) and one `DecodeAttention` call per layer.  The big pass of a rejected token writes the position
+that the little pass wrote, so that both share one cache.
+
 Offloaded experts (Sec. II-B, III-B): with one expert cache per layer the routed experts live in
 pinned host memory and every layer fetches what its router selected.  For a slot in big mode the
 router logits of its rejected little pass are known for ALL layers before the big pass starts, so
@@ -37,20 +42,79 @@ from . import binding as mm
 from . import workloads as wl
 
 
+class ToyAttention:
+    """The attention in front of every layer of a toy language model: x + out . attention(qkv . x), with the model's `norm` on what goes in and comes
+    out.  weights: per layer a dict with qkv [(n_heads + 2 n_kv_heads) head_dim, H] and out [H, n_heads head_dim] in the layers' dtype.  cache_dtype: of
+    the keys and values (default: the weights')."""
+
+    def __init__(self, n_heads: int, n_kv_heads: int, head_dim: int, weights: list, rotary: mm.Rotary, page_size: int = 16,
+                 cache_dtype: Optional[torch.dtype] = None, window: int = 0):
+        self.n_heads, self.n_kv_heads, self.head_dim, self.weights, self.rotary = n_heads, n_kv_heads, head_dim, weights, rotary
+        self.page_size, self.window = page_size, window
+        self.cache_dtype = weights[0]["qkv"].dtype if cache_dtype is None else cache_dtype
+
+    @classmethod
+    def random(cls, cfg: wl.LayerConfig, L: int, n_heads: int, n_kv_heads: int, head_dim: int, seed: int = 0, device="cuda", **more) -> "ToyAttention":
+        """Random weights that keep a row's size."""
+        g = torch.Generator(device=device)
+        g.manual_seed(seed)
+        dtype = torch.float32 if cfg.dtype == "fp32" else torch.bfloat16
+
+        def weight(n, k):
+            return (torch.randn((n, k), generator=g, device=device) * k ** -0.5).to(dtype)
+        weights = [dict(qkv=weight((n_heads + 2 * n_kv_heads) * head_dim, cfg.H), out=weight(cfg.H, n_heads * head_dim)) for _ in range(L)]
+        return cls(n_heads, n_kv_heads, head_dim, weights, mm.Rotary.scaled(head_dim, device=device), **more)
+
+
+class SequencePages:
+    """The pages of B sequences of at most `longest` positions: taken one by one as a sequence grows, given back at its end.  All layers' caches use the
+    same table."""
+
+    def __init__(self, B: int, longest: int, page_size: int, device):
+        self.page_size, self.each = page_size, -(-longest // page_size)
+        self.n_pages = B * self.each
+        self.free = list(range(self.n_pages - 1, -1, -1))
+        self.host = np.full((B, self.each), -1, np.int32)
+        self.table = torch.from_numpy(self.host).to(device)
+        self.changed = False
+
+    def reach(self, b: int, pos: int) -> None:
+        """Sequence b has a page for position pos."""
+        e = pos // self.page_size
+        if self.host[b, e] < 0:
+            self.host[b, e] = self.free.pop()
+            self.changed = True
+
+    def give_back(self, b: int) -> None:
+        for page in self.host[b][self.host[b] >= 0]:
+            self.free.append(int(page))
+        self.changed |= bool((self.host[b] >= 0).any())
+        self.host[b] = -1
+
+    def upload(self) -> torch.Tensor:
+        if self.changed:
+            self.table.copy_(torch.from_numpy(self.host))
+            self.changed = False
+        return self.table
+
+
 class ToyLMDevice:
     """A toy language model on the device: embedding [V,H], head [V,H] (both in the layers' dtype)
     and per layer a dict with Wg, gate_bias (or None), table (int64 device pointers of the E expert
     blobs) and shared (list of blobs).  `block_work` (a callable or None) is enqueued once per layer
-    in front of the MoE layer: a stand-in for the rest of a transformer block (attention), which
-    the toy model does not have, for measurements that need its time."""
+    in front of the MoE layer: a stand-in for the rest of a transformer block, for measurements that need its
+    time where the model has no `attention`."""
 
     def __init__(self, cfg: wl.LayerConfig, V: int, embed: torch.Tensor, head: torch.Tensor, layers: list,
-                 norm: bool = False, block_work=None, int8_head: bool = False):
+                 norm: bool = False, block_work=None, int8_head: bool = False, attention: Optional[ToyAttention] = None):
         if V > 256 and not int8_head:
             raise ValueError("the output head runs on the router kernel: at most 256 tokens in the vocabulary")
         self.cfg, self.V, self.device = cfg, V, embed.device
         self.embed, self.head, self.layers, self.norm = embed, head, layers, norm
         self.block_work = block_work
+        if attention is not None and len(attention.weights) != len(layers):
+            raise ValueError("one set of attention weights per layer")
+        self.attention = attention
         # a head of codes and one scale per token, for a vocabulary of any size
         self.int8_head = mm.Int8Linear.quantize(head) if int8_head else None
         # the head as a "router" over V outputs with one selected entry
@@ -58,7 +122,7 @@ class ToyLMDevice:
                                        dtype="fp32" if cfg.dtype == "fp32" else "bf16", gamma=cfg.gamma)
 
     @classmethod
-    def upload(cls, lm: wl.ToyLM, device="cuda", int8_head: bool = False) -> "ToyLMDevice":
+    def upload(cls, lm: wl.ToyLM, device="cuda", int8_head: bool = False, attention: Optional[ToyAttention] = None) -> "ToyLMDevice":
         """Device copies of a workloads.ToyLM."""
         cfg = lm.cfg
         if lm.V > 256 and not int8_head:
@@ -75,7 +139,7 @@ class ToyLMDevice:
                 experts=experts, table=table,
                 shared=[mm.to_device(b, cfg, device) for b in l.shared_w]))
         return cls(cfg, lm.V, mm.to_device(lm.embed, cfg, device), mm.to_device(lm.head, cfg, device), layers,
-                   lm.norm, int8_head=int8_head)
+                   lm.norm, int8_head=int8_head, attention=attention)
 
     def between_layers(self, out: torch.Tensor) -> torch.Tensor:
         """What the next layer (or the head) reads: the layer's stored output, with `norm` its rows
@@ -139,6 +203,12 @@ class Alg1Batch:
             self.lp = mm.LogprobBuffers(B, 0, 1, dev.V, d)
         self.tok_dev = torch.empty((B,), dtype=torch.int64, device=d)
         self.conf_dev = torch.empty((B,), dtype=torch.float32, device=d)
+        at = dev.attention
+        if at is not None:
+            self.pages = SequencePages(B, 1 + max_new, at.page_size, d)
+            self.kv = [mm.KvCache.empty(self.pages.n_pages, at.page_size, at.n_kv_heads, at.head_dim, at.cache_dtype, d) for _ in dev.layers]
+            self.attend = [mm.DecodeAttention(c, at.n_heads, window=at.window) for c in self.kv]
+            self.pos_dev, self.len_dev = (torch.empty((B,), dtype=torch.int32, device=d) for _ in range(2))
         # host state of the slots
         self.seq_id = [-1] * B
         self.tokens: List[List[int]] = [[] for _ in range(B)]
@@ -179,11 +249,24 @@ class Alg1Batch:
             self.seq_id[b] = -1
             self.tokens[b] = []
         self.from_big[b] = []
+        if self.dev.attention is not None:
+            self.pages.give_back(b)
         self.token_logp[b], self.token_entropy[b] = [], []
         self.big[b] = self.always_big
 
     def active(self) -> np.ndarray:
         return np.array([s >= 0 for s in self.seq_id])
+
+    # ---- attention in front of layer l
+    def _look_back(self, l: int, x: torch.Tensor, table: torch.Tensor, longest: int, looked: list) -> torch.Tensor:
+        at, w = self.dev.attention, self.dev.attention.weights[l]
+        rows = torch.nn.functional.linear(self.dev.between_layers(x), w["qkv"]).view(self.B, at.n_heads + 2 * at.n_kv_heads, at.head_dim)
+        q, k, v = rows.split([at.n_heads, at.n_kv_heads, at.n_kv_heads], dim=1)
+        turned = self.kv[l].append(k, v, self.pos_dev, table, rotary=at.rotary, q=q)
+        out = self.attend[l](turned, table, self.len_dev, longest)
+        if self.record is not None:
+            looked.append(dict(rows=rows.cpu(), turned=turned.cpu(), out=out.cpu()))
+        return self.dev.between_layers(x + torch.nn.functional.linear(out.view(self.B, -1), w["out"]))
 
     # ---- one step of the whole batch
     def step(self) -> None:
@@ -198,7 +281,16 @@ class Alg1Batch:
         self.tok_dev.copy_(torch.from_numpy(tok))
         self.conf_dev.copy_(torch.from_numpy(conf_in))
         x = dev.embed.index_select(0, self.tok_dev)
-        xs = [x]
+        xs, looked = [x], []
+        if dev.attention is not None:
+            # the input token's position; an empty slot has none, and nothing to look at
+            pos = np.array([len(self.tokens[b]) - 1 if act[b] else -1 for b in range(B)], np.int32)
+            for b in range(B):
+                if act[b]:
+                    self.pages.reach(b, int(pos[b]))
+            self.pos_dev.copy_(torch.from_numpy(pos))
+            self.len_dev.copy_(torch.from_numpy(pos + 1))
+            table, longest = self.pages.upload(), int(pos.max()) + 1
         L = len(dev.layers)
         if self.sched is not None:
             self._prefetch(-1)
@@ -207,6 +299,8 @@ class Alg1Batch:
                 self._prefetch(l)           # layer l is about to run: request what layer l + d will need
             if dev.block_work is not None:
                 dev.block_work()
+            if dev.attention is not None:
+                x = self._look_back(l, x, table, longest, looked)
             if self.caches is None:
                 # resident experts: a batch of at most 64 slots is one call per layer
                 step = mm.layer_decode_step if b.lws is not None else mm.layer_step
@@ -238,7 +332,7 @@ class Alg1Batch:
         if self.record is not None:
             self.record.append(dict(
                 seq_id=list(self.seq_id), pos=[len(t) for t in self.tokens], tokens_in=tok.copy(),
-                big_in=self.big.copy(), conf_in=conf_in.copy(),
+                big_in=self.big.copy(), conf_in=conf_in.copy(), attention=looked,
                 layers=[dict(x_in=xi.detach().cpu(), logits=b.logits.cpu().numpy(),
                              topk_idx=b.topk_idx.cpu().numpy(), k_t=b.k_t.cpu().numpy(),
                              important=b.important.cpu().numpy(), out=b.out.detach().cpu())
