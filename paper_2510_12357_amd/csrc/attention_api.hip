@@ -84,6 +84,7 @@ int resolve(const char* call, const moe_attention_config* cfg, const moe_kv_cach
   if (c->max_len < 0 || c->window < 0) return fail(MOE_E_BADARG, "%s: max_len=%d window=%d", call, c->max_len, c->window);
   if (c->max_len > INT32_MAX - 2 * kMaxPiece) return fail(MOE_E_UNSUPPORTED, "%s: max_len=%d", call, c->max_len);
   if (!isfinite(c->scale) || !isfinite(c->softcap) || c->softcap < 0) return fail(MOE_E_BADARG, "%s: scale %g softcap %g", call, c->scale, c->softcap);
+  if (fabsf(c->scale) > 1e30f || c->softcap > 1e30f || (c->softcap > 0 && c->softcap < 1e-30f)) return fail(MOE_E_UNSUPPORTED, "%s: scale %g softcap %g", call, c->scale, c->softcap);
   if (int rc = resolve_table(call, c->B, c->table_len, &c->table_ld)) return rc;
   if (int rc = resolve_strides(call, "q", c->B, c->heads, cache.D, &c->q_token, &c->q_head)) return rc;
   if (int rc = resolve_strides(call, "out", c->B, c->heads, cache.D, &c->out_token, &c->out_head)) return rc;

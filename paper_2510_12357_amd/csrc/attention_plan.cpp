@@ -6,7 +6,10 @@
 namespace mm {
 
 // slots: workgroups that the device runs at once.  As many have equal shares, whatever the sequences' lengths are, so that all end together.  Where the work is too little
-// for that, a workgroup has one unit or a part of one: what a second one in a row would wait for costs more.
+// for that, a workgroup has one unit or a part of one: what a second one in a row would wait for costs more
+// (us, shares / aligned: 4 sequences of up to 2000 on 8 key heads 14.9 / 10.5, 33 on a window of 1000 with 71 heads 21.4 / 17.6, 8 of up to 4096 25.3 / 24.8; where every
+// unit is short but there are more of them than workgroups, shares: 256 sequences of up to 300 50 / 55).  Parts of 4 blocks as long as there is a CU for each (4 sequences
+// of up to 2000: 12.0 with 8).
 AttentionPlan plan_attention(int sequences, int kv_heads, int group, int max_len, int window, int slots, int device_cus) {
   const int64_t units = (int64_t)sequences * kv_heads * ((group + kHeadTile - 1) / kHeadTile);
   // a window that starts inside a block reaches over one more of them

@@ -1,12 +1,18 @@
 // Attention of one new token per sequence over a paged cache (moe_paged_attention).
 //
-// The positions that all sequences' tokens see, for each key head and up to 16 of its query heads, are a line of blocks that workgroups share equally, as many as run at once
-// (attention_plan.h); of a workgroup's segments, each of one sequence and key head, its waves take blocks in turn.
+// What bounds it: reading the keys and values that are seen, once per key head.  The positions of all sequences, for each key head and up to 16 of its query heads, are a
+// line of blocks that as many workgroups as run at once share equally (attention_plan.h), whatever the lengths are: 64 sequences of 400 to 8192 positions
+// (32 heads on 8 of 128 channels, bf16, 1.1 GB) take 178 us, 6.2 TB/s; with a workgroup for each part of fixed length 191, of which the last ones ran alone.  A workgroup's
+// segments are of one sequence and key head each, of which its waves take blocks in turn.
 // Scores are the product of a tile of keys (rows: positions) and the queries (columns: heads), so that a lane has four positions of one head, which is where the
-// product with the values wants the probabilities: nothing moves between lanes.  That product runs on fp32 matrix instructions, whose operands hold one position a lane: values
-// are used as their rows lie in memory, and probabilities are not rounded.
+// product with the values wants the probabilities: nothing moves between lanes.  Values go into that product from where their rows lie, a lane with the same channels
+// of four positions: two halves of different registers make an operand's word.  Keys are loaded by whole rows, too, and change lanes in LDS: straight into the operand's
+// layout a load takes half a line of 16 rows, and the same sequences took 221 us.  Both products run on bf16 matrix instructions, exact in the keys, queries and values, with
+// probabilities in two or three bf16 terms; caches in fp32 on fp32 ones.
+// A block's keys are loaded again as soon as they are in LDS, its values as soon as they are used: a block and a half of each wave is on its way.  More waves or larger blocks
+// did not help (2 or 3 workgroups per CU, 8 or 16 KB a wave: within 1 %), fewer bytes on their way did harm (one workgroup per CU: +15 %).
 // The maximum that exponentials are taken against follows the scores only when one is 2^8 above it: sums stay far below fp32's range, and most blocks neither exchange
-// maxima nor rescale.  Waves' sums are joined in LDS, parts' sums by the last of a sequence's workgroups or, where they are many, by a second
+// maxima nor rescale.  Waves' sums are joined in LDS, parts' sums by the last of a unit's workgroups to end or, where parts are many, by a second
 // kernel, all in a fixed order.
 #include <math.h>
 
@@ -121,7 +127,8 @@ __device__ __forceinline__ void store_row(const AttentionArgs& a, int b, int hea
   if (a.lse && channel == 0) a.lse[(int64_t)b * a.heads + head] = l == 0.f ? -INFINITY : fmaf(m, kLn2, logf(l));
 }
 
-// Tiles of 16 positions of a wave's block, and waves of a SIMD that the registers are shared by.
+// Tiles of 16 positions of a wave's block, and waves of a SIMD that the registers are shared by: as many as need no spills (with 20 registers of spills the largest bf16
+// kernel took 18 % longer, on half as many workgroups again).
 constexpr int block_tiles(size_t bytes, int dims) { return std::clamp(512 / (int)(dims * bytes), 1, 2); }
 constexpr int waves_per_simd(size_t bytes, int dims, int parts) {
   if (dims > 128) return bytes < 4 && parts == 1 ? 2 : 1;
@@ -145,14 +152,14 @@ struct Block {
   typedef typename std::conditional<kF32, f32x4, i32x4>::type RawK;
   RawK k[kTiles][kLoads];
   RawV v[kTiles][4][CHUNKS];
-  float scale;                                              // of a key (lanes below 32) or value: position lane % 32
+  float scale;                                              // of a key (lanes below 32) or value: position lane % 32; through LDS to the lanes that multiply by it
   // where vector c of row r of a tile is in LDS: eight rows' vectors of the same c fall on different banks
   static __device__ __forceinline__ int place(int r, int c) {
     constexpr int kRows = kRowLanes < 16 ? 16 / kRowLanes : 1;        // of 256 bytes, all banks
     return (r * kRowLanes + (c ^ (r / kRows & (kRowLanes < 16 ? kRowLanes - 1 : 15)))) * 16;
   }
 };
-// loads past the caches: keys and values are read once
+// Loads past the caches: keys and values are read once (64 sequences as above: with ordinary loads 214 us, then 191).
 template <typename T>
 __device__ __forceinline__ T load_once(const T* p) { return __builtin_nontemporal_load(p); }
 __device__ __forceinline__ Eight load_once(const Eight* p) { return {load_once(&p->lo), load_once(&p->hi)}; }
@@ -365,6 +372,7 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNK
       for (int s = 0; s < kLoads; ++s) *reinterpret_cast<typename Blk::RawK*>(keys + u * 16 * Blk::kRowLanes * 16 + Blk::place(lane / Blk::kRowLanes * kLoads + s, lane % Blk::kRowLanes)) = r.k[u][s];
     f32x4 ks[kTiles], vs[kTiles];
     if constexpr (kCodes) s_scale[wave][lane / 32][lane % 32] = r.scale;
+    asm volatile("" ::: "memory");                          // other lanes' writes: a wave's LDS operations run in order
     if constexpr (kCodes) {
 #pragma unroll
       for (int u = 0; u < kTiles; ++u) {

@@ -2,6 +2,8 @@
 //
 // Pairs of channels (a, b) turn by t = pos freq: a' = m (a cos t - b sin t), b' = m (b cos t + a sin t).  A workgroup has a few tokens, works out their sines and cosines
 // once, one a thread, into LDS, and turns V pairs a lane of head after head; of a row's lanes each has the same pairs in all heads, so that they stay in registers.
+// What bounds it: reading and writing; few tokens, the launch.  4096 tokens of 40 heads of 128 channels, bf16 (84 MB) 16.7 us, 5.0 TB/s; an append of 16384 tokens of 32 + 8 + 8 heads
+// (400 MB) 79 us, 5.1 TB/s; of 2111 tokens into 8 bits 8.6 us (a copy of 2 GB reaches 4.9 TB/s).  With eight sines a lane and head instead, 19.7, 87 and 13.4 us.
 #include <algorithm>
 
 #include "internal.h"
@@ -226,8 +228,9 @@ int launch_units(const RotaryArgs& a, hipStream_t s) {
   int tokens = 1;
   while (2 * tokens <= slots && 2 * tokens * half <= kAngles && 2 * tokens <= a.T && (a.T / (2 * tokens) >= 1024 || slots / (2 * tokens) >= heads)) tokens *= 2;
   // few tokens: their heads over more workgroups
-  const int rows = slots / tokens, blocks = (a.T + tokens - 1) / tokens;
-  const int turns = (heads + rows - 1) / rows, parts = std::max(1, std::min(turns, 1024 / blocks));
+  const int rows = slots / tokens;
+  const int64_t blocks = ((int64_t)a.T + tokens - 1) / tokens;
+  const int turns = (heads + rows - 1) / rows, parts = (int)std::max<int64_t>(1, std::min<int64_t>(turns, 1024 / blocks));
   const int heads_each = (turns + parts - 1) / parts * rows;
   ProfScope prof(kProfRotary, s);
   // a grid of 2^32 threads and more would run as what is left of it modulo 2^32

@@ -126,7 +126,7 @@ def test_append_empty_calls():
 @pytest.mark.parametrize("change, code", [
     (dict(B=-1), SHAPE), (dict(heads=0), SHAPE), (dict(heads=5), SHAPE), (dict(dtype=4), BADARG), (dict(max_len=-1), BADARG), (dict(window=-1), BADARG),
     (dict(table_len=0), SHAPE), (dict(table_ld=1), SHAPE), (dict(max_len=2 ** 31 - 100), UNSUPPORTED), (dict(scale=NAN), BADARG), (dict(scale=-INF), BADARG),
-    (dict(softcap=-1.0), BADARG), (dict(softcap=INF), BADARG), (dict(q_head=63), SHAPE), (dict(out_token=-1), BADARG),
+    (dict(softcap=-1.0), BADARG), (dict(softcap=INF), BADARG), (dict(softcap=1e-40), UNSUPPORTED), (dict(softcap=2e38), UNSUPPORTED), (dict(scale=-1e38), UNSUPPORTED), (dict(q_head=63), SHAPE), (dict(out_token=-1), BADARG),
     (dict(B=1 << 30, heads=64), UNSUPPORTED),
 ])
 def test_attention_configs(change, code):

@@ -201,6 +201,22 @@ def test_the_same_call_has_the_same_bits_and_shares_pages():
         assert_near(again[i], want, err, BF16)
 
 
+@pytest.mark.parametrize("lengths, max_len", [([700, 3, 1900], None), ([5000, 9000], None), ([300] * 70, None)])
+def test_parts_joined_by_a_second_launch_and_results_in_place_of_the_queries(lengths, max_len):
+    """Without counters the C call joins parts in a launch of its own, to the same values; and out may be q."""
+    p, kv, q, attn, out, lse = _run(lengths, 16, 8, 2, 64, BF16, BF16, seed=7)
+    n = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    c = mm.moe_attention_config()
+    c.B, c.heads, c.dtype, c.max_len, c.table_len, c.scale = len(lengths), 8, mm.MOE_BF16, max(lengths), p.table.shape[1], 64 ** -0.5
+    need = mm.moe_paged_attention_workspace_bytes(c, p.cache.c)
+    ws = torch.full((max(need, 1),), 255, dtype=torch.uint8, device="cuda")
+    dq = q.cuda()
+    other, other_lse = torch.empty_like(dq), torch.empty_like(lse)
+    mm.moe_paged_attention(c, p.cache.c, dq, p.table.cuda(), n, other, other_lse, ws, need)
+    _check(p, kv, q, other, other_lse)
+    assert attn(dq, p.table.cuda(), n, max(lengths), out=dq) is dq and torch.equal(dq, out)
+
+
 @pytest.mark.parametrize("cache", [BF16, E4M3])
 def test_offsets_beyond_32_bits(cache):
     """Pages behind 2^32 elements of the cache."""
