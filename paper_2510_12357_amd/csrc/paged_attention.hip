@@ -637,8 +637,9 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNK
 }
 
 // The same of units of many parts: a workgroup for each workgroup of the first kernel in which a unit begins that ends in another one, and for each of its heads; four channels
-// a thread, the parts in turn over the threads of a channel.
-template <int kJoinThreads>
+// a thread, the parts in turn over the threads of a channel.  512 threads, both kernels
+// together: 21.3 us for 32 heads over 16000 positions (24.8 with 1024 threads, 20.8 with 256), 91.5 over 131072 (93.4 with 1024, 93.3 with 256).
+constexpr int kJoinThreads = 512;
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(const AttentionArgs a) {
   __shared__ float s_top[kJoinThreads / 64];
   __shared__ __attribute__((aligned(16))) f32x4 s_v[kJoinThreads];
@@ -706,7 +707,7 @@ int launch_attention(const AttentionArgs& a, hipStream_t s) {
   else if (a.cache_dtype == MOE_E4M3) rc = launch_cache<uint8_t>(a, s);
   else rc = launch_cache<__bf16>(a, s);
   if (rc || !a.started) return rc;
-  join_kernel<1024><<<dim3(a.workgroups, std::min(a.group, kHeadTile)), 1024, 0, s>>>(a);
+  join_kernel<<<dim3(a.workgroups, std::min(a.group, kHeadTile)), kJoinThreads, 0, s>>>(a);
   return hip_fail(hipGetLastError(), "join_kernel");
 }
 
