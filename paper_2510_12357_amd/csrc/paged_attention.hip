@@ -540,22 +540,26 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNK
   joined(n, &m, &l);
   const float weight = top == -INFINITY ? (sum == 0.f ? 0.f : sum) : __builtin_amdgcn_exp2f(top - m);     // a sum without a maximum is NaN
   const int64_t part_row = part_at(a, workgroup, seg.block == 0);
+  // where four channels of a head's sums are in LDS: the same ones of the 16 heads fall on different banks
+  auto sums_at = [](int head, int quad) { return 16 * (head * 4 * VW + (quad ^ (head & (4 * VW - 1)))); };
 #pragma unroll
   for (int c = 0; c < CHUNKS; ++c) {
     if (c) __syncthreads();
+    if (n < heads) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int j = 0; j < VW; j += 4)
-        *reinterpret_cast<f32x4*>(keys + 4 * (n * 16 * VW + VW * (4 * g + i) + j)) =
-            f32x4{acc[c][j][i], acc[c][j + 1][i], acc[c][j + 2][i], acc[c][j + 3][i]} * weight;
+        for (int j = 0; j < VW; j += 4)
+          *reinterpret_cast<f32x4*>(keys + sums_at(n, (VW * (4 * g + i) + j) / 4)) =
+              f32x4{acc[c][j][i], acc[c][j + 1][i], acc[c][j + 2][i], acc[c][j + 3][i]} * weight;
+    }
     __syncthreads();
-    for (int o = tid; o < 16 * 16 * VW / 4; o += kThreads) {
-      const int head = o / (4 * VW), d = o % (4 * VW) * 4, channel = 16 * VW * c + d;
+    for (int o = tid; o < heads * 4 * VW; o += kThreads) {
+      const int head = o / (4 * VW), quad = o % (4 * VW), channel = 16 * VW * c + 4 * quad;
       if (head >= heads || channel >= a.D) continue;
-      f32x4 v = *reinterpret_cast<const f32x4*>(s_mem + 4 * (head * 16 * VW + d));
+      f32x4 v = *reinterpret_cast<const f32x4*>(s_mem + sums_at(head, quad));
 #pragma unroll
-      for (int w = 1; w < kWaves; ++w) v += *reinterpret_cast<const f32x4*>(s_mem + w * kWaveBytes + 4 * (head * 16 * VW + d));
+      for (int w = 1; w < kWaves; ++w) v += *reinterpret_cast<const f32x4*>(s_mem + w * kWaveBytes + sums_at(head, quad));
       joined(head, &m, &l);
       if (seg.parts > 1) {
         float* to = a.part_out + (part_row + head) * a.D + channel;
