@@ -7,9 +7,10 @@ namespace mm {
 
 // slots: workgroups that the device runs at once.  As many have equal shares, whatever the sequences' lengths are, so that all end together.  Where the work is too little
 // for that, a workgroup has one unit or a part of one: what a second one in a row would wait for costs more
-// (us, shares / aligned: 4 sequences of up to 2000 on 8 key heads 14.9 / 10.5, 33 on a window of 1000 with 71 heads 21.4 / 17.6, 8 of up to 4096 25.3 / 24.8; where every
-// unit is short but there are more of them than workgroups, shares: 256 sequences of up to 300 50 / 55).  Parts of 4 blocks as long as there is a CU for each (4 sequences
-// of up to 2000: 12.0 with 8).
+// (us, shares / aligned: 4 sequences of up to 2000 on 8 key heads of 64 channels 16.5 / 9.9, 33 on a window of 1000 with 71 heads 19.5 / 17.0, 8 of up to 4096
+// 21.7 / 21.3), also in two rounds where every unit is one workgroup's (128 sequences of up to 300 28.4 / 24.9, of up to 128 19.9 / 18.6; not units of one block,
+// 14.2 / 16.5, units in parts, 30 of up to 2000 28.9 / 34.4, or four rounds, 256 of up to 300 43.9 / 49.5).  Parts of 4 blocks as long as there is a CU for each
+// (4 sequences of up to 2000: 2 us more with 8).
 AttentionPlan plan_attention(int sequences, int kv_heads, int group, int max_len, int window, int slots, int device_cus) {
   const int64_t units = (int64_t)sequences * kv_heads * ((group + kHeadTile - 1) / kHeadTile);
   // a window that starts inside a block reaches over one more of them
@@ -17,7 +18,7 @@ AttentionPlan plan_attention(int sequences, int kv_heads, int group, int max_len
   const int64_t blocks = std::max<int64_t>(1, (span + kSpan - 1) / kSpan);
   auto parts = [&](int64_t align) { return (blocks + align - 1) / align; };
   AttentionPlan p;
-  p.align = units * parts(4) <= device_cus ? 4 : units * parts(8) <= slots ? 8 : 0;
+  p.align = units * parts(4) <= device_cus ? 4 : units * parts(8) <= slots || (blocks > 1 && parts(8) == 1 && units <= 2 * slots) ? 8 : 0;
   p.fits = (double)units * (double)(blocks + std::max(kSetup, p.align)) < (double)(1 << 30);
   if (!p.fits) return p;
   p.workgroups = p.align ? (int)std::max<int64_t>(1, units * parts(p.align)) : std::min(slots, kMostWorkgroups);

@@ -2,7 +2,7 @@
 //
 // What bounds it: reading the keys and values that are seen, once per key head.  The positions of all sequences, for each key head and up to 16 of its query heads, are a
 // line of blocks that as many workgroups as run at once share equally (attention_plan.h), whatever the lengths are: 64 sequences of 400 to 8192 positions
-// (32 heads on 8 of 128 channels, bf16, 1.1 GB) take 178 us, 6.2 TB/s; with a workgroup for each part of fixed length 191, of which the last ones ran alone.  A workgroup's
+// (32 heads on 8 of 128 channels, bf16, 1.1 GB) take 177 us, 6.2 TB/s; with a workgroup for each part of fixed length 191, of which the last ones ran alone.  A workgroup's
 // segments are of one sequence and key head each, of which its waves take blocks in turn.
 // Scores are the product of a tile of keys (rows: positions) and the queries (columns: heads), so that a lane has four positions of one head, which is where the
 // product with the values wants the probabilities: nothing moves between lanes.  Values go into that product from where their rows lie, a lane with the same channels
@@ -11,6 +11,7 @@
 // probabilities in two or three bf16 terms; caches in fp32 on fp32 ones.
 // A block's keys are loaded again as soon as they are in LDS, its values as soon as they are used: a block and a half of each wave is on its way.  More waves or larger blocks
 // did not help (2 or 3 workgroups per CU, 8 or 16 KB a wave: within 1 %), fewer bytes on their way did harm (one workgroup per CU: +15 %).
+// Workgroups of one wave, each with a share of its own, join nothing but read units of their own all over the cache: 185 us, 5 % less only where sequences are short.
 // The maximum that exponentials are taken against follows the scores only when one is 2^8 above it: sums stay far below fp32's range, and most blocks neither exchange
 // maxima nor rescale.  Waves' sums are joined in LDS, parts' sums by the last of a unit's workgroups to end or, where parts are many, by a second
 // kernel, all in a fixed order.
