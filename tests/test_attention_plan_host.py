@@ -130,3 +130,11 @@ def test_plans(ask):
                 assert workgroups == 768 and split
     got = [p[2] if p[0] else None for p in plans]
     assert got == [0, 0, 4, 8, 4, 4, 4, None, 0, 0, 0, 0, 8] and plans[3][4] == 1 and plans[0][4] == 0
+
+
+def test_short_units_in_two_rounds(ask):
+    """Units of two to eight blocks have a workgroup each up to two rounds of them; longer, shorter or more ones share the line."""
+    cases = [(128, 300, 0), (128, 512, 0), (128, 65, 0), (128, 64, 0), (128, 513, 0), (129, 300, 0), (64, 513, 0), (32, 1024, 0), (100, 5000, 400), (100, 5000, 500)]
+    got = ask([f"plan {b} 8 4 {m} {w} 512 256" for b, m, w in cases])
+    assert [p[2] for p in got] == [8, 8, 8, 0, 0, 0, 0, 8, 8, 0]
+    assert [p[1] for p in got] == [1024, 1024, 1024, 512, 512, 512, 512, 512, 800, 512] and not any(p[3] for p in got if p[1] > 512)

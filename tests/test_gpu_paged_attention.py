@@ -217,6 +217,16 @@ def test_parts_joined_by_a_second_launch_and_results_in_place_of_the_queries(len
     assert attn(dq, p.table.cuda(), n, max(lengths), out=dq) is dq and torch.equal(dq, out)
 
 
+@pytest.mark.parametrize("cache, dim, window", [(BF16, 128, 0), (E4M3, 64, 0), (BF16, 32, 100)])
+@pytest.mark.parametrize("sequences, longest", [(70, 300), (130, 64), (130, 500), (130, 65), (290, 130), (33, 700)])
+def test_batches_of_many_short_sequences(sequences, longest, cache, dim, window):
+    """As many units as run at once and up to several times as many, one a workgroup or shared out, with sequences among them that have nothing."""
+    lengths = torch.randint(0, longest + 1, (sequences,), generator=gen(sequences + longest)).tolist()
+    lengths[3] = lengths[-1] = 0
+    lengths[5] = longest
+    _run(lengths, 16, 16, 8, dim, BF16, cache, seed=longest, max_len=longest, window=window)
+
+
 @pytest.mark.parametrize("cache", [BF16, E4M3])
 def test_offsets_beyond_32_bits(cache):
     """Pages behind 2^32 elements of the cache."""
