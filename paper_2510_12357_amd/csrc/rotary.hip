@@ -15,9 +15,9 @@ namespace {
 constexpr int kThreads = 256;
 constexpr float kCodeMax = 448.f;          // the largest E4M3 value
 
-// cos and sin of 2 pi times the turns.  What is left of the turns is exact in 64 bits (at 2^20 turns a position and 2^31 positions 2^-2 of the last
-// place of fp32's quarter turn would be lost: the bound of the documentation keeps the product's error below 2^-53 of it).  A quarter turn's rest, at
-// most 1/2, goes through the Taylor series of sine and cosine to the eleventh and twelfth power: the next terms are below 2^-33.
+// cos and sin of 2 pi times the turns.  What is left of the turns is exact in 64 bits; the turns themselves, a product with two roundings and a rounded constant, are at
+// most 3 2^-53 of them off: at 2^20 of them 2^-31 of a turn.  A quarter turn's rest, at most 1/2, goes through the Taylor series of sine and cosine to the eleventh and
+// twelfth power: the next terms are below 2^-33.
 __device__ __forceinline__ void turn(double turns, float* c, float* s) {
   const double quarters = 4.0 * (turns - floor(turns));
   const double whole = rint(quarters);
