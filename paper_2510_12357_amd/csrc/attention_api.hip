@@ -211,7 +211,7 @@ extern "C" int moe_paged_attention(const moe_attention_config* cfg, const moe_kv
   AttentionArgs a = {};
   a.B = c.B; a.heads = c.heads; a.kv_heads = kv.heads; a.group = c.heads / kv.heads; a.D = kv.D; a.dtype = c.dtype; a.cache_dtype = kv.dtype;
   a.max_len = c.max_len; a.window = c.window; a.table_len = c.table_len; a.table_ld = c.table_ld; a.n_pages = kv.n_pages; a.shift = page_shift(kv.page_size);
-  a.workgroups = p.workgroups; a.align = p.align; a.scale = c.scale; a.softcap = c.softcap;
+  a.workgroups = p.workgroups; a.waves = p.waves; a.align = p.align; a.scale = c.scale; a.softcap = c.softcap;
   a.q_token = c.q_token; a.q_head = c.q_head; a.out_token = c.out_token; a.out_head = c.out_head;
   a.page = kv.page; a.head = kv.head; a.row = kv.row;
   a.q = q; a.table = table; a.lengths = lengths; a.k = kv.k; a.v = kv.v; a.k_scale = kv.k_scale; a.v_scale = kv.v_scale;

@@ -80,9 +80,10 @@ MM_BOTH Segment segment_at(int line, int n, int align, int at, int end, int each
 // What the host knows of a call.
 constexpr int kLeast = 8;                // places of a workgroup
 constexpr int kMostWorkgroups = 4096;
+constexpr int kMostWaves = 4;
 struct AttentionPlan {
   bool fits;                             // the line's length in 31 bits
-  int workgroups, align;
+  int workgroups, waves, align;          // waves of a workgroup: kMostWaves, or 1
   bool split;                            // a unit may lie in several workgroups
   bool few_parts;                        // units are expected to lie in so few that the last one to end joins them; else a second kernel
 };

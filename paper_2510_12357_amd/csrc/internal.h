@@ -201,7 +201,7 @@ struct RotaryArgs {
 int launch_rotary(const RotaryArgs& a, int dtype, hipStream_t s);
 struct AttentionArgs {
   int B, heads, kv_heads, group, D, dtype, cache_dtype;
-  int max_len, window, table_len, n_pages, shift, workgroups, align;
+  int max_len, window, table_len, n_pages, shift, workgroups, waves, align;
   int64_t table_ld;
   float scale, softcap;
   int64_t q_token, q_head, out_token, out_head;

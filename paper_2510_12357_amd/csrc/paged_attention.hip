@@ -11,7 +11,7 @@
 // probabilities in two or three bf16 terms; caches in fp32 on fp32 ones.
 // A block's keys are loaded again as soon as they are in LDS, its values as soon as they are used: a block and a half of each wave is on its way.  More waves or larger blocks
 // did not help (2 or 3 workgroups per CU, 8 or 16 KB a wave: within 1 %), fewer bytes on their way did harm (one workgroup per CU: +15 %).
-// Workgroups of one wave, each with a share of its own, join nothing but read units of their own all over the cache: 185 us, 5 % less only where sequences are short.
+// Many short sequences are another matter: workgroups of one wave each, which have no waves to join or to wait for (128 sequences of up to 64 14.4 -> 10.4 us, on the long ones 185).
 // The maximum that exponentials are taken against follows the scores only when one is 2^8 above it: sums stay far below fp32's range, and most blocks neither exchange
 // maxima nor rescale.  Waves' sums are joined in LDS, parts' sums by the last of a unit's workgroups to end or, where parts are many, by a second
 // kernel, all in a fixed order.
@@ -27,7 +27,6 @@
 namespace mm {
 namespace {
 
-constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 constexpr float kSlack = 8.f;                               // how far (log2) scores may be above the maximum in use
 constexpr int kMaxPages = kMaxPiece / kMinPage;
@@ -173,11 +172,12 @@ __device__ __forceinline__ void hand_over(float* p, f32x2 v) {
 __device__ __forceinline__ f32x2 taken_over(const float* p) {
   return __builtin_bit_cast(f32x2, __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
 }
-// C: type of the cache's rows.  A row of the head is CHUNKS chunks of 16 VW channels, VW of them a lane (D below that: RAGGED).  PARTS: bf16 terms of a query,
+// kWaves: of a workgroup.  C: type of the cache's rows.  A row of the head is CHUNKS chunks of 16 VW channels, VW of them a lane (D below that: RAGGED).  PARTS: bf16 terms of a query,
 // 1 of a bf16 one and 3 of an fp32 one, exact; keys of fp32 are multiplied in fp32.
-template <typename C, int VW, int CHUNKS, int PARTS, bool RAGGED>
-__global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNKS, PARTS)) void attention_kernel(const AttentionArgs a) {
+template <typename C, int VW, int CHUNKS, int PARTS, bool RAGGED, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, waves_per_simd(sizeof(C), 16 * VW * CHUNKS, PARTS)) void attention_kernel(const AttentionArgs a) {
   typedef Block<C, VW, CHUNKS> Blk;
+  constexpr int kThreads = 64 * kWaves;
   constexpr bool kF32 = Blk::kF32, kCodes = Blk::kCodes;
   constexpr int kDims = Blk::kDims, kTiles = Blk::kTiles, kBlock = Blk::kPositions, kVec = Blk::kVec, kLoads = Blk::kLoads;
   constexpr int kSteps = kDims / 32;                        // of the scores' contraction: 32 channels, 8 a lane
@@ -226,13 +226,16 @@ __global__ __launch_bounds__(kThreads, waves_per_simd(sizeof(C), 16 * VW * CHUNK
         line = __builtin_amdgcn_readlane(upto, 63);
       }
   }
-  // ---- sequences without anything to see, or of a length that there is not ----
-  for (int e = blockIdx.x; e < a.B; e += gridDim.x) {
-    const Seen v = seen_of(e);
+  // ---- sequences without anything to see, or of a length that there is not: pieces of their rows to each workgroup ----
+  constexpr int kRowPiece = 4 * kThreads;
+  const int row_vecs = a.heads * (a.D / 4), pieces = (row_vecs + kRowPiece - 1) / kRowPiece;
+  for (int64_t e = blockIdx.x; e < (int64_t)a.B * pieces; e += gridDim.x) {
+    const int sequence = (int)(e / pieces), from = (int)(e % pieces) * kRowPiece;
+    const Seen v = seen_of(sequence);
     if (v.first < v.end) continue;
     const float l = v.bad ? __uint_as_float(0x7fc00000u) : 0.f;
-    for (int i = threadIdx.x; i < a.heads * a.D / 4; i += kThreads)
-      store_row(a, e, i / (a.D / 4), i % (a.D / 4) * 4, f32x4{0.f, 0.f, 0.f, 0.f}, -INFINITY, l);
+    for (int i = from + threadIdx.x; i < min(from + kRowPiece, row_vecs); i += kThreads)
+      store_row(a, sequence, i / (a.D / 4), i % (a.D / 4) * 4, f32x4{0.f, 0.f, 0.f, 0.f}, -INFINITY, l);
   }
   if (cursor >= finish) return;
   if (a.started && threadIdx.x < 4) a.started[4 * workgroup + threadIdx.x] = 0;
@@ -680,12 +683,16 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const AttentionArgs 
   store_row(a, b, head, d, v, m, l);
 }
 
+template <typename C, int VW, int CHUNKS, int PARTS, bool RAGGED>
+int launch_waves(const AttentionArgs& a, hipStream_t s) {
+  const int grid = (a.workgroups + 7) / 8 * 8;
+  if (a.waves == 1) attention_kernel<C, VW, CHUNKS, PARTS, RAGGED, 1><<<grid, 64, 0, s>>>(a);
+  else attention_kernel<C, VW, CHUNKS, PARTS, RAGGED, kMostWaves><<<grid, 64 * kMostWaves, 0, s>>>(a);
+  return hip_fail(hipGetLastError(), "attention_kernel");
+}
 template <typename C, int VW, int CHUNKS, int PARTS>
 int launch_dims(const AttentionArgs& a, hipStream_t s) {
-  const int grid = (a.workgroups + 7) / 8 * 8;
-  if (a.D < 16 * VW * CHUNKS) attention_kernel<C, VW, CHUNKS, PARTS, true><<<grid, kThreads, 0, s>>>(a);
-  else attention_kernel<C, VW, CHUNKS, PARTS, false><<<grid, kThreads, 0, s>>>(a);
-  return hip_fail(hipGetLastError(), "attention_kernel");
+  return a.D < 16 * VW * CHUNKS ? launch_waves<C, VW, CHUNKS, PARTS, true>(a, s) : launch_waves<C, VW, CHUNKS, PARTS, false>(a, s);
 }
 template <typename C, int PARTS>
 int launch_parts(const AttentionArgs& a, hipStream_t s) {

@@ -1,7 +1,7 @@
 // Reads commands, one a line, and answers with the library's rules (csrc/attention_plan.h, attention_plan.cpp).
 //   page SHIFT N_PAGES POS ENTRY...     -> page of a position, or -1
 //   seen LENGTH MAX_LEN WINDOW TABLE_LEN SHIFT            -> first end bad blocks
-//   plan SEQUENCES KV_HEADS GROUP MAX_LEN WINDOW SLOTS CUS -> fits workgroups align split few_parts
+//   plan SEQUENCES KV_HEADS GROUP MAX_LEN WINDOW SLOTS CUS -> fits workgroups align split few_parts waves
 //   line WORKGROUPS ALIGN LEAST UNITS BLOCKS...           -> for every segment: workgroup sequence unit block blocks first-workgroup parts, ended by a -1
 //   shift PAGE_SIZE
 #include <algorithm>
@@ -34,7 +34,7 @@ int main() {
       int v[7];
       for (int& x : v) in >> x;
       const mm::AttentionPlan p = mm::plan_attention(v[0], v[1], v[2], v[3], v[4], v[5], v[6]);
-      if (p.fits) std::printf("1 %d %d %d %d\n", p.workgroups, p.align, (int)p.split, (int)p.few_parts);
+      if (p.fits) std::printf("1 %d %d %d %d %d\n", p.workgroups, p.align, (int)p.split, (int)p.few_parts, p.waves);
       else std::printf("0\n");
     } else if (what == "line") {                             // the walk of every workgroup, as the kernel takes it
       int workgroups, align, least, units, total = 0;

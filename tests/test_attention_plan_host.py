@@ -116,25 +116,28 @@ def test_plans(ask):
     """Grids hold the longest line that a call can have; where there is little work a workgroup has one unit."""
     cases = [(1, 8, 4, 131072, 0), (64, 8, 4, 8192, 0), (1, 16, 1, 200, 0), (33, 1, 71, 5000, 1000), (1, 1, 1, 0, 0), (1, 1, 1, 1, 1), (0, 8, 4, 100, 0),
              (4096, 16, 24, MOST, 0), (256, 8, 8, 131072, 0), (1, 1, 16, MOST, 0), (5000, 8, 4, 500, 0), (1 << 20, 8, 4, 64, 0), (8, 8, 4, 4096, 0)]
-    plans = ask([f"plan {b} {h} {g} {m} {w} 768 256" for b, h, g, m, w in cases])
+    plans = ask([f"plan {b} {h} {g} {m} {w} 512 256" for b, h, g, m, w in cases])
     for (b, h, g, m, w), (fits, *plan) in zip(cases, plans):
         span = min(m, w + 63) if 0 < w < m else m
         units, blocks = b * h * -(-g // 16), max(1, -(-span // 64))
         assert fits == (units * (blocks + 8) < 2 ** 30) or units * (blocks + 4) >= 2 ** 29
         if fits:
-            workgroups, align, split, few = plan
+            workgroups, align, split, few, waves = plan
+            assert waves == (1 if blocks <= 8 and units > 512 else 4)
             assert workgroups * 256 < 2 ** 32 and (workgroups <= 4096 or not split)
             if align:
                 assert workgroups == max(1, units * -(-blocks // align)) and split == (blocks > align)
             else:
-                assert workgroups == 768 and split
+                assert workgroups == 2048 // waves and split
     got = [p[2] if p[0] else None for p in plans]
     assert got == [0, 0, 4, 8, 4, 4, 4, None, 0, 0, 0, 0, 8] and plans[3][4] == 1 and plans[0][4] == 0
 
 
-def test_short_units_in_two_rounds(ask):
-    """Units of two to eight blocks have a workgroup each up to two rounds of them; longer, shorter or more ones share the line."""
-    cases = [(128, 300, 0), (128, 512, 0), (128, 65, 0), (128, 64, 0), (128, 513, 0), (129, 300, 0), (64, 513, 0), (32, 1024, 0), (100, 5000, 400), (100, 5000, 500)]
+def test_units_of_their_own_waves(ask):
+    """Units of up to eight blocks have a wave each where there are more of them than workgroups, up to two rounds of waves, or one for units of one
+    block; beyond, waves share the line."""
+    cases = [(128, 300, 0), (512, 512, 0), (513, 512, 0), (65, 65, 0), (65, 64, 0), (257, 64, 0), (64, 64, 0), (64, 300, 0), (128, 513, 0), (100, 5000, 400), (100, 5000, 500)]
     got = ask([f"plan {b} 8 4 {m} {w} 512 256" for b, m, w in cases])
-    assert [p[2] for p in got] == [8, 8, 8, 0, 0, 0, 0, 8, 8, 0]
-    assert [p[1] for p in got] == [1024, 1024, 1024, 512, 512, 512, 512, 512, 800, 512] and not any(p[3] for p in got if p[1] > 512)
+    assert [p[5] for p in got] == [1, 1, 1, 1, 1, 1, 4, 4, 4, 1, 4]
+    assert [p[2] for p in got] == [8, 8, 0, 8, 8, 0, 8, 8, 0, 8, 0]
+    assert [p[1] for p in got] == [1024, 4096, 2048, 520, 520, 2048, 512, 512, 512, 800, 512]

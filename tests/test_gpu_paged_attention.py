@@ -218,13 +218,34 @@ def test_parts_joined_by_a_second_launch_and_results_in_place_of_the_queries(len
 
 
 @pytest.mark.parametrize("cache, dim, window", [(BF16, 128, 0), (E4M3, 64, 0), (BF16, 32, 100)])
-@pytest.mark.parametrize("sequences, longest", [(70, 300), (130, 64), (130, 500), (130, 65), (290, 130), (33, 700)])
+@pytest.mark.parametrize("sequences, longest", [(70, 300), (130, 64), (130, 500), (130, 65), (290, 130), (33, 700), (520, 130), (290, 40)])
 def test_batches_of_many_short_sequences(sequences, longest, cache, dim, window):
     """As many units as run at once and up to several times as many, one a workgroup or shared out, with sequences among them that have nothing."""
     lengths = torch.randint(0, longest + 1, (sequences,), generator=gen(sequences + longest)).tolist()
     lengths[3] = lengths[-1] = 0
     lengths[5] = longest
     _run(lengths, 16, 16, 8, dim, BF16, cache, seed=longest, max_len=longest, window=window)
+
+
+@pytest.mark.parametrize("sequences, heads, dim, max_len", [(40, 128, 256, 5), (3, 200, 48, 5), (130, 72, 128, 40), (30, 64, 64, 9000)])
+def test_wide_rows_without_anything(sequences, heads, dim, max_len):
+    """Zeros and NaN in whole rows of many channels, by however many workgroups write them; two sequences have something."""
+    lengths = [0] * sequences
+    lengths[1], lengths[-1] = 4, max_len
+    p = Paged(lengths, 16, 8, dim, BF16, seed=sequences)
+    kv = p.fill(1, [0] * sequences)
+    given = list(lengths)
+    for s in range(2, sequences - 1, 3):
+        given[s] = -1 if s % 2 else max_len + 1
+    q = torch.randn((sequences, heads, dim), generator=gen(2)).to(BF16)
+    out, lse = torch.full((sequences, heads, dim), 7.0, dtype=BF16, device="cuda"), torch.full((sequences, heads), 7.0, device="cuda")
+    mm.DecodeAttention(p.cache, heads)(q.cuda(), p.table.cuda(), torch.tensor(given, dtype=torch.int32, device="cuda"), max_len, out=out, lse=lse)
+    _check(p, kv, q, out, lse, only=(1, sequences - 1))
+    for s, n in enumerate(given):
+        if n == 0:
+            assert (out[s] == 0).all() and (lse[s] == -math.inf).all(), s
+        elif n < 0 or n > max_len:
+            assert out[s].isnan().all() and lse[s].isnan().all(), s
 
 
 @pytest.mark.parametrize("cache", [BF16, E4M3])
