@@ -594,7 +594,7 @@ int moe_token_logprobs(const moe_logprobs_config* cfg, const void* logits, const
  *   counters: device, MOE_ATTENTION_COUNTERS bytes, zero before the first call; every call leaves them so.  With them, sequences of a few parts are joined by
  *   the launch that computes the parts; NULL: a second one joins them.  Calls that may overlap need a workspace and counters each.
  *
- * Strides are in elements, 0 = dense; the last dimension is dense always, and heads and tokens do not overlap.  1 <= D <= 256; D and rotary_dim even; D a multiple of 16 in
+ * Strides are in elements, 0 = dense; the last dimension is dense always, and heads and tokens do not overlap.  1 <= D <= 256, heads * D < 2^29; D and rotary_dim even; D a multiple of 16 in
  * a cache, whose memory is 16-byte aligned with strides of whole 16 bytes (scales: [n_pages, heads, page_size] dense).  page_size: a power of two from 4 to 2^20.
  * Other tensors have any alignment of elements.  T, B == 0 are legal: nothing is enqueued. */
 #define MOE_E4M3 4

@@ -24,6 +24,11 @@ int resolve_table(const char* call, int64_t rows, int table_len, int64_t* ld) {
   return MOE_OK;
 }
 
+// The kernels count a token's heads, their channels and those of its keys and values in 32 bits.
+int check_heads(const char* call, int64_t heads, int D) {
+  return heads * D < (int64_t)1 << 29 ? MOE_OK : fail(MOE_E_UNSUPPORTED, "%s: %lld heads of %d channels", call, (long long)heads, D);
+}
+
 // Strides of [n, heads, D], 0 = dense: neither heads nor tokens overlap, whichever of the two is the outer one.
 int resolve_strides(const char* call, const char* what, int64_t n, int64_t heads, int64_t D, int64_t* token, int64_t* head) {
   if (*token < 0 || *head < 0) return fail(MOE_E_BADARG, "%s: negative stride of %s", call, what);
@@ -54,6 +59,7 @@ int resolve(const char* call, const moe_kv_cache* cache, moe_kv_cache* c) {
   if (!float_type(c->dtype) && c->dtype != MOE_E4M3) return fail(MOE_E_BADARG, "%s: cache dtype %d", call, c->dtype);
   if (c->reserved) return fail(MOE_E_BADARG, "%s: reserved field is %d", call, c->reserved);
   if (c->page < 0 || c->head < 0 || c->row < 0) return fail(MOE_E_BADARG, "%s: negative stride of the cache", call);
+  if (int rc = check_heads(call, c->heads, c->D)) return rc;
   const int64_t D = c->D, n = c->page_size, h = c->heads, whole = 16 / type_bytes(c->dtype), far = (int64_t)1 << 46;
   if (!c->row) c->row = D;
   if (!c->head) c->head = n * c->row;
@@ -80,6 +86,7 @@ int resolve(const char* call, const moe_attention_config* cfg, const moe_kv_cach
   *c = *cfg;
   if (c->B < 0 || c->heads <= 0) return fail(MOE_E_SHAPE, "%s: B=%d heads=%d", call, c->B, c->heads);
   if (c->heads % cache.heads) return fail(MOE_E_SHAPE, "%s: %d query heads on %d key heads", call, c->heads, cache.heads);
+  if (int rc = check_heads(call, c->heads, cache.D)) return rc;
   if (!float_type(c->dtype)) return fail(MOE_E_BADARG, "%s: dtype %d", call, c->dtype);
   if (c->max_len < 0 || c->window < 0) return fail(MOE_E_BADARG, "%s: max_len=%d window=%d", call, c->max_len, c->window);
   if (c->max_len > INT32_MAX - 2 * kMaxPiece) return fail(MOE_E_UNSUPPORTED, "%s: max_len=%d", call, c->max_len);
@@ -119,7 +126,8 @@ extern "C" int moe_rope(const moe_rope_config* cfg, const void* x, const int32_t
   if (c.D % 2 || c.D > MOE_MAX_HEAD_DIM) return fail(MOE_E_UNSUPPORTED, "%s: D=%d is no even number up to %d", call, c.D, MOE_MAX_HEAD_DIM);
   if (!float_type(c.dtype)) return fail(MOE_E_BADARG, "%s: dtype %d", call, c.dtype);
   if (c.inverse != 0 && c.inverse != 1) return fail(MOE_E_BADARG, "%s: inverse is %d", call, c.inverse);
-  int rc = check_rotation(call, c.D, c.rotary_dim, c.layout, c.mscale);
+  int rc = check_heads(call, c.heads, c.D);
+  if (!rc) rc = check_rotation(call, c.D, c.rotary_dim, c.layout, c.mscale);
   if (!rc) rc = resolve_strides(call, "x", c.T, c.heads, c.D, &c.x_token, &c.x_head);
   if (!rc) rc = resolve_strides(call, "out", c.T, c.heads, c.D, &c.out_token, &c.out_head);
   if (rc || c.T == 0) return rc;
@@ -146,7 +154,8 @@ extern "C" int moe_kv_append(const moe_append_config* cfg, const moe_kv_cache* c
   moe_append_config c = *cfg;
   if (c.T < 0 || c.heads < 0 || c.n_seqs < 0) return fail(MOE_E_SHAPE, "%s: T=%d heads=%d n_seqs=%d", call, c.T, c.heads, c.n_seqs);
   if (!float_type(c.dtype)) return fail(MOE_E_BADARG, "%s: dtype %d", call, c.dtype);
-  rc = check_rotation(call, kv.D, c.rotary_dim, c.layout, c.mscale);
+  rc = check_heads(call, c.heads, kv.D);
+  if (!rc) rc = check_rotation(call, kv.D, c.rotary_dim, c.layout, c.mscale);
   if (!rc) rc = resolve_table(call, c.n_seqs, c.table_len, &c.table_ld);
   if (!rc) rc = resolve_strides(call, "k", c.T, kv.heads, kv.D, &c.k_token, &c.k_head);
   if (!rc) rc = resolve_strides(call, "v", c.T, kv.heads, kv.D, &c.v_token, &c.v_head);

@@ -214,7 +214,7 @@ struct AttentionArgs {
   int32_t* started;                      // [workgroups, 4] for it: parts, sequence and unit of the unit that begins in a workgroup and ends in another one; then how
                                          // many workgroups there are on the line
 };
-int attention_slots(int cache_dtype, int D, int dtype);      // workgroups that the device runs at once
+int attention_slots(int cache_dtype, int D, int dtype);      // workgroups of kMostWaves waves that the device runs at once
 int launch_attention(const AttentionArgs& a, hipStream_t s);
 
 }  // namespace mm

@@ -150,3 +150,15 @@ def test_attention_workspace_and_empty_calls():
         assert attend(long, _cache(), ws=ws, ws_bytes=n) == WORKSPACE
     # the table's rows bound the lengths, and with them the workspace
     assert mm.moe_paged_attention_workspace_bytes(_attention(max_len=100000), _cache()) == 0
+
+
+def test_more_heads_than_a_token_can_have():
+    """Of a token's heads and channels there are less than 2^29; the largest numbers below pass (an empty call)."""
+    few, many = (1 << 23) - 2, 1 << 23                        # heads of 64 channels
+    assert rope(_rope(heads=many)) == UNSUPPORTED and "heads" in mm.moe_last_error()
+    assert append(_append(heads=many), _cache()) == UNSUPPORTED and "heads" in mm.moe_last_error()
+    assert attend(_attention(heads=many), _cache()) == UNSUPPORTED and "heads" in mm.moe_last_error()
+    assert append(_append(heads=0), _cache(heads=many)) == UNSUPPORTED and attend(_attention(heads=many), _cache(heads=many)) == UNSUPPORTED
+    assert rope(_rope(T=0, heads=few)) == 0 and append(_append(T=0, heads=few), _cache(heads=few)) == 0 and attend(_attention(B=0, heads=few), _cache(heads=few)) == 0
+    for heads in (1 << 30, (1 << 31) - 2):
+        assert rope(_rope(heads=heads)) == UNSUPPORTED and attend(_attention(heads=heads), _cache()) == UNSUPPORTED
