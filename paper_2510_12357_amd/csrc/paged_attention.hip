@@ -7,8 +7,8 @@
 // Scores are the product of a tile of keys (rows: positions) and the queries (columns: heads), so that a lane has four positions of one head, which is where the
 // product with the values wants the probabilities: nothing moves between lanes.  Values go into that product from where their rows lie, a lane with the same channels
 // of four positions: two halves of different registers make an operand's word.  Keys are loaded by whole rows, too, and change lanes in LDS: straight into the operand's
-// layout a load takes half a line of 16 rows, and the same sequences took 221 us.  Both products run on bf16 matrix instructions, exact in the keys, queries and values, with
-// probabilities in two or three bf16 terms; caches in fp32 on fp32 ones.
+// layout a load takes half a line of 16 rows, and the same sequences took 221 us.  Both products run on bf16 matrix instructions, exact in the keys, queries and values, and
+// probabilities in three bf16 terms; caches in fp32 on fp32 ones.
 // A block's keys are loaded again as soon as they are in LDS, its values as soon as they are used: a block and a half of each wave is on its way.  More waves or larger blocks
 // did not help (2 or 3 workgroups per CU, 8 or 16 KB a wave: within 1 %), fewer bytes on their way did harm (one workgroup per CU: +15 %).
 // Many short sequences are another matter: workgroups of one wave each, which have no waves to join or to wait for (128 sequences of up to 64 14.4 -> 10.4 us, on the long ones 185).
@@ -480,11 +480,11 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(sizeof(C), 16 * VW * CH
             for (int j = 0; j < VW; ++j)
               acc[c][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(element<C, VW>(r.v[u][i][c], j), e[u][i], acc[c][j], 0, 0, 0);
     } else {
-      // position 4 g + i of tile u is operand element 4 (u % 2) + i of lane group g in both; probabilities in two bf16 terms, 2^-17
-      // of them off, which bf16 results do not show, in three for fp32 ones
+      // position 4 g + i of tile u is operand element 4 (u % 2) + i of lane group g in both; probabilities in three bf16 terms, which hold all of their 24 bits (two
+      // would move one of 300 bf16 results by a step)
 #pragma unroll
       for (int u0 = 0; u0 < kTiles; u0 += 2) {
-        constexpr int kTerms = PARTS == 1 ? 2 : 3;
+        constexpr int kTerms = 3;
         f32x8 w;
         bf16x8 term[kTerms];
 #pragma unroll
