@@ -210,9 +210,10 @@ extern "C" int moe_paged_attention(const moe_attention_config* cfg, const moe_kv
   if (!rc) rc = check_aligned(call, "lengths", lengths, 4);
   if (!rc) rc = check_aligned(call, "out", out, type_bytes(c.dtype));
   if (!rc && lse) rc = check_aligned(call, "lse", lse, 4);
+  if (!rc && counters) rc = check_aligned(call, "counters", counters, 4);
   if (rc) return rc;
-  if (counters) rc = check_aligned(call, "counters", counters, 4);
-  if (rc) return rc;
+  // a workgroup would store over what another one reads; strides of what there is only one of do not matter
+  if (q == out && ((c.B > 1 && c.q_token != c.out_token) || (c.heads > 1 && c.q_head != c.out_head))) return fail(MOE_E_BADARG, "%s: in place with other strides", call);
   const Workspace w(c, kv, p);
   const size_t need = w.bytes;
   if (need && (!ws || ((uintptr_t)ws & 255) || ws_bytes < need))

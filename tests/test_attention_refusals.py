@@ -162,3 +162,14 @@ def test_more_heads_than_a_token_can_have():
     assert rope(_rope(T=0, heads=few)) == 0 and append(_append(T=0, heads=few), _cache(heads=few)) == 0 and attend(_attention(B=0, heads=few), _cache(heads=few)) == 0
     for heads in (1 << 30, (1 << 31) - 2):
         assert rope(_rope(heads=heads)) == UNSUPPORTED and attend(_attention(heads=heads), _cache()) == UNSUPPORTED
+
+
+def test_attention_in_place_with_other_strides():
+    """A workgroup would store results over queries that another one has still to read.  What is let through here ends at the workspace, which is missing."""
+    long = dict(max_len=100000, table_len=100000)
+    for change in (dict(q_head=128), dict(out_head=128), dict(q_token=6 * 64 + 8), dict(out_token=1024), dict(q_token=64, q_head=128), dict(out_head=72, dtype=mm.MOE_FP32)):
+        assert attend(_attention(**long, **change), _cache(), q=P, out=P) == BADARG and "in place" in mm.moe_last_error(), change
+        assert attend(_attention(**long, **change), _cache(), q=P, out=P2) == WORKSPACE, change
+    # the same strides in other words, and strides of what there is only one of
+    for change, cache in ((dict(), _cache()), (dict(q_head=64, out_token=6 * 64), _cache()), (dict(B=1, q_token=4096), _cache()), (dict(heads=1, q_head=256, q_token=64, out_token=64), _cache(heads=1))):
+        assert attend(_attention(**long, **change), cache, q=P, out=P) == WORKSPACE, change
