@@ -913,33 +913,32 @@ class Rotary(_Owner):
     def _memory(self):
         return (self._freq,)
 
-    def _call(self, x: torch.Tensor, out: torch.Tensor):
+    def _call(self, x: torch.Tensor, out: torch.Tensor, inverse: bool):
         c = moe_rope_config()
         if x.shape != out.shape or x.dtype != out.dtype:
             raise ValueError("out: shape and type of x")
         (c.x_token, c.x_head), (c.out_token, c.out_head) = _strides(x, "x"), _strides(out, "out")
         c.T, c.heads, c.D = x.shape
         c.rotary_dim, c.layout, c.mscale = self._key
-        c.dtype = _float_type(x)
+        c.dtype, c.inverse = _float_type(x), 1 if inverse else 0
         if len(self._calls) > 256:                           # a server's batches are of any size
             self._calls.clear()
-        return c, ctypes.byref(c)
+        return ctypes.byref(c)
 
     def __call__(self, x: torch.Tensor, pos: torch.Tensor, out: Optional[torch.Tensor] = None, inverse: bool = False, stream=None) -> torch.Tensor:
         """x [tokens, heads, channels] bf16 or fp32 at positions pos int32 [tokens] -> out (default: a new tensor; x itself: in place).  inverse: turned back."""
         if out is None:
             with torch.cuda.stream(_torch_stream(stream)):
                 out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        key = (x.shape, x.stride(), x.dtype, out.shape, out.stride(), out.dtype)
-        call = self._calls.get(key)
-        if call is None:
-            call = self._calls[key] = self._call(x, out)
-        c, ref = call
+        # another thread may call while the C call reads its description, which nobody writes any more
+        key = (x.shape, x.stride(), x.dtype, out.shape, out.stride(), out.dtype, bool(inverse))
+        ref = self._calls.get(key)
+        if ref is None:
+            ref = self._calls[key] = self._call(x, out, inverse)
         device = x.get_device()
         if device < 0 or device != self._freq.get_device() or device != out.get_device() or device != pos.get_device():
             raise ValueError(_DEVICES)
         _integers(pos, "pos", x.shape[:1])
-        c.inverse = 1 if inverse else 0
         s = _raw_stream(stream, device)
         if s not in self._streams:
             self._used_on(stream, s)

@@ -1,0 +1,58 @@
+"""The attention step's Python objects when two threads share one: the interpreter's lock is given up inside of a C call, so that another call of the same shapes can run
+while it reads its description.  A stand-in for the library lets that happen every time, without a GPU."""
+import os
+import threading
+
+import pytest
+import torch
+
+from paper_2510_12357_amd import binding as mm
+
+pytestmark = pytest.mark.skipif(not os.path.exists(mm.LIB_PATH), reason="libmobile_moe.so not built")
+
+
+class _Library:
+    """Whatever a call finds in its description once `meanwhile` has run in another thread."""
+
+    def __init__(self, found):
+        self.meanwhile, self.found, self.got = None, found, []
+
+    def call(self, *args):
+        other, self.meanwhile = self.meanwhile, None
+        if other is not None:
+            t = threading.Thread(target=other)
+            t.start()
+            t.join()
+        self.got.append(self.found(*args))
+        return 0
+
+
+@pytest.fixture
+def no_gpu(monkeypatch):
+    """Host tensors pass for a device's."""
+    mm.load_library()
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 0)
+    monkeypatch.setattr(mm, "_on_one_gpu", lambda *t: None)
+    monkeypatch.setattr(mm, "_raw_stream", lambda stream, device: 0)
+    monkeypatch.setattr(mm, "_call_on", lambda device, function, *args: function(*args))
+    monkeypatch.setattr(mm._Owner, "_used_on", lambda self, stream, handle: None)
+
+    def library(found, name):
+        lib = _Library(found)
+        setattr(lib, name, lib.call)
+        monkeypatch.setattr(mm, "_lib", lib)
+        return lib
+    return library
+
+
+@pytest.mark.parametrize("first", [False, True])
+def test_one_rotary_both_ways(no_gpu, first):
+    """A forward pass in one thread, the backward pass of another one's in a second."""
+    rot = mm.Rotary(torch.ones(4, dtype=torch.float64))
+    lib = no_gpu(lambda ref, *args: ref._obj.inverse, "moe_rope")
+    x, pos = torch.zeros((3, 2, 8)), torch.zeros(3, dtype=torch.int32)
+    for warm in (False, True):                               # also where both directions have been called before
+        lib.meanwhile = lambda: rot(x, pos, out=torch.zeros_like(x), inverse=not first)
+        rot(x, pos, out=torch.zeros_like(x), inverse=first)
+        assert lib.got == [int(not first), int(first)], warm
+        lib.got = []
