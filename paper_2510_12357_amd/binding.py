@@ -1087,7 +1087,8 @@ class DecodeAttention(_Owner):
             self.ws = torch.empty((need,), dtype=torch.uint8, device=self.cache.k.device)
         self._streams.clear()
 
-    def _call(self, q, out, table):
+    def _call(self, q, out, table, max_len: int):
+        """-> (description, its bound, workspace bytes) of a call with such tensors: nobody writes it any more, since another thread may call while the C call reads it."""
         c = moe_attention_config()
         if q.dim() != 3 or tuple(q.shape[1:]) != (self.n_heads, self.cache.head_dim) or out.shape != q.shape or out.dtype != q.dtype:
             raise ValueError(f"q, out: [sequences, {self.n_heads}, {self.cache.head_dim}] of one type")
@@ -1098,7 +1099,16 @@ class DecodeAttention(_Owner):
         c.window, c.scale, c.softcap = self.window, self.scale, self.softcap
         if len(self._calls) > 256:                           # a server's batches are of any size
             self._calls.clear()
-        return [c, ctypes.byref(c), 0, None]
+        return self._bounded(c, max_len)
+
+    def _bounded(self, c, max_len: int):
+        """With this bound: a batch that generates has another one in every step."""
+        if not 0 <= max_len < 2 ** 31:
+            raise ValueError(f"max_len {max_len}")
+        c = moe_attention_config.from_buffer_copy(c)
+        c.max_len = max_len
+        ref = ctypes.byref(c)
+        return ref, c.max_len, int(_lib.moe_paged_attention_workspace_bytes(ref, self.cache._ref))
 
     def __call__(self, q: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, max_len: int, out: Optional[torch.Tensor] = None,
                  lse: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
@@ -1110,7 +1120,10 @@ class DecodeAttention(_Owner):
         key = (q.shape, q.stride(), q.dtype, out.shape, out.stride(), out.dtype, table.shape, table.stride(), table.dtype)
         call = self._calls.get(key)
         if call is None:
-            call = self._calls[key] = self._call(q, out, table)
+            call = self._calls[key] = self._call(q, out, table, max_len)
+        elif call[1] != max_len:
+            call = self._calls[key] = self._bounded(call[0]._obj, max_len)
+        ref, _, need = call
         cache = self.cache
         device = cache._device
         for t in (q, table, lengths, out):
@@ -1122,12 +1135,6 @@ class DecodeAttention(_Owner):
                 raise ValueError(_DEVICES)
             if lse.dtype is not torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous():
                 raise ValueError("lse: fp32 [sequences, heads], dense")
-        c, ref, need, bound = call
-        if bound != max_len:
-            if not 0 <= max_len < 2 ** 31:
-                raise ValueError(f"max_len {max_len}")
-            c.max_len = call[3] = max_len
-            need = call[2] = int(_lib.moe_paged_attention_workspace_bytes(ref, cache._ref))
         if need and (self.ws is None or self.ws.numel() < need):
             self._workspace(need, stream)
         s = _raw_stream(stream, device)

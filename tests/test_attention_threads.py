@@ -56,3 +56,35 @@ def test_one_rotary_both_ways(no_gpu, first):
         rot(x, pos, out=torch.zeros_like(x), inverse=first)
         assert lib.got == [int(not first), int(first)], warm
         lib.got = []
+
+
+def _attention(monkeypatch, n_heads=2):
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: _NoStream())
+    return mm.DecodeAttention(mm.KvCache.empty(4, 16, 1, 16, device="cpu"), n_heads)
+
+
+class _NoStream:
+    def synchronize(self):
+        pass
+
+
+def test_one_attention_with_two_bounds(no_gpu, monkeypatch):
+    """The bound of one thread's lengths does not become the other one's, whose longer sequences would be NaN."""
+    attn = _attention(monkeypatch)
+    q, table, n = torch.zeros((3, 2, 16)), torch.zeros((3, 4), dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    lib = no_gpu(lambda ref, *args: ref._obj.max_len, "moe_paged_attention")
+    lib.moe_paged_attention_workspace_bytes = lambda c, cache: 0
+    for warm in (False, True):
+        lib.meanwhile = lambda: attn(q, table, n, 5, out=torch.zeros_like(q))
+        attn(q, table, n, 60, out=torch.zeros_like(q))
+        assert lib.got == [5, 60], warm
+        lib.got = []
+    for bound in (60, 60, 5, 7, 60):                         # each call its own one
+        attn(q, table, n, bound, out=torch.zeros_like(q))
+    assert lib.got == [60, 60, 5, 7, 60]
+    for bound in (-1, 2 ** 31):
+        with pytest.raises(ValueError):
+            attn(q, table, n, bound, out=torch.zeros_like(q))
+    attn(q, table, n, 60, out=torch.zeros_like(q))
+    assert lib.got[-1] == 60
