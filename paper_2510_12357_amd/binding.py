@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 import math
 import os
+import threading
 from typing import Optional, Sequence
 
 import torch
@@ -857,11 +858,12 @@ class _Owner:
         return ()
 
     def _used_on(self, stream, handle: int) -> None:
-        if handle not in self._streams:
+        streams = self._streams                              # of the memory that is recorded: another thread may put a larger one in its place
+        if handle not in streams:
             for t in self._memory():
                 if t is not None:
                     t.record_stream(_torch_stream(stream))
-            self._streams.add(handle)
+            streams.add(handle)
 
 
 def _call_on(device: int, function, *args) -> None:
@@ -1074,18 +1076,26 @@ class DecodeAttention(_Owner):
         torch.cuda.current_stream(cache.k.device).synchronize()
         self.ws = None
         self._outgrown = []                                  # workspaces of smaller calls: captured graphs have their addresses
+        self._growing = threading.Lock()
         self._calls = {}
 
     def _memory(self):
-        return self.ws, self.counters
+        return self.ws, self.counters, *self._outgrown
 
-    def _workspace(self, need: int, stream) -> None:
-        if self.ws is not None:                              # twice as large at least: what is kept stays below the one in use
-            need = max(need, 2 * self.ws.numel())
-            self._outgrown.append(self.ws)
-        with torch.cuda.stream(_torch_stream(stream)):
-            self.ws = torch.empty((need,), dtype=torch.uint8, device=self.cache.k.device)
-        self._streams.clear()
+    def _workspace(self, need: int, stream) -> torch.Tensor:
+        """One that is large enough; a call stays with the one that it was given, whatever other threads' calls need."""
+        with self._growing:
+            ws = self.ws
+            if ws is None or ws.numel() < need:
+                if ws is not None:                           # twice as large at least: what is kept stays below the one in use
+                    need = max(need, 2 * ws.numel())
+                with torch.cuda.stream(_torch_stream(stream)):
+                    larger = torch.empty((need,), dtype=torch.uint8, device=self.cache.k.device)
+                if ws is not None:
+                    self._outgrown.append(ws)
+                self._streams = set()                        # in front of the workspace, which no stream in it has used
+                ws = self.ws = larger
+            return ws
 
     def _call(self, q, out, table, max_len: int):
         """-> (description, its bound, workspace bytes) of a call with such tensors: nobody writes it any more, since another thread may call while the C call reads it."""
@@ -1135,14 +1145,14 @@ class DecodeAttention(_Owner):
                 raise ValueError(_DEVICES)
             if lse.dtype is not torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous():
                 raise ValueError("lse: fp32 [sequences, heads], dense")
-        if need and (self.ws is None or self.ws.numel() < need):
-            self._workspace(need, stream)
+        ws = self.ws
+        if need and (ws is None or ws.numel() < need):
+            ws = self._workspace(need, stream)
         s = _raw_stream(stream, device)
         if s not in self._streams:
             self._used_on(stream, s)
         if s not in cache._streams:
             cache._used_on(stream, s)
-        ws = self.ws
         _call_on(device, _lib.moe_paged_attention, ref, cache._ref, q.data_ptr(), table.data_ptr(), lengths.data_ptr(), out.data_ptr(),
                  None if lse is None else lse.data_ptr(), None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), self.counters.data_ptr(), s)
         return out

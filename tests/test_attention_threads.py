@@ -1,5 +1,6 @@
 """The attention step's Python objects when two threads share one: the interpreter's lock is given up inside of a C call, so that another call of the same shapes can run
 while it reads its description.  A stand-in for the library lets that happen every time, without a GPU."""
+import contextlib
 import os
 import threading
 
@@ -88,3 +89,30 @@ def test_one_attention_with_two_bounds(no_gpu, monkeypatch):
             attn(q, table, n, bound, out=torch.zeros_like(q))
     attn(q, table, n, 60, out=torch.zeros_like(q))
     assert lib.got[-1] == 60
+
+
+def test_one_attention_whose_workspace_grows_in_two_threads(no_gpu, monkeypatch):
+    """Each call gets a workspace of its size, whichever of two that grow it at once comes last; none that a call was given is let go."""
+    attn = _attention(monkeypatch)
+    q, table, n = torch.zeros((3, 2, 16)), torch.zeros((3, 4), dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    lib = no_gpu(lambda ref, cache, q, t, n, out, lse, ws, ws_bytes, *args: (ref._obj.max_len, ws, ws_bytes), "moe_paged_attention")
+    lib.moe_paged_attention_workspace_bytes = lambda c, cache: 1000 * c._obj.max_len
+    empty, other = torch.empty, []
+
+    def slow_empty(*args, **kw):
+        """Between a thread's decision for a size and its workspace another one gets its own."""
+        if kw.get("dtype") is torch.uint8 and not other:
+            other.append(threading.Thread(target=lambda: attn(q, table, n, 60, out=torch.zeros_like(q))))
+            other[0].start()
+            other[0].join(0.5)                               # or waits for this one
+        return empty(*args, **kw)
+    monkeypatch.setattr(mm, "_torch_stream", lambda stream, device=None: None)
+    monkeypatch.setattr(torch.cuda, "stream", lambda stream: contextlib.nullcontext())
+    monkeypatch.setattr(torch, "empty", slow_empty)
+    attn(q, table, n, 5, out=torch.zeros_like(q))
+    other[0].join()
+    attn(q, table, n, 60, out=torch.zeros_like(q))
+    kept = {t.data_ptr(): t.numel() for t in [attn.ws] + attn._outgrown}
+    assert len(lib.got) == 3
+    for max_len, ws, ws_bytes in lib.got:
+        assert ws in kept and ws_bytes >= 1000 * max_len and kept[ws] == ws_bytes, (max_len, ws_bytes, kept)
