@@ -194,8 +194,9 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(const RotaryArgs a, co
           float* scales = value ? a.v_scale : a.k_scale;
           scales[((page * a.kv_heads + head) << a.shift) + slot] = finite ? most / kCodeMax : __uint_as_float(0x7fc00000u);
         }
-        // quotients by the reciprocal and one step that takes the rest into account; rows of the smallest numbers times 2^64, exactly, so that it is finite
-        const float lift = most < 1e-30f ? 18446744073709551616.f : 1.f, divisor = most * lift, over = 1.f / divisor, by = kCodeMax * lift;
+        // quotients by the reciprocal and one step that takes the rest into account; rows of the smallest numbers times 2^64 and of the largest times 2^-64, exactly, so that the
+        // reciprocal and 448 y are finite
+        const float lift = most < 1e-30f ? 0x1p64f : most > 1e30f ? 0x1p-64f : 1.f, divisor = most * lift, over = 1.f / divisor, by = kCodeMax * lift;
 #pragma unroll
         for (int k = 0; k < UNITS; ++k) {
           if (!there[k]) continue;
