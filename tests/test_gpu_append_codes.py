@@ -1,4 +1,8 @@
-"""Rows of 8-bit codes at the ends of fp32's range."""
+"""Rows of 8-bit codes at the ends of fp32's range and beside the borders between two codes."""
+import math
+from fractions import Fraction
+
+import numpy as np
 import pytest
 import torch
 
@@ -37,3 +41,35 @@ def test_rows_of_every_size(dim):
         exact = rows.double() * 448 / most[:, None]
         assert ((codes.double() - exact).abs() <= torch.clamp(exact.abs() * 2.0 ** -4, min=2.0 ** -10) + exact.abs() * 2 * ULP).all()
 
+
+def test_codes_beside_their_borders():
+    """The nearest code of the nearest fp32 quotient, for numbers that lie as close to the middle between two codes as fp32 has them.  Quotients within 2^-10 steps of the middle
+    between two fp32 numbers are left out: the kernel rounds a sum whose second addend is 2^-24 of itself off."""
+    codes = sorted({float(c) for c in torch.arange(0x7f, dtype=torch.uint8).view(E4M3).float()})
+    middles = np.array([(a + b) / 2 for a, b in zip(codes, codes[1:])])
+    rng = np.random.default_rng(1)
+    largest = (rng.uniform(1.0, 2.0, 40) * 2.0 ** rng.integers(-20, 20, 40)).astype(np.float32)
+    rows, want, sure = [], [], []
+    for m in largest:
+        near = (middles * float(m) / 448).astype(np.float32)
+        for step in (-2, -1, 0, 1, 2):
+            y = near.copy()
+            for _ in range(abs(step)):
+                y = np.nextafter(y, np.float32(math.copysign(1e30, step)))
+            y = np.minimum(y, m)
+            row, exact = np.zeros(128, np.float32), [Fraction(float(v)) * 448 / Fraction(float(m)) for v in y]
+            row[:126], row[127] = y, m
+            q = np.array([np.float32(float(e)) for e in exact])      # to 53 bits, then to 24: the same unless beside a middle, see below
+            ok = np.ones(128, bool)
+            for i, (e, f) in enumerate(zip(exact, q)):
+                other = np.nextafter(f, np.float32(1e30 if Fraction(float(f)) < e else 0))
+                gap = abs(Fraction(float(other)) - Fraction(float(f)))
+                ok[i] = abs(abs(e - Fraction(float(f))) - gap / 2) > gap / 1024
+            w = np.zeros(128, np.float32)
+            w[:126], w[127] = torch.from_numpy(q).to(E4M3).float().numpy(), 448.0
+            rows.append(row), want.append(w), sure.append(ok)
+    rows, want, sure = (torch.from_numpy(np.stack(t)) for t in (rows, want, sure))
+    assert sure.float().mean() > 0.9
+    for got, _ in _stored(rows):
+        wrong = (got != want) & sure
+        assert not wrong.any(), (int(wrong.sum()), rows[wrong.any(1)][:1], got[wrong][:5], want[wrong][:5])
