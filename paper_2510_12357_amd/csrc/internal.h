@@ -211,7 +211,7 @@ struct AttentionArgs {
   void* out; float* lse;
   float *part_out, *part_stat;           // [workgroups, 2, tile heads, D] and [workgroups, 2, tile heads, 2]: a workgroup's first segment, and its last one
   int32_t* counters;                     // of the parts that have ended, zero between calls; NULL: a second kernel joins the parts
-  int32_t* started;                      // [workgroups, 4] for it: parts, sequence and unit of the unit that begins in a workgroup and ends in another one; then how
+  int32_t* started;                      // [workgroups, 4] for it: parts, sequence, unit and scale of the unit that begins in a workgroup and ends in another one; then how
                                          // many workgroups there are on the line
 };
 int attention_slots(int cache_dtype, int D, int dtype);      // workgroups of kMostWaves waves that the device runs at once

@@ -67,9 +67,9 @@ __device__ __forceinline__ float element(const typename Raw<C, N>::type& v, int 
   if constexpr (N == 8) return j < 4 ? v.lo[j & 3] : v.hi[j & 3];
   else return v[j];
 }
-// Element `at` of the operands of four channels from channel j on: bf16 values, or E4M3 codes widened exactly
+// Element `at` of the operands of four channels from channel j on: bf16 values, or E4M3 codes times `share`, a power of two, widened exactly
 template <typename C, typename R>
-__device__ __forceinline__ void widen_four(const R& v, int j, int at, bool there, bf16x8* to) {
+__device__ __forceinline__ void widen_four(const R& v, int j, int at, bool there, float share, bf16x8* to) {
   typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
   bf16x2 a, b;
   if constexpr (sizeof(C) == 2) {
@@ -77,8 +77,8 @@ __device__ __forceinline__ void widen_four(const R& v, int j, int at, bool there
     b = __builtin_bit_cast(bf16x2, there ? dword(v, j / 2 + 1) : 0);
   } else {
     const unsigned d = there ? (unsigned)dword(v, j / 4) : 0u;
-    a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(d, 1.f, false);
-    b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(d, 1.f, true);
+    a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(d, share, false);
+    b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(d, share, true);
   }
   to[0][at] = a[0]; to[1][at] = a[1]; to[2][at] = b[0]; to[3][at] = b[1];
 }
@@ -114,9 +114,13 @@ __device__ __forceinline__ int64_t part_at(const AttentionArgs& a, int workgroup
   return (2 * (int64_t)workgroup + begins) * min(a.group, kHeadTile);
 }
 
-// Four channels of a result: sums v, the maximum m (log2) that they are taken against and the sum l of the exponentials; without any, zeros.
-__device__ __forceinline__ void store_row(const AttentionArgs& a, int b, int head, int channel, f32x4 v, float m, float l) {
-  const float over = l == 0.f ? 0.f : 1.f / l;
+// Exponentials are at most 2^kSlack, but for rounding, and a sequence sees n of them: times 2^-down, exactly, their sum is at most 1/2, so that no sum of values is larger than the
+// largest value, whatever their sizes are.
+__device__ __forceinline__ int down_by(const Seen& v) { return (int)kSlack + 1 + (v.end - v.first > 1 ? 32 - __builtin_clz(v.end - v.first - 1) : 0); }
+__device__ __forceinline__ float two_to(int n) { return __int_as_float((127 + n) << 23); }
+// Four channels of a result: sums v of values times exponentials and 2^-down, the maximum m (log2) that they are taken against and the sum l of the exponentials; without any, zeros.
+__device__ __forceinline__ void store_row(const AttentionArgs& a, int b, int head, int channel, f32x4 v, float m, float l, int down) {
+  const float over = l == 0.f ? 0.f : two_to(down) / l;
   const int64_t at = (int64_t)b * a.out_token + (int64_t)head * a.out_head + channel;
   v *= over;
   if (a.dtype == MOE_FP32) {
@@ -235,7 +239,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(sizeof(C), 16 * VW * CH
     if (v.first < v.end) continue;
     const float l = v.bad ? __uint_as_float(0x7fc00000u) : 0.f;
     for (int i = from + threadIdx.x; i < min(from + kRowPiece, row_vecs); i += kThreads)
-      store_row(a, sequence, i / (a.D / 4), i % (a.D / 4) * 4, f32x4{0.f, 0.f, 0.f, 0.f}, -INFINITY, l);
+      store_row(a, sequence, i / (a.D / 4), i % (a.D / 4) * 4, f32x4{0.f, 0.f, 0.f, 0.f}, -INFINITY, l, 0);
   }
   if (cursor >= finish) return;
   if (a.started && threadIdx.x < 4) a.started[4 * workgroup + threadIdx.x] = 0;
@@ -286,6 +290,8 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(sizeof(C), 16 * VW * CH
     }
   }
   const float to_log2 = a.scale * kLog2e;
+  const int down = down_by(seen);
+  const float share = two_to(-down);
   const C* const kbase = static_cast<const C*>(a.k) + (int64_t)kvh * a.head;
   const C* const vbase = static_cast<const C*>(a.v) + (int64_t)kvh * a.head;
   const int mask = (1 << a.shift) - 1;
@@ -462,12 +468,10 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(sizeof(C), 16 * VW * CH
           for (int c = 0; c < CHUNKS; ++c) r.v[u][i][c] = no ? zeros(typename Blk::RawV{}) : r.v[u][i][c];
         }
     }
-    if constexpr (kCodes) {
 #pragma unroll
-      for (int u = 0; u < kTiles; ++u)
+    for (int u = 0; u < kTiles; ++u)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) e[u][i] *= vs[u][i];
-    }
+      for (int i = 0; i < 4; ++i) e[u][i] *= kCodes ? vs[u][i] : share;         // 8-bit values have it in their conversion, so that weights of small rows stay normal numbers
     // ---- values ----
     if constexpr (kF32) {
 #pragma unroll
@@ -504,7 +508,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(sizeof(C), 16 * VW * CH
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-              for (int i = 0; i < 4; ++i) widen_four<C>(r.v[u0 + u < kTiles ? u0 + u : 0][i][c], j, 4 * u + i, u0 + u < kTiles, value);
+              for (int i = 0; i < 4; ++i) widen_four<C>(r.v[u0 + u < kTiles ? u0 + u : 0][i][c], j, 4 * u + i, u0 + u < kTiles, share, value);
 #pragma unroll
             for (int t = kTerms - 1; t >= 0; --t)           // small terms first
 #pragma unroll
@@ -577,7 +581,7 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(sizeof(C), 16 * VW * CH
           if (channel == 0) *reinterpret_cast<f32x2*>(a.part_stat + 2 * (part_row + head)) = stat;
         }
       } else {
-        store_row(a, b, head0 + head, channel, v, m, l);
+        store_row(a, b, head0 + head, channel, v, m, l, down);
       }
     }
   }
@@ -623,11 +627,11 @@ __global__ __launch_bounds__(64 * kWaves, waves_per_simd(sizeof(C), 16 * VW * CH
             v += w * f32x4{lo[i][0], lo[i][1], hi[i][0], hi[i][1]};
           }
         }
-        store_row(a, b, head0 + head, channel, v, most, l);
+        store_row(a, b, head0 + head, channel, v, most, l, down);
       }
     }
   }
-  if (seg.parts > 1 && seg.block == 0 && a.started && tid < 4) a.started[4 * workgroup + tid] = tid == 0 ? seg.parts : tid == 1 ? b : tid == 2 ? seg.unit : 0;
+  if (seg.parts > 1 && seg.block == 0 && a.started && tid < 4) a.started[4 * workgroup + tid] = tid == 0 ? seg.parts : tid == 1 ? b : tid == 2 ? seg.unit : down;
   }
 
   __syncthreads();
@@ -652,7 +656,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const AttentionArgs 
   __shared__ float s_top[kJoinThreads / 64];
   __shared__ __attribute__((aligned(16))) f32x4 s_v[kJoinThreads];
   __shared__ float s_l[kJoinThreads];
-  const int tid = threadIdx.x, workgroup = blockIdx.x, parts = workgroup < a.started[4 * a.workgroups] ? a.started[4 * workgroup] : 0, b = a.started[4 * workgroup + 1], unit = a.started[4 * workgroup + 2];
+  const int tid = threadIdx.x, workgroup = blockIdx.x, parts = workgroup < a.started[4 * a.workgroups] ? a.started[4 * workgroup] : 0, b = a.started[4 * workgroup + 1], unit = a.started[4 * workgroup + 2], down = a.started[4 * workgroup + 3];
   const int tiles = (a.group + kHeadTile - 1) / kHeadTile, tile = unit % tiles, h = blockIdx.y, head = unit / tiles * a.group + tile * kHeadTile + h;
   if (parts == 0 || h >= a.group - tile * kHeadTile) return;
   auto at = [&](int part) { return part_at(a, workgroup + part, part == 0) + h; };
@@ -680,7 +684,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const AttentionArgs 
   __syncthreads();
   if (tid >= vecs) return;
   for (int t = 1; t < turns; ++t) { v += s_v[t * vecs + tid]; l += s_l[t * vecs + tid]; }
-  store_row(a, b, head, d, v, m, l);
+  store_row(a, b, head, d, v, m, l, down);
 }
 
 template <typename C, int VW, int CHUNKS, int PARTS, bool RAGGED>

@@ -1,11 +1,11 @@
-"""Attention over a paged cache at the ends of its numbers: probabilities held to 24 bits whatever the results' type."""
+"""Attention over a paged cache at the ends of its numbers: probabilities held to 24 bits whatever the results' type, values up to the largest ones."""
 import math
 
 import pytest
 import torch
 
 from paper_2510_12357_amd import binding as mm
-from attention_util import BF16, E4M3, FP32, ULP, Paged, half_step
+from attention_util import BF16, E4M3, FP32, ULP, Paged, assert_near, attended, gen, half_step, values
 
 pytestmark = pytest.mark.gpu
 
@@ -56,3 +56,40 @@ def test_probabilities_are_not_rounded_to_16_bits(cache, dtype):
     want = ((e - a - b) / (2.0 + e))[:, None, None]
     bound = (e * (2 * s.abs() + 2 + 1 + 9) * ULP / (2.0 + e))[:, None, None] + want.abs() * (4 * ULP + half_step(dtype))
     assert ((out - want).abs() <= bound).all(), float(((out - want).abs() / bound).max())
+
+
+@pytest.mark.parametrize("lengths, max_len", [([1, 2, 40, 700], 700), ([1, 33, 5000, 3000], 5000), ([60] * 70 + [1, 2, 33], 64), ([9000], 40000)])
+@pytest.mark.parametrize("dtype, cache", [(BF16, BF16), (FP32, BF16), (FP32, FP32), (BF16, E4M3), (FP32, E4M3)])
+@pytest.mark.parametrize("size", [3e38, 2.0 ** -100])
+def test_values_of_any_size_have_a_mean(lengths, max_len, dtype, cache, size):
+    """A weighted mean is no larger than its largest value, however many there are, whatever the order of the scores, in one part and in several."""
+    p = Paged(lengths, 16, 2, 64, cache, seed=1)
+    kv = p.fill(2, k_gain=3.0)
+    for s, n in enumerate(lengths):
+        page, off = (t.cuda() for t in p.slots(s, torch.arange(n)))
+        order = kv[s][0][:, :, 0].sum(dim=1).argsort(descending=s % 2 == 1)      # scores that rise or fall with the first channel
+        at = page[order.cuda()], off[order.cuda()]
+        p.k.view(torch.uint8)[page, :, off] = p.k.view(torch.uint8)[at[0], :, at[1]]
+        if cache is E4M3:
+            p.k_scale[page, :, off] = p.k_scale[at[0], :, at[1]]
+        k = kv[s][0][order]
+        x = (0.9 + 0.1 * torch.rand((n, 2, 64), generator=gen(3 + s))) * size
+        x[:, :, 32:] *= torch.where(torch.rand((n, 2, 32), generator=gen(4 + s)) < 0.5, -1.0, 1.0)
+        if cache is E4M3:
+            codes, sc = (x / x.abs().amax(dim=-1, keepdim=True) * 448).to(E4M3), (x.double().abs().amax(dim=-1) / 448).float()
+            p.v.view(torch.uint8)[page, :, off], p.v_scale[page, :, off] = codes.view(torch.uint8).cuda(), sc.cuda()
+            v = values(codes, sc)
+        else:
+            p.v[page, :, off] = x.to(cache).cuda()
+            v = values(x.to(cache))
+        kv[s] = k, v
+    q = torch.randn((len(lengths), 6, 64), generator=gen(5)).to(dtype)
+    q[:, :, 0] += 2.0
+    q = q.to(dtype)
+    lse = torch.zeros((len(lengths), 6), device="cuda")
+    out = mm.DecodeAttention(p.cache, 6)(q.cuda(), p.table.cuda(), torch.tensor(lengths, dtype=torch.int32, device="cuda"), max_len, lse=lse)
+    assert torch.isfinite(out).all()
+    for s in range(len(lengths)):
+        want, want_lse, err, lse_err = attended(q[s], kv[s], 0.125)
+        assert_near(out[s], want, err, dtype)
+        assert ((lse[s].cpu().double() - want_lse).abs() <= lse_err).all()
