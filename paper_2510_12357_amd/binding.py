@@ -662,10 +662,13 @@ def quantize_rows(x: torch.Tensor, stream=None):
     return q[:, :K], scale
 
 
-def _torch_stream(stream) -> torch.cuda.Stream:
+def _torch_stream(stream, device: Optional[torch.device] = None) -> torch.cuda.Stream:
+    """The stream as torch has it; None: the current one; of the current device or of the tensors' one."""
+    if device is not None and device.type != "cuda":         # of the host: refused later
+        device = None
     if stream is None:
-        return torch.cuda.current_stream()
-    return stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream))
+        return torch.cuda.current_stream(device)
+    return stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream), device=device)
 
 
 def _raw_stream(stream, device: int) -> int:
@@ -862,7 +865,7 @@ class _Owner:
         if handle not in streams:
             for t in self._memory():
                 if t is not None:
-                    t.record_stream(_torch_stream(stream))
+                    t.record_stream(_torch_stream(stream, t.device))
             streams.add(handle)
 
 
@@ -930,7 +933,7 @@ class Rotary(_Owner):
     def __call__(self, x: torch.Tensor, pos: torch.Tensor, out: Optional[torch.Tensor] = None, inverse: bool = False, stream=None) -> torch.Tensor:
         """x [tokens, heads, channels] bf16 or fp32 at positions pos int32 [tokens] -> out (default: a new tensor; x itself: in place).  inverse: turned back."""
         if out is None:
-            with torch.cuda.stream(_torch_stream(stream)):
+            with torch.cuda.stream(_torch_stream(stream, x.device)):
                 out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
         # another thread may call while the C call reads its description, which nobody writes any more
         key = (x.shape, x.stride(), x.dtype, out.shape, out.stride(), out.dtype, bool(inverse))
@@ -1029,7 +1032,7 @@ class KvCache(_Owner):
             key = (k.shape, k.stride(), k.dtype, v.shape, v.stride(), v.dtype, table.shape, table.stride(), table.dtype, rotary and rotary._key)
         else:
             if q_out is None:
-                with torch.cuda.stream(_torch_stream(stream)):
+                with torch.cuda.stream(_torch_stream(stream, q.device)):
                     q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
             key = (k.shape, k.stride(), k.dtype, v.shape, v.stride(), v.dtype, table.shape, table.stride(), table.dtype, rotary and rotary._key,
                    q.shape, q.stride(), q.dtype, q_out.shape, q_out.stride(), q_out.dtype)
@@ -1089,7 +1092,7 @@ class DecodeAttention(_Owner):
             if ws is None or ws.numel() < need:
                 if ws is not None:                           # twice as large at least: what is kept stays below the one in use
                     need = max(need, 2 * ws.numel())
-                with torch.cuda.stream(_torch_stream(stream)):
+                with torch.cuda.stream(_torch_stream(stream, self.cache.k.device)):
                     larger = torch.empty((need,), dtype=torch.uint8, device=self.cache.k.device)
                 if ws is not None:
                     self._outgrown.append(ws)
@@ -1125,7 +1128,7 @@ class DecodeAttention(_Owner):
         """q [sequences, heads, channels] bf16 or fp32, lengths int32 [sequences] (the new token's position is length - 1) of at most max_len -> out (default: a new
         tensor); lse: fp32 [sequences, heads], filled where it is given."""
         if out is None:
-            with torch.cuda.stream(_torch_stream(stream)):
+            with torch.cuda.stream(_torch_stream(stream, q.device)):
                 out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         key = (q.shape, q.stride(), q.dtype, out.shape, out.stride(), out.dtype, table.shape, table.stride(), table.dtype)
         call = self._calls.get(key)
