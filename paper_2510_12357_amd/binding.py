@@ -894,12 +894,12 @@ class Rotary(_Owner):
         if layout not in self.LAYOUTS:
             raise ValueError(f"layout {layout!r}: one of {sorted(self.LAYOUTS)}")
         _on_one_gpu(freq)
-        self._freq, self.layout, self.mscale = freq, layout, float(mscale)
-        self.rotary_dim = 2 * freq.numel()
-        self._key = (self.rotary_dim, self.LAYOUTS[layout], self.mscale)
+        self._freq, self._layout = freq, layout
+        self._key = (2 * freq.numel(), self.LAYOUTS[layout], float(mscale))
         self._calls = {}
 
-    freq = property(lambda self: self._freq)
+    freq, layout = property(lambda self: self._freq), property(lambda self: self._layout)
+    rotary_dim, mscale = property(lambda self: self._key[0]), property(lambda self: self._key[2])
 
     @classmethod
     def scaled(cls, rotary_dim: int, base: float = 10000.0, layout: str = "half", factor: float = 1.0, trained: int = 0, slow: float = 1.0,
@@ -1069,9 +1069,9 @@ class DecodeAttention(_Owner):
         super().__init__()
         if n_heads <= 0 or n_heads % cache.n_heads:
             raise ValueError(f"{n_heads} query heads on {cache.n_heads} key heads")
-        self.cache, self.n_heads = cache, n_heads
-        self.scale = 1.0 / math.sqrt(cache.head_dim) if scale is None else float(scale)
-        self.window, self.softcap = int(window), float(softcap)
+        self._cache, self._n_heads = cache, n_heads
+        self._scale = 1.0 / math.sqrt(cache.head_dim) if scale is None else float(scale)
+        self._window, self._softcap = int(window), float(softcap)
         if torch.cuda.is_current_stream_capturing():
             raise RuntimeError("made while a graph is captured: its counters have to be zero before")
         # zero before any stream's first call, and after each call again
@@ -1081,6 +1081,9 @@ class DecodeAttention(_Owner):
         self._outgrown = []                                  # workspaces of smaller calls: captured graphs have their addresses
         self._growing = threading.Lock()
         self._calls = {}
+
+    cache, n_heads = property(lambda self: self._cache), property(lambda self: self._n_heads)
+    scale, window, softcap = property(lambda self: self._scale), property(lambda self: self._window), property(lambda self: self._softcap)
 
     def _memory(self):
         return self.ws, self.counters, *self._outgrown
@@ -1137,7 +1140,7 @@ class DecodeAttention(_Owner):
         elif call[1] != max_len:
             call = self._calls[key] = self._bounded(call[0]._obj, max_len)
         ref, _, need = call
-        cache = self.cache
+        cache = self._cache
         device = cache._device
         for t in (q, table, lengths, out):
             if t.get_device() != device:

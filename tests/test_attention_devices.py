@@ -80,7 +80,7 @@ def test_results_are_taken_on_their_own_device(two_devices, monkeypatch, call, g
         else:
             attn = mm.DecodeAttention.__new__(mm.DecodeAttention)
             attn.ws, attn._growing = None, threading.Lock()
-            attn.cache = type("Cache", (), {"k": x})
+            attn._cache = type("Cache", (), {"k": x})
             if call == "attention":
                 attn(x, None, None, 1, stream=given)
             else:

@@ -116,3 +116,13 @@ def test_one_attention_whose_workspace_grows_in_two_threads(no_gpu, monkeypatch)
     assert len(lib.got) == 3
     for max_len, ws, ws_bytes in lib.got:
         assert ws in kept and ws_bytes >= 1000 * max_len and kept[ws] == ws_bytes, (max_len, ws_bytes, kept)
+
+
+def test_what_an_object_was_made_with_stays(no_gpu, monkeypatch):
+    """Calls keep their descriptions, so that another window or scale would count for some shapes and not for others: it is an object of its own."""
+    attn, rot = _attention(monkeypatch), mm.Rotary(torch.ones(4, dtype=torch.float64), mscale=2.0)
+    assert (attn.scale, attn.window, attn.softcap, attn.n_heads) == (0.25, 0, 0.0, 2) and (rot.layout, rot.mscale, rot.rotary_dim) == ("half", 2.0, 8)
+    for thing, names in ((attn, ("scale", "window", "softcap", "n_heads", "cache")), (rot, ("layout", "mscale", "rotary_dim", "freq"))):
+        for name in names:
+            with pytest.raises(AttributeError):
+                setattr(thing, name, getattr(thing, name))
