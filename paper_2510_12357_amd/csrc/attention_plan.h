@@ -47,7 +47,7 @@ MM_BOTH int blocks_of(const Seen& v) { return (int)(((int64_t)v.end - v.first / 
 // places [w each, (w + 1) each) of the line, a row of segments, each of one unit.  A unit whose own blocks lie in several workgroups has its parts joined.
 // align 0: equal shares of the whole line, on which kSetup places in front of each unit stand for what it takes to begin and end one.  Else shares are of `align`
 // places, and so is what units are rounded up to: a workgroup has one unit.
-// (128 sequences of up to 1000 on 8 key heads, with 4, 2 or 1 places to begin and end a unit: 52.1, 53.7 and 61.5 us.)
+// (128 sequences of up to 1000 on 8 key heads, with 4, 2 or 1 places to begin and end a unit: 52.7, 54.3 and 63.8 us.)
 constexpr int kSetup = 4;
 MM_BOTH int unit_places(int n, int align) { return align ? (n + align - 1) / align * align : n + kSetup; }
 MM_BOTH int line_places(int n, int align) { return n > 0 ? unit_places(n, align) : 0; }

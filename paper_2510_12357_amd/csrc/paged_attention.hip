@@ -1,8 +1,8 @@
 // Attention of one new token per sequence over a paged cache (moe_paged_attention).
 //
-// What bounds it: reading the keys and values that are seen, once per key head.  The positions of all sequences, for each key head and up to 16 of its query heads, are a
+// What bounds it: reading the keys and values that are seen, once per key head and 16 of its query heads (more heads to a key head read them again, from L2 at best).  The positions of all sequences, for each key head and up to 16 of its query heads, are a
 // line of blocks that as many workgroups as run at once share equally (attention_plan.h), whatever the lengths are: 64 sequences of 400 to 8192 positions
-// (32 heads on 8 of 128 channels, bf16, 1.1 GB) take 177 us, 6.2 TB/s; with a workgroup for each part of fixed length 191, of which the last ones ran alone.  A workgroup's
+// (32 heads on 8 of 128 channels, bf16, 1.1 GB) take 179 us, 6.2 TB/s; with a workgroup for each part of fixed length 191, of which the last ones ran alone.  A workgroup's
 // segments are of one sequence and key head each, of which its waves take blocks in turn.
 // Scores are the product of a tile of keys (rows: positions) and the queries (columns: heads), so that a lane has four positions of one head, which is where the
 // product with the values wants the probabilities: nothing moves between lanes.  Values go into that product from where their rows lie, a lane with the same channels
@@ -11,7 +11,7 @@
 // probabilities in three bf16 terms; caches in fp32 on fp32 ones.
 // A block's keys are loaded again as soon as they are in LDS, its values as soon as they are used: a block and a half of each wave is on its way.  More waves or larger blocks
 // did not help (2 or 3 workgroups per CU, 8 or 16 KB a wave: within 1 %), fewer bytes on their way did harm (one workgroup per CU: +15 %).
-// Many short sequences are another matter: workgroups of one wave each, which have no waves to join or to wait for (128 sequences of up to 64 14.4 -> 10.4 us, on the long ones 185).
+// Many short sequences are another matter: workgroups of one wave each, which have no waves to join or to wait for (128 sequences of up to 64 15.2 -> 11.0 us, on the long ones 186).
 // The maximum that exponentials are taken against follows the scores only when one is 2^8 above it: sums stay far below fp32's range, and most blocks neither exchange
 // maxima nor rescale.  Waves' sums are joined in LDS, parts' sums by the last of a unit's workgroups to end or, where parts are many, by a second
 // kernel, all in a fixed order.
@@ -131,8 +131,9 @@ __device__ __forceinline__ void store_row(const AttentionArgs& a, int b, int hea
   if (a.lse && channel == 0) a.lse[(int64_t)b * a.heads + head] = l == 0.f ? -INFINITY : fmaf(m, kLn2, logf(l));
 }
 
-// Tiles of 16 positions of a wave's block, and waves of a SIMD that the registers are shared by: as many as need no spills (with 20 registers of spills the largest bf16
-// kernel took 18 % longer, on half as many workgroups again).
+// Tiles of 16 positions of a wave's block, and waves of a SIMD that the vector registers are shared by: as many as need no spills of them (with 20 the largest bf16 kernel
+// took 18 % longer, on half as many workgroups again).  Scalar registers are short in all of these kernels: 55 to 93 of them wait in lanes of vector registers, none that the loop over
+// blocks uses, so that it is short sequences that pay for it.
 constexpr int block_tiles(size_t bytes, int dims) { return std::clamp(512 / (int)(dims * bytes), 1, 2); }
 constexpr int waves_per_simd(size_t bytes, int dims, int parts) {
   if (dims > 128) return bytes < 4 && parts == 1 ? 2 : 1;
