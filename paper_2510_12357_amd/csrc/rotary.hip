@@ -3,7 +3,7 @@
 // Pairs of channels (a, b) turn by t = pos freq: a' = m (a cos t - b sin t), b' = m (b cos t + a sin t).  A workgroup has a few tokens, works out their sines and cosines
 // once, one a thread, into LDS, and turns V pairs a lane of head after head; of a row's lanes each has the same pairs in all heads, so that they stay in registers.
 // What bounds it: reading and writing; few tokens, the launch.  4096 tokens of 40 heads of 128 channels, bf16 (84 MB) 16.7 us, 5.0 TB/s; an append of 16384 tokens of 32 + 8 + 8 heads
-// (400 MB) 79 us, 5.1 TB/s; of 2111 tokens into 8 bits 9.1 us (a copy of 2 GB reaches 4.9 TB/s).  With eight sines a lane and head instead, 19.7, 87 and 13.4 us.
+// (400 MB) 79 us, 5.1 TB/s; of 2111 tokens into 8 bits 9.1 us (copies reach 4.7 TB/s over 84 MB, 5.5 over 400 MB).  With eight sines a lane and head instead, 19.7, 87 and 13.4 us.
 #include <algorithm>
 
 #include "internal.h"
