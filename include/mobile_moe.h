@@ -588,7 +588,7 @@ int moe_token_logprobs(const moe_logprobs_config* cfg, const void* logits, const
  *   grid): a sequence whose length is negative, above max_len or behind its table row, or that sees a page outside [0, n_pages), has NaN everywhere.  Nothing
  *   of the cache behind the length or before the window is used, whatever it holds.  Of what is seen, a NaN or an infinity in a value gives NaN in its channel or an
  *   infinity, in a key whatever its score makes of it: NaN everywhere, or with a score of -inf nothing.  out may be q, with the same strides (and else must not overlap it).
- *   Results are means of the values, finite for finite ones of any size; of values below about 2^-105 they lose digits, as shares of them leave fp32's normal numbers.
+ *   Results are means of the values, finite where the mean, with the rounding of its sums, is one of the results' type; of values below about 2^-105 they lose digits, as shares of them leave fp32's normal numbers.
  *   Scores, softmax and sums are in fp32, in an order that goes by the lengths of the whole batch: the same call has the same bits again, and the same
  *   sequence in another batch may differ in the last bits.
  *   ws: device scratch of moe_paged_attention_workspace_bytes(cfg, cache) bytes, 256-byte aligned (a size of 0: NULL will do).
